@@ -1,0 +1,651 @@
+// fastrack_kv.cu -- handle, launches and small kernels of the key-value cache operators (include/fastrack_kv.h).
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <stdlib.h>
+#include <string.h>
+#include <atomic>
+#include <new>
+
+#include "../../include/fastrack_kv.h"
+#include "fastrack_kv_attend.cuh"
+#include "fastrack_kv_device.cuh"
+
+// ------------------------------------------------------------------------------------------------ rotary ----
+
+#define KV_ROT_THREADS 256
+
+// One thread turns one unit (16 channels) of a token in `per` heads: the unit's cosines and sines are made once for them.
+template <bool BF>
+__global__ void __launch_bounds__(KV_ROT_THREADS) kv_rotary_kernel(const KvShape S, const KvRows in, const KvRows out, const int64_t* __restrict__ positions,
+                                                                   const int64_t tokens, const int heads, const int per, const bool inverse)
+{
+    const int units = S.head_dim / 16, groups = (heads + per - 1) / per;
+    const int64_t idx = (int64_t)blockIdx.x * KV_ROT_THREADS + threadIdx.x;
+    if (idx >= tokens * units * groups) return;
+    const int u = (int)(idx % units), h0 = (int)(idx / units % groups) * per;
+    const int64_t token = idx / units / groups;
+    const KvUnit unit = kv_unit(S, u);
+    if (!unit.turned && in.data == out.data) return;
+    float cs[8], sn[8];
+    if (unit.turned) kv_angles(S, u, positions[token], inverse, cs, sn);
+    for (int h = h0; h < min(h0 + per, heads); h++) {
+        const uint16_t* src = (const uint16_t*)in.data + token * in.token_stride + h * in.head_stride;
+        uint16_t* dst = (uint16_t*)out.data + token * out.token_stride + h * out.head_stride;
+        uint4 a = *(const uint4*)(src + unit.a), b = *(const uint4*)(src + unit.b);
+        if (unit.turned) {
+            float x[16];
+            kv_widen8<BF>(a, x);
+            kv_widen8<BF>(b, x + 8);
+            kv_turn(S, x, cs, sn);
+            a = kv_narrow8<BF>(x);
+            b = kv_narrow8<BF>(x + 8);
+        }
+        *(uint4*)(dst + unit.a) = a;
+        *(uint4*)(dst + unit.b) = b;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ append ----
+
+#define KV_APPEND_THREADS 256
+
+struct KvAppend { KvRows k, v, q, q_out; int slots, quant_ctas, q_per; };
+
+// Values of unit u of one new token (K turned, V as it is) or, for a token from before the call, of the tail.
+template <bool BF>
+__device__ __forceinline__ void kv_load_unit(const KvShape& S, const KvBatch& B, const KvAppend& A, const KvSeq& q, int seq, int kh, int which,
+                                             int token, int u, float* x)
+{
+    const KvUnit unit = kv_unit(S, u);
+    const int j = token - (q.len - q.n);
+    const uint16_t* src;
+    if (j >= 0) {
+        const KvRows& r = which ? A.v : A.k;
+        src = (const uint16_t*)r.data + (q.start + j) * r.token_stride + kh * r.head_stride;
+    } else {
+        src = (const uint16_t*)B.tail + (uint64_t)seq * S.tail_values + ((uint64_t)(2 * kh + which) * S.block_tokens + (token & (S.block_tokens - 1))) * S.head_dim;
+    }
+    kv_widen8<BF>(*(const uint4*)(src + unit.a), x);
+    kv_widen8<BF>(*(const uint4*)(src + unit.b), x + 8);
+    if (j >= 0 && which == 0 && unit.turned) {
+        float cs[8], sn[8];
+        kv_angles(S, u, B.positions[q.start + j], false, cs, sn);
+        kv_turn(S, x, cs, sn);
+    }
+}
+
+// CTAs 0 .. quant_ctas - 1: one block that the call touches, of one kv head.  The CTA of a sequence's first block also writes the
+// head's tail, after it has read what the tail held: no other CTA touches the head's tail row.  The CTAs behind turn q.
+template <bool BF, bool E4M3>
+__global__ void __launch_bounds__(KV_APPEND_THREADS) kv_append_kernel(const KvShape S, const KvBatch B, const KvAppend A)
+{
+    const int units = S.head_dim / 16, tid = threadIdx.x;
+    if ((int)blockIdx.x >= A.quant_ctas) {
+        const int groups = (S.q_heads + A.q_per - 1) / A.q_per;
+        const int64_t idx = (int64_t)(blockIdx.x - A.quant_ctas) * KV_APPEND_THREADS + tid;
+        const int64_t token = idx / units / groups;
+        if (token >= B.total_new) return;
+        const int u = (int)(idx % units), h0 = (int)(idx / units % groups) * A.q_per;
+        const KvUnit unit = kv_unit(S, u);
+        float cs[8], sn[8];
+        if (unit.turned) kv_angles(S, u, B.positions[token], false, cs, sn);
+        for (int h = h0; h < min(h0 + A.q_per, S.q_heads); h++) {
+            const uint16_t* src = (const uint16_t*)A.q.data + token * A.q.token_stride + h * A.q.head_stride;
+            uint16_t* dst = (uint16_t*)A.q_out.data + token * A.q_out.token_stride + h * A.q_out.head_stride;
+            uint4 a = *(const uint4*)(src + unit.a), b = *(const uint4*)(src + unit.b);
+            if (unit.turned) {
+                float x[16];
+                kv_widen8<BF>(a, x);
+                kv_widen8<BF>(b, x + 8);
+                kv_turn(S, x, cs, sn);
+                a = kv_narrow8<BF>(x);
+                b = kv_narrow8<BF>(x + 8);
+            }
+            *(uint4*)(dst + unit.a) = a;
+            *(uint4*)(dst + unit.b) = b;
+        }
+        return;
+    }
+    const int kh = blockIdx.x % S.kv_heads, slot = blockIdx.x / S.kv_heads % A.slots, seq = blockIdx.x / S.kv_heads / A.slots;
+    const KvSeq q = kv_seq(S, B, seq);
+    if (q.n == 0) return;
+    const int first = max(q.len - q.n, 0), block = (first >> S.block_shift) + slot, t0 = block << S.block_shift;
+    const int items = S.block_tokens * units;
+    __shared__ uint32_t warp_max[2][KV_APPEND_THREADS / 32];
+
+    if (block < q.full) {
+        const int page = kv_page(B, seq, block);
+        if (page >= 0) {
+            uint8_t* dst = B.pool + (uint64_t)page * S.page_bytes;
+            for (int which = 0; which < 2; which++) {
+                uint32_t amax = 0;                      // as bits: a NaN is larger than everything
+                for (int i = tid; i < items; i += KV_APPEND_THREADS) {
+                    float x[16];
+                    kv_load_unit<BF>(S, B, A, q, seq, kh, which, t0 + i / units, i % units, x);
+#pragma unroll
+                    for (int e = 0; e < 16; e++) amax = max(amax, __float_as_uint(x[e]) & 0x7fffffffu);
+                }
+                amax = __reduce_max_sync(0xffffffffu, amax);
+                if ((tid & 31) == 0) warp_max[which][tid >> 5] = amax;
+                __syncthreads();
+#pragma unroll
+                for (int w = 0; w < KV_APPEND_THREADS / 32; w++) amax = max(amax, warp_max[which][w]);
+                constexpr float top = E4M3 ? 448.f : 127.f;
+                const float peak = amax < __float_as_uint(0x1p-100f) ? 0.f : __uint_as_float(amax);
+                const float factor = peak == 0.f ? 0.f : top / peak;
+                for (int i = tid; i < items; i += KV_APPEND_THREADS) {
+                    const int u = i % units;
+                    float x[16];
+                    kv_load_unit<BF>(S, B, A, q, seq, kh, which, t0 + i / units, u, x);
+#pragma unroll
+                    for (int e = 0; e < 16; e++) x[e] *= factor;
+                    const KvUnit unit = kv_unit(S, u);
+                    uint8_t* row = dst + (uint64_t)which * S.codes_bytes + ((uint64_t)kh * S.block_tokens + i / units) * S.head_dim;
+                    *(uint2*)(row + unit.a) = make_uint2(kv_codes4<E4M3>(x), kv_codes4<E4M3>(x + 4));
+                    *(uint2*)(row + unit.b) = make_uint2(kv_codes4<E4M3>(x + 8), kv_codes4<E4M3>(x + 12));
+                }
+                if (tid == 0) ((float*)kv_scales(S, B, page))[2 * kh + which] = peak / top;
+            }
+        }
+    }
+    if (slot == 0) {
+        __syncthreads();                                // the old tail has been read
+        const int from = max(q.full << S.block_shift, first);
+        for (int i = tid; i < 2 * (q.len - from) * units; i += KV_APPEND_THREADS) {
+            const int u = i % units, which = i / units & 1, token = from + i / units / 2;
+            const KvUnit unit = kv_unit(S, u);
+            float x[16];
+            kv_load_unit<BF>(S, B, A, q, seq, kh, which, token, u, x);
+            uint16_t* dst = (uint16_t*)B.tail + (uint64_t)seq * S.tail_values + ((uint64_t)(2 * kh + which) * S.block_tokens + (token & (S.block_tokens - 1))) * S.head_dim;
+            *(uint4*)(dst + unit.a) = kv_narrow8<BF>(x);
+            *(uint4*)(dst + unit.b) = kv_narrow8<BF>(x + 8);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ read ----
+
+template <bool BF, bool E4M3>
+__global__ void __launch_bounds__(256) kv_read_kernel(const KvShape S, const KvBatch B, const KvRows ko, const KvRows vo)
+{
+    const int seq = blockIdx.z, which = blockIdx.y & 1, kh = blockIdx.y >> 1, pieces = S.head_dim / 8;
+    const int i = blockIdx.x * 256 + threadIdx.x, token = i / pieces, at = i % pieces * 8;
+    if (token >= B.max_len) return;
+    const KvSeq q = kv_seq(S, B, seq);
+    const int block = token >> S.block_shift, in_block = token & (S.block_tokens - 1);
+    uint4 w = make_uint4(0, 0, 0, 0);
+    if (token < q.len) {
+        if (block == q.full) {
+            w = *(const uint4*)((const uint16_t*)B.tail + (uint64_t)seq * S.tail_values + ((uint64_t)(2 * kh + which) * S.block_tokens + in_block) * S.head_dim + at);
+        } else {
+            const int page = kv_page(B, seq, block);
+            if (page >= 0) {
+                const float scale = kv_scales(S, B, page)[2 * kh + which];
+                const uint2 codes = *(const uint2*)(B.pool + (uint64_t)page * S.page_bytes + (uint64_t)which * S.codes_bytes +
+                                                    ((uint64_t)kh * S.block_tokens + in_block) * S.head_dim + at);
+                float x[8];
+                kv_decode4<E4M3>(codes.x, scale, x);
+                kv_decode4<E4M3>(codes.y, scale, x + 4);
+                w = kv_narrow8<BF>(x);
+            }
+        }
+    }
+    const KvRows& r = which ? vo : ko;
+    *(uint4*)((uint16_t*)r.data + ((int64_t)seq * B.max_len + token) * r.token_stride + kh * r.head_stride + at) = w;
+}
+
+// ------------------------------------------------------------------------------------------------ evict ----
+
+#define KV_EVICT_THREADS 1024
+#define KV_EVICT_KEYS 49152             // scores kept in shared memory; those of later blocks are added up again where they are needed
+
+struct KvEvict {
+    int table_stride, mass_stride, budget, keep_first, keep_last, keys;
+    const int32_t *table, *lens;
+    const float* mass;
+    int32_t *table_out, *lens_out;
+    float* mass_out;
+    int32_t *evicted, *n_evicted;
+};
+
+// A float as an unsigned number of the same order; every NaN becomes the largest.
+__device__ __forceinline__ uint32_t kv_order(float x)
+{
+    if (x != x) return 0xffffffffu;
+    x += 0.f;                                           // -0 is 0
+    const uint32_t b = __float_as_uint(x);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+// Exclusive sum of `flag` over the CTA's threads in order, and the total; two barriers.
+__device__ __forceinline__ int kv_rank(bool flag, int* warp_sums, int& total)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t votes = __ballot_sync(0xffffffffu, flag);
+    __syncthreads();
+    if (lane == 0) warp_sums[warp] = __popc(votes);
+    __syncthreads();
+    int sum = warp_sums[lane];
+    int before = sum;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) { const int o = __shfl_up_sync(0xffffffffu, before, d); if (lane >= d) before += o; }
+    total = __shfl_sync(0xffffffffu, before, 31);
+    return __shfl_sync(0xffffffffu, before - sum, warp) + __popc(votes & ((1u << lane) - 1u));
+}
+
+// One CTA per sequence.  The score of the last block to leave is found by radix selection, 8 bits at a time; then one pass in block
+// order moves what stays.  An entry is read before a barrier that precedes every write at or above its place: in place is safe.
+__global__ void __launch_bounds__(KV_EVICT_THREADS) kv_evict_kernel(const KvShape S, const KvEvict A)
+{
+    extern __shared__ uint32_t keys[];
+    __shared__ int hist[256], warp_sums[32], pick[2];
+    const int seq = blockIdx.x, tid = threadIdx.x;
+    const int len = max(A.lens[seq], 0), most = min(A.table_stride, A.mass_stride);
+    const int full = min(len >> S.block_shift, most), held = min((len + S.block_tokens - 1) >> S.block_shift, most);
+    const int lo = min(A.keep_first, full), hi = max(full - A.keep_last, lo);
+    const int drop = min(max(full - A.budget, 0), hi - lo);
+    const float* mass = A.mass + (int64_t)seq * S.kv_heads * A.mass_stride;
+    auto score = [&](int b) {
+        double x = 0.;
+        for (int h = 0; h < S.kv_heads; h++) x += mass[(int64_t)h * A.mass_stride + b];
+        return kv_order((float)x);
+    };
+    auto key = [&](int b) { return b < A.keys ? keys[b] : score(b); };
+    uint32_t limit = 0;
+    int ties = 0;                                       // blocks with exactly the limit's score that leave
+    if (drop > 0) {
+        for (int b = lo + tid; b < min(hi, A.keys); b += KV_EVICT_THREADS) keys[b] = score(b);
+        int left = drop;
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            for (int i = tid; i < 256; i += KV_EVICT_THREADS) hist[i] = 0;
+            __syncthreads();
+            for (int b = lo + tid; b < hi; b += KV_EVICT_THREADS) {
+                const uint32_t k = key(b);
+                if (shift == 24 || k >> (shift + 8) == limit >> (shift + 8)) atomicAdd(&hist[k >> shift & 255], 1);
+            }
+            __syncthreads();
+            if (tid < 32) {                             // the bin in which the left-th smallest lies
+                int mine = 0, before;
+                for (int i = 0; i < 8; i++) mine += hist[8 * tid + i];
+                before = mine;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) { const int o = __shfl_up_sync(0xffffffffu, before, d); if (tid >= d) before += o; }
+                before -= mine;
+                if (before < left && left <= before + mine)
+                    for (int i = 0; i < 8; i++) {
+                        if (left <= before + hist[8 * tid + i]) { pick[0] = 8 * tid + i; pick[1] = left - before; break; }
+                        before += hist[8 * tid + i];
+                    }
+            }
+            __syncthreads();
+            limit |= (uint32_t)pick[0] << shift;
+            left = pick[1];
+        }
+        ties = left;
+    }
+    int out_at = 0, stay_at = 0, tie_at = 0;
+    for (int b0 = 0; b0 < most; b0 += KV_EVICT_THREADS) {
+        const int b = b0 + tid;
+        const bool free = drop > 0 && b >= lo && b < hi;
+        const uint32_t k = free ? key(b) : 0u;
+        int total;
+        const bool tie = free && k == limit;
+        const int tie_rank = tie_at + kv_rank(tie, warp_sums, total);
+        tie_at += total;
+        const bool out = free && (k < limit || (tie && tie_rank < ties)), stay = b < held && !out;
+        const int out_rank = out_at + kv_rank(out, warp_sums, total);
+        out_at += total;
+        const int stay_rank = stay_at + kv_rank(stay, warp_sums, total);
+        stay_at += total;
+        const int32_t page = b < held ? A.table[(int64_t)seq * A.table_stride + b] : -1;
+        __syncthreads();
+        if (stay) A.table_out[(int64_t)seq * A.table_stride + stay_rank] = page;
+        if (out) A.evicted[(int64_t)seq * A.table_stride + out_rank] = page;
+        for (int h = 0; h < S.kv_heads; h++) {
+            const int64_t row = ((int64_t)seq * S.kv_heads + h) * A.mass_stride;
+            const float w = stay ? A.mass[row + b] : 0.f;
+            __syncthreads();
+            if (stay) A.mass_out[row + stay_rank] = w;
+        }
+    }
+    __syncthreads();
+    for (int b = held - drop + tid; b < A.table_stride; b += KV_EVICT_THREADS) A.table_out[(int64_t)seq * A.table_stride + b] = -1;
+    for (int b = drop + tid; b < A.table_stride; b += KV_EVICT_THREADS) A.evicted[(int64_t)seq * A.table_stride + b] = -1;
+    for (int h = 0; h < S.kv_heads; h++)
+        for (int b = held - drop + tid; b < A.mass_stride; b += KV_EVICT_THREADS) A.mass_out[((int64_t)seq * S.kv_heads + h) * A.mass_stride + b] = 0.f;
+    if (tid == 0) {
+        A.lens_out[seq] = len - (drop << S.block_shift);
+        A.n_evicted[seq] = drop;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ handle ----
+
+struct fastrack_kv {
+    fastrack_kv_config config;
+    KvShape shape;
+    int device, num_sms;
+    uint64_t* d_turns;
+    std::atomic<int> last_cuda_error;
+    std::atomic<uint64_t> launches;
+};
+
+static int kv_cuda(fastrack_kv* kv, cudaError_t e)
+{
+    if (e == cudaSuccess) return FASTRACK_OK;
+    kv->last_cuda_error = (int)e;
+    (void)cudaGetLastError();
+    return FASTRACK_ERR_CUDA;
+}
+static int kv_launched(fastrack_kv* kv, int count = 1)
+{
+    kv->launches += (uint64_t)count;
+    return kv_cuda(kv, cudaGetLastError());
+}
+static int kv_check_device(fastrack_kv* kv)
+{
+    int dev = -1;
+    const int rc = kv_cuda(kv, cudaGetDevice(&dev));
+    return rc != FASTRACK_OK ? rc : dev == kv->device ? FASTRACK_OK : FASTRACK_ERR_ARG;
+}
+static bool kv_misaligned(const void* p, size_t a) { return p == nullptr || ((uintptr_t)p & (a - 1)) != 0; }
+static bool kv_bad_rows(const fastrack_kv_rows* r) { return !r || kv_misaligned(r->data, 16) || (r->token_stride & 7) || (r->head_stride & 7); }
+static KvRows kv_rows(const fastrack_kv_rows* r) { return {r->data, r->token_stride, r->head_stride}; }
+static int kv_log2i(int x) { int s = 0; while ((1 << s) < x) s++; return s; }
+
+static bool kv_bad_batch(const fastrack_kv* kv, const fastrack_kv_batch* b)
+{
+    if (!b || b->n_seqs < 0 || b->total_new < 0 || b->max_new < 0 || b->max_len < 0 || b->max_len > 1 << 30 || b->pool_pages < 0 || b->table_stride < 0) return true;
+    if (b->n_seqs > 65535 || b->max_new > b->total_new || b->max_len / kv->config.block_tokens > b->table_stride) return true;
+    if ((int64_t)b->max_new * kv->config.q_heads > 1 << 30 || (int64_t)b->total_new * kv->config.q_heads > INT32_MAX) return true;
+    if (b->n_seqs == 0) return false;
+    if (b->pool_pages > 0 && kv_misaligned(b->d_pool, 16)) return true;
+    return kv_misaligned(b->d_tail, 16) || kv_misaligned(b->d_lens, 4) || kv_misaligned(b->d_starts, 4) || (b->table_stride > 0 && kv_misaligned(b->d_table, 4));
+}
+static KvBatch kv_batch(const fastrack_kv_batch* b)
+{
+    return {b->n_seqs, b->total_new, b->max_new, b->max_len, b->pool_pages, b->table_stride, (uint8_t*)b->d_pool, b->d_tail, b->d_table, b->d_lens,
+            b->d_starts, b->d_positions};
+}
+
+extern "C" int fastrack_kv_create(const fastrack_kv_config* c, fastrack_kv** out)
+{
+    if (out) *out = nullptr;
+    if (!c || !out) return FASTRACK_ERR_ARG;
+    if ((c->dtype != FASTRACK_KV_BF16 && c->dtype != FASTRACK_KV_F16) || (c->format != FASTRACK_KV_INT8 && c->format != FASTRACK_KV_E4M3)) return FASTRACK_ERR_ARG;
+    if (c->kv_heads < 1 || c->q_heads < 1 || c->q_heads > 1024 || c->q_heads % c->kv_heads) return FASTRACK_ERR_ARG;
+    if (c->head_dim != 64 && c->head_dim != 96 && c->head_dim != 128) return FASTRACK_ERR_ARG;
+    if (c->block_tokens != 16 && c->block_tokens != 32 && c->block_tokens != 64 && c->block_tokens != 128) return FASTRACK_ERR_ARG;
+    if (c->rotary < FASTRACK_ROTARY_NONE || c->rotary > FASTRACK_ROTARY_INTERLEAVED) return FASTRACK_ERR_ARG;
+    if (c->rotary == FASTRACK_ROTARY_NONE ? c->rotary_dim != 0
+                                          : c->rotary_dim < 16 || c->rotary_dim > c->head_dim || c->rotary_dim % 16 || !c->frequencies || !isfinite(c->rotary_gain))
+        return FASTRACK_ERR_ARG;
+    if (!isfinite(c->softmax_scale)) return FASTRACK_ERR_ARG;
+    uint64_t turns[KV_MAX_PAIRS] = {0};
+    for (int i = 0; i < c->rotary_dim / 2; i++) {
+        if (!isfinite(c->frequencies[i])) return FASTRACK_ERR_ARG;
+        const long double t = (long double)c->frequencies[i] / 6.283185307179586476925286766559L;
+        const long double part = floorl((t - floorl(t)) * 18446744073709551616.0L);
+        turns[i] = part < 18446744073709551616.0L ? (uint64_t)part : 0u;
+    }
+    fastrack_kv* kv = new (std::nothrow) fastrack_kv();
+    if (!kv) return FASTRACK_ERR_NOMEM;
+    kv->config = *c;
+    kv->config.frequencies = nullptr;
+    kv->last_cuda_error = 0;
+    kv->launches = 0;
+    KvShape& S = kv->shape;
+    S.q_heads = c->q_heads;
+    S.kv_heads = c->kv_heads;
+    S.group = c->q_heads / c->kv_heads;
+    S.head_dim = c->head_dim;
+    S.block_tokens = c->block_tokens;
+    S.block_shift = kv_log2i(c->block_tokens);
+    S.rotary = c->rotary;
+    S.rotary_dim = c->rotary_dim;
+    S.rotary_gain = c->rotary_gain;
+    S.scale_log2 = (c->softmax_scale == 0.f ? 1.f / sqrtf((float)c->head_dim) : c->softmax_scale) * 1.4426950408889634f;
+    S.codes_bytes = (uint32_t)(c->kv_heads * c->block_tokens * c->head_dim);
+    S.page_bytes = (2ull * S.codes_bytes + 8ull * (uint64_t)c->kv_heads + 127) / 128 * 128;
+    S.tail_values = 2ull * S.codes_bytes;
+    cudaError_t e = cudaGetDevice(&kv->device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&kv->num_sms, cudaDevAttrMultiProcessorCount, kv->device);
+    if (e == cudaSuccess) e = cudaMalloc(&kv->d_turns, sizeof turns);
+    if (e == cudaSuccess) e = cudaMemcpy(kv->d_turns, turns, sizeof turns, cudaMemcpyHostToDevice);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kv_evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, KV_EVICT_KEYS * 4);
+    if (e != cudaSuccess) {
+        (void)cudaGetLastError();
+        fastrack_kv_destroy(kv);
+        return e == cudaErrorMemoryAllocation ? FASTRACK_ERR_NOMEM : FASTRACK_ERR_CUDA;
+    }
+    S.turns = kv->d_turns;
+    *out = kv;
+    return FASTRACK_OK;
+}
+
+extern "C" void fastrack_kv_destroy(fastrack_kv* kv)
+{
+    if (!kv) return;
+    if (kv->d_turns) (void)cudaFree(kv->d_turns);
+    delete kv;
+}
+
+extern "C" size_t fastrack_kv_page_bytes(const fastrack_kv* kv) { return kv ? (size_t)kv->shape.page_bytes : 0; }
+extern "C" size_t fastrack_kv_tail_bytes(const fastrack_kv* kv) { return kv ? (size_t)kv->shape.tail_values * 2 : 0; }
+extern "C" int fastrack_kv_last_cuda_error(const fastrack_kv* kv) { return kv ? kv->last_cuda_error.load() : 0; }
+extern "C" uint64_t fastrack_kv_launch_count(const fastrack_kv* kv) { return kv ? kv->launches.load() : 0; }
+
+extern "C" int fastrack_rotary_frequencies(int rotary_dim, double base, int scaling, double factor, double original_len, double* frequencies, float* gain)
+{
+    const double two_pi = 6.283185307179586476925286766559;
+    if (rotary_dim < 2 || (rotary_dim & 1) || !frequencies || !(base > 1) || !isfinite(base) || !(factor >= 1) || !isfinite(factor)) return FASTRACK_ERR_ARG;
+    if (scaling < FASTRACK_FREQ_PLAIN || scaling > FASTRACK_FREQ_RAMP) return FASTRACK_ERR_ARG;
+    if (scaling == FASTRACK_FREQ_BASE && rotary_dim < 4) return FASTRACK_ERR_ARG;
+    if (scaling == FASTRACK_FREQ_RAMP && (!(original_len > 0) || !isfinite(original_len))) return FASTRACK_ERR_ARG;
+    // the slowest pair has the exponent (rotary_dim - 2) / rotary_dim
+    if (scaling == FASTRACK_FREQ_BASE) base *= pow(factor, (double)rotary_dim / (rotary_dim - 2));
+    for (int i = 0; i < rotary_dim / 2; i++) {
+        double f = pow(base, -2.0 * i / rotary_dim);
+        if (scaling == FASTRACK_FREQ_LINEAR) f /= factor;
+        if (scaling == FASTRACK_FREQ_RAMP) {
+            const double turns = original_len * f / two_pi, keep = fmin(1.0, fmax(0.0, (turns - 1) / (32.0 - 1)));
+            f = f * keep + f / factor * (1 - keep);
+        }
+        frequencies[i] = f;
+    }
+    if (gain) *gain = scaling == FASTRACK_FREQ_RAMP ? (float)(0.1 * log(factor) + 1) : 1.f;
+    return FASTRACK_OK;
+}
+
+// Heads that one thread turns: as many as still leave every SM two CTAs.
+static int kv_heads_per_thread(const fastrack_kv* kv, int64_t tokens, int heads)
+{
+    int per = 8;
+    while (per > 1 && tokens * (kv->shape.head_dim / 16) * ((heads + per - 1) / per) < (int64_t)2 * KV_ROT_THREADS * kv->num_sms) per /= 2;
+    return per;
+}
+
+extern "C" int fastrack_rotary(fastrack_kv* kv, int64_t tokens, int heads, const fastrack_kv_rows* in, const fastrack_kv_rows* out,
+                               const int64_t* d_positions, int inverse, void* stream)
+{
+    if (!kv || tokens < 0 || heads < 0 || heads > 65536 || tokens > (int64_t)1 << 40) return FASTRACK_ERR_ARG;
+    if (tokens == 0 || heads == 0) return FASTRACK_OK;
+    if (kv_bad_rows(in) || kv_bad_rows(out) || (kv->config.rotary && kv_misaligned(d_positions, 8))) return FASTRACK_ERR_ARG;
+    if (in->data == out->data && (in->token_stride != out->token_stride || in->head_stride != out->head_stride)) return FASTRACK_ERR_ARG;
+    if (int rc = kv_check_device(kv)) return rc;
+    const int per = kv_heads_per_thread(kv, tokens, heads);
+    const int64_t threads = tokens * (kv->shape.head_dim / 16) * ((heads + per - 1) / per), ctas = (threads + KV_ROT_THREADS - 1) / KV_ROT_THREADS;
+    if (ctas > INT32_MAX) return FASTRACK_ERR_ARG;
+    auto kernel = kv->config.dtype == FASTRACK_KV_BF16 ? kv_rotary_kernel<true> : kv_rotary_kernel<false>;
+    kernel<<<(unsigned)ctas, KV_ROT_THREADS, 0, (cudaStream_t)stream>>>(kv->shape, kv_rows(in), kv_rows(out), d_positions, tokens, heads, per, inverse != 0);
+    return kv_launched(kv);
+}
+
+extern "C" int fastrack_kv_append(fastrack_kv* kv, const fastrack_kv_batch* batch, const fastrack_kv_rows* k, const fastrack_kv_rows* v,
+                                  const fastrack_kv_rows* q, const fastrack_kv_rows* q_out, void* stream)
+{
+    if (!kv || kv_bad_batch(kv, batch) || !q != !q_out) return FASTRACK_ERR_ARG;
+    if (batch->n_seqs == 0 || batch->total_new == 0 || batch->max_new == 0) return FASTRACK_OK;
+    if (kv_bad_rows(k) || kv_bad_rows(v) || (q && (kv_bad_rows(q) || kv_bad_rows(q_out))) || (kv->config.rotary && kv_misaligned(batch->d_positions, 8)))
+        return FASTRACK_ERR_ARG;
+    if (q && q->data == q_out->data && (q->token_stride != q_out->token_stride || q->head_stride != q_out->head_stride)) return FASTRACK_ERR_ARG;
+    if (int rc = kv_check_device(kv)) return rc;
+    const KvShape& S = kv->shape;
+    KvAppend A;
+    memset(&A, 0, sizeof A);
+    A.k = kv_rows(k);
+    A.v = kv_rows(v);
+    A.slots = (batch->max_new + S.block_tokens - 2) / S.block_tokens + 1;       // blocks that max_new tokens can touch
+    const int64_t quant = (int64_t)batch->n_seqs * A.slots * S.kv_heads;
+    int64_t turn = 0;
+    A.q_per = 1;
+    if (q) {
+        A.q = kv_rows(q);
+        A.q_out = kv_rows(q_out);
+        A.q_per = kv_heads_per_thread(kv, batch->total_new, S.q_heads);
+        turn = ((int64_t)batch->total_new * (S.head_dim / 16) * ((S.q_heads + A.q_per - 1) / A.q_per) + KV_APPEND_THREADS - 1) / KV_APPEND_THREADS;
+    }
+    if (quant + turn > INT32_MAX) return FASTRACK_ERR_ARG;
+    A.quant_ctas = (int)quant;
+    const bool bf = kv->config.dtype == FASTRACK_KV_BF16, e4 = kv->config.format == FASTRACK_KV_E4M3;
+    auto kernel = bf ? (e4 ? kv_append_kernel<true, true> : kv_append_kernel<true, false>) : (e4 ? kv_append_kernel<false, true> : kv_append_kernel<false, false>);
+    kernel<<<(unsigned)(quant + turn), KV_APPEND_THREADS, 0, (cudaStream_t)stream>>>(S, kv_batch(batch), A);
+    return kv_launched(kv);
+}
+
+extern "C" int fastrack_kv_read(fastrack_kv* kv, const fastrack_kv_batch* batch, const fastrack_kv_rows* k_out, const fastrack_kv_rows* v_out, void* stream)
+{
+    if (!kv || kv_bad_batch(kv, batch)) return FASTRACK_ERR_ARG;
+    if (batch->n_seqs == 0 || batch->max_len == 0) return FASTRACK_OK;
+    if (kv_bad_rows(k_out) || kv_bad_rows(v_out)) return FASTRACK_ERR_ARG;
+    if (int rc = kv_check_device(kv)) return rc;
+    const KvShape& S = kv->shape;
+    const int64_t x = ((int64_t)batch->max_len * (S.head_dim / 8) + 255) / 256;
+    const bool bf = kv->config.dtype == FASTRACK_KV_BF16, e4 = kv->config.format == FASTRACK_KV_E4M3;
+    auto kernel = bf ? (e4 ? kv_read_kernel<true, true> : kv_read_kernel<true, false>) : (e4 ? kv_read_kernel<false, true> : kv_read_kernel<false, false>);
+    kernel<<<dim3((unsigned)x, 2u * S.kv_heads, batch->n_seqs), 256, 0, (cudaStream_t)stream>>>(S, kv_batch(batch), kv_rows(k_out), kv_rows(v_out));
+    return kv_launched(kv);
+}
+
+// ------------------------------------------------------------------------------------------------ attention ----
+
+struct KvPlan { int splits, chunk, row_tiles, units; size_t ml, lse2, unit_l2, total; };   // byte offsets in the workspace, part_o at 0
+
+static KvPlan kv_plan(const fastrack_kv* kv, const fastrack_kv_batch* b, bool mass)
+{
+    const KvShape& S = kv->shape;
+    KvPlan p;
+    const int64_t rows = (int64_t)b->max_new * S.group;
+    p.row_tiles = (int)((rows + KV_ROWS - 1) / KV_ROWS);
+    const int64_t ctas = (int64_t)b->n_seqs * S.kv_heads * p.row_tiles;
+    const int64_t want = (8 * (int64_t)kv->num_sms + ctas - 1) / (ctas ? ctas : 1);
+    const int step = S.block_tokens > KV_TILE * KV_WARPS ? S.block_tokens : KV_TILE * KV_WARPS;
+    int64_t chunk = (b->max_len + want - 1) / want;
+    chunk = (chunk + step - 1) / step * step;
+    if (chunk < step) chunk = step;
+    p.chunk = (int)chunk;
+    p.splits = (int)((b->max_len + chunk - 1) / chunk);
+    if (p.splits < 1) p.splits = 1;
+    p.units = (b->max_len + KV_UNIT - 1) / KV_UNIT;
+    const size_t all = (size_t)b->total_new * S.q_heads;
+    p.ml = p.splits > 1 ? (size_t)p.splits * all * S.head_dim * 4 : 0;
+    p.lse2 = p.ml + (p.splits > 1 ? (size_t)p.splits * all * 8 : 0);
+    p.unit_l2 = (p.lse2 + all * 4 + 15) / 16 * 16;
+    p.total = p.unit_l2 + (mass ? (size_t)b->n_seqs * S.kv_heads * p.units * (size_t)rows * 4 : 0);
+    return p;
+}
+
+extern "C" size_t fastrack_kv_attention_workspace(const fastrack_kv* kv, const fastrack_kv_batch* batch, int with_mass)
+{
+    if (!kv || kv_bad_batch(kv, batch)) return 0;
+    return kv_plan(kv, batch, with_mass != 0).total + 16;
+}
+
+template <int D, bool BF>
+static void kv_attend_launch(const fastrack_kv* kv, const KvBatch& B, const KvAttend& A, cudaStream_t stream)
+{
+    const KvShape& S = kv->shape;
+    const dim3 grid(A.splits, S.kv_heads * A.row_tiles, B.n_seqs);
+    if (kv->config.format == FASTRACK_KV_E4M3) kv_attend_kernel<D, BF, true><<<grid, 32 * KV_WARPS, 0, stream>>>(S, B, A);
+    else kv_attend_kernel<D, BF, false><<<grid, 32 * KV_WARPS, 0, stream>>>(S, B, A);
+    if (A.splits > 1) kv_join_kernel<D, BF><<<dim3((unsigned)(((int64_t)B.max_new * S.q_heads + 7) / 8), B.n_seqs), 256, 0, stream>>>(S, B, A, KV_ROWS);
+}
+
+extern "C" int fastrack_kv_attention(fastrack_kv* kv, const fastrack_kv_batch* batch, const fastrack_kv_rows* q, const fastrack_kv_rows* out, float* d_lse,
+                                     int window, const float* d_mass_in, float* d_mass_out, int mass_stride, void* d_workspace, size_t workspace_bytes,
+                                     void* stream)
+{
+    if (!kv || kv_bad_batch(kv, batch) || window < 0 || !d_mass_in != !d_mass_out) return FASTRACK_ERR_ARG;
+    if (batch->n_seqs == 0 || batch->max_len == 0 && batch->total_new == 0) return FASTRACK_OK;
+    const KvShape& S = kv->shape;
+    const bool mass = d_mass_out != nullptr;
+    if (mass && (kv_misaligned(d_mass_in, 4) || kv_misaligned(d_mass_out, 4) || mass_stride < (batch->max_len + S.block_tokens - 1) / S.block_tokens)) return FASTRACK_ERR_ARG;
+    if (batch->total_new > 0 && (kv_bad_rows(q) || kv_bad_rows(out) || (d_lse && kv_misaligned(d_lse, 4)))) return FASTRACK_ERR_ARG;
+    const KvPlan p = kv_plan(kv, batch, mass);
+    if (kv_misaligned(d_workspace, 16) || workspace_bytes < p.total || (int64_t)S.kv_heads * p.row_tiles > 65535) return FASTRACK_ERR_ARG;
+    if (int rc = kv_check_device(kv)) return rc;
+    const KvBatch B = kv_batch(batch);
+    KvAttend A;
+    memset(&A, 0, sizeof A);
+    char* const ws = (char*)d_workspace;
+    A.lse = d_lse;
+    A.window = window;
+    A.splits = p.splits;
+    A.chunk = p.chunk;
+    A.row_tiles = p.row_tiles;
+    A.units = p.units;
+    A.part_o = (float*)ws;
+    A.part_ml = (float*)(ws + p.ml);
+    A.lse2 = (float*)(ws + p.lse2);
+    A.unit_l2 = mass ? (float*)(ws + p.unit_l2) : nullptr;
+    A.mass_in = d_mass_in;
+    A.mass_out = d_mass_out;
+    A.mass_stride = mass_stride;
+    int launches = 0;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (batch->total_new > 0 && batch->max_new > 0) {
+        A.q = kv_rows(q);
+        A.out = kv_rows(out);
+        const bool bf = kv->config.dtype == FASTRACK_KV_BF16;
+        switch (S.head_dim) {
+        case 64: bf ? kv_attend_launch<64, true>(kv, B, A, st) : kv_attend_launch<64, false>(kv, B, A, st); break;
+        case 96: bf ? kv_attend_launch<96, true>(kv, B, A, st) : kv_attend_launch<96, false>(kv, B, A, st); break;
+        default: bf ? kv_attend_launch<128, true>(kv, B, A, st) : kv_attend_launch<128, false>(kv, B, A, st); break;
+        }
+        launches += 1 + (p.splits > 1);
+    }
+    if (mass && batch->max_len > 0) {
+        const int blocks = (batch->max_len + S.block_tokens - 1) / S.block_tokens;
+        kv_mass_kernel<<<dim3((blocks + 7) / 8, S.kv_heads, batch->n_seqs), 256, 0, st>>>(S, B, A, 4);
+        launches++;
+    }
+    return kv_launched(kv, launches);
+}
+
+extern "C" int fastrack_kv_evict(fastrack_kv* kv, const fastrack_kv_eviction* e, void* stream)
+{
+    if (!kv || !e || e->n_seqs < 0 || e->table_stride < 0 || e->mass_stride < 0 || e->budget < 0 || e->keep_first < 0 || e->keep_last < 0) return FASTRACK_ERR_ARG;
+    if (e->n_seqs == 0) return FASTRACK_OK;
+    const void* need[] = {e->d_table, e->d_lens, e->d_mass, e->d_table_out, e->d_lens_out, e->d_mass_out, e->d_evicted, e->d_n_evicted};
+    for (const void* p : need) if (kv_misaligned(p, 4)) return FASTRACK_ERR_ARG;
+    if (int rc = kv_check_device(kv)) return rc;
+    KvEvict A;
+    A.table_stride = e->table_stride;
+    A.mass_stride = e->mass_stride;
+    A.budget = e->budget;
+    A.keep_first = e->keep_first;
+    A.keep_last = e->keep_last;
+    const int most = e->table_stride < e->mass_stride ? e->table_stride : e->mass_stride;
+    A.keys = most < KV_EVICT_KEYS ? most : KV_EVICT_KEYS;
+    A.table = e->d_table;
+    A.lens = e->d_lens;
+    A.mass = e->d_mass;
+    A.table_out = e->d_table_out;
+    A.lens_out = e->d_lens_out;
+    A.mass_out = e->d_mass_out;
+    A.evicted = e->d_evicted;
+    A.n_evicted = e->d_n_evicted;
+    kv_evict_kernel<<<e->n_seqs, KV_EVICT_THREADS, (size_t)A.keys * 4, (cudaStream_t)stream>>>(kv->shape, A);
+    return kv_launched(kv);
+}

@@ -1,4 +1,6 @@
 // fastrack_kv.cu -- handle, launches and small kernels of the key-value cache operators (include/fastrack_kv.h).
+#include <cuda.h>
+#include <cudaTypedefs.h>
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -327,9 +329,26 @@ struct fastrack_kv {
     KvShape shape;
     int device, num_sms;
     uint64_t* d_turns;
+    PFN_cuTensorMapEncodeTiled_v12000 encode;
     std::atomic<int> last_cuda_error;
     std::atomic<uint64_t> launches;
 };
+
+// Shared memory beyond the default has to be asked for, once per kernel and device.
+template <int D> static cudaError_t kv_attend_prepare()
+{
+    cudaError_t e = cudaSuccess;
+    auto ask = [&](const void* kernel, int rows) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kv_attend_smem<D>(rows) + 16 * KV_WARPS); };
+    ask((const void*)kv_attend_kernel<D, true, true, 1>, 8);
+    ask((const void*)kv_attend_kernel<D, true, false, 1>, 8);
+    ask((const void*)kv_attend_kernel<D, false, true, 1>, 8);
+    ask((const void*)kv_attend_kernel<D, false, false, 1>, 8);
+    ask((const void*)kv_attend_kernel<D, true, true, 2>, 16);
+    ask((const void*)kv_attend_kernel<D, true, false, 2>, 16);
+    ask((const void*)kv_attend_kernel<D, false, true, 2>, 16);
+    ask((const void*)kv_attend_kernel<D, false, false, 2>, 16);
+    return e;
+}
 
 static int kv_cuda(fastrack_kv* kv, cudaError_t e)
 {
@@ -411,9 +430,15 @@ extern "C" int fastrack_kv_create(const fastrack_kv_config* c, fastrack_kv** out
     S.tail_values = 2ull * S.codes_bytes;
     cudaError_t e = cudaGetDevice(&kv->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&kv->num_sms, cudaDevAttrMultiProcessorCount, kv->device);
+    void* encode = nullptr;
+    cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+    if (e == cudaSuccess) e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &encode, 12000, cudaEnableDefault, &found);
+    if (e == cudaSuccess && (found != cudaDriverEntryPointSuccess || !encode)) e = cudaErrorNotSupported;
+    kv->encode = (PFN_cuTensorMapEncodeTiled_v12000)encode;
     if (e == cudaSuccess) e = cudaMalloc(&kv->d_turns, sizeof turns);
     if (e == cudaSuccess) e = cudaMemcpy(kv->d_turns, turns, sizeof turns, cudaMemcpyHostToDevice);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kv_evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, KV_EVICT_KEYS * 4);
+    if (e == cudaSuccess) e = c->head_dim == 64 ? kv_attend_prepare<64>() : c->head_dim == 96 ? kv_attend_prepare<96>() : kv_attend_prepare<128>();
     if (e != cudaSuccess) {
         (void)cudaGetLastError();
         fastrack_kv_destroy(kv);
@@ -530,24 +555,26 @@ extern "C" int fastrack_kv_read(fastrack_kv* kv, const fastrack_kv_batch* batch,
 
 // ------------------------------------------------------------------------------------------------ attention ----
 
-struct KvPlan { int splits, chunk, row_tiles, units; size_t ml, lse2, unit_l2, total; };   // byte offsets in the workspace, part_o at 0
+#define KV_WAVES 4                      // times that the chunks fill the SMs
+
+struct KvPlan { int rows, splits, chunk, row_tiles, units; size_t ml, lse2, unit_l2, total; };   // byte offsets in the workspace, part_o at 0
 
 static KvPlan kv_plan(const fastrack_kv* kv, const fastrack_kv_batch* b, bool mass)
 {
     const KvShape& S = kv->shape;
     KvPlan p;
     const int64_t rows = (int64_t)b->max_new * S.group;
-    p.row_tiles = (int)((rows + KV_ROWS - 1) / KV_ROWS);
+    p.rows = rows <= 8 ? 8 : 16;
+    p.row_tiles = (int)((rows + p.rows - 1) / p.rows);
     const int64_t ctas = (int64_t)b->n_seqs * S.kv_heads * p.row_tiles;
-    const int64_t want = (8 * (int64_t)kv->num_sms + ctas - 1) / (ctas ? ctas : 1);
-    const int step = S.block_tokens > KV_TILE * KV_WARPS ? S.block_tokens : KV_TILE * KV_WARPS;
+    const int64_t want = (KV_WAVES * 4 * (int64_t)kv->num_sms + ctas - 1) / (ctas ? ctas : 1);
     int64_t chunk = (b->max_len + want - 1) / want;
-    chunk = (chunk + step - 1) / step * step;
-    if (chunk < step) chunk = step;
+    chunk = (chunk + KV_STEP - 1) / KV_STEP * KV_STEP;
+    if (chunk < KV_STEP) chunk = KV_STEP;
     p.chunk = (int)chunk;
     p.splits = (int)((b->max_len + chunk - 1) / chunk);
     if (p.splits < 1) p.splits = 1;
-    p.units = (b->max_len + KV_UNIT - 1) / KV_UNIT;
+    p.units = (b->max_len + KV_HALF - 1) / KV_HALF;
     const size_t all = (size_t)b->total_new * S.q_heads;
     p.ml = p.splits > 1 ? (size_t)p.splits * all * S.head_dim * 4 : 0;
     p.lse2 = p.ml + (p.splits > 1 ? (size_t)p.splits * all * 8 : 0);
@@ -562,14 +589,50 @@ extern "C" size_t fastrack_kv_attention_workspace(const fastrack_kv* kv, const f
     return kv_plan(kv, batch, with_mass != 0).total + 16;
 }
 
+// A launch whose start may overlap the end of the kernel before it in the stream; the kernel waits (griddepcontrol.wait) before it
+// reads anything that one wrote.
+template <class... P, class... Q>
+static void kv_launch_after(cudaStream_t stream, dim3 grid, int threads, void (*kernel)(P...), Q... args)
+{
+    cudaLaunchConfig_t c = {};
+    cudaLaunchAttribute overlap;
+    overlap.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    overlap.val.programmaticStreamSerializationAllowed = 1;
+    c.gridDim = grid;
+    c.blockDim = dim3(threads);
+    c.stream = stream;
+    c.attrs = &overlap;
+    c.numAttrs = 1;
+    (void)cudaLaunchKernelEx(&c, kernel, P(args)...);    // an error stays for cudaGetLastError
+}
+
 template <int D, bool BF>
-static void kv_attend_launch(const fastrack_kv* kv, const KvBatch& B, const KvAttend& A, cudaStream_t stream)
+static void kv_attend_launch(const fastrack_kv* kv, const KvBatch& B, const KvAttend& A, const CUtensorMap& pool, cudaStream_t stream)
 {
     const KvShape& S = kv->shape;
-    const dim3 grid(A.splits, S.kv_heads * A.row_tiles, B.n_seqs);
-    if (kv->config.format == FASTRACK_KV_E4M3) kv_attend_kernel<D, BF, true><<<grid, 32 * KV_WARPS, 0, stream>>>(S, B, A);
-    else kv_attend_kernel<D, BF, false><<<grid, 32 * KV_WARPS, 0, stream>>>(S, B, A);
-    if (A.splits > 1) kv_join_kernel<D, BF><<<dim3((unsigned)(((int64_t)B.max_new * S.q_heads + 7) / 8), B.n_seqs), 256, 0, stream>>>(S, B, A, KV_ROWS);
+    const bool e4 = kv->config.format == FASTRACK_KV_E4M3;
+    auto kernel = A.rows == 8 ? (e4 ? kv_attend_kernel<D, BF, true, 1> : kv_attend_kernel<D, BF, false, 1>)
+                              : (e4 ? kv_attend_kernel<D, BF, true, 2> : kv_attend_kernel<D, BF, false, 2>);
+    kernel<<<dim3(A.splits, S.kv_heads * A.row_tiles, B.n_seqs), 32 * KV_WARPS, kv_attend_smem<D>(A.rows) + 16 * KV_WARPS, stream>>>(S, B, A, pool);
+    if (A.splits > 1)
+        kv_launch_after(stream, dim3((unsigned)(((int64_t)B.max_new * S.q_heads + KV_WARPS - 1) / KV_WARPS), B.n_seqs), 32 * KV_WARPS, kv_join_kernel<D, BF>, S, B, A);
+}
+
+// The pool as a tensor of bytes (head_dim, rows of a page: K of all heads, then V, pages); boxes of 16 rows of one page.
+static int kv_pool_map(fastrack_kv* kv, const KvBatch& B, CUtensorMap* map)
+{
+    const KvShape& S = kv->shape;
+    memset(map, 0, sizeof *map);
+    if (B.pool_pages == 0) return FASTRACK_OK;           // every page is absent
+    const cuuint64_t dims[3] = {(cuuint64_t)S.head_dim, 2ull * S.kv_heads * S.block_tokens, (cuuint64_t)B.pool_pages};
+    const cuuint64_t strides[2] = {(cuuint64_t)S.head_dim, S.page_bytes};
+    const cuuint32_t box[3] = {(cuuint32_t)S.head_dim, KV_HALF, 1}, steps[3] = {1, 1, 1};
+    const CUtensorMapSwizzle swizzle = S.head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : S.head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE;
+    const CUresult r = kv->encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, B.pool, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r == CUDA_SUCCESS) return FASTRACK_OK;
+    kv->last_cuda_error = (int)r;
+    return FASTRACK_ERR_CUDA;
 }
 
 extern "C" int fastrack_kv_attention(fastrack_kv* kv, const fastrack_kv_batch* batch, const fastrack_kv_rows* q, const fastrack_kv_rows* out, float* d_lse,
@@ -583,7 +646,7 @@ extern "C" int fastrack_kv_attention(fastrack_kv* kv, const fastrack_kv_batch* b
     if (mass && (kv_misaligned(d_mass_in, 4) || kv_misaligned(d_mass_out, 4) || mass_stride < (batch->max_len + S.block_tokens - 1) / S.block_tokens)) return FASTRACK_ERR_ARG;
     if (batch->total_new > 0 && (kv_bad_rows(q) || kv_bad_rows(out) || (d_lse && kv_misaligned(d_lse, 4)))) return FASTRACK_ERR_ARG;
     const KvPlan p = kv_plan(kv, batch, mass);
-    if (kv_misaligned(d_workspace, 16) || workspace_bytes < p.total || (int64_t)S.kv_heads * p.row_tiles > 65535) return FASTRACK_ERR_ARG;
+    if (kv_misaligned(d_workspace, 16) || workspace_bytes < p.total) return FASTRACK_ERR_ARG;
     if (int rc = kv_check_device(kv)) return rc;
     const KvBatch B = kv_batch(batch);
     KvAttend A;
@@ -591,6 +654,7 @@ extern "C" int fastrack_kv_attention(fastrack_kv* kv, const fastrack_kv_batch* b
     char* const ws = (char*)d_workspace;
     A.lse = d_lse;
     A.window = window;
+    A.rows = p.rows;
     A.splits = p.splits;
     A.chunk = p.chunk;
     A.row_tiles = p.row_tiles;
@@ -608,16 +672,19 @@ extern "C" int fastrack_kv_attention(fastrack_kv* kv, const fastrack_kv_batch* b
         A.q = kv_rows(q);
         A.out = kv_rows(out);
         const bool bf = kv->config.dtype == FASTRACK_KV_BF16;
+        CUtensorMap pool;
+        if (int rc = kv_pool_map(kv, B, &pool)) return rc;
         switch (S.head_dim) {
-        case 64: bf ? kv_attend_launch<64, true>(kv, B, A, st) : kv_attend_launch<64, false>(kv, B, A, st); break;
-        case 96: bf ? kv_attend_launch<96, true>(kv, B, A, st) : kv_attend_launch<96, false>(kv, B, A, st); break;
-        default: bf ? kv_attend_launch<128, true>(kv, B, A, st) : kv_attend_launch<128, false>(kv, B, A, st); break;
+        case 64: bf ? kv_attend_launch<64, true>(kv, B, A, pool, st) : kv_attend_launch<64, false>(kv, B, A, pool, st); break;
+        case 96: bf ? kv_attend_launch<96, true>(kv, B, A, pool, st) : kv_attend_launch<96, false>(kv, B, A, pool, st); break;
+        default: bf ? kv_attend_launch<128, true>(kv, B, A, pool, st) : kv_attend_launch<128, false>(kv, B, A, pool, st); break;
         }
         launches += 1 + (p.splits > 1);
     }
     if (mass && batch->max_len > 0) {
         const int blocks = (batch->max_len + S.block_tokens - 1) / S.block_tokens;
-        kv_mass_kernel<<<dim3((blocks + 7) / 8, S.kv_heads, batch->n_seqs), 256, 0, st>>>(S, B, A, 4);
+        if ((int64_t)batch->max_new * S.group <= KV_MASS_ROWS) kv_launch_after(st, dim3((blocks + 255) / 256, S.kv_heads, batch->n_seqs), 256, kv_mass_kernel<true>, S, B, A, 4);
+        else kv_launch_after(st, dim3((blocks + 7) / 8, S.kv_heads, batch->n_seqs), 256, kv_mass_kernel<false>, S, B, A, 4);
         launches++;
     }
     return kv_launched(kv, launches);

@@ -1,25 +1,32 @@
 // fastrack_kv_attend.cuh -- attention of few query rows over the 8-bit cache: the kernel that single tokens take.
 #pragma once
+#include <cuda.h>
 #include "fastrack_kv_device.cuh"
 
 #define KV_WARPS 4
-#define KV_ROWS 16          // (query, head of the group) rows of a CTA: the M of one matrix instruction
-#define KV_TILE 16          // tokens of a warp's step, inside one block
-#define KV_UNIT 16          // tokens whose weight is written down together
+#define KV_HALF 16          // tokens that lie inside one block for sure
+#define KV_TILE 32          // tokens of a warp's step: two halves
 #define KV_LAZY 4.0f        // a running maximum is raised only when exceeded by this many powers of two
 // Weights enter the second product as f16, times V's scale over its reference (at most 1), times this: 2^4 * 2^11 stays below
 // f16's largest, and a weight down to 2^-25 of the largest keeps all 11 bits, so that a token of little weight whose values are
 // orders above the others' is not lost.
 #define KV_P_SCALE 2048.0f
 
+// A call's work is cut into chunks of each span, a CTA for each: equal pieces of whatever length sequences have, several times as many as
+// the SMs hold, so that one CTA's start and end pass under the others' loads.  (Tried instead: CTAs that stay and take equal runs of
+// one line of all work; every one of them starts and ends at the same time, and 61 sequences of up to 4096 tokens took 148 us
+// against 98.)
+#define KV_STEP (KV_TILE * KV_WARPS)
+
 struct KvAttend {
     KvRows q, out;
     float* lse;             // natural, or NULL
     int window;
-    int splits, chunk;      // chunks of the span, tokens of a chunk (a multiple of the block)
+    int rows;               // of a CTA: 8 or 16
+    int splits, chunk;      // chunks of the span, tokens of a chunk (a multiple of KV_STEP and of the block)
     int row_tiles, units;   // units: per sequence, for weights
     float* part_o;          // [splits][total_new * q_heads][head_dim]
-    float* part_ml;         // [splits][total_new * q_heads][2]
+    float* part_ml;         // [splits][total_new * q_heads][2]: running maximum and sum
     float* lse2;            // [total_new * q_heads], base 2
     float* unit_l2;         // [n_seqs][kv_heads][units][max_new * group]: log2 of the sum of exponentials of a unit; NULL without weights
     const float* mass_in;
@@ -39,28 +46,69 @@ __device__ __forceinline__ float kv_log2(float x)
     asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ void kv_mma(float* d, const uint32_t* a, uint32_t b0, uint32_t b1)
+__device__ __forceinline__ void kv_mma(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const uint32_t* b)
 {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]));
+}
+__device__ __forceinline__ uint32_t kv_transpose(uint32_t x)                 // an 8 x 8 matrix of f16 held by the warp
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 
-// Two codes as two f16, exactly: of bytes J and K of the eight in (lo, hi).
+// Codes as pairs of f16, exactly.
+//   e4m3: every code is an f16 number; there is an instruction that widens two.
 //   int8: 0x64 in front of a byte u is the f16 number 1024 + u; with the code's sign bit flipped u = code + 128, so that
 //         subtracting 1152 leaves the code.
-//   e4m3: sign, exponent and fraction moved to their places in an f16, which has 8 more in its exponent bias: code * 2^-8.
-//         Exact for subnormal codes too.  No code becomes a NaN.  The 2^8 is made good in the scale (KV_CODE_SCALE).
-template <bool E4M3, int J, int K> __device__ __forceinline__ uint32_t kv_two(uint32_t lo, uint32_t hi)
+__device__ __forceinline__ uint32_t kv_widen_e4m3(uint32_t two)
 {
-    if (E4M3) {
-        const uint32_t p = __byte_perm(lo, hi, J << 4 | K << 12);
-        return (p & 0x80008000u) | ((p >> 1) & 0x3f803f80u);
-    }
-    const uint32_t p = (__byte_perm(lo, hi, J | K << 8) & 0x00ff00ffu) ^ 0x64806480u;
+    uint32_t d;
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t}" : "=r"(d) : "r"(two));
+    return d;
+}
+__device__ __forceinline__ uint32_t kv_minus_1152(uint32_t p)
+{
     const __half2 h = __hsub2(*(const __half2*)&p, __half2half2(__ushort_as_half(0x6480)));
     return *(const uint32_t*)&h;
 }
-template <bool E4M3> __device__ __forceinline__ float kv_code_scale() { return E4M3 ? 256.f : 1.f; }
+// bytes (0, 1) and (2, 3) of w
+template <bool E4M3> __device__ __forceinline__ void kv_widen4(uint32_t w, uint32_t& b0, uint32_t& b1)
+{
+    if (E4M3) {
+        b0 = kv_widen_e4m3(w);
+        b1 = kv_widen_e4m3(w >> 16);
+    } else {
+        const uint32_t u = w ^ 0x80808080u;
+        b0 = kv_minus_1152(__byte_perm(u, 0x64646464u, 0x4140));
+        b1 = kv_minus_1152(__byte_perm(u, 0x64646464u, 0x4342));
+    }
+}
+// byte i of w and of x, for i = 0 .. 3
+template <bool E4M3> __device__ __forceinline__ void kv_widen_pairs(uint32_t w, uint32_t x, uint32_t* d)
+{
+    const uint32_t lo = __byte_perm(w, x, 0x5140), hi = __byte_perm(w, x, 0x7362);
+    kv_widen4<E4M3>(lo, d[0], d[1]);
+    kv_widen4<E4M3>(hi, d[2], d[3]);
+}
+
+// 16 rows of head_dim bytes from the pool, as tensor (head_dim, rows of a page, pages), to shared memory
+__device__ __forceinline__ void kv_tma(uint32_t smem, const CUtensorMap* map, int row, int page, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(smem), "l"(map), "r"(0), "r"(row), "r"(page), "r"(bar) : "memory");
+}
+// Whether the barrier's phase of this parity has ended, after waiting for it a bounded number of times (each attempt gives up by
+// itself after a while; in practice the first or second succeeds).
+__device__ __forceinline__ bool kv_wait(uint32_t bar, uint32_t parity)
+{
+    uint32_t done = 0;
+    for (int attempt = 0; attempt < 1 << 16 && !done; attempt++)
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
+}
 
 // 2^e with 2^e <= x < 2^(e+1) for finite x > 0 (1 for zero, the largest for what is not finite): dividing by it is exact.
 __device__ __forceinline__ float kv_power_below(uint32_t abs_bits)
@@ -74,43 +122,375 @@ __device__ __forceinline__ float kv_power_below(uint32_t abs_bits)
 // An infinite scale counts as NaN, so that a block with one shows in every answer that sees it.
 __device__ __forceinline__ float kv_finite(float x) { return fabsf(x) < KV_INF ? x : __int_as_float(0x7fffffff); }
 
-// One CTA: 16 rows of one kv head of one sequence, one chunk of the tokens they see.  Each of the four warps takes every fourth
-// tile of 16 tokens with statistics and an accumulator of its own; they are joined in shared memory at the end.
-//
-// In the matrix instructions the channels that a lane holds are permuted so that what it needs of K is 16 (8 at 96 channels)
-// bytes in a row of one token, and of V head_dim / 8 bytes in a row of four tokens: codes go from memory to registers in whole
-// sectors, are widened there and enter the product, without passing through shared memory.
-template <int D, bool BF, bool E4M3>
-__global__ void __launch_bounds__(32 * KV_WARPS) kv_attend_kernel(const KvShape S, const KvBatch B, const KvAttend A)
+// How a warp computes 16 tokens.  K and V take the side of the matrix instruction m16n8k16 that is 16 wide, and the rows, of which a
+// single token has few, the side of 8:
+//     S^T[16 tokens, 8 rows] += K[16 tokens, 16 channels] q^T,     O^T[16 channels, 8 rows] += V^T[16 channels, 16 tokens] P^T.
+// The channels may be permuted at will (those of q and of the answer alike), and so may the tokens of a half; both are, so that a
+// lane's share of K and V is made of whole runs of bytes and is read from shared memory without bank conflicts:
+//     K: lane (g, c) holds, of tokens token(g) and token(g) + 8, every fourth run of KB bytes from run c on;
+//     V: of tokens token(2c), token(2c+1), token(2c) + 8, token(2c+1) + 8, head_dim / 8 bytes: 8 or 16 in a row, at 96 channels 8 and 4.
+// The codes come by tensor copies, which turn the 16-byte pieces of a row around by the row's number (at 64 and 128 channels; a row of 96
+// bytes needs none): with token(g) = 0 5 2 7 4 1 6 3 the eight lanes of a phase read eight different pieces.
+// A warp has room for one tile: the next tile's K is sent for as soon as this one's is read, its V likewise, so that half a tile or
+// more is on its way at any time; with 16 warps that is more than the 35 KB that an SM needs in flight, and the room that
+// further stages would take goes to warps.
+template <int D> struct KvTile {
+    static constexpr int KB = D % 64 == 0 ? 16 : 8, KRUNS = D / (4 * KB);
+    static constexpr int STEPS = D / 16;                                     // of QK^T along the channels, and tiles of 16 channels of O
+    static constexpr int VW = D / 32;                                        // words of V per token and lane
+    static constexpr int BYTES = KV_HALF * D;                                // K, or V, of a half
+    static constexpr int STAGE = (4 * BYTES + 1023) / 1024 * 1024;           // K of both halves, V of both
+    __device__ static int k_channel(int step, int c) { return ((step * 4 / KB) * 4 + c) * KB + step * 4 % KB; }
+    __device__ static int v_channel(int g, int i) { return D != 96 ? g * (D / 8) + i : i < 8 ? 8 * g + i : 64 + 4 * g + i - 8; }
+    __device__ static int token(int g) { return (g & 6) ^ ((g & 1) * 5); }
+    // byte `at` (in a piece of 16 that does not cross) of a row
+    __device__ static int place(int row, int at)
+    {
+        return row * D + (D == 128 ? at ^ (row & 7) << 4 : D == 64 ? at ^ (row >> 1 & 3) << 4 : at);
+    }
+};
+
+template <int D> __host__ __device__ constexpr int kv_attend_smem(int rows)
 {
-    constexpr int PB = D % 64 == 0 ? 16 : 8, PW = PB / 4, STEPS = D / 16, NT = D / 8, VW = D / 32;
+    const int tiles = KV_WARPS * KvTile<D>::STAGE, join = KV_WARPS * rows * (D + 4) * 4 + KV_WARPS * rows * 8;
+    return tiles > join ? tiles : join;                                      // and 16 bytes of barriers per warp behind
+}
+
+// What a warp carries along its tokens.
+template <int D, int NR> struct KvState {
+    uint32_t qb[NR][D / 16][2];                          // queries as f16: row 8 r + g
+    float factor[NR][2];                                 // of the scores of rows 8 r + 2 c + e
+    float m[NR][2], l[NR][2];
+    float o[NR][D / 16][4];
+    float vref, vinv;                                    // power of two that V's scales are measured by (o is in its units), KV_P_SCALE over it
+};
+
+// Scores in base 2 and times their scales, -inf where hidden: raises the running maxima where one is exceeded by far, turns the
+// scores into weights (unrounded; their sums go to l) and leaves the rows' bases.
+template <int D, int NR, int HALVES>
+__device__ __forceinline__ void kv_weigh(KvState<D, NR>& W, float (&s)[HALVES][NR][4], float (&base)[NR][2])
+{
+    bool higher = false;
+#pragma unroll
+    for (int r = 0; r < NR; r++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+            float top = fmaxf(s[0][r][e], s[0][r][2 + e]);
+            if (HALVES == 2) top = fmaxf(top, fmaxf(s[HALVES - 1][r][e], s[HALVES - 1][r][2 + e]));
+            base[r][e] = top;
+            higher |= top > W.m[r][e] + KV_LAZY;
+        }
+    if (__any_sync(0xffffffffu, higher)) {
+#pragma unroll
+        for (int r = 0; r < NR; r++)
+#pragma unroll
+            for (int e = 0; e < 2; e++) {
+                float top = base[r][e];
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                top = fmaxf(W.m[r][e], top);
+                const float f = top == -KV_INF ? 1.f : kv_exp2(W.m[r][e] - top);
+                W.m[r][e] = top;
+                W.l[r][e] *= f;
+#pragma unroll
+                for (int i = 0; i < D / 16; i++) { W.o[r][i][e] *= f; W.o[r][i][2 + e] *= f; }
+            }
+    }
+#pragma unroll
+    for (int r = 0; r < NR; r++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+            base[r][e] = W.m[r][e] == -KV_INF ? 0.f : W.m[r][e];
+#pragma unroll
+            for (int h = 0; h < HALVES; h++) {
+                s[h][r][e] = kv_exp2(s[h][r][e] - base[r][e]);
+                s[h][r][2 + e] = kv_exp2(s[h][r][2 + e] - base[r][e]);
+                W.l[r][e] += s[h][r][e] + s[h][r][2 + e];
+            }
+        }
+}
+
+// log2 of the rows' sums of the weights of halves h0 .. h1 - 1, to out[row]
+template <int D, int NR, int HALVES>
+__device__ __forceinline__ void kv_note(const float (&s)[HALVES][NR][4], const float (&base)[NR][2], int h0, int h1, float* out, int rows_left, int g, int c)
+{
+#pragma unroll
+    for (int r = 0; r < NR; r++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+            float sum = 0.f;
+#pragma unroll
+            for (int h = 0; h < HALVES; h++)
+                if (h >= h0 && h < h1) sum += s[h][r][e] + s[h][r][2 + e];
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            const int at = 8 * r + 2 * c + e;
+            if (g == 0 && at < rows_left) out[at] = kv_log2(sum) + base[r][e];
+        }
+}
+
+template <int D, int NR> __device__ __forceinline__ void kv_refer(KvState<D, NR>& W, float vs)
+{
+    if (vs > W.vref) {                                   // the warp as a whole
+        const float next = 4.f * kv_power_below(__float_as_uint(vs)), f = W.vref / next;
+#pragma unroll
+        for (int r = 0; r < NR; r++)
+#pragma unroll
+            for (int i = 0; i < D / 16; i++) { W.o[r][i][0] *= f; W.o[r][i][1] *= f; W.o[r][i][2] *= f; W.o[r][i][3] *= f; }
+        W.vref = next;
+        W.vinv = KV_P_SCALE / next;
+    }
+}
+
+// One tile of full blocks.  RAGGED: some of its tokens are hidden from some rows, or a half is not there; hidden has a bit for each of s.
+// k_wait and v_wait wait for K and V, k_read and v_read are called when they have been read.
+template <int D, bool E4M3, int NR, bool RAGGED, class KWait, class KRead, class VWait, class VRead>
+__device__ __forceinline__ void kv_tile(KvState<D, NR>& W, const uint8_t* slot, int t0, const float (&ks)[2], const float (&vs)[2], const bool (&there)[2],
+                                        const int (&place)[NR][2], int window, float* unit_out, int unit_stride, bool one_unit, int rows_left, int lane,
+                                        KWait k_wait, KRead k_read, VWait v_wait, VRead v_read)
+{
+    using T = KvTile<D>;
+    const int g = lane >> 2, c = lane & 3, token = T::token(g);
+    float s[2][NR][4];
+#pragma unroll
+    for (int h = 0; h < 2; h++)
+#pragma unroll
+        for (int r = 0; r < NR; r++) s[h][r][0] = s[h][r][1] = s[h][r][2] = s[h][r][3] = 0.f;
+    bool fine = k_wait();
+#pragma unroll
+    for (int p = 0; p < T::KRUNS; p++)
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            uint32_t w[2][T::KB / 4];
+#pragma unroll
+            for (int up = 0; up < 2; up++) {
+                const uint8_t* const src = slot + h * T::BYTES + T::place(8 * up + token, (p * 4 + c) * T::KB);
+                if (T::KB == 16) *(uint4*)w[up] = *(const uint4*)src;
+                else *(uint2*)w[up] = *(const uint2*)src;
+            }
+#pragma unroll
+            for (int i = 0; i < T::KB / 4; i++) {
+                uint32_t a[4];
+                kv_widen4<E4M3>(w[0][i], a[0], a[2]);
+                kv_widen4<E4M3>(w[1][i], a[1], a[3]);
+#pragma unroll
+                for (int r = 0; r < NR; r++) kv_mma(s[h][r], a[0], a[1], a[2], a[3], W.qb[r][p * (T::KB / 4) + i]);
+            }
+        }
+    k_read();
+    uint32_t hidden = 0;
+#pragma unroll
+    for (int h = 0; h < 2; h++)
+#pragma unroll
+        for (int r = 0; r < NR; r++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                s[h][r][i] *= ks[h] * W.factor[r][i & 1];
+                if (RAGGED) {
+                    const int t = t0 + KV_HALF * h + 8 * (i >> 1) + token, at = place[r][i & 1];
+                    if (t > at || (window > 0 && t <= at - window) || !there[h]) {
+                        s[h][r][i] = -KV_INF;
+                        hidden |= 1u << (8 * r + 4 * h + i);
+                    }
+                }
+            }
+    float base[NR][2];
+    kv_weigh<D, NR, 2>(W, s, base);
+    if (unit_out) {
+        if (one_unit) kv_note<D, NR, 2>(s, base, 0, 2, unit_out, rows_left, g, c);
+        else {
+            kv_note<D, NR, 2>(s, base, 0, 1, unit_out, rows_left, g, c);
+            if (there[1]) kv_note<D, NR, 2>(s, base, 1, 2, unit_out + unit_stride, rows_left, g, c);
+        }
+    }
+    kv_refer<D, NR>(W, fmaxf(vs[0], vs[1]));
+    fine = v_wait() && fine;
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+        const float vf = !fine ? __int_as_float(0x7fffffff) : W.vref > 0.f ? vs[h] * W.vinv : vs[h];     // bytes that never came: NaN
+        uint32_t pb[NR][2];
+#pragma unroll
+        for (int r = 0; r < NR; r++)
+#pragma unroll
+            for (int up = 0; up < 2; up++) {
+                float x = s[h][r][2 * up] * vf, y = s[h][r][2 * up + 1] * vf;
+                if (RAGGED) {                            // a masked token's scale, whatever it is, does not count
+                    if (hidden >> (8 * r + 4 * h + 2 * up) & 1) x = 0.f;
+                    if (hidden >> (8 * r + 4 * h + 2 * up + 1) & 1) y = 0.f;
+                }
+                pb[r][up] = kv_transpose(kv_pack<false>(x, y));
+            }
+        uint32_t vw[4][T::VW];
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const uint8_t* const src = slot + (2 + h) * T::BYTES;
+            const int row = T::token(2 * c + (j & 1)) + 8 * (j >> 1);
+            if (D == 128) *(uint4*)vw[j] = *(const uint4*)(src + T::place(row, 16 * g));
+            else *(uint2*)vw[j] = *(const uint2*)(src + T::place(row, 8 * g));
+            if (D == 96) vw[j][T::VW - 1] = *(const uint32_t*)(src + T::place(row, 64 + 4 * g));
+            if (RAGGED && !there[h])
+#pragma unroll
+                for (int w = 0; w < T::VW; w++) vw[j][w] = 0u;
+        }
+#pragma unroll
+        for (int w = 0; w < T::VW; w++) {
+            uint32_t a[4], b[4];
+            kv_widen_pairs<E4M3>(vw[0][w], vw[1][w], a);
+            kv_widen_pairs<E4M3>(vw[2][w], vw[3][w], b);
+#pragma unroll
+            for (int r = 0; r < NR; r++) {
+                kv_mma(W.o[r][2 * w], a[0], a[1], b[0], b[1], pb[r]);
+                kv_mma(W.o[r][2 * w + 1], a[2], a[3], b[2], b[3], pb[r]);
+            }
+        }
+    }
+    v_read();
+}
+
+// 16 tokens of the unfinished block: 16-bit values, tokens behind the last as zeros.  bf16 goes to f16 by a power of two near the
+// largest of the 16 tokens; it is looked for first, and the values are read again (once per sequence and head, from L1).
+template <int D, bool BF, int NR>
+__device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* k, const uint16_t* v, int t0, int len, const int (&place)[NR][2], int window,
+                                             float* unit_out, int rows_left, int lane)
+{
+    using T = KvTile<D>;
+    constexpr int STEPS = D / 16;
+    const int g = lane >> 2, c = lane & 3;
+    float scale[2] = {1.f, 1.f};
+    if (BF)
+        for (int which = 0; which < 2; which++) {
+            const uint16_t* const src = which ? v : k;
+            uint32_t amax = 0;
+            for (int i = lane; i < KV_HALF * D / 8; i += 32) {
+                if (t0 + i / (D / 8) >= len) break;
+                const uint4 w = *(const uint4*)(src + 8 * i);
+                amax = max(max(max(amax, max(w.x << 16 & 0x7fffffffu, w.x & 0x7fff0000u)), max(w.y << 16 & 0x7fffffffu, w.y & 0x7fff0000u)),
+                           max(max(w.z << 16 & 0x7fffffffu, w.z & 0x7fff0000u), max(w.w << 16 & 0x7fffffffu, w.w & 0x7fff0000u)));
+            }
+            scale[which] = kv_power_below(__reduce_max_sync(0xffffffffu, amax));
+        }
+    const float ki = 1.f / scale[0], vi = 1.f / scale[1];
+    auto narrow = [](uint32_t w, float inv) {
+        if (!BF) return w;
+        const float2 x = kv_unpack<true>(w);
+        return kv_pack<false>(x.x * inv, x.y * inv);
+    };
+    float s[1][NR][4], base[NR][2];
+#pragma unroll
+    for (int r = 0; r < NR; r++) s[0][r][0] = s[0][r][1] = s[0][r][2] = s[0][r][3] = 0.f;
+#pragma unroll
+    for (int i = 0; i < STEPS; i++) {
+        const uint2 lo = t0 + g < len ? *(const uint2*)(k + g * D + T::k_channel(i, c)) : make_uint2(0, 0);
+        const uint2 hi = t0 + 8 + g < len ? *(const uint2*)(k + (8 + g) * D + T::k_channel(i, c)) : make_uint2(0, 0);
+#pragma unroll
+        for (int r = 0; r < NR; r++) kv_mma(s[0][r], narrow(lo.x, ki), narrow(hi.x, ki), narrow(lo.y, ki), narrow(hi.y, ki), W.qb[r][i]);
+    }
+    uint32_t hidden = 0;
+#pragma unroll
+    for (int r = 0; r < NR; r++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            s[0][r][i] *= scale[0] * W.factor[r][i & 1];
+            const int t = t0 + 8 * (i >> 1) + g, at = place[r][i & 1];
+            if (t > at || (window > 0 && t <= at - window)) {
+                s[0][r][i] = -KV_INF;
+                hidden |= 1u << (4 * r + i);
+            }
+        }
+    kv_weigh<D, NR, 1>(W, s, base);
+    if (unit_out) kv_note<D, NR, 1>(s, base, 0, 1, unit_out, rows_left, g, c);
+    kv_refer<D, NR>(W, scale[1]);
+    const float vf = scale[1] * W.vinv;
+    uint32_t pb[NR][2];
+#pragma unroll
+    for (int r = 0; r < NR; r++)
+#pragma unroll
+        for (int up = 0; up < 2; up++)
+            pb[r][up] = kv_transpose(kv_pack<false>(hidden >> (4 * r + 2 * up) & 1 ? 0.f : s[0][r][2 * up] * vf, hidden >> (4 * r + 2 * up + 1) & 1 ? 0.f : s[0][r][2 * up + 1] * vf));
+#pragma unroll
+    for (int i = 0; i < STEPS; i++) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int t = 2 * c + (j & 1) + (j >> 1) * 8;
+            w[j] = t0 + t < len ? narrow(*(const uint32_t*)(v + t * D + T::v_channel(g, 2 * i)), vi) : 0u;
+        }
+#pragma unroll
+        for (int r = 0; r < NR; r++)
+            kv_mma(W.o[r][i], __byte_perm(w[0], w[1], 0x5410), __byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x5410), __byte_perm(w[2], w[3], 0x7632), pb[r]);
+    }
+}
+
+// One CTA: 8 NR rows of one kv head of one sequence, one chunk of the tokens they see.  Each of the four warps takes every fourth
+// tile with statistics and an accumulator of its own; they are joined in shared memory at the end.
+template <int D, bool BF, bool E4M3, int NR>
+__global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? 4 : 3) kv_attend_kernel(const KvShape S, const KvBatch B, const KvAttend A,
+                                                                                  const __grid_constant__ CUtensorMap pool)
+{
+    using T = KvTile<D>;
+    constexpr int STEPS = T::STEPS, ROWS = 8 * NR;
+    extern __shared__ __align__(1024) uint8_t kv_smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
-    const int chunk = blockIdx.x, kh = blockIdx.y % S.kv_heads, tile_row = blockIdx.y / S.kv_heads * KV_ROWS, seq = blockIdx.z;
+    const int chunk = blockIdx.x, kh = blockIdx.y % S.kv_heads, tile_row = blockIdx.y / S.kv_heads * ROWS, seq = blockIdx.z;
+    asm volatile("griddepcontrol.launch_dependents;");   // the join may take its place; it waits for this kernel's end
     const KvSeq q = kv_seq(S, B, seq);
-    const KvSpan span = kv_span(S, q, A.window, tile_row, KV_ROWS);
-    if (tile_row >= q.n * S.group) return;
+    const KvSpan span = kv_span(S, q, A.window, tile_row, ROWS);
+    const int rows = q.n * S.group;
+    if (tile_row >= rows) return;
     const int begin = span.begin + chunk * A.chunk, end = min(span.end, begin + A.chunk);
     if (begin >= end && chunk > 0) return;
 
-    // queries: two rows per lane, as f16; a bf16 row is first divided by a power of two near its largest magnitude
-    uint32_t qa[STEPS][4];
-    float row_scale[2];
-    int place[2];                                       // where the row's query stands; -1 for rows behind the last
+    // tiles begin + 32 (warp + 4 i) of full blocks; a half behind the last full block, or on an absent page, is not there
+    uint8_t* const slot = kv_smem + warp * T::STAGE;
+    const uint32_t slot_at = (uint32_t)__cvta_generic_to_shared(slot), bars = (uint32_t)__cvta_generic_to_shared(kv_smem + kv_attend_smem<D>(ROWS) + 16 * warp);
+    const int tail_begin = q.full << S.block_shift, full_end = min(end, tail_begin);
+    const int32_t* const table = B.table + (int64_t)seq * B.table_stride;
+    if (lane == 0) {
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars) : "memory");
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + 8) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    auto page_of = [&](int t) {
+        const int b = t >> S.block_shift, p = t < full_end && b < B.table_stride ? __ldg(table + b) : -1;
+        return p < B.pool_pages ? p : -1;
+    };
+    // K (which = 0) or V (1) of the tile: lane 0 sends for the halves that are there; the barrier's phase ends when they have arrived
+    auto fetch = [&](int which, int t0, int2 pages) {
+        if (lane == 0 && t0 < full_end) {
+            const uint32_t bar = bars + 8 * which, at = slot_at + 2 * which * T::BYTES;
+            const int row = (which * S.kv_heads + kh) * S.block_tokens, bytes = ((pages.x >= 0) + (pages.y >= 0)) * T::BYTES;
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+            if (pages.x >= 0) kv_tma(at, &pool, row + (t0 & (S.block_tokens - 1)), pages.x, bar);
+            if (pages.y >= 0) kv_tma(at + T::BYTES, &pool, row + ((t0 + KV_HALF) & (S.block_tokens - 1)), pages.y, bar);
+        }
+    };
+    auto scales_of = [&](int page) { return page >= 0 ? __ldg((const float2*)(kv_scales(S, B, page) + 2 * kh)) : make_float2(0.f, 0.f); };
+    constexpr int STRIDE = KV_TILE * KV_WARPS;
+    const int first = begin + KV_TILE * warp;
+    int2 pages = make_int2(page_of(first), page_of(first + KV_HALF)), next = make_int2(page_of(first + STRIDE), page_of(first + STRIDE + KV_HALF));
+    fetch(0, first, pages);
+    fetch(1, first, pages);
+    float2 scale[2] = {scales_of(pages.x), scales_of(pages.y)};
+
+    // queries: row g (and g + 8) of a lane, as f16; a bf16 row is first divided by a power of two near its largest magnitude.  The
+    // products come out with rows 2c and 2c + 1 in a lane: their factors and places.
+    KvState<D, NR> W;
+    int place[NR][2];
 #pragma unroll
-    for (int r = 0; r < 2; r++) {
-        const int row = tile_row + g + 8 * r;
-        const bool valid = row < q.n * S.group;
-        const int token = row / S.group, head = kh * S.group + row % S.group;
-        place[r] = valid ? q.len - q.n + token : -1;
-        const uint16_t* src = (const uint16_t*)A.q.data + (q.start + token) * A.q.token_stride + head * A.q.head_stride;
-        uint2 raw[STEPS];
+    for (int r = 0; r < NR; r++) {
+        const int row = tile_row + 8 * r + g;
+        const bool valid = row < rows;
+        const uint16_t* src = (const uint16_t*)A.q.data + (q.start + row / S.group) * A.q.token_stride + (kh * S.group + row % S.group) * A.q.head_stride;
         uint32_t amax = 0;
 #pragma unroll
         for (int s = 0; s < STEPS; s++) {
-            raw[s] = valid ? *(const uint2*)(src + ((s / PW) * 4 + c) * PB + (s % PW) * 4) : make_uint2(0, 0);
+            const uint2 raw = valid ? *(const uint2*)(src + T::k_channel(s, c)) : make_uint2(0, 0);
+            W.qb[r][s][0] = raw.x;
+            W.qb[r][s][1] = raw.y;
             if (BF) {
-                amax = max(amax, max(raw[s].x << 16 & 0x7fffffffu, raw[s].x & 0x7fff0000u));
-                amax = max(amax, max(raw[s].y << 16 & 0x7fffffffu, raw[s].y & 0x7fff0000u));
+                amax = max(amax, max(raw.x << 16 & 0x7fffffffu, raw.x & 0x7fff0000u));
+                amax = max(amax, max(raw.y << 16 & 0x7fffffffu, raw.y & 0x7fff0000u));
             }
         }
         float p = 1.f;
@@ -118,223 +498,82 @@ __global__ void __launch_bounds__(32 * KV_WARPS) kv_attend_kernel(const KvShape 
             amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
             amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
             p = kv_power_below(amax);
-        }
-        row_scale[r] = p * S.scale_log2 * kv_code_scale<E4M3>();
-        const float inv = 1.f / p;
+            const float inv = 1.f / p;
 #pragma unroll
-        for (int s = 0; s < STEPS; s++) {
-            if (BF) {
-                const float2 x = kv_unpack<true>(raw[s].x), y = kv_unpack<true>(raw[s].y);
-                qa[s][r] = kv_pack<false>(x.x * inv, x.y * inv);
-                qa[s][2 + r] = kv_pack<false>(y.x * inv, y.y * inv);
-            } else {
-                qa[s][r] = raw[s].x;
-                qa[s][2 + r] = raw[s].y;
-            }
-        }
-    }
-    const int last_row = min(tile_row + KV_ROWS, q.n * S.group) - 1;
-    const int see_all = q.len - q.n + tile_row / S.group;                    // tokens up to here are seen by every row (without a window)
-    const int low_all = A.window > 0 ? q.len - q.n + last_row / S.group - A.window : -1;   // tokens behind here are in every row's window
-
-    float o[NT][4];
-#pragma unroll
-    for (int i = 0; i < NT; i++) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    float m[2] = {-KV_INF, -KV_INF}, l[2] = {0.f, 0.f};
-    float vref = 0.f;                                    // power of two that V's scales are measured by: o is in its units
-
-    for (int t0 = begin + KV_TILE * warp; t0 < end; t0 += KV_TILE * KV_WARPS) {
-        const int block = t0 >> S.block_shift, at = t0 & (S.block_tokens - 1);
-        const bool tail = block == q.full;
-        uint32_t kb[2][STEPS][2], vb[NT][2];
-        float ks, vs;
-        if (!tail) {
-            const int page = kv_page(B, seq, block);
-            if (page < 0) continue;
-            const float2 sc = *(const float2*)(kv_scales(S, B, page) + 2 * kh);
-            ks = kv_finite(sc.x);
-            vs = kv_finite(sc.y);
-            const uint8_t* kp = B.pool + (uint64_t)page * S.page_bytes + ((uint64_t)kh * S.block_tokens + at) * D;
-            const uint8_t* vp = kp + S.codes_bytes;
-            uint32_t kw[2][STEPS], vw[4][VW];
-#pragma unroll
-            for (int nt = 0; nt < 2; nt++)
-#pragma unroll
-                for (int p = 0; p < STEPS / PW; p++) {
-                    const uint8_t* src = kp + (8 * nt + g) * D + (p * 4 + c) * PB;
-                    if (PB == 16) *(uint4*)&kw[nt][p * PW] = __ldg((const uint4*)src);
-                    else *(uint2*)&kw[nt][p * PW] = __ldg((const uint2*)src);
-                }
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const uint8_t* src = vp + (2 * c + (j & 1) + (j >> 1) * 8) * D + g * (D / 8);
-                if (VW == 4) *(uint4*)vw[j] = __ldg((const uint4*)src);
-                else if (VW == 2) *(uint2*)vw[j] = __ldg((const uint2*)src);
-                else
-#pragma unroll
-                    for (int w = 0; w < VW; w++) vw[j][w] = __ldg((const uint32_t*)src + w);
-            }
-#pragma unroll
-            for (int nt = 0; nt < 2; nt++)
-#pragma unroll
-                for (int s = 0; s < STEPS; s++) {
-                    kb[nt][s][0] = kv_two<E4M3, 0, 1>(kw[nt][s], 0);
-                    kb[nt][s][1] = kv_two<E4M3, 2, 3>(kw[nt][s], 0);
-                }
-#pragma unroll
-            for (int w = 0; w < VW; w++) {
-                vb[4 * w][0] = kv_two<E4M3, 0, 4>(vw[0][w], vw[1][w]); vb[4 * w][1] = kv_two<E4M3, 0, 4>(vw[2][w], vw[3][w]);
-                vb[4 * w + 1][0] = kv_two<E4M3, 1, 5>(vw[0][w], vw[1][w]); vb[4 * w + 1][1] = kv_two<E4M3, 1, 5>(vw[2][w], vw[3][w]);
-                vb[4 * w + 2][0] = kv_two<E4M3, 2, 6>(vw[0][w], vw[1][w]); vb[4 * w + 2][1] = kv_two<E4M3, 2, 6>(vw[2][w], vw[3][w]);
-                vb[4 * w + 3][0] = kv_two<E4M3, 3, 7>(vw[0][w], vw[1][w]); vb[4 * w + 3][1] = kv_two<E4M3, 3, 7>(vw[2][w], vw[3][w]);
-            }
-        } else {
-            // the unfinished block: 16-bit values, tokens behind the last as zeros; bf16 goes to f16 by a power of two near the tile's largest
-            const uint16_t* kp = (const uint16_t*)B.tail + (uint64_t)seq * S.tail_values + ((uint64_t)kh * 2 * S.block_tokens + at) * D;
-            const uint16_t* vp = kp + (uint64_t)S.block_tokens * D;
-            uint32_t kmax = 0, vmax = 0, raw[4][NT / 2];
-#pragma unroll
-            for (int nt = 0; nt < 2; nt++)
-#pragma unroll
-                for (int s = 0; s < STEPS; s++) {
-                    const bool there = t0 + 8 * nt + g < q.len;
-                    const uint2 w = there ? *(const uint2*)(kp + (8 * nt + g) * D + ((s / PW) * 4 + c) * PB + (s % PW) * 4) : make_uint2(0, 0);
-                    kb[nt][s][0] = w.x;
-                    kb[nt][s][1] = w.y;
-                    if (BF) {
-                        kmax = max(kmax, max(w.x << 16 & 0x7fffffffu, w.x & 0x7fff0000u));
-                        kmax = max(kmax, max(w.y << 16 & 0x7fffffffu, w.y & 0x7fff0000u));
-                    }
-                }
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const int t = 2 * c + (j & 1) + (j >> 1) * 8;
-#pragma unroll
-                for (int i = 0; i < NT / 2; i++) {
-                    raw[j][i] = t0 + t < q.len ? *(const uint32_t*)(vp + t * D + g * (D / 8) + 2 * i) : 0u;
-                    if (BF) vmax = max(vmax, max(raw[j][i] << 16 & 0x7fffffffu, raw[j][i] & 0x7fff0000u));
-                }
-            }
-            float kp2 = 1.f, vp2 = 1.f;
-            if (BF) {
-                kp2 = kv_power_below(__reduce_max_sync(0xffffffffu, kmax));
-                vp2 = kv_power_below(__reduce_max_sync(0xffffffffu, vmax));
-                const float ki = 1.f / kp2, vi = 1.f / vp2;
-#pragma unroll
-                for (int nt = 0; nt < 2; nt++)
-#pragma unroll
-                    for (int s = 0; s < STEPS; s++)
-#pragma unroll
-                        for (int h = 0; h < 2; h++) {
-                            const float2 x = kv_unpack<true>(kb[nt][s][h]);
-                            kb[nt][s][h] = kv_pack<false>(x.x * ki, x.y * ki);
-                        }
-#pragma unroll
-                for (int j = 0; j < 4; j++)
-#pragma unroll
-                    for (int i = 0; i < NT / 2; i++) {
-                        const float2 x = kv_unpack<true>(raw[j][i]);
-                        raw[j][i] = kv_pack<false>(x.x * vi, x.y * vi);
-                    }
-            }
-#pragma unroll
-            for (int i = 0; i < NT / 2; i++)
+            for (int s = 0; s < STEPS; s++)
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
-                    vb[2 * i][h] = __byte_perm(raw[2 * h][i], raw[2 * h + 1][i], 0x5410);
-                    vb[2 * i + 1][h] = __byte_perm(raw[2 * h][i], raw[2 * h + 1][i], 0x7632);
-                }
-            ks = kp2 / kv_code_scale<E4M3>();
-            vs = vp2 / kv_code_scale<E4M3>();
-        }
-
-        float s[2][4];
-#pragma unroll
-        for (int nt = 0; nt < 2; nt++) {
-            s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
-#pragma unroll
-            for (int k = 0; k < STEPS; k++) kv_mma(s[nt], qa[k], kb[nt][k][0], kb[nt][k][1]);
-#pragma unroll
-            for (int e = 0; e < 4; e++) s[nt][e] *= ks * row_scale[e >> 1];
-        }
-        const bool ragged = t0 + KV_TILE - 1 > see_all || t0 <= low_all;
-        if (ragged) {
-#pragma unroll
-            for (int nt = 0; nt < 2; nt++)
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const int t = t0 + 8 * nt + 2 * c + (e & 1), at_row = place[e >> 1];
-                    if (t > at_row || (A.window > 0 && t <= at_row - A.window)) s[nt][e] = -KV_INF;
+                    const float2 x = kv_unpack<true>(W.qb[r][s][h]);
+                    W.qb[r][s][h] = kv_pack<false>(x.x * inv, x.y * inv);
                 }
         }
-        float top[2] = {fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1])), fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]))};
-        if (__any_sync(0xffffffffu, top[0] > m[0] + KV_LAZY || top[1] > m[1] + KV_LAZY)) {
 #pragma unroll
-            for (int r = 0; r < 2; r++) {
-                top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
-                top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
-                const float higher = fmaxf(m[r], top[r]);
-                const float f = higher == -KV_INF ? 1.f : kv_exp2(m[r] - higher);
-                m[r] = higher;
-                l[r] *= f;
-#pragma unroll
-                for (int i = 0; i < NT; i++) { o[i][2 * r] *= f; o[i][2 * r + 1] *= f; }
-            }
+        for (int e = 0; e < 2; e++) {
+            const int mine = tile_row + 8 * r + 2 * c + e;
+            W.factor[r][e] = S.scale_log2 * __shfl_sync(0xffffffffu, p, 4 * (2 * c + e));
+            place[r][e] = mine < rows ? q.len - q.n + mine / S.group : -1;
+            W.m[r][e] = -KV_INF;
+            W.l[r][e] = 0.f;
         }
-        if (vs > vref) {                // the warp as a whole: vs is the tile's
-            const float higher = 4.f * kv_power_below(__float_as_uint(vs));
-            const float f = vref / higher;
 #pragma unroll
-            for (int i = 0; i < NT; i++) { o[i][0] *= f; o[i][1] *= f; o[i][2] *= f; o[i][3] *= f; }
-            vref = higher;
-        }
-        const float vf = vref > 0.f ? vs / vref * KV_P_SCALE : vs;
-        const float base[2] = {m[0] == -KV_INF ? 0.f : m[0], m[1] == -KV_INF ? 0.f : m[1]};
-        float sum[2] = {0.f, 0.f};
-#pragma unroll
-        for (int nt = 0; nt < 2; nt++)
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-                const bool hidden = ragged && s[nt][e] == -KV_INF;       // so that a masked token's scale, whatever it is, does not count
-                const float p = kv_exp2(s[nt][e] - base[e >> 1]);
-                sum[e >> 1] += p;
-                s[nt][e] = hidden ? 0.f : p * vf;
-            }
-        l[0] += sum[0];
-        l[1] += sum[1];
-        if (A.unit_l2) {
-#pragma unroll
-            for (int r = 0; r < 2; r++) {
-                sum[r] += __shfl_xor_sync(0xffffffffu, sum[r], 1);
-                sum[r] += __shfl_xor_sync(0xffffffffu, sum[r], 2);
-                const int row = tile_row + g + 8 * r;
-                if (c == 0 && row < q.n * S.group)
-                    A.unit_l2[(((int64_t)seq * S.kv_heads + kh) * A.units + t0 / KV_UNIT) * (B.max_new * S.group) + row] = kv_log2(sum[r]) + base[r];
-            }
-        }
-        const uint32_t pa[4] = {kv_pack<false>(s[0][0], s[0][1]), kv_pack<false>(s[0][2], s[0][3]), kv_pack<false>(s[1][0], s[1][1]),
-                                kv_pack<false>(s[1][2], s[1][3])};
-#pragma unroll
-        for (int i = 0; i < NT; i++) kv_mma(o[i], pa, vb[i][0], vb[i][1]);
+        for (int i = 0; i < STEPS; i++) W.o[r][i][0] = W.o[r][i][1] = W.o[r][i][2] = W.o[r][i][3] = 0.f;
     }
+    W.vref = W.vinv = 0.f;
+    const int last_row = min(tile_row + ROWS, rows) - 1;
+    const int see_all = q.len - q.n + tile_row / S.group;                    // tokens up to here are seen by every row (without a window)
+    const int low_all = A.window > 0 ? q.len - q.n + last_row / S.group - A.window : -1;   // tokens behind here are in every row's window
+    const int unit_stride = B.max_new * S.group;
+    float* const units = A.unit_l2 ? A.unit_l2 + ((int64_t)seq * S.kv_heads + kh) * A.units * unit_stride + tile_row : nullptr;
+    const bool one_unit = S.block_tokens >= KV_TILE;
 
-    // join the warps
-    __shared__ float sm_o[KV_WARPS][KV_ROWS][D + 4], sm_m[KV_WARPS][KV_ROWS], sm_l[KV_WARPS][KV_ROWS];
-#pragma unroll
-    for (int r = 0; r < 2; r++) {
-        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-        if (c == 0) { sm_m[warp][g + 8 * r] = m[r]; sm_l[warp][g + 8 * r] = l[r]; }
-        const float unit = vref > 0.f ? vref * (kv_code_scale<E4M3>() / KV_P_SCALE) : 1.f;   // without a reference o is 0 or NaN
-#pragma unroll
-        for (int i = 0; i < NT; i++)
-#pragma unroll
-            for (int e = 0; e < 2; e++) sm_o[warp][g + 8 * r][(2 * c + e) * (D / 8) + i] = o[i][2 * r + e] * unit;
+    uint32_t phase = 0;
+    for (int t0 = first; t0 < full_end; t0 += STRIDE) {
+        float* const unit_out = units ? units + (int64_t)(t0 / KV_HALF) * unit_stride : nullptr;
+        const bool there[2] = {pages.x >= 0, pages.y >= 0};
+        const float ks[2] = {kv_finite(scale[0].x), kv_finite(scale[1].x)}, vs[2] = {kv_finite(scale[0].y), kv_finite(scale[1].y)};
+        auto k_wait = [&] { return kv_wait(bars, phase); };
+        auto k_read = [&] { __syncwarp(); fetch(0, t0 + STRIDE, pages); };
+        auto v_wait = [&] { return kv_wait(bars + 8, phase); };
+        auto v_read = [&] { __syncwarp(); fetch(1, t0 + STRIDE, pages); };
+        pages = next;
+        scale[0] = scales_of(pages.x);
+        scale[1] = scales_of(pages.y);
+        next = make_int2(page_of(t0 + 2 * STRIDE), page_of(t0 + 2 * STRIDE + KV_HALF));
+        if (t0 + KV_TILE - 1 <= see_all && t0 > low_all && there[0] && there[1])
+            kv_tile<D, E4M3, NR, false>(W, slot, t0, ks, vs, there, place, A.window, unit_out, unit_stride, one_unit, rows - tile_row, lane, k_wait, k_read, v_wait, v_read);
+        else
+            kv_tile<D, E4M3, NR, true>(W, slot, t0, ks, vs, there, place, A.window, unit_out, unit_stride, one_unit, rows - tile_row, lane, k_wait, k_read, v_wait, v_read);
+        phase ^= 1;
     }
+    const uint16_t* const tail_k = (const uint16_t*)B.tail + (uint64_t)seq * S.tail_values + (uint64_t)kh * 2 * S.block_tokens * D;
+    for (int t0 = max(begin, tail_begin) + KV_HALF * warp; t0 < end; t0 += KV_HALF * KV_WARPS)
+        kv_tail_tile<D, BF, NR>(W, tail_k + (t0 - tail_begin) * D, tail_k + (S.block_tokens + t0 - tail_begin) * D, t0, q.len, place, A.window,
+                                units ? units + (int64_t)(t0 / KV_HALF) * unit_stride : nullptr, rows - tile_row, lane);
+
+    // join the warps, in the tiles' memory
     __syncthreads();
-    for (int idx = threadIdx.x; idx < KV_ROWS * (D / 2); idx += 32 * KV_WARPS) {
+    float (*const sm_o)[ROWS][D + 4] = (float (*)[ROWS][D + 4])kv_smem;
+    float (*const sm_m)[ROWS] = (float (*)[ROWS])(kv_smem + KV_WARPS * ROWS * (D + 4) * 4);
+    float (*const sm_l)[ROWS] = sm_m + KV_WARPS;
+    const float unit = W.vref > 0.f ? W.vref / KV_P_SCALE : 1.f;             // without a reference o is 0 or NaN
+#pragma unroll
+    for (int r = 0; r < NR; r++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+            const int row = 8 * r + 2 * c + e;
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) W.l[r][e] += __shfl_xor_sync(0xffffffffu, W.l[r][e], d);
+            if (g == 0) { sm_m[warp][row] = W.m[r][e]; sm_l[warp][row] = W.l[r][e]; }
+#pragma unroll
+            for (int i = 0; i < STEPS; i++) {
+                sm_o[warp][row][T::v_channel(g, 2 * i)] = W.o[r][i][e] * unit;
+                sm_o[warp][row][T::v_channel(g, 2 * i + 1)] = W.o[r][i][2 + e] * unit;
+            }
+        }
+    __syncthreads();
+    for (int idx = threadIdx.x; idx < ROWS * (D / 2); idx += 32 * KV_WARPS) {
         const int row = idx / (D / 2), ch = idx % (D / 2) * 2, all = tile_row + row;
-        if (all >= q.n * S.group) break;
+        if (all >= rows) break;
         float top = -KV_INF;
 #pragma unroll
         for (int w = 0; w < KV_WARPS; w++) top = fmaxf(top, sm_m[w][row]);
@@ -367,28 +606,34 @@ __global__ void __launch_bounds__(32 * KV_WARPS) kv_attend_kernel(const KvShape 
 
 // Joins the chunks of each row: a warp per row.
 template <int D, bool BF>
-__global__ void __launch_bounds__(256) kv_join_kernel(const KvShape S, const KvBatch B, const KvAttend A, const int rows_per_tile)
+__global__ void __launch_bounds__(32 * KV_WARPS) kv_join_kernel(const KvShape S, const KvBatch B, const KvAttend A)
 {
     constexpr int V = D / 32;
-    const int lane = threadIdx.x & 31, seq = blockIdx.y, idx = blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31, seq = blockIdx.y, idx = blockIdx.x * KV_WARPS + (threadIdx.x >> 5);
+    asm volatile("griddepcontrol.launch_dependents;");
     const KvSeq q = kv_seq(S, B, seq);
-    if (idx >= q.n * S.q_heads) return;
     const int token = idx / S.q_heads, head = idx % S.q_heads;
-    const int row = token * S.group + head % S.group;
-    const KvSpan span = kv_span(S, q, A.window, row / rows_per_tile * rows_per_tile, rows_per_tile);
+    const KvSpan span = kv_span(S, q, A.window, (token * S.group + head % S.group) / A.rows * A.rows, A.rows);
     const int chunks = max(1, (span.end - span.begin + A.chunk - 1) / A.chunk);
     const int64_t first = (int64_t)(q.start + token) * S.q_heads + head, step = (int64_t)B.total_new * S.q_heads;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (idx >= q.n * S.q_heads) return;
+    // the largest maximum first, then every chunk's sum and answer by its distance from it: loads that do not wait for one another
     float m = -KV_INF, l = 0.f, acc[V];
+    for (int k = lane; k < chunks; k += 32) m = fmaxf(m, A.part_ml[2 * (first + k * step)]);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    const float base = m == -KV_INF ? 0.f : m;
 #pragma unroll
     for (int i = 0; i < V; i++) acc[i] = 0.f;
+#pragma unroll 8
     for (int k = 0; k < chunks; k++) {
         const float2 ml = *(const float2*)(A.part_ml + 2 * (first + k * step));
         const float* src = A.part_o + (first + k * step) * D + lane * V;
-        const float top = fmaxf(m, ml.x), base = top == -KV_INF ? 0.f : top, f = kv_exp2(m - base), h = kv_exp2(ml.x - base);
-        m = top;
-        l = l * f + ml.y * h;
+        const float h = kv_exp2(ml.x - base);
+        l += ml.y * h;
 #pragma unroll
-        for (int i = 0; i < V; i++) acc[i] = acc[i] * f + src[i] * h;
+        for (int i = 0; i < V; i++) acc[i] += src[i] * h;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     uint16_t* dst = (uint16_t*)A.out.data + (q.start + token) * A.out.token_stride + head * A.out.head_stride + lane * V;
@@ -401,30 +646,48 @@ __global__ void __launch_bounds__(256) kv_join_kernel(const KvShape S, const KvB
     }
 }
 
-// Weight of each block: a warp per block adds exp2(log2 of the unit's sum - log2 of the row's sum) over the block's units and the
-// rows that see any of it, in an order of its own that never changes.
+// Weight of each block: sum over the block's units and the rows that see any of it of exp2(log2 of the unit's sum - log2 of the row's
+// sum).  FEW (at most KV_MASS_ROWS rows per sequence and kv head): a thread per block; otherwise a warp per block.  The order of the
+// sum is always the same.
+#define KV_MASS_ROWS 32
+template <bool FEW>
 __global__ void __launch_bounds__(256) kv_mass_kernel(const KvShape S, const KvBatch B, const KvAttend A, const int unit_shift)
 {
-    const int lane = threadIdx.x & 31, block = blockIdx.x * 8 + (threadIdx.x >> 5), kh = blockIdx.y, seq = blockIdx.z;
+    const int lane = threadIdx.x & 31, kh = blockIdx.y, seq = blockIdx.z;
+    const int block = FEW ? blockIdx.x * 256 + threadIdx.x : blockIdx.x * 8 + (threadIdx.x >> 5);
+    __shared__ float row_l2[KV_MASS_ROWS];
     const KvSeq q = kv_seq(S, B, seq);
-    if (block << S.block_shift >= q.len) return;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int rows = q.n * S.group, stride = B.max_new * S.group;
+    if (FEW) {
+        if (blockIdx.x * 256 << S.block_shift >= q.len) return;
+        if (threadIdx.x < rows) row_l2[threadIdx.x] = A.lse2[(int64_t)(q.start + threadIdx.x / S.group) * S.q_heads + kh * S.group + threadIdx.x % S.group];
+        __syncthreads();
+    }
+    if (block << S.block_shift >= q.len) return;
     const int unit0 = block << S.block_shift >> unit_shift, unit1 = (min((block + 1) << S.block_shift, q.len) - 1 >> unit_shift) + 1;
+    const bool there = block == q.full || kv_page(B, seq, block) >= 0;
+    const int step = block < q.full && S.block_tokens >= KV_TILE ? KV_TILE / KV_HALF : 1;    // full blocks have a sum per tile
     float sum = 0.f;
-    if (block == q.full || kv_page(B, seq, block) >= 0)
-        for (int unit = unit0; unit < unit1; unit++) {
+    if (there)
+        for (int unit = unit0; unit < unit1; unit += step) {
             const float* src = A.unit_l2 + (((int64_t)seq * S.kv_heads + kh) * A.units + unit) * stride;
-            const int t0 = unit << unit_shift, t1 = t0 + (1 << unit_shift) - 1;
-            for (int row = lane; row < rows; row += 32) {
-                const int token = row / S.group, place = q.len - q.n + token;
-                if (t0 > place || (A.window > 0 && t1 <= place - A.window)) continue;
-                sum += kv_exp2(src[row] - A.lse2[(int64_t)(q.start + token) * S.q_heads + kh * S.group + row % S.group]);
+            const int t0 = unit << unit_shift, t1 = t0 + (step << unit_shift) - 1;
+            // the first token whose query sees the unit at all, and the last that has it in its window
+            const int lo = max(t0 - (q.len - q.n), 0), hi = A.window > 0 ? min(q.n - 1, t1 + A.window - 1 - (q.len - q.n)) : q.n - 1;
+            if (FEW) {
+#pragma unroll 4
+                for (int row = lo * S.group; row < (hi + 1) * S.group; row++) sum += kv_exp2(src[row] - row_l2[row]);
+            } else {
+                for (int row = lo * S.group + lane; row < (hi + 1) * S.group; row += 32)
+                    sum += kv_exp2(src[row] - A.lse2[(int64_t)(q.start + row / S.group) * S.q_heads + kh * S.group + row % S.group]);
             }
         }
+    if (!FEW) {
 #pragma unroll
-    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    if (lane == 0) {
-        const int64_t at = ((int64_t)seq * S.kv_heads + kh) * A.mass_stride + block;
-        A.mass_out[at] = A.mass_in[at] + sum;
+        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (lane) return;
     }
+    const int64_t at = ((int64_t)seq * S.kv_heads + kh) * A.mass_stride + block;
+    A.mass_out[at] = A.mass_in[at] + sum;
 }

@@ -63,7 +63,7 @@ typedef struct {
     int rotary_dim;             /* channels that are turned, from the first on: a multiple of 16, at most head_dim; 0 without rotary */
     const double* frequencies;  /* host, rotary_dim / 2: radians per position of each pair, finite; copied */
     float rotary_gain;          /* turned channels are multiplied by it (1 for none) */
-    float softmax_scale;        /* 0: 1 / sqrt(head_dim) */
+    float softmax_scale;        /* >= 0; 0: 1 / sqrt(head_dim) */
 } fastrack_kv_config;
 
 /* The sequences of a call.  The new tokens of all sequences lie packed: sequence i has rows d_starts[i] .. d_starts[i+1]-1

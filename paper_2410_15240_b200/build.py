@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfastrack.so")
 SOURCES = [os.path.join(CSRC, "fastrack.cu"), os.path.join(CSRC, "fastrack_kv.cu")]
-DEPS = SOURCES + [os.path.join(CSRC, "fastrack_kv_device.cuh"), os.path.join(CSRC, "fastrack_kv_attend.cuh"),
+DEPS = SOURCES + [os.path.join(CSRC, "fastrack_kv_device.cuh"), os.path.join(CSRC, "fastrack_kv_attend.cuh"), os.path.join(CSRC, "fastrack_kv_prompt.cuh"),
                   os.path.join(os.path.dirname(HERE), "include", "fastrack_kv.h"),
                   os.path.join(CSRC, "fastrack_device.cuh"), os.path.join(CSRC, "fastrack_keysetup.h"), os.path.join(CSRC, "fastrack_plan.h"),
                   os.path.join(os.path.dirname(HERE), "include", "fastrack.h")]

@@ -12,6 +12,7 @@
 #include "../../include/fastrack_kv.h"
 #include "fastrack_kv_attend.cuh"
 #include "fastrack_kv_device.cuh"
+#include "fastrack_kv_prompt.cuh"
 
 // ------------------------------------------------------------------------------------------------ rotary ----
 
@@ -347,6 +348,11 @@ template <int D> static cudaError_t kv_attend_prepare()
     ask((const void*)kv_attend_kernel<D, true, false, 2>, 16);
     ask((const void*)kv_attend_kernel<D, false, true, 2>, 16);
     ask((const void*)kv_attend_kernel<D, false, false, 2>, 16);
+    auto ask_prompt = [&](const void* kernel) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, KvPrompt<D>::SMEM); };
+    ask_prompt((const void*)kv_prompt_kernel<D, true, true>);
+    ask_prompt((const void*)kv_prompt_kernel<D, true, false>);
+    ask_prompt((const void*)kv_prompt_kernel<D, false, true>);
+    ask_prompt((const void*)kv_prompt_kernel<D, false, false>);
     return e;
 }
 
@@ -400,7 +406,7 @@ extern "C" int fastrack_kv_create(const fastrack_kv_config* c, fastrack_kv** out
     if (c->rotary == FASTRACK_ROTARY_NONE ? c->rotary_dim != 0
                                           : c->rotary_dim < 16 || c->rotary_dim > c->head_dim || c->rotary_dim % 16 || !c->frequencies || !isfinite(c->rotary_gain))
         return FASTRACK_ERR_ARG;
-    if (!isfinite(c->softmax_scale)) return FASTRACK_ERR_ARG;
+    if (!isfinite(c->softmax_scale) || c->softmax_scale < 0.f) return FASTRACK_ERR_ARG;
     uint64_t turns[KV_MAX_PAIRS] = {0};
     for (int i = 0; i < c->rotary_dim / 2; i++) {
         if (!isfinite(c->frequencies[i])) return FASTRACK_ERR_ARG;
@@ -557,24 +563,26 @@ extern "C" int fastrack_kv_read(fastrack_kv* kv, const fastrack_kv_batch* batch,
 
 #define KV_WAVES 4                      // times that the chunks fill the SMs
 
-struct KvPlan { int rows, splits, chunk, row_tiles, units; size_t ml, lse2, unit_l2, total; };   // byte offsets in the workspace, part_o at 0
+struct KvPlan { int rows, splits, chunk, row_tiles, units, unit_shift; size_t ml, lse2, unit_l2, total; };   // byte offsets in the workspace, part_o at 0
 
 static KvPlan kv_plan(const fastrack_kv* kv, const fastrack_kv_batch* b, bool mass)
 {
     const KvShape& S = kv->shape;
     KvPlan p;
     const int64_t rows = (int64_t)b->max_new * S.group;
-    p.rows = rows <= 8 ? 8 : 16;
+    p.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : 2 * KV_P_ROWS;
     p.row_tiles = (int)((rows + p.rows - 1) / p.rows);
-    const int64_t ctas = (int64_t)b->n_seqs * S.kv_heads * p.row_tiles;
-    const int64_t want = (KV_WAVES * 4 * (int64_t)kv->num_sms + ctas - 1) / (ctas ? ctas : 1);
+    const bool prompt = p.rows > 16;
+    const int64_t ctas = (int64_t)b->n_seqs * S.kv_heads * p.row_tiles, step = prompt ? KV_P_TOKENS : KV_STEP;
+    const int64_t want = ((prompt ? 1 : KV_WAVES * 4) * (int64_t)kv->num_sms + ctas - 1) / (ctas ? ctas : 1);
     int64_t chunk = (b->max_len + want - 1) / want;
-    chunk = (chunk + KV_STEP - 1) / KV_STEP * KV_STEP;
-    if (chunk < KV_STEP) chunk = KV_STEP;
+    chunk = (chunk + step - 1) / step * step;
+    if (chunk < step) chunk = step;
     p.chunk = (int)chunk;
     p.splits = (int)((b->max_len + chunk - 1) / chunk);
     if (p.splits < 1) p.splits = 1;
-    p.units = (b->max_len + KV_HALF - 1) / KV_HALF;
+    p.unit_shift = prompt ? S.block_shift : 4;
+    p.units = (b->max_len + (1 << p.unit_shift) - 1) >> p.unit_shift;
     const size_t all = (size_t)b->total_new * S.q_heads;
     p.ml = p.splits > 1 ? (size_t)p.splits * all * S.head_dim * 4 : 0;
     p.lse2 = p.ml + (p.splits > 1 ? (size_t)p.splits * all * 8 : 0);
@@ -611,9 +619,11 @@ static void kv_attend_launch(const fastrack_kv* kv, const KvBatch& B, const KvAt
 {
     const KvShape& S = kv->shape;
     const bool e4 = kv->config.format == FASTRACK_KV_E4M3;
+    const dim3 grid(A.splits, S.kv_heads * A.row_tiles, B.n_seqs);
+    if (A.rows > 16) (e4 ? kv_prompt_kernel<D, BF, true> : kv_prompt_kernel<D, BF, false>)<<<grid, KV_P_THREADS, KvPrompt<D>::SMEM, stream>>>(S, B, A);
     auto kernel = A.rows == 8 ? (e4 ? kv_attend_kernel<D, BF, true, 1> : kv_attend_kernel<D, BF, false, 1>)
                               : (e4 ? kv_attend_kernel<D, BF, true, 2> : kv_attend_kernel<D, BF, false, 2>);
-    kernel<<<dim3(A.splits, S.kv_heads * A.row_tiles, B.n_seqs), 32 * KV_WARPS, kv_attend_smem<D>(A.rows) + 16 * KV_WARPS, stream>>>(S, B, A, pool);
+    if (A.rows <= 16) kernel<<<grid, 32 * KV_WARPS, kv_attend_smem<D>(A.rows) + 16 * KV_WARPS, stream>>>(S, B, A, pool);
     if (A.splits > 1)
         kv_launch_after(stream, dim3((unsigned)(((int64_t)B.max_new * S.q_heads + KV_WARPS - 1) / KV_WARPS), B.n_seqs), 32 * KV_WARPS, kv_join_kernel<D, BF>, S, B, A);
 }
@@ -683,8 +693,8 @@ extern "C" int fastrack_kv_attention(fastrack_kv* kv, const fastrack_kv_batch* b
     }
     if (mass && batch->max_len > 0) {
         const int blocks = (batch->max_len + S.block_tokens - 1) / S.block_tokens;
-        if ((int64_t)batch->max_new * S.group <= KV_MASS_ROWS) kv_launch_after(st, dim3((blocks + 255) / 256, S.kv_heads, batch->n_seqs), 256, kv_mass_kernel<true>, S, B, A, 4);
-        else kv_launch_after(st, dim3((blocks + 7) / 8, S.kv_heads, batch->n_seqs), 256, kv_mass_kernel<false>, S, B, A, 4);
+        if ((int64_t)batch->max_new * S.group <= KV_MASS_ROWS) kv_launch_after(st, dim3((blocks + 255) / 256, S.kv_heads, batch->n_seqs), 256, kv_mass_kernel<true>, S, B, A, p.unit_shift);
+        else kv_launch_after(st, dim3((blocks + 7) / 8, S.kv_heads, batch->n_seqs), 256, kv_mass_kernel<false>, S, B, A, p.unit_shift);
         launches++;
     }
     return kv_launched(kv, launches);

@@ -22,12 +22,12 @@ struct KvAttend {
     KvRows q, out;
     float* lse;             // natural, or NULL
     int window;
-    int rows;               // of a CTA: 8 or 16
+    int rows;               // of a CTA: 8, 16 or 256
     int splits, chunk;      // chunks of the span, tokens of a chunk (a multiple of KV_STEP and of the block)
     int row_tiles, units;   // units: per sequence, for weights
     float* part_o;          // [splits][total_new * q_heads][head_dim]
     float* part_ml;         // [splits][total_new * q_heads][2]: running maximum and sum
-    float* lse2;            // [total_new * q_heads], base 2
+    float* lse2;            // [total_new * q_heads], base 2, see kv_lse2_at
     float* unit_l2;         // [n_seqs][kv_heads][units][max_new * group]: log2 of the sum of exponentials of a unit; NULL without weights
     const float* mass_in;
     float* mass_out;
@@ -117,6 +117,19 @@ __device__ __forceinline__ float kv_power_below(uint32_t abs_bits)
     if (abs_bits == 0) return 1.f;
     e = e < 2u ? 2u : e > 252u ? 252u : e;
     return __uint_as_float(e << 23);
+}
+
+// The largest magnitude of 8 bf16 values, as bits
+__device__ __forceinline__ uint32_t kv_amax8(const uint4& w)
+{
+    const uint32_t a = max(max(w.x << 16 & 0x7fffffffu, w.x & 0x7fff0000u), max(w.y << 16 & 0x7fffffffu, w.y & 0x7fff0000u));
+    return max(a, max(max(w.z << 16 & 0x7fffffffu, w.z & 0x7fff0000u), max(w.w << 16 & 0x7fffffffu, w.w & 0x7fff0000u)));
+}
+
+// Where a row's sum stands in lse2: the rows of a sequence and kv head are neighbours.
+__device__ __forceinline__ int64_t kv_lse2_at(const KvShape& S, const KvSeq& q, int kh, int row)
+{
+    return ((int64_t)q.start * S.kv_heads + (int64_t)kh * q.n) * S.group + row;
 }
 
 // An infinite scale counts as NaN, so that a block with one shows in every answer that sees it.
@@ -363,9 +376,7 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
             uint32_t amax = 0;
             for (int i = lane; i < KV_HALF * D / 8; i += 32) {
                 if (t0 + i / (D / 8) >= len) break;
-                const uint4 w = *(const uint4*)(src + 8 * i);
-                amax = max(max(max(amax, max(w.x << 16 & 0x7fffffffu, w.x & 0x7fff0000u)), max(w.y << 16 & 0x7fffffffu, w.y & 0x7fff0000u)),
-                           max(max(w.z << 16 & 0x7fffffffu, w.z & 0x7fff0000u), max(w.w << 16 & 0x7fffffffu, w.w & 0x7fff0000u)));
+                amax = max(amax, kv_amax8(*(const uint4*)(src + 8 * i)));
             }
             scale[which] = kv_power_below(__reduce_max_sync(0xffffffffu, amax));
         }
@@ -594,7 +605,7 @@ __global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? 4 : 3) kv_attend_kern
             if (ch == 0) {
                 const float l2 = sum == 0.f ? -KV_INF : base + log2f(sum);
                 if (A.lse) A.lse[token * S.q_heads + head] = l2 * 0.6931471805599453f;
-                A.lse2[token * S.q_heads + head] = l2;
+                A.lse2[kv_lse2_at(S, q, kh, all)] = l2;
             }
         } else {
             const int64_t at = ((int64_t)chunk * B.total_new + token) * S.q_heads + head;
@@ -642,7 +653,7 @@ __global__ void __launch_bounds__(32 * KV_WARPS) kv_join_kernel(const KvShape S,
     if (lane == 0) {
         const float l2 = l == 0.f ? -KV_INF : m + log2f(l);
         if (A.lse) A.lse[first] = l2 * 0.6931471805599453f;
-        A.lse2[first] = l2;
+        A.lse2[kv_lse2_at(S, q, head / S.group, token * S.group + head % S.group)] = l2;
     }
 }
 
@@ -661,13 +672,13 @@ __global__ void __launch_bounds__(256) kv_mass_kernel(const KvShape S, const KvB
     const int rows = q.n * S.group, stride = B.max_new * S.group;
     if (FEW) {
         if (blockIdx.x * 256 << S.block_shift >= q.len) return;
-        if (threadIdx.x < rows) row_l2[threadIdx.x] = A.lse2[(int64_t)(q.start + threadIdx.x / S.group) * S.q_heads + kh * S.group + threadIdx.x % S.group];
+        if (threadIdx.x < rows) row_l2[threadIdx.x] = A.lse2[kv_lse2_at(S, q, kh, threadIdx.x)];
         __syncthreads();
     }
     if (block << S.block_shift >= q.len) return;
     const int unit0 = block << S.block_shift >> unit_shift, unit1 = (min((block + 1) << S.block_shift, q.len) - 1 >> unit_shift) + 1;
     const bool there = block == q.full || kv_page(B, seq, block) >= 0;
-    const int step = block < q.full && S.block_tokens >= KV_TILE ? KV_TILE / KV_HALF : 1;    // full blocks have a sum per tile
+    const int step = unit_shift == 4 && block < q.full && S.block_tokens >= KV_TILE ? KV_TILE / KV_HALF : 1;   // of kv_attend_kernel's full blocks: a sum per tile
     float sum = 0.f;
     if (there)
         for (int unit = unit0; unit < unit1; unit += step) {
@@ -679,8 +690,9 @@ __global__ void __launch_bounds__(256) kv_mass_kernel(const KvShape S, const KvB
 #pragma unroll 4
                 for (int row = lo * S.group; row < (hi + 1) * S.group; row++) sum += kv_exp2(src[row] - row_l2[row]);
             } else {
-                for (int row = lo * S.group + lane; row < (hi + 1) * S.group; row += 32)
-                    sum += kv_exp2(src[row] - A.lse2[(int64_t)(q.start + row / S.group) * S.q_heads + kh * S.group + row % S.group]);
+                const float* l2 = A.lse2 + kv_lse2_at(S, q, kh, 0);
+#pragma unroll 8
+                for (int row = lo * S.group + lane; row < (hi + 1) * S.group; row += 32) sum += kv_exp2(src[row] - l2[row]);
             }
         }
     if (!FEW) {

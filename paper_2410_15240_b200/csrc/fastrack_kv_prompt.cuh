@@ -1,0 +1,509 @@
+// fastrack_kv_prompt.cuh -- attention of many query rows over the 8-bit cache, on the 5th-generation tensor cores.
+#pragma once
+#include "fastrack_kv_attend.cuh"
+
+// One CTA takes 256 rows (two tiles of 128) of one kv head of one sequence against a chunk of the tokens, 128 at a time:
+//     S_m = Q_m K^T  (128 x 128, tensor memory)  ->  P_m = weights as f16 (tensor memory, over S_m)  ->  O_m += P_m V.
+// Warps 0-3 and 4-7 make P_0 and P_1 (a thread per row: no exchange between lanes), warps 8-11 bring the codes and widen them to f16
+// in shared memory, where the tensor cores read them, and one thread of warp 12 issues the products.  The two row tiles take turns:
+// while one's weights are made, the other's products run.  Both share the widened K and V.
+//
+// What bounds it, per 128 tokens and SM: the products 4 x 512 cycles; shared memory the same (Q and K for S, V for O, the widened
+// codes' way in: 256 KB at 128 B a cycle); the exponentials 2 x 128 x 128 at 16 a cycle, again 2048.
+#define KV_P_ROWS 128                   // of a row tile
+#define KV_P_TOKENS 128
+#define KV_P_THREADS 416
+#define KV_P_GROUPS (KV_P_TOKENS / KV_HALF)
+#define KV_P_LAZY 4.0f
+#define KV_P_LEAST 0x1p-40f             // a block's V scale counts for at least this share of the reference (below it V is lost to 11 bits anyway)
+
+template <int D> struct KvPrompt {
+    static constexpr int HALVES = (D + 63) / 64;                             // runs of 64 channels: 128-byte rows, swizzled by the row's number
+    static constexpr int TILE = HALVES * KV_P_TOKENS * 128;                  // bytes of a tile of 128 rows as f16
+    static constexpr int Q = 0, K = 2 * TILE, V = 4 * TILE, SCALES = 6 * TILE, BARS = SCALES + 4 * (KV_P_GROUPS + 1) * 16, END = BARS + 256;
+    static constexpr int SMEM = END + 1024;                                  // the base is rounded up to 1024
+    // byte of the 16-byte piece that holds channels ch .. ch + 7 of a row
+    __device__ static int at(int row, int ch) { return (ch >> 6) * KV_P_TOKENS * 128 + row * 128 + (((ch >> 3 & 7) ^ (row & 7)) << 4); }
+};
+
+__device__ __forceinline__ uint64_t kv_desc(uint32_t smem, uint32_t lbo, uint32_t sbo)   // swizzle of 128 bytes
+{
+    return (uint64_t)((smem >> 4) & 0x3fff) | (uint64_t)((lbo >> 4) & 0x3fff) << 16 | (uint64_t)((sbo >> 4) & 0x3fff) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+__device__ __forceinline__ void kv_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void kv_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void kv_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void kv_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+
+#define KV_R8(x, i) "=r"(x[i]), "=r"(x[i + 1]), "=r"(x[i + 2]), "=r"(x[i + 3]), "=r"(x[i + 4]), "=r"(x[i + 5]), "=r"(x[i + 6]), "=r"(x[i + 7])
+#define KV_W8(x, i) "r"(x[i]), "r"(x[i + 1]), "r"(x[i + 2]), "r"(x[i + 3]), "r"(x[i + 4]), "r"(x[i + 5]), "r"(x[i + 6]), "r"(x[i + 7])
+__device__ __forceinline__ void kv_tmem_load32(uint32_t (&x)[32], uint32_t at)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : KV_R8(x, 0), KV_R8(x, 8), KV_R8(x, 16), KV_R8(x, 24) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void kv_tmem_store32(const uint32_t (&x)[32], uint32_t at)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+                 ::KV_W8(x, 0), KV_W8(x, 8), KV_W8(x, 16), KV_W8(x, 24), "r"(at) : "memory");
+}
+__device__ __forceinline__ void kv_tmem_store16(const uint32_t (&x)[16], uint32_t at)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+                 ::KV_W8(x, 0), KV_W8(x, 8), "r"(at) : "memory");
+}
+// The load's registers go through the wait, so that nothing reads them before it.
+__device__ __forceinline__ void kv_tmem_loaded(uint32_t (&x)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 32; i++) asm volatile("" : "+r"(x[i]));
+}
+
+// Bounded wait that also ends when another warp has given up.
+__device__ __forceinline__ bool kv_wait_or_stop(uint32_t bar, uint32_t parity, volatile int* stop)
+{
+    for (int i = 0; i < 1 << 10; i++) {
+        uint32_t done = 0;
+        for (int attempt = 0; attempt < 64 && !done; attempt++)
+            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                         : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+        if (done) return true;
+        if (*stop) return false;
+    }
+    *stop = 1;
+    return false;
+}
+
+// 16 codes as 16 f16
+template <bool E4M3> __device__ __forceinline__ void kv_widen16(const uint4& w, uint4& lo, uint4& hi)
+{
+    kv_widen4<E4M3>(w.x, lo.x, lo.y);
+    kv_widen4<E4M3>(w.y, lo.z, lo.w);
+    kv_widen4<E4M3>(w.z, hi.x, hi.y);
+    kv_widen4<E4M3>(w.w, hi.z, hi.w);
+}
+
+// Barriers, 8 bytes each from T::BARS on.  K_IN has four phases in turn because the scales beside K stay until the weights are made; by
+// the time that a tile's K comes in, the weights of the fourth tile before it are done.
+enum { KV_K_IN = 0, KV_K_OUT = 4, KV_V_IN = 6, KV_V_OUT = 8, KV_S_IN = 10, KV_P_IN = 12, KV_Q_IN = 14, KV_TAIL = 15, KV_END = 16, KV_BARS = 17 };
+
+// What a tile's slot of T::SCALES holds: per 16 tokens {K's scale, log2 of V's scale over the reference, one over that share, whether the
+// tokens are there}; the tile's change of the reference and the reference itself stand behind the groups.
+struct KvSlot { float4 group[KV_P_GROUPS]; float step, unit, pad[2]; };
+
+// log2 of 128 (query, head) rows' weights, made tile by tile by 128 threads, a row each; see the head of this file.
+template <int D, bool BF>
+__device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& B, const KvAttend& A, const KvSeq& q, int seq, int kh, int tile_row, int m_tile,
+                                               int chunk, int begin, int end, int tiles, uint8_t* sm, uint32_t bars, volatile int* stop, uint32_t tmem)
+{
+    using T = KvPrompt<D>;
+    const int warp = threadIdx.x >> 5, r = threadIdx.x & 127, rows = q.n * S.group, row = tile_row + KV_P_ROWS * m_tile + r;
+    const bool valid = row < rows;
+    const int64_t token = q.start + row / S.group;
+    const int head = kh * S.group + row % S.group, place = valid ? q.len - q.n + row / S.group : -1;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21, s_at = tmem + lanes + 128 * m_tile, o_at = tmem + lanes + 256 + 128 * m_tile;
+    const KvSlot* const slots = (const KvSlot*)(sm + T::SCALES);
+    float factor = S.scale_log2;
+    {
+        // the row of Q, as f16 (bf16: over a power of two near its largest), to shared memory
+        const uint16_t* src = (const uint16_t*)A.q.data + token * A.q.token_stride + head * A.q.head_stride;
+        uint4 w[D / 8];
+        uint32_t amax = 0;
+#pragma unroll
+        for (int i = 0; i < D / 8; i++) {
+            w[i] = valid ? *(const uint4*)(src + 8 * i) : make_uint4(0, 0, 0, 0);
+            if (BF) amax = max(amax, kv_amax8(w[i]));
+        }
+        float inv = 1.f;
+        if (BF) {
+            const float p = kv_power_below(amax);
+            factor *= p;
+            inv = 1.f / p;
+        }
+#pragma unroll
+        for (int i = 0; i < D / 8; i++) {
+            if (BF) {
+                float x[8];
+                kv_widen8<true>(w[i], x);
+#pragma unroll
+                for (int e = 0; e < 8; e++) x[e] *= inv;
+                w[i] = kv_narrow8<false>(x);
+            }
+            *(uint4*)(sm + T::Q + m_tile * T::TILE + T::at(r, 8 * i)) = w[i];
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        kv_arrive(bars + 8 * KV_Q_IN);
+    }
+    // rows of this warp: tokens up to see_all are seen by all of them, tokens behind low_all are in every one's window
+    const int first_row = tile_row + KV_P_ROWS * m_tile + 32 * (warp & 3), last_row = min(first_row + 31, rows - 1);
+    const int see_all = first_row + 31 < rows ? q.len - q.n + first_row / S.group : -1;
+    const int low_all = A.window > 0 ? q.len - q.n + last_row / S.group - A.window : -1;
+    const int unit_stride = B.max_new * S.group, per_block = S.block_tokens / KV_HALF, per_shift = S.block_shift - 4;
+    float* const units = A.unit_l2 && valid ? A.unit_l2 + ((int64_t)seq * S.kv_heads + kh) * A.units * unit_stride + row : nullptr;
+    float m = -KV_INF, l = 0.f, unit = 1.f;
+    bool fine = true;
+    for (int j = 0; j < tiles; j++) {
+        const int t0 = begin + KV_P_TOKENS * j;
+        fine = __all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * (KV_K_IN + (j & 3)), j >> 2 & 1, stop) && kv_wait_or_stop(bars + 8 * (KV_S_IN + m_tile), j & 1, stop));
+        if (!fine) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const KvSlot& slot = slots[j & 3];
+        const bool ragged = slot.pad[0] != 0.f || t0 + KV_P_TOKENS - 1 > see_all || t0 <= low_all;
+        auto hidden = [&](int col) {
+            const int t = t0 + col;
+            return t > place || (A.window > 0 && t <= place - A.window) || slot.group[col >> 4].w == 0.f;
+        };
+        // the row's largest score; a scale is not negative, so that of 16 tokens with one scale the largest product is the largest score
+        float top = -KV_INF;
+        uint32_t x[32];
+#pragma unroll
+        for (int b = 0; b < 4; b++) {
+            kv_tmem_load32(x, s_at + 32 * b);
+            kv_tmem_loaded(x);
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const float f = slot.group[2 * b + h].x * factor;
+                float g = -KV_INF;
+                if (ragged) {
+#pragma unroll
+                    for (int i = 0; i < 16; i++) g = fmaxf(g, hidden(32 * b + 16 * h + i) ? -KV_INF : __uint_as_float(x[16 * h + i]));
+                    if (g > -KV_INF) top = fmaxf(top, g * f);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; i++) g = fmaxf(g, __uint_as_float(x[16 * h + i]));
+                    top = fmaxf(top, g * f);
+                }
+            }
+        }
+        float step = slot.step;                          // O is in units of V's reference, l is not
+        unit = slot.unit;
+        if (top > m + KV_P_LAZY) {
+            const float fall = kv_exp2(m - top);
+            l *= fall;
+            step *= fall;
+            m = top;
+        }
+        if (j > 0 && __any_sync(0xffffffffu, step != 1.f)) {
+#pragma unroll
+            for (int b = 0; b < D / 32; b++) {
+                kv_tmem_load32(x, o_at + 32 * b);
+                kv_tmem_loaded(x);
+#pragma unroll
+                for (int i = 0; i < 32; i++) x[i] = __float_as_uint(__uint_as_float(x[i]) * step);
+                kv_tmem_store32(x, o_at + 32 * b);
+            }
+        }
+        // weights times V's share of the reference: the share's logarithm goes into the exponent, and out of the sum again by its inverse
+        const float base = m == -KV_INF ? 0.f : m;
+        float block_sum = 0.f;
+#pragma unroll
+        for (int b = 0; b < 4; b++) {
+            kv_tmem_load32(x, s_at + 32 * b);
+            kv_tmem_loaded(x);
+            uint32_t p[16];
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const float4 sc = slot.group[2 * b + h];
+                const float f = sc.x * factor, up = sc.y - base;
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    float y = kv_exp2(fmaf(__uint_as_float(x[16 * h + i]), f, up)), z = kv_exp2(fmaf(__uint_as_float(x[16 * h + i + 1]), f, up));
+                    if (ragged) {
+                        if (hidden(32 * b + 16 * h + i)) y = 0.f;
+                        if (hidden(32 * b + 16 * h + i + 1)) z = 0.f;
+                    }
+                    sum += y + z;
+                    p[8 * h + i / 2] = kv_pack<false>(y, z);
+                }
+                sum = sum == 0.f ? 0.f : sum * sc.z;     // a hidden block's scale may be NaN
+                l += sum;
+                if (units) {
+                    block_sum += sum;
+                    if (((2 * b + h + 1) & (per_block - 1)) == 0) {
+                        const int block = (t0 >> S.block_shift) + (2 * b + h >> per_shift);
+                        if (block << S.block_shift < end) units[(int64_t)block * unit_stride] = kv_log2(block_sum) + base;
+                        block_sum = 0.f;
+                    }
+                }
+            }
+            kv_tmem_store16(p, s_at + 16 * b);
+        }
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        kv_arrive(bars + 8 * (KV_P_IN + m_tile));
+    }
+    if (fine && tiles > 0) fine = __all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * (KV_S_IN + m_tile), tiles & 1, stop));      // the last product
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const float nan = __int_as_float(0x7fffffff), inv = !fine ? nan : l == 0.f ? 0.f : 1.f / l;
+    const float out_factor = A.splits == 1 ? inv * unit : fine ? unit : nan;
+#pragma unroll
+    for (int b = 0; b < D / 32; b++) {
+        uint32_t x[32];
+        if (tiles > 0) {
+            kv_tmem_load32(x, o_at + 32 * b);
+            kv_tmem_loaded(x);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; i++) x[i] = 0u;
+        }
+        if (!valid) continue;
+        float y[32];
+#pragma unroll
+        for (int i = 0; i < 32; i++) y[i] = l == 0.f && fine ? 0.f : __uint_as_float(x[i]) * out_factor;
+        if (A.splits == 1) {
+            uint16_t* dst = (uint16_t*)A.out.data + token * A.out.token_stride + head * A.out.head_stride + 32 * b;
+#pragma unroll
+            for (int i = 0; i < 4; i++) *(uint4*)(dst + 8 * i) = kv_narrow8<BF>(y + 8 * i);
+        } else {
+            float* dst = A.part_o + (((int64_t)chunk * B.total_new + token) * S.q_heads + head) * D + 32 * b;
+#pragma unroll
+            for (int i = 0; i < 8; i++) *(float4*)(dst + 4 * i) = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+        }
+    }
+    if (!valid) return;
+    if (A.splits == 1) {
+        const float l2 = l == 0.f ? -KV_INF : m + log2f(l);
+        if (A.lse) A.lse[token * S.q_heads + head] = l2 * 0.6931471805599453f;
+        A.lse2[kv_lse2_at(S, q, kh, row)] = l2;
+    } else {
+        *(float2*)(A.part_ml + 2 * (((int64_t)chunk * B.total_new + token) * S.q_heads + head)) = make_float2(m, l);
+    }
+}
+
+// K and V of the tiles, widened to f16: 128 threads, of which warp w has tokens 32 w .. 32 w + 31 of a tile.
+template <int D, bool BF, bool E4M3>
+__device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch& B, const KvSeq& q, int seq, int kh, int begin, int end, int tiles, uint8_t* sm,
+                                                uint32_t bars, volatile int* stop)
+{
+    using T = KvPrompt<D>;
+    constexpr int P = D / 16;                            // pieces of 16 channels in a row; a lane has items lane + 32 i, i < P, of the warp's 32 P
+    const int warp = threadIdx.x >> 5 & 3, lane = threadIdx.x & 31;
+    const int tail_begin = q.full << S.block_shift;
+    KvSlot* const slots = (KvSlot*)(sm + T::SCALES);
+    const uint16_t* const tail = (const uint16_t*)B.tail + (uint64_t)seq * S.tail_values + (uint64_t)kh * 2 * S.block_tokens * D;
+    // 16 tokens from t on: page >= 0, absent or behind the end -1, of the tail -2
+    auto kind_of = [&](int t) { return t >= end ? -1 : t >= tail_begin ? -2 : kv_page(B, seq, t >> S.block_shift); };
+    auto codes = [&](uint4 (&w)[P], int which, int t0, int2 kind) {
+#pragma unroll
+        for (int i = 0; i < P; i++) {
+            const int row = (lane + 32 * i) / P, piece = (lane + 32 * i) % P, page = row < KV_HALF ? kind.x : kind.y;
+            w[i] = make_uint4(0, 0, 0, 0);
+            if (page >= 0)
+                w[i] = __ldg((const uint4*)(B.pool + (uint64_t)page * S.page_bytes + (uint64_t)which * S.codes_bytes +
+                                            ((uint64_t)kh * S.block_tokens + ((t0 + row) & (S.block_tokens - 1))) * D + 16 * piece));
+        }
+    };
+    // the largest magnitude of 16 tail tokens from t on, as a power of two not above it
+    auto tail_power = [&](int which, int t) {
+        uint32_t amax = 0;
+        for (int i = lane; i < KV_HALF * D / 8; i += 32)
+            if (t + i / (D / 8) < q.len) amax = max(amax, kv_amax8(*(const uint4*)(tail + ((uint64_t)which * S.block_tokens + t - tail_begin) * D + 8 * i)));
+        return kv_power_below(__reduce_max_sync(0xffffffffu, amax));
+    };
+    auto store = [&](const uint4 (&w)[P], int which, int t0, int2 kind, float2 power, uint8_t* dst) {
+#pragma unroll
+        for (int i = 0; i < P; i++) {
+            const int row = (lane + 32 * i) / P, piece = (lane + 32 * i) % P, page = row < KV_HALF ? kind.x : kind.y;
+            uint4 lo, hi;
+            if (page == -2) {
+                lo = hi = make_uint4(0, 0, 0, 0);
+                if (t0 + row < q.len) {
+                    const uint4* src = (const uint4*)(tail + ((uint64_t)which * S.block_tokens + t0 + row - tail_begin) * D + 16 * piece);
+                    lo = src[0];
+                    hi = src[1];
+                    if (BF) {
+                        const float inv = 1.f / (row < KV_HALF ? power.x : power.y);
+                        float x[16];
+                        kv_widen8<true>(lo, x);
+                        kv_widen8<true>(hi, x + 8);
+#pragma unroll
+                        for (int e = 0; e < 16; e++) x[e] *= inv;
+                        lo = kv_narrow8<false>(x);
+                        hi = kv_narrow8<false>(x + 8);
+                    }
+                }
+            } else {
+                kv_widen16<E4M3>(w[i], lo, hi);          // an absent page's zero bytes are zeros
+            }
+            *(uint4*)(dst + T::at(32 * warp + row, 16 * piece)) = lo;
+            *(uint4*)(dst + T::at(32 * warp + row, 16 * piece + 8)) = hi;
+        }
+    };
+    float vref = 0.f;                                    // by the first warp's lanes
+    uint4 kw[P], vw[P];
+    int t0 = begin + 32 * warp;
+    int2 kind = make_int2(kind_of(t0), kind_of(t0 + KV_HALF));
+    codes(kw, 0, t0, kind);
+    codes(vw, 1, t0, kind);
+    for (int j = 0; j < tiles; j++, t0 += KV_P_TOKENS) {
+        const int2 next = make_int2(kind_of(t0 + KV_P_TOKENS), kind_of(t0 + KV_P_TOKENS + KV_HALF));
+        float2 kp = make_float2(1.f, 1.f), vp = kp;
+        KvSlot& slot = slots[j & 3];
+        const int tile0 = begin + KV_P_TOKENS * j;
+        if (!__all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * (KV_K_OUT + (j & 1)), (j >> 1 & 1) ^ 1, stop))) return;
+        if (BF && tile0 + KV_P_TOKENS > tail_begin && tail_begin < end) {
+            // the tail's powers of two go through the slot: y K's, z V's
+            if (kind.x == -2) { kp.x = tail_power(0, t0); vp.x = tail_power(1, t0); }
+            if (kind.y == -2) { kp.y = tail_power(0, t0 + KV_HALF); vp.y = tail_power(1, t0 + KV_HALF); }
+            if (lane == 0) {
+                slot.group[2 * warp].y = kp.x;
+                slot.group[2 * warp].z = vp.x;
+                slot.group[2 * warp + 1].y = kp.y;
+                slot.group[2 * warp + 1].z = vp.y;
+            }
+            __syncwarp();
+            if (lane == 0) kv_arrive(bars + 8 * KV_TAIL);
+            if (warp == 0 && !__all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * KV_TAIL, 0, stop))) return;   // once: the tail lies in one tile
+        }
+        if (warp == 0) {
+            // lane g < 8: 16 tokens' scales
+            const int t = tile0 + KV_HALF * (lane & 7), page = kind_of(t);
+            float ks = 0.f, vs = 0.f;
+            if (page >= 0) {
+                const float2 sc = __ldg((const float2*)(kv_scales(S, B, page) + 2 * kh));
+                ks = kv_finite(sc.x);
+                vs = kv_finite(sc.y);
+            } else if (page == -2) {
+                ks = BF ? slot.group[lane & 7].y : 1.f;
+                vs = BF ? slot.group[lane & 7].z : 1.f;
+            }
+            float most = vs;
+#pragma unroll
+            for (int d = 1; d < 8; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+            float step = 1.f;
+            if (most > vref) {
+                const float higher = 4.f * kv_power_below(__float_as_uint(most));
+                step = vref / higher;
+                vref = higher;
+            }
+            const float share = vref > 0.f ? fmaxf(vs / vref, KV_P_LEAST) * KV_P_SCALE : 1.f;
+            const bool some_absent = __any_sync(0xffffffffu, page == -1);
+            if (lane < 8) slot.group[lane] = make_float4(ks, vs == vs ? log2f(share) : vs, 1.f / share, page == -1 ? 0.f : 1.f);
+            if (lane == 0) {
+                slot.step = step;
+                slot.unit = vref > 0.f ? vref / KV_P_SCALE : 1.f;
+                slot.pad[0] = some_absent ? 1.f : 0.f;
+            }
+        }
+        store(kw, 0, t0, kind, kp, sm + T::K + (j & 1) * T::TILE);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        kv_arrive(bars + 8 * (KV_K_IN + (j & 3)));
+        codes(kw, 0, t0 + KV_P_TOKENS, next);
+        if (!__all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * (KV_V_OUT + (j & 1)), (j >> 1 & 1) ^ 1, stop))) return;
+        store(vw, 1, t0, kind, vp, sm + T::V + (j & 1) * T::TILE);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        kv_arrive(bars + 8 * (KV_V_IN + (j & 1)));
+        codes(vw, 1, t0 + KV_P_TOKENS, next);
+        kind = next;
+    }
+}
+
+// The products, by one thread.  They run in the order in which they are issued: a tile's S is written over the weights of the tile
+// before it after those have been used.
+template <int D>
+__device__ __forceinline__ void kv_prompt_products(int tiles, int parts, uint32_t sm_at, uint32_t bars, volatile int* stop, uint32_t tmem)
+{
+    using T = KvPrompt<D>;
+    // f32 += f16 * f16; M = 128, N in eights; V is the operand whose N runs along the row
+    constexpr uint32_t shape = 1u << 4 | (uint32_t)(KV_P_ROWS / 16) << 24;
+    constexpr uint32_t s_what = shape | (uint32_t)(KV_P_TOKENS / 8) << 17, o_what = shape | (uint32_t)(D / 8) << 17 | 1u << 16;
+    auto scores = [&](int j, int m) {
+        const uint64_t a = kv_desc(sm_at + T::Q + m * T::TILE, 16, 1024), b = kv_desc(sm_at + T::K + (j & 1) * T::TILE, 16, 1024);
+#pragma unroll
+        for (int s = 0; s < D / 16; s++) {
+            const uint32_t off = ((s >> 2) * KV_P_TOKENS * 128 + (s & 3) * 32) >> 4;
+            kv_mma_ss(tmem + 128 * m, a + off, b + off, s_what, s > 0);
+        }
+        kv_commit(bars + 8 * (KV_S_IN + m));
+    };
+    auto answers = [&](int j, int m) {
+        const uint64_t b = kv_desc(sm_at + T::V + (j & 1) * T::TILE, KV_P_TOKENS * 128, 1024);
+#pragma unroll
+        for (int s = 0; s < KV_P_TOKENS / 16; s++) kv_mma_ts(tmem + 256 + 128 * m, tmem + 128 * m + 8 * s, b + (s * 2048 >> 4), o_what, j > 0 || s > 0);
+    };
+    if (!kv_wait_or_stop(bars + 8 * KV_Q_IN, 0, stop)) return;
+    for (int j = 0; j <= tiles; j++) {
+        if (j < tiles && !kv_wait_or_stop(bars + 8 * (KV_K_IN + (j & 3)), j >> 2 & 1, stop)) return;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        for (int m = 0; m < parts; m++) {
+            if (j > 0) {
+                if (m == 0 && !kv_wait_or_stop(bars + 8 * (KV_V_IN + ((j - 1) & 1)), (j - 1) >> 1 & 1, stop)) return;
+                if (!kv_wait_or_stop(bars + 8 * (KV_P_IN + m), (j - 1) & 1, stop)) return;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                answers(j - 1, m);
+            }
+            if (j < tiles) scores(j, m);
+            else kv_commit(bars + 8 * (KV_S_IN + m));    // the last answers
+        }
+        if (j > 0) kv_commit(bars + 8 * (KV_V_OUT + ((j - 1) & 1)));
+        if (j < tiles) kv_commit(bars + 8 * (KV_K_OUT + (j & 1)));
+    }
+}
+
+template <int D, bool BF, bool E4M3>
+__global__ void __launch_bounds__(KV_P_THREADS, 1) kv_prompt_kernel(const KvShape S, const KvBatch B, const KvAttend A)
+{
+    using T = KvPrompt<D>;
+    extern __shared__ uint8_t kv_raw[];
+    uint8_t* const sm = (uint8_t*)(((uintptr_t)kv_raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t sm_at = (uint32_t)__cvta_generic_to_shared(sm), bars = sm_at + T::BARS;
+    const int warp = threadIdx.x >> 5;
+    const int chunk = blockIdx.x, kh = blockIdx.y % S.kv_heads, tile_row = blockIdx.y / S.kv_heads * A.rows, seq = blockIdx.z;
+    asm volatile("griddepcontrol.launch_dependents;");
+    const KvSeq q = kv_seq(S, B, seq);
+    const KvSpan span = kv_span(S, q, A.window, tile_row, A.rows);
+    const int rows = q.n * S.group;
+    if (tile_row >= rows) return;
+    const int begin = span.begin + chunk * A.chunk, end = min(span.end, begin + A.chunk);
+    if (begin >= end && chunk > 0) return;
+    const int tiles = max((end - begin + KV_P_TOKENS - 1) / KV_P_TOKENS, 0), parts = tile_row + KV_P_ROWS < rows ? 2 : 1;
+
+    volatile int* const stop = (volatile int*)(sm + T::BARS + 8 * KV_BARS);
+    uint32_t* const tmem_at = (uint32_t*)(sm + T::BARS + 8 * KV_BARS + 4);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < KV_BARS; i++) {
+            const int count = i < KV_K_OUT || i == KV_V_IN || i == KV_V_IN + 1 || i == KV_P_IN || i == KV_P_IN + 1 ? 128 : i == KV_Q_IN ? 128 * parts : i == KV_TAIL ? 4 : 1;
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bars + 8 * i), "r"(count) : "memory");
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        *stop = 0;
+    }
+    if (warp == 12) asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"((uint32_t)__cvta_generic_to_shared(tmem_at)) : "memory");
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = *(volatile uint32_t*)tmem_at;  // S_0, S_1, O_0, O_1: 128 columns each
+
+    if (warp < 8) {
+        if (warp < 4 * parts) kv_prompt_rows<D, BF>(S, B, A, q, seq, kh, tile_row, warp >> 2, chunk, begin, end, tiles, sm, bars, stop, tmem);
+    } else if (warp < 12) {
+        kv_prompt_bring<D, BF, E4M3>(S, B, q, seq, kh, begin, end, tiles, sm, bars, stop);
+    } else {
+        if ((threadIdx.x & 31) == 0) {
+            kv_prompt_products<D>(tiles, parts, sm_at, bars, stop, tmem);
+            kv_commit(bars + 8 * KV_END);                // nothing is on its way any more when the memory is given back
+            kv_wait(bars + 8 * KV_END, 0);
+        }
+        __syncwarp();
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 12) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    }
+}

@@ -57,7 +57,7 @@ def test_null_handles():
 BAD_CONFIGS = [dict(dtype=2), dict(format=-1), dict(q_heads=0), dict(q_heads=1025), dict(q_heads=9), dict(kv_heads=0), dict(head_dim=80), dict(block_tokens=48),
                dict(block_tokens=8), dict(rotary=3), dict(rotary=1), dict(rotary=1, frequencies=[1.0] * 7), dict(rotary=1, frequencies=[1.0] * 72),
                dict(rotary=2, frequencies=[1.0] * 7 + [math.inf]), dict(frequencies=[1.0] * 8), dict(rotary=1, frequencies=[1.0] * 8, rotary_gain=math.nan),
-               dict(softmax_scale=math.inf)]
+               dict(softmax_scale=math.inf), dict(softmax_scale=-0.1)]
 
 
 @pytest.mark.parametrize("change", BAD_CONFIGS, ids=str)

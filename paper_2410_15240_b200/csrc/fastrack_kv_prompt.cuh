@@ -71,6 +71,32 @@ __device__ __forceinline__ void kv_tmem_loaded(uint32_t (&x)[32])
     for (int i = 0; i < 32; i++) asm volatile("" : "+r"(x[i]));
 }
 
+// Two 32-bit floats in one instruction
+__device__ __forceinline__ uint64_t kv_pair(float a, float b)
+{
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ float2 kv_unpair(uint64_t d)
+{
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(d));
+    return f;
+}
+__device__ __forceinline__ uint64_t kv_fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t kv_add2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
 // Bounded wait that also ends when another warp has given up.
 __device__ __forceinline__ bool kv_wait_or_stop(uint32_t bar, uint32_t parity, volatile int* stop)
 {
@@ -150,9 +176,9 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
     const int first_row = tile_row + KV_P_ROWS * m_tile + 32 * (warp & 3), last_row = min(first_row + 31, rows - 1);
     const int see_all = first_row + 31 < rows ? q.len - q.n + first_row / S.group : -1;
     const int low_all = A.window > 0 ? q.len - q.n + last_row / S.group - A.window : -1;
-    const int unit_stride = B.max_new * S.group, per_block = S.block_tokens / KV_HALF, per_shift = S.block_shift - 4;
+    const int unit_stride = B.max_new * S.group, per_block = S.block_tokens / KV_HALF;
     float* const units = A.unit_l2 && valid ? A.unit_l2 + ((int64_t)seq * S.kv_heads + kh) * A.units * unit_stride + row : nullptr;
-    float m = -KV_INF, l = 0.f, unit = 1.f;
+    float m = -KV_INF, l = 0.f, unit = 1.f, half_block = 0.f;
     bool fine = true;
     for (int j = 0; j < tiles; j++) {
         const int t0 = begin + KV_P_TOKENS * j;
@@ -161,31 +187,40 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const KvSlot& slot = slots[j & 3];
         const bool ragged = slot.pad[0] != 0.f || t0 + KV_P_TOKENS - 1 > see_all || t0 <= low_all;
-        auto hidden = [&](int col) {
-            const int t = t0 + col;
-            return t > place || (A.window > 0 && t <= place - A.window) || slot.group[col >> 4].w == 0.f;
+        // which of the tokens t0 + 32 b .. + 31 the row sees
+        auto visible = [&](int b) {
+            const int t = t0 + 32 * b, upto = min(max(place - t + 1, 0), 32), from = A.window > 0 ? min(max(place - A.window + 1 - t, 0), 32) : 0;
+            uint32_t bits = (uint32_t)(((uint64_t)1 << upto) - 1) & ~(uint32_t)(((uint64_t)1 << from) - 1);
+            if (slot.group[2 * b].w == 0.f) bits &= 0xffff0000u;
+            if (slot.group[2 * b + 1].w == 0.f) bits &= 0x0000ffffu;
+            return bits;
         };
         // the row's largest score; a scale is not negative, so that of 16 tokens with one scale the largest product is the largest score
         float top = -KV_INF;
-        uint32_t x[32];
+        uint32_t x[2][32];
+        auto largest = [&](int b, uint32_t (&y)[32]) {
+            if (ragged) {
+                const uint32_t bits = visible(b);
 #pragma unroll
-        for (int b = 0; b < 4; b++) {
-            kv_tmem_load32(x, s_at + 32 * b);
-            kv_tmem_loaded(x);
+                for (int i = 0; i < 32; i++) y[i] = bits >> i & 1 ? y[i] : 0xff800000u;
+            }
 #pragma unroll
             for (int h = 0; h < 2; h++) {
-                const float f = slot.group[2 * b + h].x * factor;
-                float g = -KV_INF;
-                if (ragged) {
+                float g = fmaxf(__uint_as_float(y[16 * h]), __uint_as_float(y[16 * h + 1]));
 #pragma unroll
-                    for (int i = 0; i < 16; i++) g = fmaxf(g, hidden(32 * b + 16 * h + i) ? -KV_INF : __uint_as_float(x[16 * h + i]));
-                    if (g > -KV_INF) top = fmaxf(top, g * f);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; i++) g = fmaxf(g, __uint_as_float(x[16 * h + i]));
-                    top = fmaxf(top, g * f);
-                }
+                for (int i = 2; i < 16; i += 2) g = fmaxf(fmaxf(g, __uint_as_float(y[16 * h + i])), __uint_as_float(y[16 * h + i + 1]));
+                g *= slot.group[2 * b + h].x * factor;
+                if (g == g) top = fmaxf(top, g);         // 0 times -inf where 16 hidden tokens have a scale of 0
             }
+        };
+#pragma unroll
+        for (int c = 0; c < 2; c++) {
+            kv_tmem_load32(x[0], s_at + 64 * c);
+            kv_tmem_load32(x[1], s_at + 64 * c + 32);
+            kv_tmem_loaded(x[0]);
+            kv_tmem_loaded(x[1]);
+            largest(2 * c, x[0]);
+            largest(2 * c + 1, x[1]);
         }
         float step = slot.step;                          // O is in units of V's reference, l is not
         unit = slot.unit;
@@ -196,50 +231,80 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
             m = top;
         }
         if (j > 0 && __any_sync(0xffffffffu, step != 1.f)) {
-#pragma unroll
+#pragma unroll 1
             for (int b = 0; b < D / 32; b++) {
-                kv_tmem_load32(x, o_at + 32 * b);
-                kv_tmem_loaded(x);
+                uint32_t y[32];
+                kv_tmem_load32(y, o_at + 32 * b);
+                kv_tmem_loaded(y);
 #pragma unroll
-                for (int i = 0; i < 32; i++) x[i] = __float_as_uint(__uint_as_float(x[i]) * step);
-                kv_tmem_store32(x, o_at + 32 * b);
+                for (int i = 0; i < 32; i++) y[i] = __float_as_uint(__uint_as_float(y[i]) * step);
+                kv_tmem_store32(y, o_at + 32 * b);
             }
         }
-        // weights times V's share of the reference: the share's logarithm goes into the exponent, and out of the sum again by its inverse
+        // weights times V's share of the reference: the share's logarithm goes into the exponent, and out of the sum again by its inverse.
+        // The second half's scores are in registers still, the first half's are read again.
         const float base = m == -KV_INF ? 0.f : m;
-        float block_sum = 0.f;
+#pragma unroll 1
+        for (int c = 1; c >= 0; c--) {
+            if (c == 0) {
+                kv_tmem_load32(x[0], s_at);
+                kv_tmem_load32(x[1], s_at + 32);
+                kv_tmem_loaded(x[0]);
+                kv_tmem_loaded(x[1]);
+            }
+            float sums[4];
 #pragma unroll
-        for (int b = 0; b < 4; b++) {
-            kv_tmem_load32(x, s_at + 32 * b);
-            kv_tmem_loaded(x);
-            uint32_t p[16];
+            for (int b = 0; b < 2; b++) {
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const float4 sc = slot.group[2 * b + h];
-                const float f = sc.x * factor, up = sc.y - base;
-                float sum = 0.f;
+                for (int h = 0; h < 2; h++) {
+                    const float4 sc = slot.group[4 * c + 2 * b + h];
+                    const float f = sc.x * factor, up = sc.y - base;
+                    const uint64_t ff = kv_pair(f, f), uu = kv_pair(up, up);
 #pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    float y = kv_exp2(fmaf(__uint_as_float(x[16 * h + i]), f, up)), z = kv_exp2(fmaf(__uint_as_float(x[16 * h + i + 1]), f, up));
-                    if (ragged) {
-                        if (hidden(32 * b + 16 * h + i)) y = 0.f;
-                        if (hidden(32 * b + 16 * h + i + 1)) z = 0.f;
+                    for (int i = 0; i < 16; i += 2) {
+                        const float2 z = kv_unpair(kv_fma2(kv_pair(__uint_as_float(x[b][16 * h + i]), __uint_as_float(x[b][16 * h + i + 1])), ff, uu));
+                        x[b][16 * h + i] = __float_as_uint(kv_exp2(z.x));
+                        x[b][16 * h + i + 1] = __float_as_uint(kv_exp2(z.y));
                     }
-                    sum += y + z;
-                    p[8 * h + i / 2] = kv_pack<false>(y, z);
                 }
-                sum = sum == 0.f ? 0.f : sum * sc.z;     // a hidden block's scale may be NaN
-                l += sum;
-                if (units) {
-                    block_sum += sum;
-                    if (((2 * b + h + 1) & (per_block - 1)) == 0) {
-                        const int block = (t0 >> S.block_shift) + (2 * b + h >> per_shift);
-                        if (block << S.block_shift < end) units[(int64_t)block * unit_stride] = kv_log2(block_sum) + base;
-                        block_sum = 0.f;
+                if (ragged) {
+                    const uint32_t bits = visible(2 * c + b);
+#pragma unroll
+                    for (int i = 0; i < 32; i++) x[b][i] = bits >> i & 1 ? x[b][i] : 0u;
+                }
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    uint64_t sum = kv_pair(__uint_as_float(x[b][16 * h]), __uint_as_float(x[b][16 * h + 1]));
+#pragma unroll
+                    for (int i = 2; i < 16; i += 2) sum = kv_add2(sum, kv_pair(__uint_as_float(x[b][16 * h + i]), __uint_as_float(x[b][16 * h + i + 1])));
+                    const float2 z = kv_unpair(sum);
+                    const float all = z.x + z.y;
+                    sums[2 * b + h] = all == 0.f ? 0.f : all * slot.group[4 * c + 2 * b + h].z;     // a hidden block's scale may be NaN
+                    l += sums[2 * b + h];
+                }
+#pragma unroll
+                for (int i = 0; i < 16; i++) x[0][16 * b + i] = kv_pack<false>(__uint_as_float(x[b][2 * i]), __uint_as_float(x[b][2 * i + 1]));
+            }
+            kv_tmem_store32(x[0], s_at + 64 * c);        // the weights of tokens 64 c .. 64 c + 63
+            if (units) {
+                const int first = (t0 + 64 * c) >> S.block_shift;
+                if (per_block >= 4) {                    // blocks of 64 tokens, or half a block of 128
+                    float sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+                    if (per_block == 8) {
+                        half_block += sum;
+                        sum = half_block;
                     }
+                    if ((per_block == 4 || c == 0) && first << S.block_shift < end) units[(int64_t)first * unit_stride] = kv_log2(sum) + base;
+                    if (c == 0) half_block = 0.f;
+                } else {
+#pragma unroll
+                    for (int g = 0; g < 4; g++)
+                        if (per_block == 1 || (g & 1)) {
+                            const int block = first + (per_block == 1 ? g : g >> 1);
+                            if (block << S.block_shift < end) units[(int64_t)block * unit_stride] = kv_log2(per_block == 1 ? sums[g] : sums[g - (g > 0)] + sums[g]) + base;
+                        }
                 }
             }
-            kv_tmem_store16(p, s_at + 16 * b);
         }
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -289,21 +354,25 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
                                                 uint32_t bars, volatile int* stop)
 {
     using T = KvPrompt<D>;
-    constexpr int P = D / 16;                            // pieces of 16 channels in a row; a lane has items lane + 32 i, i < P, of the warp's 32 P
+    // A lane's share of 16 tokens, P pieces of 16 channels.  Eight rows by four pieces of 64 channels at a time: eight lanes then write
+    // pieces of two neighbouring rows, which the swizzle keeps apart.  The last 32 of 96 channels go sixteen rows by two pieces.
+    constexpr int P = D / 32;
+    auto row_of = [](int lane, int i) { return D == 96 && i == 2 ? lane >> 1 : (lane >> 2) + 8 * (D == 128 ? i >> 1 : i); };
+    auto channel_of = [](int lane, int i) { return D == 96 && i == 2 ? 64 + 16 * (lane & 1) : 16 * (lane & 3) + 64 * (D == 128 ? i & 1 : 0); };
     const int warp = threadIdx.x >> 5 & 3, lane = threadIdx.x & 31;
     const int tail_begin = q.full << S.block_shift;
     KvSlot* const slots = (KvSlot*)(sm + T::SCALES);
     const uint16_t* const tail = (const uint16_t*)B.tail + (uint64_t)seq * S.tail_values + (uint64_t)kh * 2 * S.block_tokens * D;
     // 16 tokens from t on: page >= 0, absent or behind the end -1, of the tail -2
     auto kind_of = [&](int t) { return t >= end ? -1 : t >= tail_begin ? -2 : kv_page(B, seq, t >> S.block_shift); };
-    auto codes = [&](uint4 (&w)[P], int which, int t0, int2 kind) {
+    auto codes = [&](uint4 (&w)[2][P], int which, int t0, int2 kind) {
 #pragma unroll
-        for (int i = 0; i < P; i++) {
-            const int row = (lane + 32 * i) / P, piece = (lane + 32 * i) % P, page = row < KV_HALF ? kind.x : kind.y;
-            w[i] = make_uint4(0, 0, 0, 0);
-            if (page >= 0)
-                w[i] = __ldg((const uint4*)(B.pool + (uint64_t)page * S.page_bytes + (uint64_t)which * S.codes_bytes +
-                                            ((uint64_t)kh * S.block_tokens + ((t0 + row) & (S.block_tokens - 1))) * D + 16 * piece));
+        for (int h = 0; h < 2; h++) {
+            const int page = h ? kind.y : kind.x;
+            const uint8_t* src = B.pool + (uint64_t)page * S.page_bytes + (uint64_t)which * S.codes_bytes +
+                                 ((uint64_t)kh * S.block_tokens + ((t0 + KV_HALF * h) & (S.block_tokens - 1))) * D;
+#pragma unroll
+            for (int i = 0; i < P; i++) w[h][i] = page >= 0 ? __ldg((const uint4*)(src + row_of(lane, i) * D + channel_of(lane, i))) : make_uint4(0, 0, 0, 0);
         }
     };
     // the largest magnitude of 16 tail tokens from t on, as a power of two not above it
@@ -313,37 +382,46 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
             if (t + i / (D / 8) < q.len) amax = max(amax, kv_amax8(*(const uint4*)(tail + ((uint64_t)which * S.block_tokens + t - tail_begin) * D + 8 * i)));
         return kv_power_below(__reduce_max_sync(0xffffffffu, amax));
     };
-    auto store = [&](const uint4 (&w)[P], int which, int t0, int2 kind, float2 power, uint8_t* dst) {
+    auto store = [&](const uint4 (&w)[2][P], int which, int t0, int2 kind, float2 power, uint8_t* dst) {
 #pragma unroll
-        for (int i = 0; i < P; i++) {
-            const int row = (lane + 32 * i) / P, piece = (lane + 32 * i) % P, page = row < KV_HALF ? kind.x : kind.y;
-            uint4 lo, hi;
-            if (page == -2) {
-                lo = hi = make_uint4(0, 0, 0, 0);
-                if (t0 + row < q.len) {
-                    const uint4* src = (const uint4*)(tail + ((uint64_t)which * S.block_tokens + t0 + row - tail_begin) * D + 16 * piece);
-                    lo = src[0];
-                    hi = src[1];
-                    if (BF) {
-                        const float inv = 1.f / (row < KV_HALF ? power.x : power.y);
-                        float x[16];
-                        kv_widen8<true>(lo, x);
-                        kv_widen8<true>(hi, x + 8);
+        for (int h = 0; h < 2; h++) {
+            if ((h ? kind.y : kind.x) != -2) {
 #pragma unroll
-                        for (int e = 0; e < 16; e++) x[e] *= inv;
-                        lo = kv_narrow8<false>(x);
-                        hi = kv_narrow8<false>(x + 8);
-                    }
+                for (int i = 0; i < P; i++) {
+                    const int row = 32 * warp + KV_HALF * h + row_of(lane, i), ch = channel_of(lane, i);
+                    uint4 lo, hi;
+                    kv_widen16<E4M3>(w[h][i], lo, hi);   // an absent page's zero bytes are zeros
+                    *(uint4*)(dst + T::at(row, ch)) = lo;
+                    *(uint4*)(dst + T::at(row, ch + 8)) = hi;
                 }
-            } else {
-                kv_widen16<E4M3>(w[i], lo, hi);          // an absent page's zero bytes are zeros
+                continue;
             }
-            *(uint4*)(dst + T::at(32 * warp + row, 16 * piece)) = lo;
-            *(uint4*)(dst + T::at(32 * warp + row, 16 * piece + 8)) = hi;
+            const float inv = 1.f / (h ? power.y : power.x);
+#pragma unroll 1
+            for (int i = 0; i < P; i++) {
+                const int row = KV_HALF * h + row_of(lane, i), ch = channel_of(lane, i);
+                uint4 v[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+                if (t0 + row < q.len) {
+                    const uint4* src = (const uint4*)(tail + ((uint64_t)which * S.block_tokens + t0 + row - tail_begin) * D + ch);
+                    v[0] = src[0];
+                    v[1] = src[1];
+                    if (BF)
+#pragma unroll
+                        for (int k = 0; k < 2; k++) {
+                            float x[8];
+                            kv_widen8<true>(v[k], x);
+#pragma unroll
+                            for (int e = 0; e < 8; e++) x[e] *= inv;
+                            v[k] = kv_narrow8<false>(x);
+                        }
+                }
+                *(uint4*)(dst + T::at(32 * warp + row, ch)) = v[0];
+                *(uint4*)(dst + T::at(32 * warp + row, ch + 8)) = v[1];
+            }
         }
     };
     float vref = 0.f;                                    // by the first warp's lanes
-    uint4 kw[P], vw[P];
+    uint4 kw[2][P], vw[2][P];
     int t0 = begin + 32 * warp;
     int2 kind = make_int2(kind_of(t0), kind_of(t0 + KV_HALF));
     codes(kw, 0, t0, kind);
@@ -432,7 +510,7 @@ __device__ __forceinline__ void kv_prompt_products(int tiles, int parts, uint32_
     auto answers = [&](int j, int m) {
         const uint64_t b = kv_desc(sm_at + T::V + (j & 1) * T::TILE, KV_P_TOKENS * 128, 1024);
 #pragma unroll
-        for (int s = 0; s < KV_P_TOKENS / 16; s++) kv_mma_ts(tmem + 256 + 128 * m, tmem + 128 * m + 8 * s, b + (s * 2048 >> 4), o_what, j > 0 || s > 0);
+        for (int s = 0; s < KV_P_TOKENS / 16; s++) kv_mma_ts(tmem + 256 + 128 * m, tmem + 128 * m + 64 * (s >> 2) + 8 * (s & 3), b + (s * 2048 >> 4), o_what, j > 0 || s > 0);
     };
     if (!kv_wait_or_stop(bars + 8 * KV_Q_IN, 0, stop)) return;
     for (int j = 0; j <= tiles; j++) {

@@ -14,7 +14,6 @@
 #define KV_P_TOKENS 128
 #define KV_P_THREADS 416
 #define KV_P_GROUPS (KV_P_TOKENS / KV_HALF)
-#define KV_P_LAZY 4.0f
 #define KV_P_LEAST 0x1p-40f             // a block's V scale counts for at least this share of the reference (below it V is lost to 11 bits anyway)
 
 template <int D> struct KvPrompt {
@@ -97,14 +96,30 @@ __device__ __forceinline__ uint64_t kv_add2(uint64_t a, uint64_t b)
     return d;
 }
 
-// Bounded wait that also ends when another warp has given up.
+// 16 f16 of a lane in tensor memory, times f
+__device__ __forceinline__ void kv_tmem_scale8(uint32_t at, __half2 f)
+{
+    uint32_t x[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];" : KV_R8(x, 0) : "r"(at) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        asm volatile("" : "+r"(x[i]));
+        const __half2 h = __hmul2(*(const __half2*)&x[i], f);
+        x[i] = *(const uint32_t*)&h;
+    }
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::KV_W8(x, 0), "r"(at) : "memory");
+}
+struct KvYes { static constexpr bool value = true; };
+struct KvNo { static constexpr bool value = false; };
+
+// Bounded wait that also ends when another warp has given up.  An attempt waits for a while by itself.
 __device__ __forceinline__ bool kv_wait_or_stop(uint32_t bar, uint32_t parity, volatile int* stop)
 {
-    for (int i = 0; i < 1 << 10; i++) {
-        uint32_t done = 0;
-        for (int attempt = 0; attempt < 64 && !done; attempt++)
-            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                         : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    for (int i = 0; i < 1 << 15; i++) {
+        uint32_t done;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done) : "r"(bar), "r"(parity) : "memory");
         if (done) return true;
         if (*stop) return false;
     }
@@ -145,29 +160,26 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
     {
         // the row of Q, as f16 (bf16: over a power of two near its largest), to shared memory
         const uint16_t* src = (const uint16_t*)A.q.data + token * A.q.token_stride + head * A.q.head_stride;
-        uint4 w[D / 8];
-        uint32_t amax = 0;
-#pragma unroll
-        for (int i = 0; i < D / 8; i++) {
-            w[i] = valid ? *(const uint4*)(src + 8 * i) : make_uint4(0, 0, 0, 0);
-            if (BF) amax = max(amax, kv_amax8(w[i]));
-        }
         float inv = 1.f;
         if (BF) {
+            uint32_t amax = 0;
+#pragma unroll 4
+            for (int i = 0; i < D / 8; i++) amax = max(amax, valid ? kv_amax8(*(const uint4*)(src + 8 * i)) : 0u);
             const float p = kv_power_below(amax);
             factor *= p;
             inv = 1.f / p;
         }
-#pragma unroll
+#pragma unroll 4
         for (int i = 0; i < D / 8; i++) {
+            uint4 w = valid ? *(const uint4*)(src + 8 * i) : make_uint4(0, 0, 0, 0);
             if (BF) {
                 float x[8];
-                kv_widen8<true>(w[i], x);
+                kv_widen8<true>(w, x);
 #pragma unroll
                 for (int e = 0; e < 8; e++) x[e] *= inv;
-                w[i] = kv_narrow8<false>(x);
+                w = kv_narrow8<false>(x);
             }
-            *(uint4*)(sm + T::Q + m_tile * T::TILE + T::at(r, 8 * i)) = w[i];
+            *(uint4*)(sm + T::Q + m_tile * T::TILE + T::at(r, 8 * i)) = w;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         kv_arrive(bars + 8 * KV_Q_IN);
@@ -176,60 +188,110 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
     const int first_row = tile_row + KV_P_ROWS * m_tile + 32 * (warp & 3), last_row = min(first_row + 31, rows - 1);
     const int see_all = first_row + 31 < rows ? q.len - q.n + first_row / S.group : -1;
     const int low_all = A.window > 0 ? q.len - q.n + last_row / S.group - A.window : -1;
-    const int unit_stride = B.max_new * S.group, per_block = S.block_tokens / KV_HALF;
+    const int unit_stride = B.max_new * S.group, per_block = S.block_tokens / KV_HALF, per_shift = S.block_shift - 4;
     float* const units = A.unit_l2 && valid ? A.unit_l2 + ((int64_t)seq * S.kv_heads + kh) * A.units * unit_stride + row : nullptr;
-    float m = -KV_INF, l = 0.f, unit = 1.f, half_block = 0.f;
+    float m = -KV_INF, l = 0.f, unit = 1.f;
     bool fine = true;
     for (int j = 0; j < tiles; j++) {
         const int t0 = begin + KV_P_TOKENS * j;
-        fine = __all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * (KV_K_IN + (j & 3)), j >> 2 & 1, stop) && kv_wait_or_stop(bars + 8 * (KV_S_IN + m_tile), j & 1, stop));
+        fine = __all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * (KV_S_IN + m_tile), j & 1, stop) && kv_wait_or_stop(bars + 8 * (KV_K_IN + (j & 3)), j >> 2 & 1, stop));
         if (!fine) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const KvSlot& slot = slots[j & 3];
         const bool ragged = slot.pad[0] != 0.f || t0 + KV_P_TOKENS - 1 > see_all || t0 <= low_all;
-        // which of the tokens t0 + 32 b .. + 31 the row sees
-        auto visible = [&](int b) {
-            const int t = t0 + 32 * b, upto = min(max(place - t + 1, 0), 32), from = A.window > 0 ? min(max(place - A.window + 1 - t, 0), 32) : 0;
-            uint32_t bits = (uint32_t)(((uint64_t)1 << upto) - 1) & ~(uint32_t)(((uint64_t)1 << from) - 1);
-            if (slot.group[2 * b].w == 0.f) bits &= 0xffff0000u;
-            if (slot.group[2 * b + 1].w == 0.f) bits &= 0x0000ffffu;
-            return bits;
-        };
-        // the row's largest score; a scale is not negative, so that of 16 tokens with one scale the largest product is the largest score
-        float top = -KV_INF;
-        uint32_t x[2][32];
-        auto largest = [&](int b, uint32_t (&y)[32]) {
-            if (ragged) {
-                const uint32_t bits = visible(b);
-#pragma unroll
-                for (int i = 0; i < 32; i++) y[i] = bits >> i & 1 ? y[i] : 0xff800000u;
-            }
-#pragma unroll
-            for (int h = 0; h < 2; h++) {
-                float g = fmaxf(__uint_as_float(y[16 * h]), __uint_as_float(y[16 * h + 1]));
-#pragma unroll
-                for (int i = 2; i < 16; i += 2) g = fmaxf(fmaxf(g, __uint_as_float(y[16 * h + i])), __uint_as_float(y[16 * h + i + 1]));
-                g *= slot.group[2 * b + h].x * factor;
-                if (g == g) top = fmaxf(top, g);         // 0 times -inf where 16 hidden tokens have a scale of 0
-            }
-        };
-#pragma unroll
-        for (int c = 0; c < 2; c++) {
-            kv_tmem_load32(x[0], s_at + 64 * c);
-            kv_tmem_load32(x[1], s_at + 64 * c + 32);
-            kv_tmem_loaded(x[0]);
-            kv_tmem_loaded(x[1]);
-            largest(2 * c, x[0]);
-            largest(2 * c + 1, x[1]);
-        }
-        float step = slot.step;                          // O is in units of V's reference, l is not
+        float step = slot.step, block_sum = 0.f;         // of O: it is in units of V's reference, l is not
         unit = slot.unit;
-        if (top > m + KV_P_LAZY) {
-            const float fall = kv_exp2(m - top);
-            l *= fall;
-            step *= fall;
-            m = top;
-        }
+        auto pass = [&](auto some_hidden) {
+            constexpr bool RAGGED = decltype(some_hidden)::value;
+            // not unrolled: the three kinds of warps run different code at a time, and more of it than this comes in too slowly
+#pragma unroll 1
+            for (int b = 0; b < KV_P_TOKENS / 32; b++) {
+                uint32_t y[32];
+                kv_tmem_load32(y, s_at + 32 * b);
+                kv_tmem_loaded(y);
+                uint32_t seen = 0xffffffffu;             // which of the 32 tokens the row sees
+                if (RAGGED) {
+                    const int t = t0 + 32 * b, upto = min(max(place - t + 1, 0), 32), from = A.window > 0 ? min(max(place - A.window + 1 - t, 0), 32) : 0;
+                    seen = (uint32_t)(((uint64_t)1 << upto) - 1) & ~(uint32_t)(((uint64_t)1 << from) - 1);
+                    if (slot.group[2 * b].w == 0.f) seen &= 0xffff0000u;
+                    if (slot.group[2 * b + 1].w == 0.f) seen &= 0x0000ffffu;
+#pragma unroll
+                    for (int i = 0; i < 32; i++) y[i] = seen >> i & 1 ? y[i] : 0xff800000u;
+                }
+                const float4 sc[2] = {slot.group[2 * b], slot.group[2 * b + 1]};
+                // the largest score; a scale is not negative, so that of 16 tokens with one scale the largest product is the largest score
+                float top = -KV_INF;
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    float g = fmaxf(__uint_as_float(y[16 * h]), __uint_as_float(y[16 * h + 1]));
+#pragma unroll
+                    for (int i = 2; i < 16; i += 2) g = fmaxf(fmaxf(g, __uint_as_float(y[16 * h + i])), __uint_as_float(y[16 * h + i + 1]));
+                    g *= sc[h].x * factor;
+                    if (!RAGGED || g == g) top = fmaxf(top, g);                  // 0 times -inf where 16 hidden tokens have a scale of 0
+                }
+                if (__any_sync(0xffffffffu, top > m + KV_LAZY)) {
+                    // rare after the first tile: the weights that this tile has already go down with all earlier ones
+                    float fall = 1.f;
+                    if (top > m + KV_LAZY) {
+                        fall = kv_exp2(m - top);
+                        m = top;
+                    }
+                    l *= fall;
+                    step *= fall;
+                    block_sum *= fall;
+                    if (b > 0) asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                    const __half2 down = __float2half2_rn(fall);
+#pragma unroll 1
+                    for (int k = 0; k < 16 * b; k += 8) kv_tmem_scale8(s_at + k, down);
+                }
+                // weights times V's share of the reference: the share's logarithm goes into the exponent, and out of the sum again by its inverse
+                const float base = m == -KV_INF ? 0.f : m;
+                // In three stages of 32 values, each in place: an exponential takes some 40 cycles, and a sequence that used each result at
+                // once would wait for every one of them (measured: 1000 cycles for 32 values against 400).
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    const float f = sc[h].x * factor, up = sc[h].y - base;
+                    const uint64_t ff = kv_pair(f, f), uu = kv_pair(up, up);
+#pragma unroll
+                    for (int i = 16 * h; i < 16 * h + 16; i += 2) {
+                        const float2 z = kv_unpair(kv_fma2(kv_pair(__uint_as_float(y[i]), __uint_as_float(y[i + 1])), ff, uu));
+                        y[i] = __float_as_uint(z.x);
+                        y[i + 1] = __float_as_uint(z.y);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 32; i++) asm volatile("ex2.approx.ftz.f32 %0, %0;" : "+r"(y[i]));
+                if (RAGGED)
+#pragma unroll
+                    for (int i = 0; i < 32; i++) y[i] = seen >> i & 1 ? y[i] : 0u;
+                uint32_t p[16];
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    uint64_t sum[2] = {0, 0};
+#pragma unroll
+                    for (int i = 0; i < 16; i += 2) {
+                        const float u = __uint_as_float(y[16 * h + i]), w = __uint_as_float(y[16 * h + i + 1]);
+                        sum[i >> 1 & 1] = kv_add2(sum[i >> 1 & 1], kv_pair(u, w));
+                        p[8 * h + i / 2] = kv_pack<false>(u, w);
+                    }
+                    const float2 z = kv_unpair(kv_add2(sum[0], sum[1]));
+                    float all = z.x + z.y;
+                    all = RAGGED && all == 0.f ? 0.f : all * sc[h].z;            // a hidden block's scale may be NaN
+                    l += all;
+                    if (units) {
+                        block_sum += all;
+                        if (((2 * b + h + 1) & (per_block - 1)) == 0) {
+                            const int block = (t0 >> S.block_shift) + (2 * b + h >> per_shift);
+                            if (block << S.block_shift < end) units[(int64_t)block * unit_stride] = kv_log2(block_sum) + base;
+                            block_sum = 0.f;
+                        }
+                    }
+                }
+                kv_tmem_store16(p, s_at + 16 * b);
+            }
+        };
+        if (ragged) pass(KvYes());
+        else pass(KvNo());
         if (j > 0 && __any_sync(0xffffffffu, step != 1.f)) {
 #pragma unroll 1
             for (int b = 0; b < D / 32; b++) {
@@ -239,71 +301,6 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
 #pragma unroll
                 for (int i = 0; i < 32; i++) y[i] = __float_as_uint(__uint_as_float(y[i]) * step);
                 kv_tmem_store32(y, o_at + 32 * b);
-            }
-        }
-        // weights times V's share of the reference: the share's logarithm goes into the exponent, and out of the sum again by its inverse.
-        // The second half's scores are in registers still, the first half's are read again.
-        const float base = m == -KV_INF ? 0.f : m;
-#pragma unroll 1
-        for (int c = 1; c >= 0; c--) {
-            if (c == 0) {
-                kv_tmem_load32(x[0], s_at);
-                kv_tmem_load32(x[1], s_at + 32);
-                kv_tmem_loaded(x[0]);
-                kv_tmem_loaded(x[1]);
-            }
-            float sums[4];
-#pragma unroll
-            for (int b = 0; b < 2; b++) {
-#pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    const float4 sc = slot.group[4 * c + 2 * b + h];
-                    const float f = sc.x * factor, up = sc.y - base;
-                    const uint64_t ff = kv_pair(f, f), uu = kv_pair(up, up);
-#pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        const float2 z = kv_unpair(kv_fma2(kv_pair(__uint_as_float(x[b][16 * h + i]), __uint_as_float(x[b][16 * h + i + 1])), ff, uu));
-                        x[b][16 * h + i] = __float_as_uint(kv_exp2(z.x));
-                        x[b][16 * h + i + 1] = __float_as_uint(kv_exp2(z.y));
-                    }
-                }
-                if (ragged) {
-                    const uint32_t bits = visible(2 * c + b);
-#pragma unroll
-                    for (int i = 0; i < 32; i++) x[b][i] = bits >> i & 1 ? x[b][i] : 0u;
-                }
-#pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    uint64_t sum = kv_pair(__uint_as_float(x[b][16 * h]), __uint_as_float(x[b][16 * h + 1]));
-#pragma unroll
-                    for (int i = 2; i < 16; i += 2) sum = kv_add2(sum, kv_pair(__uint_as_float(x[b][16 * h + i]), __uint_as_float(x[b][16 * h + i + 1])));
-                    const float2 z = kv_unpair(sum);
-                    const float all = z.x + z.y;
-                    sums[2 * b + h] = all == 0.f ? 0.f : all * slot.group[4 * c + 2 * b + h].z;     // a hidden block's scale may be NaN
-                    l += sums[2 * b + h];
-                }
-#pragma unroll
-                for (int i = 0; i < 16; i++) x[0][16 * b + i] = kv_pack<false>(__uint_as_float(x[b][2 * i]), __uint_as_float(x[b][2 * i + 1]));
-            }
-            kv_tmem_store32(x[0], s_at + 64 * c);        // the weights of tokens 64 c .. 64 c + 63
-            if (units) {
-                const int first = (t0 + 64 * c) >> S.block_shift;
-                if (per_block >= 4) {                    // blocks of 64 tokens, or half a block of 128
-                    float sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-                    if (per_block == 8) {
-                        half_block += sum;
-                        sum = half_block;
-                    }
-                    if ((per_block == 4 || c == 0) && first << S.block_shift < end) units[(int64_t)first * unit_stride] = kv_log2(sum) + base;
-                    if (c == 0) half_block = 0.f;
-                } else {
-#pragma unroll
-                    for (int g = 0; g < 4; g++)
-                        if (per_block == 1 || (g & 1)) {
-                            const int block = first + (per_block == 1 ? g : g >> 1);
-                            if (block << S.block_shift < end) units[(int64_t)block * unit_stride] = kv_log2(per_block == 1 ? sums[g] : sums[g - (g > 0)] + sums[g]) + base;
-                        }
-                }
             }
         }
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
@@ -420,12 +417,15 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
             }
         }
     };
-    float vref = 0.f;                                    // by the first warp's lanes
+    float vref = 0.f, vinv = 0.f;                        // by the first warp's lanes
     uint4 kw[2][P], vw[2][P];
     int t0 = begin + 32 * warp;
     int2 kind = make_int2(kind_of(t0), kind_of(t0 + KV_HALF));
     codes(kw, 0, t0, kind);
     codes(vw, 1, t0, kind);
+    auto scale_of = [&](int page) { return page >= 0 ? __ldg((const float2*)(kv_scales(S, B, page) + 2 * kh)) : make_float2(0.f, 0.f); };
+    int scale_page = kind_of(begin + KV_HALF * (lane & 7)), scale_next = kind_of(begin + KV_P_TOKENS + KV_HALF * (lane & 7));
+    float2 scale = scale_of(scale_page);
     for (int j = 0; j < tiles; j++, t0 += KV_P_TOKENS) {
         const int2 next = make_int2(kind_of(t0 + KV_P_TOKENS), kind_of(t0 + KV_P_TOKENS + KV_HALF));
         float2 kp = make_float2(1.f, 1.f), vp = kp;
@@ -447,17 +447,16 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
             if (warp == 0 && !__all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * KV_TAIL, 0, stop))) return;   // once: the tail lies in one tile
         }
         if (warp == 0) {
-            // lane g < 8: 16 tokens' scales
-            const int t = tile0 + KV_HALF * (lane & 7), page = kind_of(t);
-            float ks = 0.f, vs = 0.f;
-            if (page >= 0) {
-                const float2 sc = __ldg((const float2*)(kv_scales(S, B, page) + 2 * kh));
-                ks = kv_finite(sc.x);
-                vs = kv_finite(sc.y);
-            } else if (page == -2) {
+            // lane g < 8: 16 tokens' scales, asked for a tile ahead
+            float ks = kv_finite(scale.x), vs = kv_finite(scale.y);
+            const int page = scale_page;
+            if (page == -2) {
                 ks = BF ? slot.group[lane & 7].y : 1.f;
                 vs = BF ? slot.group[lane & 7].z : 1.f;
             }
+            scale_page = scale_next;
+            scale = scale_of(scale_page);
+            scale_next = kind_of(tile0 + 2 * KV_P_TOKENS + KV_HALF * (lane & 7));
             float most = vs;
 #pragma unroll
             for (int d = 1; d < 8; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
@@ -466,10 +465,11 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
                 const float higher = 4.f * kv_power_below(__float_as_uint(most));
                 step = vref / higher;
                 vref = higher;
+                vinv = 1.f / higher;
             }
-            const float share = vref > 0.f ? fmaxf(vs / vref, KV_P_LEAST) * KV_P_SCALE : 1.f;
+            const float share = vref > 0.f ? fmaxf(vs * vinv, KV_P_LEAST) * KV_P_SCALE : 1.f;
             const bool some_absent = __any_sync(0xffffffffu, page == -1);
-            if (lane < 8) slot.group[lane] = make_float4(ks, vs == vs ? log2f(share) : vs, 1.f / share, page == -1 ? 0.f : 1.f);
+            if (lane < 8) slot.group[lane] = make_float4(ks, vs == vs ? kv_log2(share) : vs, 1.f / share, page == -1 ? 0.f : 1.f);
             if (lane == 0) {
                 slot.step = step;
                 slot.unit = vref > 0.f ? vref / KV_P_SCALE : 1.f;
@@ -510,7 +510,7 @@ __device__ __forceinline__ void kv_prompt_products(int tiles, int parts, uint32_
     auto answers = [&](int j, int m) {
         const uint64_t b = kv_desc(sm_at + T::V + (j & 1) * T::TILE, KV_P_TOKENS * 128, 1024);
 #pragma unroll
-        for (int s = 0; s < KV_P_TOKENS / 16; s++) kv_mma_ts(tmem + 256 + 128 * m, tmem + 128 * m + 64 * (s >> 2) + 8 * (s & 3), b + (s * 2048 >> 4), o_what, j > 0 || s > 0);
+        for (int s = 0; s < KV_P_TOKENS / 16; s++) kv_mma_ts(tmem + 256 + 128 * m, tmem + 128 * m + 8 * s, b + (s * 2048 >> 4), o_what, j > 0 || s > 0);
     };
     if (!kv_wait_or_stop(bars + 8 * KV_Q_IN, 0, stop)) return;
     for (int j = 0; j <= tiles; j++) {
@@ -536,7 +536,8 @@ __global__ void __launch_bounds__(KV_P_THREADS, 1) kv_prompt_kernel(const KvShap
 {
     using T = KvPrompt<D>;
     extern __shared__ uint8_t kv_raw[];
-    uint8_t* const sm = (uint8_t*)(((uintptr_t)kv_raw + 1023) & ~(uintptr_t)1023);
+    // rounded up by an offset, so that the compiler still knows it for shared memory
+    uint8_t* const sm = kv_raw + (-(uint32_t)__cvta_generic_to_shared(kv_raw) & 1023u);
     const uint32_t sm_at = (uint32_t)__cvta_generic_to_shared(sm), bars = sm_at + T::BARS;
     const int warp = threadIdx.x >> 5;
     const int chunk = blockIdx.x, kh = blockIdx.y % S.kv_heads, tile_row = blockIdx.y / S.kv_heads * A.rows, seq = blockIdx.z;

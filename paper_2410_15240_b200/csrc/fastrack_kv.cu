@@ -581,7 +581,7 @@ static KvPlan kv_plan(const fastrack_kv* kv, const fastrack_kv_batch* b, bool ma
     p.chunk = (int)chunk;
     p.splits = (int)((b->max_len + chunk - 1) / chunk);
     if (p.splits < 1) p.splits = 1;
-    p.unit_shift = prompt ? S.block_shift : 4;
+    p.unit_shift = prompt ? (S.block_shift < 6 ? S.block_shift : 6) : 4;   // blocks of up to 64 tokens, or 16 tokens
     p.units = (b->max_len + (1 << p.unit_shift) - 1) >> p.unit_shift;
     const size_t all = (size_t)b->total_new * S.q_heads;
     p.ml = p.splits > 1 ? (size_t)p.splits * all * S.head_dim * 4 : 0;

@@ -14,6 +14,7 @@
 #define KV_P_TOKENS 128
 #define KV_P_THREADS 416
 #define KV_P_GROUPS (KV_P_TOKENS / KV_HALF)
+#define KV_P_AHEAD 4                   // pairs of values between an exponential and the use of its result
 #define KV_P_LEAST 0x1p-40f             // a block's V scale counts for at least this share of the reference (below it V is lost to 11 bits anyway)
 
 template <int D> struct KvPrompt {
@@ -113,14 +114,18 @@ __device__ __forceinline__ void kv_tmem_scale8(uint32_t at, __half2 f)
 struct KvYes { static constexpr bool value = true; };
 struct KvNo { static constexpr bool value = false; };
 
-// Bounded wait that also ends when another warp has given up.  An attempt waits for a while by itself.
+// Bounded wait that also ends when another warp has given up.
 __device__ __forceinline__ bool kv_wait_or_stop(uint32_t bar, uint32_t parity, volatile int* stop)
 {
-    for (int i = 0; i < 1 << 15; i++) {
-        uint32_t done;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-        if (done) return true;
+#pragma unroll 1
+    for (int i = 0; i < 1 << 14; i++) {
+#pragma unroll 1
+        for (int k = 0; k < 16; k++) {
+            uint32_t done;
+            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                         : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+            if (done) return true;
+        }
         if (*stop) return false;
     }
     *stop = 1;
@@ -188,8 +193,9 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
     const int first_row = tile_row + KV_P_ROWS * m_tile + 32 * (warp & 3), last_row = min(first_row + 31, rows - 1);
     const int see_all = first_row + 31 < rows ? q.len - q.n + first_row / S.group : -1;
     const int low_all = A.window > 0 ? q.len - q.n + last_row / S.group - A.window : -1;
-    const int unit_stride = B.max_new * S.group, per_block = S.block_tokens / KV_HALF, per_shift = S.block_shift - 4;
+    const int unit_stride = B.max_new * S.group;        // units of weights: 64 tokens, or smaller blocks
     float* const units = A.unit_l2 && valid ? A.unit_l2 + ((int64_t)seq * S.kv_heads + kh) * A.units * unit_stride + row : nullptr;
+    const bool small_units = units && S.block_tokens < 64;
     float m = -KV_INF, l = 0.f, unit = 1.f;
     bool fine = true;
     for (int j = 0; j < tiles; j++) {
@@ -199,36 +205,46 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const KvSlot& slot = slots[j & 3];
         const bool ragged = slot.pad[0] != 0.f || t0 + KV_P_TOKENS - 1 > see_all || t0 <= low_all;
-        float step = slot.step, block_sum = 0.f;         // of O: it is in units of V's reference, l is not
+        float step = slot.step;                          // of O: it is in units of V's reference, l is not
         unit = slot.unit;
+        float sums[2] = {0.f, 0.f}, bases[2] = {0.f, 0.f};                   // of 64 tokens each, for the blocks' weights
         auto pass = [&](auto some_hidden) {
             constexpr bool RAGGED = decltype(some_hidden)::value;
-            // not unrolled: the three kinds of warps run different code at a time, and more of it than this comes in too slowly
-#pragma unroll 1
-            for (int b = 0; b < KV_P_TOKENS / 32; b++) {
-                uint32_t y[32];
-                kv_tmem_load32(y, s_at + 32 * b);
-                kv_tmem_loaded(y);
-                uint32_t seen = 0xffffffffu;             // which of the 32 tokens the row sees
+            float top, f0, f1, y0, y1, z0, z1;           // of the chunk that comes next: its largest score and its two scales
+            uint32_t seen = 0xffffffffu;                 // which of 32 tokens the row sees
+            // the largest score of chunk b; a scale is not negative, so that of 16 tokens with one scale the largest product is the largest score
+            auto largest = [&](uint32_t (&y)[32], int b) {
+                const float4 s0 = slot.group[2 * b], s1 = slot.group[2 * b + 1];
+                f0 = s0.x * factor;
+                f1 = s1.x * factor;
+                y0 = s0.y;
+                y1 = s1.y;
+                z0 = s0.z;
+                z1 = s1.z;
                 if (RAGGED) {
                     const int t = t0 + 32 * b, upto = min(max(place - t + 1, 0), 32), from = A.window > 0 ? min(max(place - A.window + 1 - t, 0), 32) : 0;
                     seen = (uint32_t)(((uint64_t)1 << upto) - 1) & ~(uint32_t)(((uint64_t)1 << from) - 1);
-                    if (slot.group[2 * b].w == 0.f) seen &= 0xffff0000u;
-                    if (slot.group[2 * b + 1].w == 0.f) seen &= 0x0000ffffu;
+                    if (s0.w == 0.f) seen &= 0xffff0000u;
+                    if (s1.w == 0.f) seen &= 0x0000ffffu;
 #pragma unroll
                     for (int i = 0; i < 32; i++) y[i] = seen >> i & 1 ? y[i] : 0xff800000u;
                 }
-                const float4 sc[2] = {slot.group[2 * b], slot.group[2 * b + 1]};
-                // the largest score; a scale is not negative, so that of 16 tokens with one scale the largest product is the largest score
-                float top = -KV_INF;
+                float most[2];
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
-                    float g = fmaxf(__uint_as_float(y[16 * h]), __uint_as_float(y[16 * h + 1]));
+                    float g[2] = {__uint_as_float(y[16 * h]), __uint_as_float(y[16 * h + 1])};
 #pragma unroll
-                    for (int i = 2; i < 16; i += 2) g = fmaxf(fmaxf(g, __uint_as_float(y[16 * h + i])), __uint_as_float(y[16 * h + i + 1]));
-                    g *= sc[h].x * factor;
-                    if (!RAGGED || g == g) top = fmaxf(top, g);                  // 0 times -inf where 16 hidden tokens have a scale of 0
+                    for (int i = 2; i < 14; i += 4) {
+                        g[0] = fmaxf(fmaxf(g[0], __uint_as_float(y[16 * h + i])), __uint_as_float(y[16 * h + i + 1]));
+                        g[1] = fmaxf(fmaxf(g[1], __uint_as_float(y[16 * h + i + 2])), __uint_as_float(y[16 * h + i + 3]));
+                    }
+                    g[0] = fmaxf(fmaxf(g[0], __uint_as_float(y[16 * h + 14])), __uint_as_float(y[16 * h + 15]));
+                    most[h] = fmaxf(g[0], g[1]) * (h ? f1 : f0);
                 }
+                top = fmaxf(most[0], most[1]);           // a NaN (0 times -inf where 16 hidden tokens have a scale of 0) does not count
+            };
+            auto chunk = [&](uint32_t (&y)[32], uint32_t (&next)[32], int b, bool more) {
+                if (more) kv_tmem_load32(next, s_at + 32 * (b + 1));
                 if (__any_sync(0xffffffffu, top > m + KV_LAZY)) {
                     // rare after the first tile: the weights that this tile has already go down with all earlier ones
                     float fall = 1.f;
@@ -238,57 +254,69 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
                     }
                     l *= fall;
                     step *= fall;
-                    block_sum *= fall;
-                    if (b > 0) asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-                    const __half2 down = __float2half2_rn(fall);
+                    if (b & 1) sums[b >> 1] *= fall;
+                    if (b > 0) {
+                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                        const __half2 down = __float2half2_rn(fall);
 #pragma unroll 1
-                    for (int k = 0; k < 16 * b; k += 8) kv_tmem_scale8(s_at + k, down);
-                }
-                // weights times V's share of the reference: the share's logarithm goes into the exponent, and out of the sum again by its inverse
-                const float base = m == -KV_INF ? 0.f : m;
-                // In three stages of 32 values, each in place: an exponential takes some 40 cycles, and a sequence that used each result at
-                // once would wait for every one of them (measured: 1000 cycles for 32 values against 400).
-#pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    const float f = sc[h].x * factor, up = sc[h].y - base;
-                    const uint64_t ff = kv_pair(f, f), uu = kv_pair(up, up);
-#pragma unroll
-                    for (int i = 16 * h; i < 16 * h + 16; i += 2) {
-                        const float2 z = kv_unpair(kv_fma2(kv_pair(__uint_as_float(y[i]), __uint_as_float(y[i + 1])), ff, uu));
-                        y[i] = __float_as_uint(z.x);
-                        y[i + 1] = __float_as_uint(z.y);
+                        for (int k = 0; k < 16 * b; k += 8) kv_tmem_scale8(s_at + k, down);
                     }
                 }
-#pragma unroll
-                for (int i = 0; i < 32; i++) asm volatile("ex2.approx.ftz.f32 %0, %0;" : "+r"(y[i]));
-                if (RAGGED)
-#pragma unroll
-                    for (int i = 0; i < 32; i++) y[i] = seen >> i & 1 ? y[i] : 0u;
+                // weights times V's share of the reference: the share's logarithm goes into the exponent, and out of the sum again by its
+                // inverse.  A pair of values takes three steps, some pairs apart: an exponential's result comes after some 40 cycles, and the
+                // unit takes one of a warp every 8, between which there is room for the other steps.
+                const float base = m == -KV_INF ? 0.f : m;
+                const uint64_t ff[2] = {kv_pair(f0, f0), kv_pair(f1, f1)}, uu[2] = {kv_pair(y0 - base, y0 - base), kv_pair(y1 - base, y1 - base)};
+                uint64_t sum[2] = {0, 0};
                 uint32_t p[16];
 #pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    uint64_t sum[2] = {0, 0};
-#pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        const float u = __uint_as_float(y[16 * h + i]), w = __uint_as_float(y[16 * h + i + 1]);
-                        sum[i >> 1 & 1] = kv_add2(sum[i >> 1 & 1], kv_pair(u, w));
-                        p[8 * h + i / 2] = kv_pack<false>(u, w);
+                for (int i = 0; i < 16 + KV_P_AHEAD; i++) {
+                    if (i < 16) {
+                        const float2 z = kv_unpair(kv_fma2(kv_pair(__uint_as_float(y[2 * i]), __uint_as_float(y[2 * i + 1])), ff[i >> 3], uu[i >> 3]));
+                        y[2 * i] = __float_as_uint(z.x);
+                        y[2 * i + 1] = __float_as_uint(z.y);
+                        asm volatile("ex2.approx.ftz.f32 %0, %0;" : "+r"(y[2 * i]));
+                        asm volatile("ex2.approx.ftz.f32 %0, %0;" : "+r"(y[2 * i + 1]));
                     }
-                    const float2 z = kv_unpair(kv_add2(sum[0], sum[1]));
-                    float all = z.x + z.y;
-                    all = RAGGED && all == 0.f ? 0.f : all * sc[h].z;            // a hidden block's scale may be NaN
-                    l += all;
-                    if (units) {
-                        block_sum += all;
-                        if (((2 * b + h + 1) & (per_block - 1)) == 0) {
-                            const int block = (t0 >> S.block_shift) + (2 * b + h >> per_shift);
-                            if (block << S.block_shift < end) units[(int64_t)block * unit_stride] = kv_log2(block_sum) + base;
-                            block_sum = 0.f;
+                    if (i >= KV_P_AHEAD) {
+                        const int k = i - KV_P_AHEAD;
+                        if (RAGGED) {
+                            y[2 * k] = seen >> (2 * k) & 1 ? y[2 * k] : 0u;
+                            y[2 * k + 1] = seen >> (2 * k + 1) & 1 ? y[2 * k + 1] : 0u;
                         }
+                        asm volatile("{\n\t.reg .b64 t;\n\tmov.b64 t, {%1, %2};\n\tadd.rn.f32x2 %0, %0, t;\n\t}" : "+l"(sum[k >> 3]) : "r"(y[2 * k]), "r"(y[2 * k + 1]));
+                        asm volatile("cvt.rn.f16x2.f32 %0, %2, %1;" : "=r"(p[k]) : "r"(y[2 * k]), "r"(y[2 * k + 1]));
                     }
                 }
                 kv_tmem_store16(p, s_at + 16 * b);
-            }
+                const float2 a0 = kv_unpair(sum[0]), a1 = kv_unpair(sum[1]);
+                float w0 = a0.x + a0.y, w1 = a1.x + a1.y;
+                w0 = RAGGED && w0 == 0.f ? 0.f : w0 * z0;                        // a hidden block's scale may be NaN
+                w1 = RAGGED && w1 == 0.f ? 0.f : w1 * z1;
+                const float both = w0 + w1;
+                l += both;
+                sums[b >> 1] += both;
+                bases[b >> 1] = base;
+                if (small_units) {
+                    const int at = t0 + 32 * b;
+                    float* const to = units + (int64_t)(at >> S.block_shift) * unit_stride;
+                    if (at < end) *to = kv_log2(S.block_tokens == 32 ? both : w0) + base;
+                    if (S.block_tokens == 16 && at + KV_HALF < end) to[unit_stride] = kv_log2(w1) + base;
+                }
+                if (more) {
+                    kv_tmem_loaded(next);
+                    largest(next, b + 1);
+                }
+            };
+            uint32_t x[2][32];
+            kv_tmem_load32(x[0], s_at);
+            kv_tmem_loaded(x[0]);
+            largest(x[0], 0);
+            chunk(x[0], x[1], 0, true);
+            chunk(x[1], x[0], 1, true);
+            chunk(x[0], x[1], 2, true);
+            chunk(x[1], x[0], 3, false);
         };
         if (ragged) pass(KvYes());
         else pass(KvNo());
@@ -306,6 +334,11 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         kv_arrive(bars + 8 * (KV_P_IN + m_tile));
+        if (units && !small_units) {
+#pragma unroll
+            for (int c = 0; c < 2; c++)
+                if (t0 + 64 * c < end) units[(int64_t)((t0 >> 6) + c) * unit_stride] = kv_log2(sums[c]) + bases[c];
+        }
     }
     if (fine && tiles > 0) fine = __all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * (KV_S_IN + m_tile), tiles & 1, stop));      // the last product
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");

@@ -30,19 +30,21 @@ __device__ __forceinline__ uint64_t kv_desc(uint32_t smem, uint32_t lbo, uint32_
 {
     return (uint64_t)((smem >> 4) & 0x3fff) | (uint64_t)((lbo >> 4) & 0x3fff) << 16 | (uint64_t)((sbo >> 4) & 0x3fff) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
+// One thread of the warp issues; the warp as a whole comes here, so that the compiler keeps addresses and descriptors in uniform
+// registers, where the instruction wants them (moved there one by one they held up each instruction by 60 cycles).
 __device__ __forceinline__ void kv_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+    asm volatile("{\n\t.reg .pred p, e;\n\telect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                  ::"r"(d), "l"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
 }
 __device__ __forceinline__ void kv_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+    asm volatile("{\n\t.reg .pred p, e;\n\telect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
                  ::"r"(d), "r"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
 }
 __device__ __forceinline__ void kv_commit(uint32_t bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void kv_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 
@@ -57,11 +59,6 @@ __device__ __forceinline__ void kv_tmem_store32(const uint32_t (&x)[32], uint32_
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
                  ::KV_W8(x, 0), KV_W8(x, 8), KV_W8(x, 16), KV_W8(x, 24), "r"(at) : "memory");
-}
-__device__ __forceinline__ void kv_tmem_store16(const uint32_t (&x)[16], uint32_t at)
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
-                 ::KV_W8(x, 0), KV_W8(x, 8), "r"(at) : "memory");
 }
 // The load's registers go through the wait, so that nothing reads them before it.
 __device__ __forceinline__ void kv_tmem_loaded(uint32_t (&x)[32])
@@ -97,20 +94,6 @@ __device__ __forceinline__ uint64_t kv_add2(uint64_t a, uint64_t b)
     return d;
 }
 
-// 16 f16 of a lane in tensor memory, times f
-__device__ __forceinline__ void kv_tmem_scale8(uint32_t at, __half2 f)
-{
-    uint32_t x[8];
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];" : KV_R8(x, 0) : "r"(at) : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-        asm volatile("" : "+r"(x[i]));
-        const __half2 h = __hmul2(*(const __half2*)&x[i], f);
-        x[i] = *(const uint32_t*)&h;
-    }
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::KV_W8(x, 0), "r"(at) : "memory");
-}
 struct KvYes { static constexpr bool value = true; };
 struct KvNo { static constexpr bool value = false; };
 
@@ -143,7 +126,8 @@ template <bool E4M3> __device__ __forceinline__ void kv_widen16(const uint4& w, 
 
 // Barriers, 8 bytes each from T::BARS on.  K_IN has four phases in turn because the scales beside K stay until the weights are made; by
 // the time that a tile's K comes in, the weights of the fourth tile before it are done.
-enum { KV_K_IN = 0, KV_K_OUT = 4, KV_V_IN = 6, KV_V_OUT = 8, KV_S_IN = 10, KV_P_IN = 12, KV_Q_IN = 14, KV_TAIL = 15, KV_END = 16, KV_BARS = 17 };
+// S_IN and P_IN: [row tile][half of the tile's tokens]; O_IN: an answer product of the row tile is done.
+enum { KV_K_IN = 0, KV_K_OUT = 4, KV_V_IN = 6, KV_V_OUT = 8, KV_S_IN = 10, KV_P_IN = 14, KV_O_IN = 18, KV_Q_IN = 20, KV_TAIL = 21, KV_END = 22, KV_BARS = 23 };
 
 // What a tile's slot of T::SCALES holds: per 16 tokens {K's scale, log2 of V's scale over the reference, one over that share, whether the
 // tokens are there}; the tile's change of the reference and the reference itself stand behind the groups.
@@ -198,129 +182,114 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
     const bool small_units = units && S.block_tokens < 64;
     float m = -KV_INF, l = 0.f, unit = 1.f;
     bool fine = true;
-    for (int j = 0; j < tiles; j++) {
-        const int t0 = begin + KV_P_TOKENS * j;
-        fine = __all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * (KV_S_IN + m_tile), j & 1, stop) && kv_wait_or_stop(bars + 8 * (KV_K_IN + (j & 3)), j >> 2 & 1, stop));
+    // Steps of 64 tokens: while this one's weights are made, the next one's scores are (in the other half of S).
+    for (int s = 0; s < 2 * tiles && fine; s++) {
+        const int j = s >> 1, half = s & 1, t0 = begin + 64 * s;
+        const uint32_t at = s_at + 64 * half;
+        fine = __all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * (KV_S_IN + 2 * m_tile + half), j & 1, stop) && kv_wait_or_stop(bars + 8 * (KV_K_IN + (j & 3)), j >> 2 & 1, stop));
         if (!fine) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        uint32_t x[2][32];
+        kv_tmem_load32(x[0], at);
+        kv_tmem_load32(x[1], at + 32);
         const KvSlot& slot = slots[j & 3];
-        const bool ragged = slot.pad[0] != 0.f || t0 + KV_P_TOKENS - 1 > see_all || t0 <= low_all;
-        float step = slot.step;                          // of O: it is in units of V's reference, l is not
+        const float4* const group = slot.group + 4 * half;
+        const bool ragged = slot.pad[0] != 0.f || t0 + 63 > see_all || t0 <= low_all;
+        float step = half ? 1.f : slot.step;             // of O: it is in units of V's reference, l is not
         unit = slot.unit;
-        float sums[2] = {0.f, 0.f}, bases[2] = {0.f, 0.f};                   // of 64 tokens each, for the blocks' weights
+        float total = 0.f, base = 0.f;
         auto pass = [&](auto some_hidden) {
             constexpr bool RAGGED = decltype(some_hidden)::value;
-            float top, f0, f1, y0, y1, z0, z1;           // of the chunk that comes next: its largest score and its two scales
-            uint32_t seen = 0xffffffffu;                 // which of 32 tokens the row sees
-            // the largest score of chunk b; a scale is not negative, so that of 16 tokens with one scale the largest product is the largest score
-            auto largest = [&](uint32_t (&y)[32], int b) {
-                const float4 s0 = slot.group[2 * b], s1 = slot.group[2 * b + 1];
-                f0 = s0.x * factor;
-                f1 = s1.x * factor;
-                y0 = s0.y;
-                y1 = s1.y;
-                z0 = s0.z;
-                z1 = s1.z;
-                if (RAGGED) {
+            uint32_t seen[2] = {0xffffffffu, 0xffffffffu};                   // which of 32 tokens the row sees
+            float f[4];
+#pragma unroll
+            for (int g = 0; g < 4; g++) f[g] = group[g].x * factor;
+            if (RAGGED)
+#pragma unroll
+                for (int b = 0; b < 2; b++) {
                     const int t = t0 + 32 * b, upto = min(max(place - t + 1, 0), 32), from = A.window > 0 ? min(max(place - A.window + 1 - t, 0), 32) : 0;
-                    seen = (uint32_t)(((uint64_t)1 << upto) - 1) & ~(uint32_t)(((uint64_t)1 << from) - 1);
-                    if (s0.w == 0.f) seen &= 0xffff0000u;
-                    if (s1.w == 0.f) seen &= 0x0000ffffu;
-#pragma unroll
-                    for (int i = 0; i < 32; i++) y[i] = seen >> i & 1 ? y[i] : 0xff800000u;
+                    seen[b] = (uint32_t)(((uint64_t)1 << upto) - 1) & ~(uint32_t)(((uint64_t)1 << from) - 1);
+                    if (group[2 * b].w == 0.f) seen[b] &= 0xffff0000u;
+                    if (group[2 * b + 1].w == 0.f) seen[b] &= 0x0000ffffu;
                 }
-                float most[2];
-#pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    float g[2] = {__uint_as_float(y[16 * h]), __uint_as_float(y[16 * h + 1])};
-#pragma unroll
-                    for (int i = 2; i < 14; i += 4) {
-                        g[0] = fmaxf(fmaxf(g[0], __uint_as_float(y[16 * h + i])), __uint_as_float(y[16 * h + i + 1]));
-                        g[1] = fmaxf(fmaxf(g[1], __uint_as_float(y[16 * h + i + 2])), __uint_as_float(y[16 * h + i + 3]));
-                    }
-                    g[0] = fmaxf(fmaxf(g[0], __uint_as_float(y[16 * h + 14])), __uint_as_float(y[16 * h + 15]));
-                    most[h] = fmaxf(g[0], g[1]) * (h ? f1 : f0);
-                }
-                top = fmaxf(most[0], most[1]);           // a NaN (0 times -inf where 16 hidden tokens have a scale of 0) does not count
-            };
-            auto chunk = [&](uint32_t (&y)[32], uint32_t (&next)[32], int b, bool more) {
-                if (more) kv_tmem_load32(next, s_at + 32 * (b + 1));
-                if (__any_sync(0xffffffffu, top > m + KV_LAZY)) {
-                    // rare after the first tile: the weights that this tile has already go down with all earlier ones
-                    float fall = 1.f;
-                    if (top > m + KV_LAZY) {
-                        fall = kv_exp2(m - top);
-                        m = top;
-                    }
-                    l *= fall;
-                    step *= fall;
-                    if (b & 1) sums[b >> 1] *= fall;
-                    if (b > 0) {
-                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-                        const __half2 down = __float2half2_rn(fall);
-#pragma unroll 1
-                        for (int k = 0; k < 16 * b; k += 8) kv_tmem_scale8(s_at + k, down);
-                    }
-                }
-                // weights times V's share of the reference: the share's logarithm goes into the exponent, and out of the sum again by its
-                // inverse.  A pair of values takes three steps, some pairs apart: an exponential's result comes after some 40 cycles, and the
-                // unit takes one of a warp every 8, between which there is room for the other steps.
-                const float base = m == -KV_INF ? 0.f : m;
-                const uint64_t ff[2] = {kv_pair(f0, f0), kv_pair(f1, f1)}, uu[2] = {kv_pair(y0 - base, y0 - base), kv_pair(y1 - base, y1 - base)};
-                uint64_t sum[2] = {0, 0};
-                uint32_t p[16];
-#pragma unroll
-                for (int i = 0; i < 16 + KV_P_AHEAD; i++) {
-                    if (i < 16) {
-                        const float2 z = kv_unpair(kv_fma2(kv_pair(__uint_as_float(y[2 * i]), __uint_as_float(y[2 * i + 1])), ff[i >> 3], uu[i >> 3]));
-                        y[2 * i] = __float_as_uint(z.x);
-                        y[2 * i + 1] = __float_as_uint(z.y);
-                        asm volatile("ex2.approx.ftz.f32 %0, %0;" : "+r"(y[2 * i]));
-                        asm volatile("ex2.approx.ftz.f32 %0, %0;" : "+r"(y[2 * i + 1]));
-                    }
-                    if (i >= KV_P_AHEAD) {
-                        const int k = i - KV_P_AHEAD;
-                        if (RAGGED) {
-                            y[2 * k] = seen >> (2 * k) & 1 ? y[2 * k] : 0u;
-                            y[2 * k + 1] = seen >> (2 * k + 1) & 1 ? y[2 * k + 1] : 0u;
-                        }
-                        asm volatile("{\n\t.reg .b64 t;\n\tmov.b64 t, {%1, %2};\n\tadd.rn.f32x2 %0, %0, t;\n\t}" : "+l"(sum[k >> 3]) : "r"(y[2 * k]), "r"(y[2 * k + 1]));
-                        asm volatile("cvt.rn.f16x2.f32 %0, %2, %1;" : "=r"(p[k]) : "r"(y[2 * k]), "r"(y[2 * k + 1]));
-                    }
-                }
-                kv_tmem_store16(p, s_at + 16 * b);
-                const float2 a0 = kv_unpair(sum[0]), a1 = kv_unpair(sum[1]);
-                float w0 = a0.x + a0.y, w1 = a1.x + a1.y;
-                w0 = RAGGED && w0 == 0.f ? 0.f : w0 * z0;                        // a hidden block's scale may be NaN
-                w1 = RAGGED && w1 == 0.f ? 0.f : w1 * z1;
-                const float both = w0 + w1;
-                l += both;
-                sums[b >> 1] += both;
-                bases[b >> 1] = base;
-                if (small_units) {
-                    const int at = t0 + 32 * b;
-                    float* const to = units + (int64_t)(at >> S.block_shift) * unit_stride;
-                    if (at < end) *to = kv_log2(S.block_tokens == 32 ? both : w0) + base;
-                    if (S.block_tokens == 16 && at + KV_HALF < end) to[unit_stride] = kv_log2(w1) + base;
-                }
-                if (more) {
-                    kv_tmem_loaded(next);
-                    largest(next, b + 1);
-                }
-            };
-            uint32_t x[2][32];
-            kv_tmem_load32(x[0], s_at);
             kv_tmem_loaded(x[0]);
-            largest(x[0], 0);
-            chunk(x[0], x[1], 0, true);
-            chunk(x[1], x[0], 1, true);
-            chunk(x[0], x[1], 2, true);
-            chunk(x[1], x[0], 3, false);
+            kv_tmem_loaded(x[1]);
+            // the largest score; a scale is not negative, so that of 16 tokens with one scale the largest product is the largest score
+            float top = -KV_INF;
+#pragma unroll
+            for (int g = 0; g < 4; g++) {
+                uint32_t (&y)[32] = x[g >> 1];
+                if (RAGGED)
+#pragma unroll
+                    for (int i = 16 * (g & 1); i < 16 * (g & 1) + 16; i++) y[i] = seen[g >> 1] >> i & 1 ? y[i] : 0xff800000u;
+                const int o = 16 * (g & 1);
+                float u = fmaxf(fmaxf(__uint_as_float(y[o]), __uint_as_float(y[o + 1])), __uint_as_float(y[o + 2]));
+                float w = fmaxf(fmaxf(__uint_as_float(y[o + 3]), __uint_as_float(y[o + 4])), __uint_as_float(y[o + 5]));
+                u = fmaxf(fmaxf(u, __uint_as_float(y[o + 6])), __uint_as_float(y[o + 7]));
+                w = fmaxf(fmaxf(w, __uint_as_float(y[o + 8])), __uint_as_float(y[o + 9]));
+                u = fmaxf(fmaxf(u, __uint_as_float(y[o + 10])), __uint_as_float(y[o + 11]));
+                w = fmaxf(fmaxf(w, __uint_as_float(y[o + 12])), __uint_as_float(y[o + 13]));
+                u = fmaxf(fmaxf(u, __uint_as_float(y[o + 14])), __uint_as_float(y[o + 15]));
+                top = fmaxf(top, fmaxf(u, w) * f[g]);    // a NaN (0 times -inf where 16 hidden tokens have a scale of 0) does not count
+            }
+            if (top > m + KV_LAZY) {
+                const float fall = kv_exp2(m - top);
+                l *= fall;
+                step *= fall;
+                m = top;
+            }
+            // weights times V's share of the reference: the share's logarithm goes into the exponent, and out of the sum again by its
+            // inverse.  A pair of values takes three steps, some pairs apart: an exponential's result comes after some 40 cycles, and the
+            // unit takes one of a warp every 8, between which there is room for the other steps.
+            base = m == -KV_INF ? 0.f : m;
+            uint32_t p[32];
+            uint64_t sum[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < 32 + KV_P_AHEAD; i++) {
+                if (i < 32) {
+                    const float fg = f[i >> 3], ug = group[i >> 3].y - base;
+                    uint32_t &u = x[i >> 4][2 * i & 31], &w = x[i >> 4][(2 * i & 31) + 1];
+                    const float2 z = kv_unpair(kv_fma2(kv_pair(__uint_as_float(u), __uint_as_float(w)), kv_pair(fg, fg), kv_pair(ug, ug)));
+                    u = __float_as_uint(z.x);
+                    w = __float_as_uint(z.y);
+                    asm volatile("ex2.approx.ftz.f32 %0, %0;" : "+r"(u));
+                    asm volatile("ex2.approx.ftz.f32 %0, %0;" : "+r"(w));
+                }
+                if (i >= KV_P_AHEAD) {
+                    const int k = i - KV_P_AHEAD;
+                    uint32_t &u = x[k >> 4][2 * k & 31], &w = x[k >> 4][(2 * k & 31) + 1];
+                    if (RAGGED) {
+                        u = seen[k >> 4] >> (2 * k & 31) & 1 ? u : 0u;
+                        w = seen[k >> 4] >> ((2 * k & 31) + 1) & 1 ? w : 0u;
+                    }
+                    asm volatile("{\n\t.reg .b64 t;\n\tmov.b64 t, {%1, %2};\n\tadd.rn.f32x2 %0, %0, t;\n\t}" : "+l"(sum[k >> 3]) : "r"(u), "r"(w));
+                    asm volatile("cvt.rn.f16x2.f32 %0, %2, %1;" : "=r"(p[k]) : "r"(u), "r"(w));
+                }
+            }
+            kv_tmem_store32(p, at);                      // over the scores of the first 32 tokens
+            float w[4];
+#pragma unroll
+            for (int g = 0; g < 4; g++) {
+                const float2 z = kv_unpair(sum[g]);
+                w[g] = z.x + z.y;
+                w[g] = RAGGED && w[g] == 0.f ? 0.f : w[g] * group[g].z;      // a hidden block's scale may be NaN
+            }
+            total = (w[0] + w[1]) + (w[2] + w[3]);
+            l += total;
+            if (small_units)
+#pragma unroll
+                for (int g = 0; g < 4; g++) {
+                    const int t = t0 + KV_HALF * g;
+                    if (t < end && (S.block_tokens == 16 || !(g & 1)))
+                        units[(int64_t)(t >> S.block_shift) * unit_stride] = kv_log2(S.block_tokens == 16 ? w[g] : w[g] + w[g | 1]) + base;
+                }
         };
         if (ragged) pass(KvYes());
         else pass(KvNo());
-        if (j > 0 && __any_sync(0xffffffffu, step != 1.f)) {
+        if (s > 0 && __any_sync(0xffffffffu, step != 1.f)) {
+            // behind the product of the step before, the last that has been issued
+            fine = __all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * (KV_O_IN + m_tile), (s - 1) & 1, stop));
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
             for (int b = 0; b < D / 32; b++) {
                 uint32_t y[32];
@@ -333,14 +302,10 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
         }
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        kv_arrive(bars + 8 * (KV_P_IN + m_tile));
-        if (units && !small_units) {
-#pragma unroll
-            for (int c = 0; c < 2; c++)
-                if (t0 + 64 * c < end) units[(int64_t)((t0 >> 6) + c) * unit_stride] = kv_log2(sums[c]) + bases[c];
-        }
+        kv_arrive(bars + 8 * (KV_P_IN + 2 * m_tile + half));
+        if (units && !small_units && t0 < end) units[(int64_t)(t0 >> 6) * unit_stride] = kv_log2(total) + base;
     }
-    if (fine && tiles > 0) fine = __all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * (KV_S_IN + m_tile), tiles & 1, stop));      // the last product
+    if (fine && tiles > 0) fine = __all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * (KV_S_IN + 2 * m_tile), tiles & 1, stop));     // all products
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const float nan = __int_as_float(0x7fffffff), inv = !fine ? nan : l == 0.f ? 0.f : 1.f / l;
     const float out_factor = A.splits == 1 ? inv * unit : fine ? unit : nan;
@@ -522,45 +487,51 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
     }
 }
 
-// The products, by one thread.  They run in the order in which they are issued: a tile's S is written over the weights of the tile
-// before it after those have been used.
+// The products, by one warp.  They run in the order in which they are issued: scores are written over weights after those have been
+// used.
 template <int D>
 __device__ __forceinline__ void kv_prompt_products(int tiles, int parts, uint32_t sm_at, uint32_t bars, volatile int* stop, uint32_t tmem)
 {
     using T = KvPrompt<D>;
     // f32 += f16 * f16; M = 128, N in eights; V is the operand whose N runs along the row
     constexpr uint32_t shape = 1u << 4 | (uint32_t)(KV_P_ROWS / 16) << 24;
-    constexpr uint32_t s_what = shape | (uint32_t)(KV_P_TOKENS / 8) << 17, o_what = shape | (uint32_t)(D / 8) << 17 | 1u << 16;
-    auto scores = [&](int j, int m) {
-        const uint64_t a = kv_desc(sm_at + T::Q + m * T::TILE, 16, 1024), b = kv_desc(sm_at + T::K + (j & 1) * T::TILE, 16, 1024);
+    constexpr uint32_t s_what = shape | (uint32_t)(64 / 8) << 17, o_what = shape | (uint32_t)(D / 8) << 17 | 1u << 16;
+    auto scores = [&](int s, int m) {                    // of 64 tokens
+        const int j = s >> 1, half = s & 1;
+        const uint64_t a = kv_desc(sm_at + T::Q + m * T::TILE, 16, 1024), b = kv_desc(sm_at + T::K + (j & 1) * T::TILE + half * 64 * 128, 16, 1024);
 #pragma unroll
-        for (int s = 0; s < D / 16; s++) {
-            const uint32_t off = ((s >> 2) * KV_P_TOKENS * 128 + (s & 3) * 32) >> 4;
-            kv_mma_ss(tmem + 128 * m, a + off, b + off, s_what, s > 0);
+        for (int k = 0; k < D / 16; k++) {
+            const uint32_t off = ((k >> 2) * KV_P_TOKENS * 128 + (k & 3) * 32) >> 4;
+            kv_mma_ss(tmem + 128 * m + 64 * half, a + off, b + off, s_what, k > 0);
         }
-        kv_commit(bars + 8 * (KV_S_IN + m));
+        kv_commit(bars + 8 * (KV_S_IN + 2 * m + half));
     };
-    auto answers = [&](int j, int m) {
-        const uint64_t b = kv_desc(sm_at + T::V + (j & 1) * T::TILE, KV_P_TOKENS * 128, 1024);
+    auto answers = [&](int s, int m) {
+        const int j = s >> 1, half = s & 1;
+        const uint64_t b = kv_desc(sm_at + T::V + (j & 1) * T::TILE + half * 64 * 128, KV_P_TOKENS * 128, 1024);
 #pragma unroll
-        for (int s = 0; s < KV_P_TOKENS / 16; s++) kv_mma_ts(tmem + 256 + 128 * m, tmem + 128 * m + 8 * s, b + (s * 2048 >> 4), o_what, j > 0 || s > 0);
+        for (int k = 0; k < 4; k++) kv_mma_ts(tmem + 256 + 128 * m, tmem + 128 * m + 64 * half + 8 * k, b + (k * 2048 >> 4), o_what, s > 0 || k > 0);
+        kv_commit(bars + 8 * (KV_O_IN + m));
     };
-    if (!kv_wait_or_stop(bars + 8 * KV_Q_IN, 0, stop)) return;
-    for (int j = 0; j <= tiles; j++) {
-        if (j < tiles && !kv_wait_or_stop(bars + 8 * (KV_K_IN + (j & 3)), j >> 2 & 1, stop)) return;
+    kv_wait_or_stop(bars + 8 * KV_Q_IN, 0, stop);
+    // step s of a row tile: its answers when its weights are made, and then the scores of step s + 2, in the place of those weights
+    for (int s = -2; s < 2 * tiles; s++) {
+        const int next = s + 2, j = next >> 1;
+        if (next < 2 * tiles && !(next & 1)) kv_wait_or_stop(bars + 8 * (KV_K_IN + (j & 3)), j >> 2 & 1, stop);
+        if (s >= 0 && !(s & 1)) kv_wait_or_stop(bars + 8 * (KV_V_IN + (s >> 1 & 1)), s >> 2 & 1, stop);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         for (int m = 0; m < parts; m++) {
-            if (j > 0) {
-                if (m == 0 && !kv_wait_or_stop(bars + 8 * (KV_V_IN + ((j - 1) & 1)), (j - 1) >> 1 & 1, stop)) return;
-                if (!kv_wait_or_stop(bars + 8 * (KV_P_IN + m), (j - 1) & 1, stop)) return;
+            if (s >= 0) {
+                kv_wait_or_stop(bars + 8 * (KV_P_IN + 2 * m + (s & 1)), s >> 1 & 1, stop);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                answers(j - 1, m);
+                answers(s, m);
             }
-            if (j < tiles) scores(j, m);
-            else kv_commit(bars + 8 * (KV_S_IN + m));    // the last answers
+            if (next < 2 * tiles) scores(next, m);
         }
-        if (j > 0) kv_commit(bars + 8 * (KV_V_OUT + ((j - 1) & 1)));
-        if (j < tiles) kv_commit(bars + 8 * (KV_K_OUT + (j & 1)));
+        if (s == 2 * tiles - 1)
+            for (int m = 0; m < parts; m++) kv_commit(bars + 8 * (KV_S_IN + 2 * m));         // the end
+        if (s >= 0 && (s & 1)) kv_commit(bars + 8 * (KV_V_OUT + (s >> 1 & 1)));
+        if (next < 2 * tiles && (next & 1)) kv_commit(bars + 8 * (KV_K_OUT + (j & 1)));
     }
 }
 
@@ -587,7 +558,7 @@ __global__ void __launch_bounds__(KV_P_THREADS, 1) kv_prompt_kernel(const KvShap
     uint32_t* const tmem_at = (uint32_t*)(sm + T::BARS + 8 * KV_BARS + 4);
     if (threadIdx.x == 0) {
         for (int i = 0; i < KV_BARS; i++) {
-            const int count = i < KV_K_OUT || i == KV_V_IN || i == KV_V_IN + 1 || i == KV_P_IN || i == KV_P_IN + 1 ? 128 : i == KV_Q_IN ? 128 * parts : i == KV_TAIL ? 4 : 1;
+            const int count = i < KV_K_OUT || i == KV_V_IN || i == KV_V_IN + 1 || (i >= KV_P_IN && i < KV_O_IN) ? 128 : i == KV_Q_IN ? 128 * parts : i == KV_TAIL ? 4 : 1;
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bars + 8 * i), "r"(count) : "memory");
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -604,11 +575,10 @@ __global__ void __launch_bounds__(KV_P_THREADS, 1) kv_prompt_kernel(const KvShap
     } else if (warp < 12) {
         kv_prompt_bring<D, BF, E4M3>(S, B, q, seq, kh, begin, end, tiles, sm, bars, stop);
     } else {
-        if ((threadIdx.x & 31) == 0) {
-            kv_prompt_products<D>(tiles, parts, sm_at, bars, stop, tmem);
-            kv_commit(bars + 8 * KV_END);                // nothing is on its way any more when the memory is given back
-            kv_wait(bars + 8 * KV_END, 0);
-        }
+        kv_prompt_products<D>(tiles, parts, sm_at, bars, stop, tmem);
+        __syncwarp();
+        kv_commit(bars + 8 * KV_END);                    // nothing is on its way any more when the memory is given back
+        kv_wait(bars + 8 * KV_END, 0);
         __syncwarp();
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");

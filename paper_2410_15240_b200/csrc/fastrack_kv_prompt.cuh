@@ -46,7 +46,12 @@ __device__ __forceinline__ void kv_commit(uint32_t bar)
 {
     asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void kv_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// For a whole warp, when all its lanes have come
+__device__ __forceinline__ void kv_warp_arrive(uint32_t bar)
+{
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
 
 #define KV_R8(x, i) "=r"(x[i]), "=r"(x[i + 1]), "=r"(x[i + 2]), "=r"(x[i + 3]), "=r"(x[i + 4]), "=r"(x[i + 5]), "=r"(x[i + 6]), "=r"(x[i + 7])
 #define KV_W8(x, i) "r"(x[i]), "r"(x[i + 1]), "r"(x[i + 2]), "r"(x[i + 3]), "r"(x[i + 4]), "r"(x[i + 5]), "r"(x[i + 6]), "r"(x[i + 7])
@@ -115,6 +120,12 @@ __device__ __forceinline__ bool kv_wait_or_stop(uint32_t bar, uint32_t parity, v
     return false;
 }
 
+// The same answer for a whole warp.  All lanes ask: where one lane does, the compiler carries on with that lane apart from the others.
+__device__ __forceinline__ bool kv_warp_wait(uint32_t bar, uint32_t parity, volatile int* stop)
+{
+    return __all_sync(0xffffffffu, kv_wait_or_stop(bar, parity, stop));
+}
+
 // 16 codes as 16 f16
 template <bool E4M3> __device__ __forceinline__ void kv_widen16(const uint4& w, uint4& lo, uint4& hi)
 {
@@ -171,7 +182,7 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
             *(uint4*)(sm + T::Q + m_tile * T::TILE + T::at(r, 8 * i)) = w;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        kv_arrive(bars + 8 * KV_Q_IN);
+        kv_warp_arrive(bars + 8 * KV_Q_IN);
     }
     // rows of this warp: tokens up to see_all are seen by all of them, tokens behind low_all are in every one's window
     const int first_row = tile_row + KV_P_ROWS * m_tile + 32 * (warp & 3), last_row = min(first_row + 31, rows - 1);
@@ -186,7 +197,7 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
     for (int s = 0; s < 2 * tiles && fine; s++) {
         const int j = s >> 1, half = s & 1, t0 = begin + 64 * s;
         const uint32_t at = s_at + 64 * half;
-        fine = __all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * (KV_S_IN + 2 * m_tile + half), j & 1, stop) && kv_wait_or_stop(bars + 8 * (KV_K_IN + (j & 3)), j >> 2 & 1, stop));
+        fine = kv_warp_wait(bars + 8 * (KV_S_IN + 2 * m_tile + half), j & 1, stop) && (half || kv_warp_wait(bars + 8 * (KV_K_IN + (j & 3)), j >> 2 & 1, stop));
         if (!fine) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         uint32_t x[2][32];
@@ -197,7 +208,8 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
         const bool ragged = slot.pad[0] != 0.f || t0 + 63 > see_all || t0 <= low_all;
         float step = half ? 1.f : slot.step;             // of O: it is in units of V's reference, l is not
         unit = slot.unit;
-        float total = 0.f, base = 0.f;
+        float base = 0.f;
+        uint64_t sum[4] = {0, 0, 0, 0};                  // of 16 tokens' weights each
         auto pass = [&](auto some_hidden) {
             constexpr bool RAGGED = decltype(some_hidden)::value;
             uint32_t seen[2] = {0xffffffffu, 0xffffffffu};                   // which of 32 tokens the row sees
@@ -243,7 +255,6 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
             // unit takes one of a warp every 8, between which there is room for the other steps.
             base = m == -KV_INF ? 0.f : m;
             uint32_t p[32];
-            uint64_t sum[4] = {0, 0, 0, 0};
 #pragma unroll
             for (int i = 0; i < 32 + KV_P_AHEAD; i++) {
                 if (i < 32) {
@@ -267,28 +278,12 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
                 }
             }
             kv_tmem_store32(p, at);                      // over the scores of the first 32 tokens
-            float w[4];
-#pragma unroll
-            for (int g = 0; g < 4; g++) {
-                const float2 z = kv_unpair(sum[g]);
-                w[g] = z.x + z.y;
-                w[g] = RAGGED && w[g] == 0.f ? 0.f : w[g] * group[g].z;      // a hidden block's scale may be NaN
-            }
-            total = (w[0] + w[1]) + (w[2] + w[3]);
-            l += total;
-            if (small_units)
-#pragma unroll
-                for (int g = 0; g < 4; g++) {
-                    const int t = t0 + KV_HALF * g;
-                    if (t < end && (S.block_tokens == 16 || !(g & 1)))
-                        units[(int64_t)(t >> S.block_shift) * unit_stride] = kv_log2(S.block_tokens == 16 ? w[g] : w[g] + w[g | 1]) + base;
-                }
         };
         if (ragged) pass(KvYes());
         else pass(KvNo());
         if (s > 0 && __any_sync(0xffffffffu, step != 1.f)) {
             // behind the product of the step before, the last that has been issued
-            fine = __all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * (KV_O_IN + m_tile), (s - 1) & 1, stop));
+            fine = kv_warp_wait(bars + 8 * (KV_O_IN + m_tile), (s - 1) & 1, stop);
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
             for (int b = 0; b < D / 32; b++) {
@@ -302,10 +297,29 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
         }
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        kv_arrive(bars + 8 * (KV_P_IN + 2 * m_tile + half));
-        if (units && !small_units && t0 < end) units[(int64_t)(t0 >> 6) * unit_stride] = kv_log2(total) + base;
+        kv_warp_arrive(bars + 8 * (KV_P_IN + 2 * m_tile + half));
+        // behind the arrival: the row's sum, and the units'
+        float w[4];
+#pragma unroll
+        for (int g = 0; g < 4; g++) {
+            const float2 z = kv_unpair(sum[g]);
+            w[g] = z.x + z.y;
+            w[g] = w[g] == 0.f ? 0.f : w[g] * group[g].z;                    // a hidden block's scale may be NaN
+        }
+        const float total = (w[0] + w[1]) + (w[2] + w[3]);
+        l += total;
+        if (units && !small_units) {
+            if (t0 < end) units[(int64_t)(t0 >> 6) * unit_stride] = kv_log2(total) + base;
+        } else if (units) {
+#pragma unroll
+            for (int g = 0; g < 4; g++) {
+                const int t = t0 + KV_HALF * g;
+                if (t < end && (S.block_tokens == 16 || !(g & 1)))
+                    units[(int64_t)(t >> S.block_shift) * unit_stride] = kv_log2(S.block_tokens == 16 ? w[g] : w[g] + w[g | 1]) + base;
+            }
+        }
     }
-    if (fine && tiles > 0) fine = __all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * (KV_S_IN + 2 * m_tile), tiles & 1, stop));     // all products
+    if (fine && tiles > 0) fine = kv_warp_wait(bars + 8 * (KV_S_IN + 2 * m_tile), tiles & 1, stop);     // all products
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const float nan = __int_as_float(0x7fffffff), inv = !fine ? nan : l == 0.f ? 0.f : 1.f / l;
     const float out_factor = A.splits == 1 ? inv * unit : fine ? unit : nan;
@@ -429,7 +443,7 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
         float2 kp = make_float2(1.f, 1.f), vp = kp;
         KvSlot& slot = slots[j & 3];
         const int tile0 = begin + KV_P_TOKENS * j;
-        if (!__all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * (KV_K_OUT + (j & 1)), (j >> 1 & 1) ^ 1, stop))) return;
+        if (!kv_warp_wait(bars + 8 * (KV_K_OUT + (j & 1)), (j >> 1 & 1) ^ 1, stop)) return;
         if (BF && tile0 + KV_P_TOKENS > tail_begin && tail_begin < end) {
             // the tail's powers of two go through the slot: y K's, z V's
             if (kind.x == -2) { kp.x = tail_power(0, t0); vp.x = tail_power(1, t0); }
@@ -440,9 +454,8 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
                 slot.group[2 * warp + 1].y = kp.y;
                 slot.group[2 * warp + 1].z = vp.y;
             }
-            __syncwarp();
-            if (lane == 0) kv_arrive(bars + 8 * KV_TAIL);
-            if (warp == 0 && !__all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * KV_TAIL, 0, stop))) return;   // once: the tail lies in one tile
+            kv_warp_arrive(bars + 8 * KV_TAIL);
+            if (warp == 0 && !kv_warp_wait(bars + 8 * KV_TAIL, 0, stop)) return;   // once: the tail lies in one tile
         }
         if (warp == 0) {
             // lane g < 8: 16 tokens' scales, asked for a tile ahead
@@ -476,12 +489,12 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
         }
         store(kw, 0, t0, kind, kp, sm + T::K + (j & 1) * T::TILE);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        kv_arrive(bars + 8 * (KV_K_IN + (j & 3)));
+        kv_warp_arrive(bars + 8 * (KV_K_IN + (j & 3)));
         codes(kw, 0, t0 + KV_P_TOKENS, next);
-        if (!__all_sync(0xffffffffu, kv_wait_or_stop(bars + 8 * (KV_V_OUT + (j & 1)), (j >> 1 & 1) ^ 1, stop))) return;
+        if (!kv_warp_wait(bars + 8 * (KV_V_OUT + (j & 1)), (j >> 1 & 1) ^ 1, stop)) return;
         store(vw, 1, t0, kind, vp, sm + T::V + (j & 1) * T::TILE);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        kv_arrive(bars + 8 * (KV_V_IN + (j & 1)));
+        kv_warp_arrive(bars + 8 * (KV_V_IN + (j & 1)));
         codes(vw, 1, t0 + KV_P_TOKENS, next);
         kind = next;
     }
@@ -558,7 +571,7 @@ __global__ void __launch_bounds__(KV_P_THREADS, 1) kv_prompt_kernel(const KvShap
     uint32_t* const tmem_at = (uint32_t*)(sm + T::BARS + 8 * KV_BARS + 4);
     if (threadIdx.x == 0) {
         for (int i = 0; i < KV_BARS; i++) {
-            const int count = i < KV_K_OUT || i == KV_V_IN || i == KV_V_IN + 1 || (i >= KV_P_IN && i < KV_O_IN) ? 128 : i == KV_Q_IN ? 128 * parts : i == KV_TAIL ? 4 : 1;
+            const int count = i < KV_K_OUT || i == KV_V_IN || i == KV_V_IN + 1 || (i >= KV_P_IN && i < KV_O_IN) ? 4 : i == KV_Q_IN ? 4 * parts : i == KV_TAIL ? 4 : 1;
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bars + 8 * i), "r"(count) : "memory");
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");

@@ -55,24 +55,24 @@ __device__ __forceinline__ void kv_warp_arrive(uint32_t bar)
 
 #define KV_R8(x, i) "=r"(x[i]), "=r"(x[i + 1]), "=r"(x[i + 2]), "=r"(x[i + 3]), "=r"(x[i + 4]), "=r"(x[i + 5]), "=r"(x[i + 6]), "=r"(x[i + 7])
 #define KV_W8(x, i) "r"(x[i]), "r"(x[i + 1]), "r"(x[i + 2]), "r"(x[i + 3]), "r"(x[i + 4]), "r"(x[i + 5]), "r"(x[i + 6]), "r"(x[i + 7])
+// Loads with their wait: between the two the registers are not there yet, but the compiler, which does not know, might move them.
 __device__ __forceinline__ void kv_tmem_load32(uint32_t (&x)[32], uint32_t at)
 {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;"
                  : KV_R8(x, 0), KV_R8(x, 8), KV_R8(x, 16), KV_R8(x, 24) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void kv_tmem_load64(uint32_t (&x)[64], uint32_t at)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : KV_R8(x, 0), KV_R8(x, 8), KV_R8(x, 16), KV_R8(x, 24), KV_R8(x, 32), KV_R8(x, 40), KV_R8(x, 48), KV_R8(x, 56) : "r"(at) : "memory");
 }
 __device__ __forceinline__ void kv_tmem_store32(const uint32_t (&x)[32], uint32_t at)
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
                  ::KV_W8(x, 0), KV_W8(x, 8), KV_W8(x, 16), KV_W8(x, 24), "r"(at) : "memory");
 }
-// The load's registers go through the wait, so that nothing reads them before it.
-__device__ __forceinline__ void kv_tmem_loaded(uint32_t (&x)[32])
-{
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < 32; i++) asm volatile("" : "+r"(x[i]));
-}
-
 // Two 32-bit floats in one instruction
 __device__ __forceinline__ uint64_t kv_pair(float a, float b)
 {
@@ -120,6 +120,14 @@ __device__ __forceinline__ bool kv_wait_or_stop(uint32_t bar, uint32_t parity, v
     return false;
 }
 
+// Whether the phase has ended: one question, whose answer may be used much later.  (While the tensor cores read their operands, an
+// access to shared memory, a barrier's too, takes 150 to 300 cycles.)
+__device__ __forceinline__ uint32_t kv_ended(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done;
+}
 // The same answer for a whole warp.  All lanes ask: where one lane does, the compiler carries on with that lane apart from the others.
 __device__ __forceinline__ bool kv_warp_wait(uint32_t bar, uint32_t parity, volatile int* stop)
 {
@@ -194,81 +202,89 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
     float m = -KV_INF, l = 0.f, unit = 1.f;
     bool fine = true;
     // Steps of 64 tokens: while this one's weights are made, the next one's scores are (in the other half of S).
+    uint32_t ended = 0;                                  // whether this step's scores are known to be there
     for (int s = 0; s < 2 * tiles && fine; s++) {
         const int j = s >> 1, half = s & 1, t0 = begin + 64 * s;
         const uint32_t at = s_at + 64 * half;
-        fine = kv_warp_wait(bars + 8 * (KV_S_IN + 2 * m_tile + half), j & 1, stop) && (half || kv_warp_wait(bars + 8 * (KV_K_IN + (j & 3)), j >> 2 & 1, stop));
+        const KvSlot& slot = slots[j & 3];
+        if (!half) fine = kv_warp_wait(bars + 8 * (KV_K_IN + (j & 3)), j >> 2 & 1, stop);
+        float4 sc[4];                                    // the scales of the 16-token groups
+#pragma unroll
+        for (int g = 0; g < 4; g++) sc[g] = slot.group[4 * half + g];
+        if (!__all_sync(0xffffffffu, ended)) fine = kv_warp_wait(bars + 8 * (KV_S_IN + 2 * m_tile + half), j & 1, stop) && fine;
         if (!fine) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        uint32_t x[2][32];
-        kv_tmem_load32(x[0], at);
-        kv_tmem_load32(x[1], at + 32);
-        const KvSlot& slot = slots[j & 3];
-        const float4* const group = slot.group + 4 * half;
         const bool ragged = slot.pad[0] != 0.f || t0 + 63 > see_all || t0 <= low_all;
         float step = half ? 1.f : slot.step;             // of O: it is in units of V's reference, l is not
         unit = slot.unit;
-        float base = 0.f;
+        float base = 0.f, z[4];
         uint64_t sum[4] = {0, 0, 0, 0};                  // of 16 tokens' weights each
         auto pass = [&](auto some_hidden) {
             constexpr bool RAGGED = decltype(some_hidden)::value;
             uint32_t seen[2] = {0xffffffffu, 0xffffffffu};                   // which of 32 tokens the row sees
             float f[4];
 #pragma unroll
-            for (int g = 0; g < 4; g++) f[g] = group[g].x * factor;
+            for (int g = 0; g < 4; g++) f[g] = sc[g].x * factor;
             if (RAGGED)
 #pragma unroll
                 for (int b = 0; b < 2; b++) {
                     const int t = t0 + 32 * b, upto = min(max(place - t + 1, 0), 32), from = A.window > 0 ? min(max(place - A.window + 1 - t, 0), 32) : 0;
                     seen[b] = (uint32_t)(((uint64_t)1 << upto) - 1) & ~(uint32_t)(((uint64_t)1 << from) - 1);
-                    if (group[2 * b].w == 0.f) seen[b] &= 0xffff0000u;
-                    if (group[2 * b + 1].w == 0.f) seen[b] &= 0x0000ffffu;
+                    if (sc[2 * b].w == 0.f) seen[b] &= 0xffff0000u;
+                    if (sc[2 * b + 1].w == 0.f) seen[b] &= 0x0000ffffu;
                 }
-            kv_tmem_loaded(x[0]);
-            kv_tmem_loaded(x[1]);
+            uint32_t x[64];
+            kv_tmem_load64(x, at);
             // the largest score; a scale is not negative, so that of 16 tokens with one scale the largest product is the largest score
             float top = -KV_INF;
 #pragma unroll
             for (int g = 0; g < 4; g++) {
-                uint32_t (&y)[32] = x[g >> 1];
                 if (RAGGED)
 #pragma unroll
-                    for (int i = 16 * (g & 1); i < 16 * (g & 1) + 16; i++) y[i] = seen[g >> 1] >> i & 1 ? y[i] : 0xff800000u;
-                const int o = 16 * (g & 1);
-                float u = fmaxf(fmaxf(__uint_as_float(y[o]), __uint_as_float(y[o + 1])), __uint_as_float(y[o + 2]));
-                float w = fmaxf(fmaxf(__uint_as_float(y[o + 3]), __uint_as_float(y[o + 4])), __uint_as_float(y[o + 5]));
-                u = fmaxf(fmaxf(u, __uint_as_float(y[o + 6])), __uint_as_float(y[o + 7]));
-                w = fmaxf(fmaxf(w, __uint_as_float(y[o + 8])), __uint_as_float(y[o + 9]));
-                u = fmaxf(fmaxf(u, __uint_as_float(y[o + 10])), __uint_as_float(y[o + 11]));
-                w = fmaxf(fmaxf(w, __uint_as_float(y[o + 12])), __uint_as_float(y[o + 13]));
-                u = fmaxf(fmaxf(u, __uint_as_float(y[o + 14])), __uint_as_float(y[o + 15]));
+                    for (int i = 16 * g; i < 16 * g + 16; i++) x[i] = seen[g >> 1] >> (i & 31) & 1 ? x[i] : 0xff800000u;
+                const int o = 16 * g;
+                float u = fmaxf(fmaxf(__uint_as_float(x[o]), __uint_as_float(x[o + 1])), __uint_as_float(x[o + 2]));
+                float w = fmaxf(fmaxf(__uint_as_float(x[o + 3]), __uint_as_float(x[o + 4])), __uint_as_float(x[o + 5]));
+                u = fmaxf(fmaxf(u, __uint_as_float(x[o + 6])), __uint_as_float(x[o + 7]));
+                w = fmaxf(fmaxf(w, __uint_as_float(x[o + 8])), __uint_as_float(x[o + 9]));
+                u = fmaxf(fmaxf(u, __uint_as_float(x[o + 10])), __uint_as_float(x[o + 11]));
+                w = fmaxf(fmaxf(w, __uint_as_float(x[o + 12])), __uint_as_float(x[o + 13]));
+                u = fmaxf(fmaxf(u, __uint_as_float(x[o + 14])), __uint_as_float(x[o + 15]));
                 top = fmaxf(top, fmaxf(u, w) * f[g]);    // a NaN (0 times -inf where 16 hidden tokens have a scale of 0) does not count
             }
-            if (top > m + KV_LAZY) {
-                const float fall = kv_exp2(m - top);
-                l *= fall;
-                step *= fall;
-                m = top;
-            }
+            // without a branch, behind which the compiler might leave the rows apart: the tensor memory's instructions want the warp whole
+            const bool higher = top > m + KV_LAZY;
+            const float fall = higher ? kv_exp2(m - top) : 1.f;
+            l *= fall;
+            step *= fall;
+            m = higher ? top : m;
             // weights times V's share of the reference: the share's logarithm goes into the exponent, and out of the sum again by its
             // inverse.  A pair of values takes three steps, some pairs apart: an exponential's result comes after some 40 cycles, and the
             // unit takes one of a warp every 8, between which there is room for the other steps.
             base = m == -KV_INF ? 0.f : m;
+            float up[4];
+#pragma unroll
+            for (int g = 0; g < 4; g++) {
+                up[g] = sc[g].y - base;
+                z[g] = sc[g].z;
+            }
+            // ask for the next step's scores now
+            ended = kv_ended(bars + 8 * (KV_S_IN + 2 * m_tile + (half ^ 1)), (s + 1) >> 1 & 1);
             uint32_t p[32];
 #pragma unroll
             for (int i = 0; i < 32 + KV_P_AHEAD; i++) {
                 if (i < 32) {
-                    const float fg = f[i >> 3], ug = group[i >> 3].y - base;
-                    uint32_t &u = x[i >> 4][2 * i & 31], &w = x[i >> 4][(2 * i & 31) + 1];
-                    const float2 z = kv_unpair(kv_fma2(kv_pair(__uint_as_float(u), __uint_as_float(w)), kv_pair(fg, fg), kv_pair(ug, ug)));
-                    u = __float_as_uint(z.x);
-                    w = __float_as_uint(z.y);
+                    const float fg = f[i >> 3], ug = up[i >> 3];
+                    uint32_t &u = x[2 * i], &w = x[2 * i + 1];
+                    const float2 e = kv_unpair(kv_fma2(kv_pair(__uint_as_float(u), __uint_as_float(w)), kv_pair(fg, fg), kv_pair(ug, ug)));
+                    u = __float_as_uint(e.x);
+                    w = __float_as_uint(e.y);
                     asm volatile("ex2.approx.ftz.f32 %0, %0;" : "+r"(u));
                     asm volatile("ex2.approx.ftz.f32 %0, %0;" : "+r"(w));
                 }
                 if (i >= KV_P_AHEAD) {
                     const int k = i - KV_P_AHEAD;
-                    uint32_t &u = x[k >> 4][2 * k & 31], &w = x[k >> 4][(2 * k & 31) + 1];
+                    uint32_t &u = x[2 * k], &w = x[2 * k + 1];
                     if (RAGGED) {
                         u = seen[k >> 4] >> (2 * k & 31) & 1 ? u : 0u;
                         w = seen[k >> 4] >> ((2 * k & 31) + 1) & 1 ? w : 0u;
@@ -289,7 +305,6 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
             for (int b = 0; b < D / 32; b++) {
                 uint32_t y[32];
                 kv_tmem_load32(y, o_at + 32 * b);
-                kv_tmem_loaded(y);
 #pragma unroll
                 for (int i = 0; i < 32; i++) y[i] = __float_as_uint(__uint_as_float(y[i]) * step);
                 kv_tmem_store32(y, o_at + 32 * b);
@@ -302,9 +317,9 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
         float w[4];
 #pragma unroll
         for (int g = 0; g < 4; g++) {
-            const float2 z = kv_unpair(sum[g]);
-            w[g] = z.x + z.y;
-            w[g] = w[g] == 0.f ? 0.f : w[g] * group[g].z;                    // a hidden block's scale may be NaN
+            const float2 e = kv_unpair(sum[g]);
+            w[g] = e.x + e.y;
+            w[g] = w[g] == 0.f ? 0.f : w[g] * z[g];                          // a hidden block's scale may be NaN
         }
         const float total = (w[0] + w[1]) + (w[2] + w[3]);
         l += total;
@@ -328,7 +343,6 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
         uint32_t x[32];
         if (tiles > 0) {
             kv_tmem_load32(x, o_at + 32 * b);
-            kv_tmem_loaded(x);
         } else {
 #pragma unroll
             for (int i = 0; i < 32; i++) x[i] = 0u;

@@ -561,11 +561,18 @@ extern "C" int fastrack_kv_read(fastrack_kv* kv, const fastrack_kv_batch* batch,
 
 // ------------------------------------------------------------------------------------------------ attention ----
 
-#define KV_WAVES 4                      // times that the chunks fill the SMs
+#define KV_WAVES 4                      // times that chunks fill the SMs, where there is so much
+#define KV_CHUNK_LEAST 512              // tokens of a chunk, where chunks fill the SMs once with more
+#define KV_CHUNK_CLUSTER 2048           // tokens of a chunk in a cluster: above, more chunks than a cluster has are worth the join (where a cluster
+                                        // would have less than 4 chunks, 61 sequences of up to 4096 tokens took 88 us against 77)
 
 struct KvPlan { int rows, splits, chunk, row_tiles, units, unit_shift; size_t ml, lse2, unit_l2, total; };   // byte offsets in the workspace, part_o at 0
 
-static KvPlan kv_plan(const fastrack_kv* kv, const fastrack_kv_batch* b, bool mass)
+// Whether chunks go through the workspace
+static bool kv_parts(const KvPlan& p) { return p.splits > 1 && p.chunk > 0; }
+
+// A plan for a window needs no more of the workspace than the plan without one.
+static KvPlan kv_plan(const fastrack_kv* kv, const fastrack_kv_batch* b, bool mass, int window)
 {
     const KvShape& S = kv->shape;
     KvPlan p;
@@ -573,19 +580,23 @@ static KvPlan kv_plan(const fastrack_kv* kv, const fastrack_kv_batch* b, bool ma
     p.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : 2 * KV_P_ROWS;
     p.row_tiles = (int)((rows + p.rows - 1) / p.rows);
     const bool prompt = p.rows > 16;
-    const int64_t ctas = (int64_t)b->n_seqs * S.kv_heads * p.row_tiles, step = prompt ? KV_P_TOKENS : KV_STEP;
-    const int64_t want = ((prompt ? 1 : KV_WAVES * 4) * (int64_t)kv->num_sms + ctas - 1) / (ctas ? ctas : 1);
-    int64_t chunk = (b->max_len + want - 1) / want;
-    chunk = (chunk + step - 1) / step * step;
-    if (chunk < step) chunk = step;
-    p.chunk = (int)chunk;
-    p.splits = (int)((b->max_len + chunk - 1) / chunk);
-    if (p.splits < 1) p.splits = 1;
+    const int64_t seen = (int64_t)window + b->max_new + S.block_tokens, span = window > 0 && seen < b->max_len ? seen : b->max_len;
+    const int64_t spans = (int64_t)b->n_seqs * S.kv_heads * p.row_tiles > 0 ? (int64_t)b->n_seqs * S.kv_heads * p.row_tiles : 1;
+    const int64_t step = prompt ? KV_P_TOKENS : KV_STEP, most = (span + step - 1) / step;
+    const int64_t room = (prompt ? 1 : 4) * (int64_t)kv->num_sms, fill = (room + spans - 1) / spans;       // chunks of a span that fill the SMs
+    int64_t splits = prompt ? fill : KV_WAVES * fill < span / KV_CHUNK_LEAST ? KV_WAVES * fill : span / KV_CHUNK_LEAST > fill ? span / KV_CHUNK_LEAST : fill;
+    const bool cluster = !prompt && fill >= 4 && span <= KV_CHUNK_CLUSTER * (fill < KV_CLUSTER ? fill : KV_CLUSTER);
+    if (cluster) splits = fill < KV_CLUSTER ? fill : KV_CLUSTER;
+    if (splits > most) splits = most;
+    if (splits < 1) splits = 1;
+    const size_t room_for = cluster || splits < 2 ? 0 : (size_t)splits;       // grows with the span, as the chunks, rounded to steps, need not
+    p.chunk = cluster ? 0 : (int)(((span + splits - 1) / splits + step - 1) / step * step);
+    p.splits = cluster || p.chunk == 0 ? (int)splits : (int)((span + p.chunk - 1) / p.chunk);
     p.unit_shift = prompt ? (S.block_shift < 6 ? S.block_shift : 6) : 4;   // blocks of up to 64 tokens, or 16 tokens
     p.units = (b->max_len + (1 << p.unit_shift) - 1) >> p.unit_shift;
     const size_t all = (size_t)b->total_new * S.q_heads;
-    p.ml = p.splits > 1 ? (size_t)p.splits * all * S.head_dim * 4 : 0;
-    p.lse2 = p.ml + (p.splits > 1 ? (size_t)p.splits * all * 8 : 0);
+    p.ml = room_for * all * S.head_dim * 4;
+    p.lse2 = p.ml + room_for * all * 8;
     p.unit_l2 = (p.lse2 + all * 4 + 15) / 16 * 16;
     p.total = p.unit_l2 + (mass ? (size_t)b->n_seqs * S.kv_heads * p.units * (size_t)rows * 4 : 0);
     return p;
@@ -594,7 +605,7 @@ static KvPlan kv_plan(const fastrack_kv* kv, const fastrack_kv_batch* b, bool ma
 extern "C" size_t fastrack_kv_attention_workspace(const fastrack_kv* kv, const fastrack_kv_batch* batch, int with_mass)
 {
     if (!kv || kv_bad_batch(kv, batch)) return 0;
-    return kv_plan(kv, batch, with_mass != 0).total + 16;
+    return kv_plan(kv, batch, with_mass != 0, 0).total + 16;
 }
 
 // A launch whose start may overlap the end of the kernel before it in the stream; the kernel waits (griddepcontrol.wait) before it
@@ -615,7 +626,7 @@ static void kv_launch_after(cudaStream_t stream, dim3 grid, int threads, void (*
 }
 
 template <int D, bool BF>
-static void kv_attend_launch(const fastrack_kv* kv, const KvBatch& B, const KvAttend& A, const CUtensorMap& pool, cudaStream_t stream)
+static void kv_attend_launch(const fastrack_kv* kv, const KvBatch& B, const KvAttend& A, const CUtensorMap& pool, bool parts, cudaStream_t stream)
 {
     const KvShape& S = kv->shape;
     const bool e4 = kv->config.format == FASTRACK_KV_E4M3;
@@ -623,9 +634,21 @@ static void kv_attend_launch(const fastrack_kv* kv, const KvBatch& B, const KvAt
     if (A.rows > 16) (e4 ? kv_prompt_kernel<D, BF, true> : kv_prompt_kernel<D, BF, false>)<<<grid, KV_P_THREADS, KvPrompt<D>::SMEM, stream>>>(S, B, A);
     auto kernel = A.rows == 8 ? (e4 ? kv_attend_kernel<D, BF, true, 1> : kv_attend_kernel<D, BF, false, 1>)
                               : (e4 ? kv_attend_kernel<D, BF, true, 2> : kv_attend_kernel<D, BF, false, 2>);
-    if (A.rows <= 16) kernel<<<grid, 32 * KV_WARPS, kv_attend_smem<D>(A.rows) + 16 * KV_WARPS, stream>>>(S, B, A, pool);
-    if (A.splits > 1)
-        kv_launch_after(stream, dim3((unsigned)(((int64_t)B.max_new * S.q_heads + KV_WARPS - 1) / KV_WARPS), B.n_seqs), 32 * KV_WARPS, kv_join_kernel<D, BF>, S, B, A);
+    if (A.rows <= 16) {
+        cudaLaunchConfig_t c = {};
+        cudaLaunchAttribute cluster;
+        cluster.id = cudaLaunchAttributeClusterDimension;
+        cluster.val.clusterDim.x = A.chunk == 0 ? A.splits : 1;
+        cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+        c.gridDim = grid;
+        c.blockDim = dim3(32 * KV_WARPS);
+        c.dynamicSmemBytes = kv_attend_smem<D>(A.rows) + 16 * KV_WARPS;
+        c.stream = stream;
+        c.attrs = &cluster;
+        c.numAttrs = 1;
+        (void)cudaLaunchKernelEx(&c, kernel, S, B, A, pool);                 // an error stays for cudaGetLastError
+    }
+    if (parts) kv_launch_after(stream, dim3((unsigned)(B.max_new * S.q_heads), B.n_seqs), 32 * KV_WARPS, kv_join_kernel<D, BF>, S, B, A);
 }
 
 // The pool as a tensor of bytes (head_dim, rows of a page: K of all heads, then V, pages); boxes of 16 rows of one page.
@@ -655,7 +678,7 @@ extern "C" int fastrack_kv_attention(fastrack_kv* kv, const fastrack_kv_batch* b
     const bool mass = d_mass_out != nullptr;
     if (mass && (kv_misaligned(d_mass_in, 4) || kv_misaligned(d_mass_out, 4) || mass_stride < (batch->max_len + S.block_tokens - 1) / S.block_tokens)) return FASTRACK_ERR_ARG;
     if (batch->total_new > 0 && (kv_bad_rows(q) || kv_bad_rows(out) || (d_lse && kv_misaligned(d_lse, 4)))) return FASTRACK_ERR_ARG;
-    const KvPlan p = kv_plan(kv, batch, mass);
+    const KvPlan p = kv_plan(kv, batch, mass, window);
     if (kv_misaligned(d_workspace, 16) || workspace_bytes < p.total) return FASTRACK_ERR_ARG;
     if (int rc = kv_check_device(kv)) return rc;
     const KvBatch B = kv_batch(batch);
@@ -685,11 +708,11 @@ extern "C" int fastrack_kv_attention(fastrack_kv* kv, const fastrack_kv_batch* b
         CUtensorMap pool;
         if (int rc = kv_pool_map(kv, B, &pool)) return rc;
         switch (S.head_dim) {
-        case 64: bf ? kv_attend_launch<64, true>(kv, B, A, pool, st) : kv_attend_launch<64, false>(kv, B, A, pool, st); break;
-        case 96: bf ? kv_attend_launch<96, true>(kv, B, A, pool, st) : kv_attend_launch<96, false>(kv, B, A, pool, st); break;
-        default: bf ? kv_attend_launch<128, true>(kv, B, A, pool, st) : kv_attend_launch<128, false>(kv, B, A, pool, st); break;
+        case 64: bf ? kv_attend_launch<64, true>(kv, B, A, pool, kv_parts(p), st) : kv_attend_launch<64, false>(kv, B, A, pool, kv_parts(p), st); break;
+        case 96: bf ? kv_attend_launch<96, true>(kv, B, A, pool, kv_parts(p), st) : kv_attend_launch<96, false>(kv, B, A, pool, kv_parts(p), st); break;
+        default: bf ? kv_attend_launch<128, true>(kv, B, A, pool, kv_parts(p), st) : kv_attend_launch<128, false>(kv, B, A, pool, kv_parts(p), st); break;
         }
-        launches += 1 + (p.splits > 1);
+        launches += 1 + kv_parts(p);
     }
     if (mass && batch->max_len > 0) {
         const int blocks = (batch->max_len + S.block_tokens - 1) / S.block_tokens;

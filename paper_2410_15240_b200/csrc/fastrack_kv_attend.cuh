@@ -12,10 +12,13 @@
 // orders above the others' is not lost.
 #define KV_P_SCALE 2048.0f
 
-// A call's work is cut into chunks of each span, a CTA for each: equal pieces of whatever length sequences have, several times as many as
-// the SMs hold, so that one CTA's start and end pass under the others' loads.  (Tried instead: CTAs that stay and take equal runs of
-// one line of all work; every one of them starts and ends at the same time, and 61 sequences of up to 4096 tokens took 148 us
-// against 98.)
+// Every span is cut into chunks, a CTA for each.  Where the chunks fill the SMs several times, they are equal pieces of whatever length
+// a sequence has, so that one CTA's start and end pass under the others' loads; they are joined through the workspace by a kernel of its
+// own.  Where there is less than the SMs hold, a span is cut into up to KV_CLUSTER equal chunks, whose CTAs are a cluster and join
+// their answers through each other's shared memory.  (One sequence of 700 tokens: 12.3 us in a cluster, 14.3 us with the join's
+// launch; 61 sequences of up to 4096: 103 and 77 us, because the CTAs of short sequences wait for nothing in a cluster's place.
+// Tried instead: CTAs that stay and take equal runs of one line of all work; all of them start and end at the same time, 148 us.)
+#define KV_CLUSTER 8
 #define KV_STEP (KV_TILE * KV_WARPS)
 
 struct KvAttend {
@@ -23,7 +26,8 @@ struct KvAttend {
     float* lse;             // natural, or NULL
     int window;
     int rows;               // of a CTA: 8, 16 or 256
-    int splits, chunk;      // chunks of the span, tokens of a chunk (a multiple of KV_STEP and of the block)
+    int splits;             // most chunks of a span
+    int chunk;              // tokens of a chunk; 0: the chunks of a span are a cluster and equal
     int row_tiles, units;   // units: per sequence, for weights
     float* part_o;          // [splits][total_new * q_heads][head_dim]
     float* part_ml;         // [splits][total_new * q_heads][2]: running maximum and sum
@@ -110,6 +114,20 @@ __device__ __forceinline__ bool kv_wait(uint32_t bar, uint32_t parity)
     return done != 0;
 }
 
+__device__ __forceinline__ void kv_cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The same place in the shared memory of the cluster's CTA `rank`
+__device__ __forceinline__ float2 kv_peer_load(const float2* p, int rank)
+{
+    uint32_t at;
+    float2 v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
+    return v;
+}
+
 // 2^e with 2^e <= x < 2^(e+1) for finite x > 0 (1 for zero, the largest for what is not finite): dividing by it is exact.
 __device__ __forceinline__ float kv_power_below(uint32_t abs_bits)
 {
@@ -165,7 +183,7 @@ template <int D> struct KvTile {
 
 template <int D> __host__ __device__ constexpr int kv_attend_smem(int rows)
 {
-    const int tiles = KV_WARPS * KvTile<D>::STAGE, join = KV_WARPS * rows * (D + 4) * 4 + KV_WARPS * rows * 8;
+    const int tiles = KV_WARPS * KvTile<D>::STAGE, join = KV_WARPS * rows * (D + 4) * 4 + KV_WARPS * rows * 8 + rows * 8;
     return tiles > join ? tiles : join;                                      // and 16 bytes of barriers per warp behind
 }
 
@@ -447,9 +465,10 @@ __global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? 4 : 3) kv_attend_kern
     const KvSeq q = kv_seq(S, B, seq);
     const KvSpan span = kv_span(S, q, A.window, tile_row, ROWS);
     const int rows = q.n * S.group;
-    if (tile_row >= rows) return;
-    const int begin = span.begin + chunk * A.chunk, end = min(span.end, begin + A.chunk);
-    if (begin >= end && chunk > 0) return;
+    if (tile_row >= rows) return;                        // the cluster as a whole
+    const int size = A.chunk ? A.chunk : (max((span.end - span.begin + A.splits - 1) / A.splits, 1) + KV_STEP - 1) / KV_STEP * KV_STEP, begin = span.begin + chunk * size, end = min(span.end, begin + size);
+    const bool cluster = A.chunk == 0 && A.splits > 1;
+    if (begin >= end && chunk > 0 && !cluster) return;
 
     // tiles begin + 32 (warp + 4 i) of full blocks; a half behind the last full block, or on an absent page, is not there
     uint8_t* const slot = kv_smem + warp * T::STAGE;
@@ -582,6 +601,19 @@ __global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? 4 : 3) kv_attend_kern
             }
         }
     __syncthreads();
+    // A chunk's answer: rows' maxima and sums, and o relative to the maximum, over the first warp's (a thread reads what it writes over).
+    float2* const sm_ml = (float2*)(sm_l + KV_WARPS);
+    auto answer = [&](int row, int ch, float top, float sum, float x, float y) {
+        const int all = tile_row + row, head = kh * S.group + all % S.group;
+        const int64_t token = q.start + all / S.group;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        *(uint32_t*)((uint16_t*)A.out.data + token * A.out.token_stride + head * A.out.head_stride + ch) = kv_pack<BF>(x * inv, y * inv);
+        if (ch == 0) {
+            const float l2 = sum == 0.f ? -KV_INF : top + log2f(sum);
+            if (A.lse) A.lse[token * S.q_heads + head] = l2 * 0.6931471805599453f;
+            A.lse2[kv_lse2_at(S, q, kh, all)] = l2;
+        }
+    };
     for (int idx = threadIdx.x; idx < ROWS * (D / 2); idx += 32 * KV_WARPS) {
         const int row = idx / (D / 2), ch = idx % (D / 2) * 2, all = tile_row + row;
         if (all >= rows) break;
@@ -597,60 +629,92 @@ __global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? 4 : 3) kv_attend_kern
             x += f * sm_o[w][row][ch];
             y += f * sm_o[w][row][ch + 1];
         }
-        const int64_t token = q.start + all / S.group;
-        const int head = kh * S.group + all % S.group;
         if (A.splits == 1) {
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            *(uint32_t*)((uint16_t*)A.out.data + token * A.out.token_stride + head * A.out.head_stride + ch) = kv_pack<BF>(x * inv, y * inv);
-            if (ch == 0) {
-                const float l2 = sum == 0.f ? -KV_INF : base + log2f(sum);
-                if (A.lse) A.lse[token * S.q_heads + head] = l2 * 0.6931471805599453f;
-                A.lse2[kv_lse2_at(S, q, kh, all)] = l2;
-            }
+            answer(row, ch, top, sum, x, y);
+        } else if (cluster) {
+            *(float2*)&sm_o[0][row][ch] = make_float2(x, y);
+            if (ch == 0) sm_ml[row] = make_float2(top, sum);
         } else {
-            const int64_t at = ((int64_t)chunk * B.total_new + token) * S.q_heads + head;
+            const int64_t at = ((int64_t)chunk * B.total_new + q.start + all / S.group) * S.q_heads + kh * S.group + all % S.group;
             *(float2*)(A.part_o + at * D + ch) = make_float2(x, y);
             if (ch == 0) *(float2*)(A.part_ml + 2 * at) = make_float2(top, sum);
         }
     }
+    if (!cluster) return;
+    // every CTA of the cluster joins its share of the answers
+    kv_cluster_sync();
+    for (int idx = chunk * 32 * KV_WARPS + threadIdx.x; idx < ROWS * (D / 2); idx += A.splits * 32 * KV_WARPS) {
+        const int row = idx / (D / 2), ch = idx % (D / 2) * 2;
+        if (tile_row + row >= rows) break;
+        float2 ml[KV_CLUSTER], o[KV_CLUSTER];
+        float top = -KV_INF;
+#pragma unroll
+        for (int k = 0; k < KV_CLUSTER; k++) {
+            ml[k] = k < A.splits ? kv_peer_load(&sm_ml[row], k) : make_float2(-KV_INF, 0.f);
+            o[k] = k < A.splits ? kv_peer_load((const float2*)&sm_o[0][row][ch], k) : make_float2(0.f, 0.f);
+        }
+#pragma unroll
+        for (int k = 0; k < KV_CLUSTER; k++) top = fmaxf(top, ml[k].x);
+        const float base = top == -KV_INF ? 0.f : top;
+        float x = 0.f, y = 0.f, sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < KV_CLUSTER; k++) {
+            const float f = kv_exp2(ml[k].x - base);
+            sum += f * ml[k].y;
+            x += f * o[k].x;
+            y += f * o[k].y;
+        }
+        answer(row, ch, top, sum, x, y);
+    }
+    kv_cluster_sync();                                   // nobody leaves while others read its memory
 }
 
-// Joins the chunks of each row: a warp per row.
+// Joins the chunks of each row: a CTA per row, of which a warp takes every fourth chunk.
 template <int D, bool BF>
 __global__ void __launch_bounds__(32 * KV_WARPS) kv_join_kernel(const KvShape S, const KvBatch B, const KvAttend A)
 {
     constexpr int V = D / 32;
-    const int lane = threadIdx.x & 31, seq = blockIdx.y, idx = blockIdx.x * KV_WARPS + (threadIdx.x >> 5);
+    __shared__ float sm_acc[KV_WARPS][D], sm_sum[KV_WARPS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, seq = blockIdx.y, token = blockIdx.x / S.q_heads, head = blockIdx.x % S.q_heads;
     asm volatile("griddepcontrol.launch_dependents;");
     const KvSeq q = kv_seq(S, B, seq);
-    const int token = idx / S.q_heads, head = idx % S.q_heads;
     const KvSpan span = kv_span(S, q, A.window, (token * S.group + head % S.group) / A.rows * A.rows, A.rows);
     const int chunks = max(1, (span.end - span.begin + A.chunk - 1) / A.chunk);
-    const int64_t first = (int64_t)(q.start + token) * S.q_heads + head, step = (int64_t)B.total_new * S.q_heads;
+    const int64_t first = (int64_t)(q.start + token) * S.q_heads + head, stride = (int64_t)B.total_new * S.q_heads;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (idx >= q.n * S.q_heads) return;
+    if (token >= q.n) return;
     // the largest maximum first, then every chunk's sum and answer by its distance from it: loads that do not wait for one another
     float m = -KV_INF, l = 0.f, acc[V];
-    for (int k = lane; k < chunks; k += 32) m = fmaxf(m, A.part_ml[2 * (first + k * step)]);
+    for (int k = lane; k < chunks; k += 32) m = fmaxf(m, A.part_ml[2 * (first + k * stride)]);
 #pragma unroll
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
     const float base = m == -KV_INF ? 0.f : m;
 #pragma unroll
     for (int i = 0; i < V; i++) acc[i] = 0.f;
 #pragma unroll 8
-    for (int k = 0; k < chunks; k++) {
-        const float2 ml = *(const float2*)(A.part_ml + 2 * (first + k * step));
-        const float* src = A.part_o + (first + k * step) * D + lane * V;
+    for (int k = warp; k < chunks; k += KV_WARPS) {
+        const float2 ml = *(const float2*)(A.part_ml + 2 * (first + k * stride));
+        const float* src = A.part_o + (first + k * stride) * D + lane;
         const float h = kv_exp2(ml.x - base);
         l += ml.y * h;
 #pragma unroll
-        for (int i = 0; i < V; i++) acc[i] += src[i] * h;
+        for (int i = 0; i < V; i++) acc[i] += src[32 * i] * h;
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    uint16_t* dst = (uint16_t*)A.out.data + (q.start + token) * A.out.token_stride + head * A.out.head_stride + lane * V;
 #pragma unroll
-    for (int i = 0; i < V; i++) dst[i] = (uint16_t)kv_pack<BF>(acc[i] * inv, 0.f);
-    if (lane == 0) {
+    for (int i = 0; i < V; i++) sm_acc[warp][32 * i + lane] = acc[i];
+    if (lane == 0) sm_sum[warp] = l;
+    __syncthreads();
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < KV_WARPS; w++) l += sm_sum[w];
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (threadIdx.x < D / 2) {
+        float2 x = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < KV_WARPS; w++) { x.x += sm_acc[w][2 * threadIdx.x]; x.y += sm_acc[w][2 * threadIdx.x + 1]; }
+        *(uint32_t*)((uint16_t*)A.out.data + (q.start + token) * A.out.token_stride + head * A.out.head_stride + 2 * threadIdx.x) = kv_pack<BF>(x.x * inv, x.y * inv);
+    }
+    if (threadIdx.x == 0) {
         const float l2 = l == 0.f ? -KV_INF : m + log2f(l);
         if (A.lse) A.lse[first] = l2 * 0.6931471805599453f;
         A.lse2[kv_lse2_at(S, q, head / S.group, token * S.group + head % S.group)] = l2;

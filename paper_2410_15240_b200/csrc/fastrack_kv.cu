@@ -8,6 +8,7 @@
 #include <string.h>
 #include <atomic>
 #include <new>
+#include <type_traits>
 
 #include "../../include/fastrack_kv.h"
 #include "fastrack_kv_attend.cuh"
@@ -18,35 +19,62 @@
 
 #define KV_ROT_THREADS 256
 
-// One thread turns one unit (16 channels) of a token in `per` heads: the unit's cosines and sines are made once for them.
+template <bool BF> __device__ __forceinline__ void kv_turn_raw(const KvShape& S, const float* cs, const float* sn, uint4& a, uint4& b)
+{
+    float x[16];
+    kv_widen8<BF>(a, x);
+    kv_widen8<BF>(b, x + 8);
+    kv_turn(S, x, cs, sn);
+    a = kv_narrow8<BF>(x);
+    b = kv_narrow8<BF>(x + 8);
+}
+template <bool BF> __device__ __forceinline__ void kv_turn16(const KvShape& S, int u, int64_t position, uint4& a, uint4& b)
+{
+    float cs[8], sn[8];
+    kv_angles(S, u, position, false, cs, sn);
+    kv_turn_raw<BF>(S, cs, sn, a, b);
+}
+
+// One thread turns one unit (16 channels) of a token in heads h0 .. h0 + per - 1: the unit's cosines and sines are made once for them, while
+// the first heads' values are on their way.
+template <bool BF>
+__device__ __forceinline__ void kv_turn_heads(const KvShape& S, const KvRows& in, const KvRows& out, const int64_t* positions, int64_t token, int u, int h0, int per,
+                                              int heads, bool inverse)
+{
+    const KvUnit unit = kv_unit(S, u);
+    if (!unit.turned && in.data == out.data) return;
+    const uint16_t* src = (const uint16_t*)in.data + token * in.token_stride + h0 * in.head_stride;
+    uint16_t* dst = (uint16_t*)out.data + token * out.token_stride + h0 * out.head_stride;
+    const int n = min(per, heads - h0);
+    float cs[8], sn[8];
+    constexpr int AHEAD = 4;
+    for (int h = 0; h < n; h += AHEAD) {
+        uint4 a[AHEAD], b[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; k++)
+            if (h + k < n) {
+                a[k] = *(const uint4*)(src + (h + k) * in.head_stride + unit.a);
+                b[k] = *(const uint4*)(src + (h + k) * in.head_stride + unit.b);
+            }
+        if (h == 0 && unit.turned) kv_angles(S, u, positions[token], inverse, cs, sn);
+#pragma unroll
+        for (int k = 0; k < AHEAD; k++)
+            if (h + k < n) {
+                if (unit.turned) kv_turn_raw<BF>(S, cs, sn, a[k], b[k]);
+                *(uint4*)(dst + (h + k) * out.head_stride + unit.a) = a[k];
+                *(uint4*)(dst + (h + k) * out.head_stride + unit.b) = b[k];
+            }
+    }
+}
+
 template <bool BF>
 __global__ void __launch_bounds__(KV_ROT_THREADS) kv_rotary_kernel(const KvShape S, const KvRows in, const KvRows out, const int64_t* __restrict__ positions,
                                                                    const int64_t tokens, const int heads, const int per, const bool inverse)
 {
     const int units = S.head_dim / 16, groups = (heads + per - 1) / per;
-    const int64_t idx = (int64_t)blockIdx.x * KV_ROT_THREADS + threadIdx.x;
-    if (idx >= tokens * units * groups) return;
-    const int u = (int)(idx % units), h0 = (int)(idx / units % groups) * per;
-    const int64_t token = idx / units / groups;
-    const KvUnit unit = kv_unit(S, u);
-    if (!unit.turned && in.data == out.data) return;
-    float cs[8], sn[8];
-    if (unit.turned) kv_angles(S, u, positions[token], inverse, cs, sn);
-    for (int h = h0; h < min(h0 + per, heads); h++) {
-        const uint16_t* src = (const uint16_t*)in.data + token * in.token_stride + h * in.head_stride;
-        uint16_t* dst = (uint16_t*)out.data + token * out.token_stride + h * out.head_stride;
-        uint4 a = *(const uint4*)(src + unit.a), b = *(const uint4*)(src + unit.b);
-        if (unit.turned) {
-            float x[16];
-            kv_widen8<BF>(a, x);
-            kv_widen8<BF>(b, x + 8);
-            kv_turn(S, x, cs, sn);
-            a = kv_narrow8<BF>(x);
-            b = kv_narrow8<BF>(x + 8);
-        }
-        *(uint4*)(dst + unit.a) = a;
-        *(uint4*)(dst + unit.b) = b;
-    }
+    const int64_t idx = (int64_t)blockIdx.x * KV_ROT_THREADS + threadIdx.x, token = idx / units / groups;
+    if (token >= tokens) return;
+    kv_turn_heads<BF>(S, in, out, positions, token, (int)(idx % units), (int)(idx / units % groups) * per, per, heads, inverse);
 }
 
 // ------------------------------------------------------------------------------------------------ append ----
@@ -55,33 +83,88 @@ __global__ void __launch_bounds__(KV_ROT_THREADS) kv_rotary_kernel(const KvShape
 
 struct KvAppend { KvRows k, v, q, q_out; int slots, quant_ctas, q_per; };
 
-// Values of unit u of one new token (K turned, V as it is) or, for a token from before the call, of the tail.
-template <bool BF>
-__device__ __forceinline__ void kv_load_unit(const KvShape& S, const KvBatch& B, const KvAppend& A, const KvSeq& q, int seq, int kh, int which,
-                                             int token, int u, float* x)
+// Raw values of unit u of a token: K (which = 0) or V of a new token, or what the tail has of one from before the call.
+__device__ __forceinline__ const uint16_t* kv_unit_source(const KvShape& S, const KvBatch& B, const KvAppend& A, const KvSeq& q, int seq, int kh, int which, int token)
 {
-    const KvUnit unit = kv_unit(S, u);
     const int j = token - (q.len - q.n);
-    const uint16_t* src;
-    if (j >= 0) {
-        const KvRows& r = which ? A.v : A.k;
-        src = (const uint16_t*)r.data + (q.start + j) * r.token_stride + kh * r.head_stride;
-    } else {
-        src = (const uint16_t*)B.tail + (uint64_t)seq * S.tail_values + ((uint64_t)(2 * kh + which) * S.block_tokens + (token & (S.block_tokens - 1))) * S.head_dim;
-    }
-    kv_widen8<BF>(*(const uint4*)(src + unit.a), x);
-    kv_widen8<BF>(*(const uint4*)(src + unit.b), x + 8);
-    if (j >= 0 && which == 0 && unit.turned) {
-        float cs[8], sn[8];
-        kv_angles(S, u, B.positions[q.start + j], false, cs, sn);
-        kv_turn(S, x, cs, sn);
+    if (j < 0) return (const uint16_t*)B.tail + (uint64_t)seq * S.tail_values + ((uint64_t)(2 * kh + which) * S.block_tokens + (token & (S.block_tokens - 1))) * S.head_dim;
+    const KvRows& r = which ? A.v : A.k;
+    return (const uint16_t*)r.data + (q.start + j) * r.token_stride + kh * r.head_stride;
+}
+
+// The largest magnitude over the CTA, as bits (a NaN is larger than everything)
+__device__ __forceinline__ uint32_t kv_cta_max(uint32_t amax, uint32_t* warp_max)
+{
+    amax = __reduce_max_sync(0xffffffffu, amax);
+    if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = amax;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < KV_APPEND_THREADS / 32; w++) amax = max(amax, warp_max[w]);
+    return amax;
+}
+
+// One full block of one kv head: every value is read once and stays in registers between the search for the largest and the rounding.
+// N: units per thread of K, and of V.  All loads go out before the first use.
+template <bool BF, bool E4M3, int N>
+__device__ __forceinline__ void kv_append_block(const KvShape& S, const KvBatch& B, const KvAppend& A, const KvSeq& q, int seq, int kh, int t0, int page,
+                                                uint32_t (*warp_max)[KV_APPEND_THREADS / 32])
+{
+    constexpr float top = E4M3 ? 448.f : 127.f;
+    const int units = S.head_dim / 16, items = S.block_tokens * units, tid = threadIdx.x;
+    uint8_t* const dst = B.pool + (uint64_t)page * S.page_bytes;
+    uint4 w[2][N][2];
+#pragma unroll
+    for (int which = 0; which < 2; which++)
+#pragma unroll
+        for (int k = 0; k < N; k++) {
+            const int i = tid + k * KV_APPEND_THREADS;
+            if (i < items) {
+                const uint16_t* src = kv_unit_source(S, B, A, q, seq, kh, which, t0 + i / units);
+                const KvUnit unit = kv_unit(S, i % units);
+                w[which][k][0] = *(const uint4*)(src + unit.a);
+                w[which][k][1] = *(const uint4*)(src + unit.b);
+            } else {
+                w[which][k][0] = w[which][k][1] = make_uint4(0, 0, 0, 0);
+            }
+        }
+#pragma unroll
+    for (int which = 0; which < 2; which++) {
+        float x[N][16];
+        uint32_t amax = 0;
+#pragma unroll
+        for (int k = 0; k < N; k++) {
+            const int i = tid + k * KV_APPEND_THREADS, u = i % units, j = t0 + i / units - (q.len - q.n);
+            kv_widen8<BF>(w[which][k][0], x[k]);
+            kv_widen8<BF>(w[which][k][1], x[k] + 8);
+            if (which == 0 && i < items && j >= 0 && kv_unit(S, u).turned) {
+                float cs[8], sn[8];
+                kv_angles(S, u, B.positions[q.start + j], false, cs, sn);
+                kv_turn(S, x[k], cs, sn);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; e++) amax = max(amax, __float_as_uint(x[k][e]) & 0x7fffffffu);
+        }
+        amax = kv_cta_max(amax, warp_max[which]);
+        const float peak = amax < __float_as_uint(0x1p-100f) ? 0.f : __uint_as_float(amax), factor = peak == 0.f ? 0.f : top / peak;
+#pragma unroll
+        for (int k = 0; k < N; k++) {
+            const int i = tid + k * KV_APPEND_THREADS;
+            if (i >= items) break;
+#pragma unroll
+            for (int e = 0; e < 16; e++) x[k][e] *= factor;
+            const KvUnit unit = kv_unit(S, i % units);
+            uint8_t* row = dst + (uint64_t)which * S.codes_bytes + ((uint64_t)kh * S.block_tokens + i / units) * S.head_dim;
+            *(uint2*)(row + unit.a) = make_uint2(kv_codes4<E4M3>(x[k]), kv_codes4<E4M3>(x[k] + 4));
+            *(uint2*)(row + unit.b) = make_uint2(kv_codes4<E4M3>(x[k] + 8), kv_codes4<E4M3>(x[k] + 12));
+        }
+        if (tid == 0) ((float*)kv_scales(S, B, page))[2 * kh + which] = peak / top;
     }
 }
 
 // CTAs 0 .. quant_ctas - 1: one block that the call touches, of one kv head.  The CTA of a sequence's first block also writes the
 // head's tail, after it has read what the tail held: no other CTA touches the head's tail row.  The CTAs behind turn q.
-template <bool BF, bool E4M3>
-__global__ void __launch_bounds__(KV_APPEND_THREADS) kv_append_kernel(const KvShape S, const KvBatch B, const KvAppend A)
+template <bool BF, bool E4M3, int N>
+__global__ void __launch_bounds__(KV_APPEND_THREADS, N < 4 ? 3 : 2) kv_append_kernel(const KvShape S, const KvBatch B, const KvAppend A)
 {
     const int units = S.head_dim / 16, tid = threadIdx.x;
     if ((int)blockIdx.x >= A.quant_ctas) {
@@ -89,68 +172,17 @@ __global__ void __launch_bounds__(KV_APPEND_THREADS) kv_append_kernel(const KvSh
         const int64_t idx = (int64_t)(blockIdx.x - A.quant_ctas) * KV_APPEND_THREADS + tid;
         const int64_t token = idx / units / groups;
         if (token >= B.total_new) return;
-        const int u = (int)(idx % units), h0 = (int)(idx / units % groups) * A.q_per;
-        const KvUnit unit = kv_unit(S, u);
-        float cs[8], sn[8];
-        if (unit.turned) kv_angles(S, u, B.positions[token], false, cs, sn);
-        for (int h = h0; h < min(h0 + A.q_per, S.q_heads); h++) {
-            const uint16_t* src = (const uint16_t*)A.q.data + token * A.q.token_stride + h * A.q.head_stride;
-            uint16_t* dst = (uint16_t*)A.q_out.data + token * A.q_out.token_stride + h * A.q_out.head_stride;
-            uint4 a = *(const uint4*)(src + unit.a), b = *(const uint4*)(src + unit.b);
-            if (unit.turned) {
-                float x[16];
-                kv_widen8<BF>(a, x);
-                kv_widen8<BF>(b, x + 8);
-                kv_turn(S, x, cs, sn);
-                a = kv_narrow8<BF>(x);
-                b = kv_narrow8<BF>(x + 8);
-            }
-            *(uint4*)(dst + unit.a) = a;
-            *(uint4*)(dst + unit.b) = b;
-        }
+        kv_turn_heads<BF>(S, A.q, A.q_out, B.positions, token, (int)(idx % units), (int)(idx / units % groups) * A.q_per, A.q_per, S.q_heads, false);
         return;
     }
     const int kh = blockIdx.x % S.kv_heads, slot = blockIdx.x / S.kv_heads % A.slots, seq = blockIdx.x / S.kv_heads / A.slots;
     const KvSeq q = kv_seq(S, B, seq);
     if (q.n == 0) return;
-    const int first = max(q.len - q.n, 0), block = (first >> S.block_shift) + slot, t0 = block << S.block_shift;
-    const int items = S.block_tokens * units;
+    const int first = max(q.len - q.n, 0), block = (first >> S.block_shift) + slot;
     __shared__ uint32_t warp_max[2][KV_APPEND_THREADS / 32];
-
     if (block < q.full) {
         const int page = kv_page(B, seq, block);
-        if (page >= 0) {
-            uint8_t* dst = B.pool + (uint64_t)page * S.page_bytes;
-            for (int which = 0; which < 2; which++) {
-                uint32_t amax = 0;                      // as bits: a NaN is larger than everything
-                for (int i = tid; i < items; i += KV_APPEND_THREADS) {
-                    float x[16];
-                    kv_load_unit<BF>(S, B, A, q, seq, kh, which, t0 + i / units, i % units, x);
-#pragma unroll
-                    for (int e = 0; e < 16; e++) amax = max(amax, __float_as_uint(x[e]) & 0x7fffffffu);
-                }
-                amax = __reduce_max_sync(0xffffffffu, amax);
-                if ((tid & 31) == 0) warp_max[which][tid >> 5] = amax;
-                __syncthreads();
-#pragma unroll
-                for (int w = 0; w < KV_APPEND_THREADS / 32; w++) amax = max(amax, warp_max[which][w]);
-                constexpr float top = E4M3 ? 448.f : 127.f;
-                const float peak = amax < __float_as_uint(0x1p-100f) ? 0.f : __uint_as_float(amax);
-                const float factor = peak == 0.f ? 0.f : top / peak;
-                for (int i = tid; i < items; i += KV_APPEND_THREADS) {
-                    const int u = i % units;
-                    float x[16];
-                    kv_load_unit<BF>(S, B, A, q, seq, kh, which, t0 + i / units, u, x);
-#pragma unroll
-                    for (int e = 0; e < 16; e++) x[e] *= factor;
-                    const KvUnit unit = kv_unit(S, u);
-                    uint8_t* row = dst + (uint64_t)which * S.codes_bytes + ((uint64_t)kh * S.block_tokens + i / units) * S.head_dim;
-                    *(uint2*)(row + unit.a) = make_uint2(kv_codes4<E4M3>(x), kv_codes4<E4M3>(x + 4));
-                    *(uint2*)(row + unit.b) = make_uint2(kv_codes4<E4M3>(x + 8), kv_codes4<E4M3>(x + 12));
-                }
-                if (tid == 0) ((float*)kv_scales(S, B, page))[2 * kh + which] = peak / top;
-            }
-        }
+        if (page >= 0) kv_append_block<BF, E4M3, N>(S, B, A, q, seq, kh, block << S.block_shift, page, warp_max);
     }
     if (slot == 0) {
         __syncthreads();                                // the old tail has been read
@@ -158,11 +190,12 @@ __global__ void __launch_bounds__(KV_APPEND_THREADS) kv_append_kernel(const KvSh
         for (int i = tid; i < 2 * (q.len - from) * units; i += KV_APPEND_THREADS) {
             const int u = i % units, which = i / units & 1, token = from + i / units / 2;
             const KvUnit unit = kv_unit(S, u);
-            float x[16];
-            kv_load_unit<BF>(S, B, A, q, seq, kh, which, token, u, x);
+            const uint16_t* src = kv_unit_source(S, B, A, q, seq, kh, which, token);
+            uint4 a = *(const uint4*)(src + unit.a), b = *(const uint4*)(src + unit.b);
+            if (which == 0 && unit.turned) kv_turn16<BF>(S, u, B.positions[q.start + token - (q.len - q.n)], a, b);
             uint16_t* dst = (uint16_t*)B.tail + (uint64_t)seq * S.tail_values + ((uint64_t)(2 * kh + which) * S.block_tokens + (token & (S.block_tokens - 1))) * S.head_dim;
-            *(uint4*)(dst + unit.a) = kv_narrow8<BF>(x);
-            *(uint4*)(dst + unit.b) = kv_narrow8<BF>(x + 8);
+            *(uint4*)(dst + unit.a) = a;
+            *(uint4*)(dst + unit.b) = b;
         }
     }
 }
@@ -540,7 +573,12 @@ extern "C" int fastrack_kv_append(fastrack_kv* kv, const fastrack_kv_batch* batc
     if (quant + turn > INT32_MAX) return FASTRACK_ERR_ARG;
     A.quant_ctas = (int)quant;
     const bool bf = kv->config.dtype == FASTRACK_KV_BF16, e4 = kv->config.format == FASTRACK_KV_E4M3;
-    auto kernel = bf ? (e4 ? kv_append_kernel<true, true> : kv_append_kernel<true, false>) : (e4 ? kv_append_kernel<false, true> : kv_append_kernel<false, false>);
+    const int each = (S.block_tokens * (S.head_dim / 16) + KV_APPEND_THREADS - 1) / KV_APPEND_THREADS;     // units per thread: 1 .. 4
+    auto pick = [&](auto n) {
+        constexpr int N = decltype(n)::value;
+        return bf ? (e4 ? kv_append_kernel<true, true, N> : kv_append_kernel<true, false, N>) : (e4 ? kv_append_kernel<false, true, N> : kv_append_kernel<false, false, N>);
+    };
+    auto kernel = each == 1 ? pick(std::integral_constant<int, 1>()) : each == 2 ? pick(std::integral_constant<int, 2>()) : pick(std::integral_constant<int, 4>());
     kernel<<<(unsigned)(quant + turn), KV_APPEND_THREADS, 0, (cudaStream_t)stream>>>(S, kv_batch(batch), A);
     return kv_launched(kv);
 }
@@ -561,8 +599,8 @@ extern "C" int fastrack_kv_read(fastrack_kv* kv, const fastrack_kv_batch* batch,
 
 // ------------------------------------------------------------------------------------------------ attention ----
 
-#define KV_WAVES 4                      // times that chunks fill the SMs, where there is so much
-#define KV_CHUNK_LEAST 512              // tokens of a chunk, where chunks fill the SMs once with more
+#define KV_WAVES 3                      // times that chunks fill the SMs, where there is so much
+#define KV_CHUNK_LEAST 1024             // tokens of a chunk, where chunks fill the SMs once with more
 #define KV_CHUNK_CLUSTER 2048           // tokens of a chunk in a cluster: above, more chunks than a cluster has are worth the join (where a cluster
                                         // would have less than 4 chunks, 61 sequences of up to 4096 tokens took 88 us against 77)
 

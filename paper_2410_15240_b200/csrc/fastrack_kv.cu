@@ -37,7 +37,7 @@ template <bool BF> __device__ __forceinline__ void kv_turn16(const KvShape& S, i
 
 // One thread turns one unit (16 channels) of a token in heads h0 .. h0 + per - 1: the unit's cosines and sines are made once for them, while
 // the first heads' values are on their way.
-template <bool BF>
+template <bool BF, int AHEAD>
 __device__ __forceinline__ void kv_turn_heads(const KvShape& S, const KvRows& in, const KvRows& out, const int64_t* positions, int64_t token, int u, int h0, int per,
                                               int heads, bool inverse)
 {
@@ -47,7 +47,6 @@ __device__ __forceinline__ void kv_turn_heads(const KvShape& S, const KvRows& in
     uint16_t* dst = (uint16_t*)out.data + token * out.token_stride + h0 * out.head_stride;
     const int n = min(per, heads - h0);
     float cs[8], sn[8];
-    constexpr int AHEAD = 4;
     for (int h = 0; h < n; h += AHEAD) {
         uint4 a[AHEAD], b[AHEAD];
 #pragma unroll
@@ -74,7 +73,7 @@ __global__ void __launch_bounds__(KV_ROT_THREADS) kv_rotary_kernel(const KvShape
     const int units = S.head_dim / 16, groups = (heads + per - 1) / per;
     const int64_t idx = (int64_t)blockIdx.x * KV_ROT_THREADS + threadIdx.x, token = idx / units / groups;
     if (token >= tokens) return;
-    kv_turn_heads<BF>(S, in, out, positions, token, (int)(idx % units), (int)(idx / units % groups) * per, per, heads, inverse);
+    kv_turn_heads<BF, 4>(S, in, out, positions, token, (int)(idx % units), (int)(idx / units % groups) * per, per, heads, inverse);
 }
 
 // ------------------------------------------------------------------------------------------------ append ----
@@ -130,7 +129,7 @@ __device__ __forceinline__ void kv_append_block(const KvShape& S, const KvBatch&
 #pragma unroll
     for (int which = 0; which < 2; which++) {
         float x[N][16];
-        uint32_t amax = 0;
+        float most = 0.f;
 #pragma unroll
         for (int k = 0; k < N; k++) {
             const int i = tid + k * KV_APPEND_THREADS, u = i % units, j = t0 + i / units - (q.len - q.n);
@@ -142,16 +141,16 @@ __device__ __forceinline__ void kv_append_block(const KvShape& S, const KvBatch&
                 kv_turn(S, x[k], cs, sn);
             }
 #pragma unroll
-            for (int e = 0; e < 16; e++) amax = max(amax, __float_as_uint(x[k][e]) & 0x7fffffffu);
+            for (int e = 0; e < 16; e++) most = kv_max_nan(most, x[k][e]);
         }
-        amax = kv_cta_max(amax, warp_max[which]);
+        const uint32_t amax = kv_cta_max(__float_as_uint(most) & 0x7fffffffu, warp_max[which]);
         const float peak = amax < __float_as_uint(0x1p-100f) ? 0.f : __uint_as_float(amax), factor = peak == 0.f ? 0.f : top / peak;
 #pragma unroll
         for (int k = 0; k < N; k++) {
             const int i = tid + k * KV_APPEND_THREADS;
             if (i >= items) break;
 #pragma unroll
-            for (int e = 0; e < 16; e++) x[k][e] *= factor;
+            for (int e = 0; e < 16; e++) x[k][e] = __fmul_rn(x[k][e], factor);
             const KvUnit unit = kv_unit(S, i % units);
             uint8_t* row = dst + (uint64_t)which * S.codes_bytes + ((uint64_t)kh * S.block_tokens + i / units) * S.head_dim;
             *(uint2*)(row + unit.a) = make_uint2(kv_codes4<E4M3>(x[k]), kv_codes4<E4M3>(x[k] + 4));
@@ -172,7 +171,7 @@ __global__ void __launch_bounds__(KV_APPEND_THREADS, N < 4 ? 3 : 2) kv_append_ke
         const int64_t idx = (int64_t)(blockIdx.x - A.quant_ctas) * KV_APPEND_THREADS + tid;
         const int64_t token = idx / units / groups;
         if (token >= B.total_new) return;
-        kv_turn_heads<BF>(S, A.q, A.q_out, B.positions, token, (int)(idx % units), (int)(idx / units % groups) * A.q_per, A.q_per, S.q_heads, false);
+        kv_turn_heads<BF, 2>(S, A.q, A.q_out, B.positions, token, (int)(idx % units), (int)(idx / units % groups) * A.q_per, A.q_per, S.q_heads, false);
         return;
     }
     const int kh = blockIdx.x % S.kv_heads, slot = blockIdx.x / S.kv_heads % A.slots, seq = blockIdx.x / S.kv_heads / A.slots;

@@ -258,97 +258,114 @@ __device__ __forceinline__ int kv_rank(bool flag, int* warp_sums, int& total)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t votes = __ballot_sync(0xffffffffu, flag);
-    __syncthreads();
     if (lane == 0) warp_sums[warp] = __popc(votes);
     __syncthreads();
-    int sum = warp_sums[lane];
+    const int sum = warp_sums[lane];
     int before = sum;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) { const int o = __shfl_up_sync(0xffffffffu, before, d); if (lane >= d) before += o; }
     total = __shfl_sync(0xffffffffu, before, 31);
+    __syncthreads();
     return __shfl_sync(0xffffffffu, before - sum, warp) + __popc(votes & ((1u << lane) - 1u));
 }
 
+#define KV_EVICT_COUNTS 8               // copies of the histogram: weights have few exponents, and one counter for all warps holds them up
+#define KV_EVICT_HEADS 8                // heads whose weights a thread moves between two barriers
+
 // One CTA per sequence.  The score of the last block to leave is found by radix selection, 8 bits at a time; then one pass in block
-// order moves what stays.  An entry is read before a barrier that precedes every write at or above its place: in place is safe.
+// order moves what stays: a block's new place is its place less the blocks before it that leave.  What 1024 blocks have is read
+// before a barrier that precedes every write at or above their places: in place is safe.
+// Bound by the latency of these dependent passes (4 x 3 barriers, then 4 per 1024 blocks and 8 heads), not by its bytes.
 __global__ void __launch_bounds__(KV_EVICT_THREADS) kv_evict_kernel(const KvShape S, const KvEvict A)
 {
     extern __shared__ uint32_t keys[];
-    __shared__ int hist[256], warp_sums[32], pick[2];
+    __shared__ int hist[KV_EVICT_COUNTS][256], warp_sums[32], pick[3];
     const int seq = blockIdx.x, tid = threadIdx.x;
     const int len = max(A.lens[seq], 0), most = min(A.table_stride, A.mass_stride);
     const int full = min(len >> S.block_shift, most), held = min((len + S.block_tokens - 1) >> S.block_shift, most);
     const int lo = min(A.keep_first, full), hi = max(full - A.keep_last, lo);
     const int drop = min(max(full - A.budget, 0), hi - lo);
-    const float* mass = A.mass + (int64_t)seq * S.kv_heads * A.mass_stride;
+    const float* const mass = A.mass + (int64_t)seq * S.kv_heads * A.mass_stride;
+    float* const mass_out = A.mass_out + (int64_t)seq * S.kv_heads * A.mass_stride;
     auto score = [&](int b) {
         double x = 0.;
+#pragma unroll 8
         for (int h = 0; h < S.kv_heads; h++) x += mass[(int64_t)h * A.mass_stride + b];
         return kv_order((float)x);
     };
     auto key = [&](int b) { return b < A.keys ? keys[b] : score(b); };
     uint32_t limit = 0;
-    int ties = 0;                                       // blocks with exactly the limit's score that leave
+    int ties = 0, equal = 0;                            // of the blocks with exactly the limit's score: those that leave, and all
     if (drop > 0) {
-        for (int b = lo + tid; b < min(hi, A.keys); b += KV_EVICT_THREADS) keys[b] = score(b);
-        int left = drop;
+        for (int i = tid; i < KV_EVICT_COUNTS * 256; i += KV_EVICT_THREADS) hist[i >> 8][i & 255] = 0;
+        __syncthreads();
+        ties = drop;
         for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = tid; i < 256; i += KV_EVICT_THREADS) hist[i] = 0;
-            __syncthreads();
             for (int b = lo + tid; b < hi; b += KV_EVICT_THREADS) {
-                const uint32_t k = key(b);
-                if (shift == 24 || k >> (shift + 8) == limit >> (shift + 8)) atomicAdd(&hist[k >> shift & 255], 1);
+                const uint32_t k = shift == 24 ? score(b) : key(b);
+                if (shift == 24 && b < A.keys) keys[b] = k;
+                if (shift == 24 || k >> (shift + 8) == limit >> (shift + 8)) atomicAdd(&hist[tid >> 5 & (KV_EVICT_COUNTS - 1)][k >> shift & 255], 1);
             }
             __syncthreads();
-            if (tid < 32) {                             // the bin in which the left-th smallest lies
-                int mine = 0, before;
-                for (int i = 0; i < 8; i++) mine += hist[8 * tid + i];
-                before = mine;
+            int mine = 0, upto = 0;
+            if (tid < 256) {
 #pragma unroll
-                for (int d = 1; d < 32; d <<= 1) { const int o = __shfl_up_sync(0xffffffffu, before, d); if (tid >= d) before += o; }
-                before -= mine;
-                if (before < left && left <= before + mine)
-                    for (int i = 0; i < 8; i++) {
-                        if (left <= before + hist[8 * tid + i]) { pick[0] = 8 * tid + i; pick[1] = left - before; break; }
-                        before += hist[8 * tid + i];
-                    }
+                for (int c = 0; c < KV_EVICT_COUNTS; c++) { mine += hist[c][tid]; hist[c][tid] = 0; }
+                upto = mine;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) { const int o = __shfl_up_sync(0xffffffffu, upto, d); if ((tid & 31) >= d) upto += o; }
+                if ((tid & 31) == 31) warp_sums[tid >> 5] = upto;
+            }
+            __syncthreads();
+            if (tid < 256) {
+#pragma unroll
+                for (int w = 0; w < 8; w++) upto += w < tid >> 5 ? warp_sums[w] : 0;
+                if (upto - mine < ties && ties <= upto) { pick[0] = tid; pick[1] = ties - (upto - mine); pick[2] = mine; }
             }
             __syncthreads();
             limit |= (uint32_t)pick[0] << shift;
-            left = pick[1];
+            ties = pick[1];
+            equal = pick[2];
         }
-        ties = left;
     }
-    int out_at = 0, stay_at = 0, tie_at = 0;
-    for (int b0 = 0; b0 < most; b0 += KV_EVICT_THREADS) {
+    int out_at = 0, tie_at = 0;
+    for (int b0 = 0; b0 < held; b0 += KV_EVICT_THREADS) {
         const int b = b0 + tid;
         const bool free = drop > 0 && b >= lo && b < hi;
         const uint32_t k = free ? key(b) : 0u;
-        int total;
         const bool tie = free && k == limit;
-        const int tie_rank = tie_at + kv_rank(tie, warp_sums, total);
-        tie_at += total;
-        const bool out = free && (k < limit || (tie && tie_rank < ties)), stay = b < held && !out;
-        const int out_rank = out_at + kv_rank(out, warp_sums, total);
+        bool out = free && (k < limit || tie);
+        int total;
+        if (ties < equal) {                             // of equals the lowest places leave
+            const int rank = tie_at + kv_rank(tie, warp_sums, total);
+            tie_at += total;
+            if (tie && rank >= ties) out = false;
+        }
+        const int before = out_at + kv_rank(out, warp_sums, total);
         out_at += total;
-        const int stay_rank = stay_at + kv_rank(stay, warp_sums, total);
-        stay_at += total;
+        const bool stay = b < held && !out;
+        const int to = b - before;
         const int32_t page = b < held ? A.table[(int64_t)seq * A.table_stride + b] : -1;
-        __syncthreads();
-        if (stay) A.table_out[(int64_t)seq * A.table_stride + stay_rank] = page;
-        if (out) A.evicted[(int64_t)seq * A.table_stride + out_rank] = page;
-        for (int h = 0; h < S.kv_heads; h++) {
-            const int64_t row = ((int64_t)seq * S.kv_heads + h) * A.mass_stride;
-            const float w = stay ? A.mass[row + b] : 0.f;
+        for (int h0 = 0; h0 < S.kv_heads; h0 += KV_EVICT_HEADS) {
+            float w[KV_EVICT_HEADS];
+#pragma unroll
+            for (int h = 0; h < KV_EVICT_HEADS; h++) w[h] = stay && h0 + h < S.kv_heads ? mass[(int64_t)(h0 + h) * A.mass_stride + b] : 0.f;
             __syncthreads();
-            if (stay) A.mass_out[row + stay_rank] = w;
+            if (h0 == 0) {
+                if (stay) A.table_out[(int64_t)seq * A.table_stride + to] = page;
+                if (out) A.evicted[(int64_t)seq * A.table_stride + before] = page;
+            }
+            if (stay)
+#pragma unroll
+                for (int h = 0; h < KV_EVICT_HEADS; h++)
+                    if (h0 + h < S.kv_heads) mass_out[(int64_t)(h0 + h) * A.mass_stride + to] = w[h];
         }
     }
     __syncthreads();
     for (int b = held - drop + tid; b < A.table_stride; b += KV_EVICT_THREADS) A.table_out[(int64_t)seq * A.table_stride + b] = -1;
     for (int b = drop + tid; b < A.table_stride; b += KV_EVICT_THREADS) A.evicted[(int64_t)seq * A.table_stride + b] = -1;
-    for (int h = 0; h < S.kv_heads; h++)
-        for (int b = held - drop + tid; b < A.mass_stride; b += KV_EVICT_THREADS) A.mass_out[((int64_t)seq * S.kv_heads + h) * A.mass_stride + b] = 0.f;
+    for (int b = held - drop + tid; b < A.mass_stride; b += KV_EVICT_THREADS)
+        for (int h = 0; h < S.kv_heads; h++) mass_out[(int64_t)h * A.mass_stride + b] = 0.f;
     if (tid == 0) {
         A.lens_out[seq] = len - (drop << S.block_shift);
         A.n_evicted[seq] = drop;

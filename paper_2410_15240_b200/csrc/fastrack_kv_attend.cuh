@@ -379,7 +379,7 @@ __device__ __forceinline__ void kv_tile(KvState<D, NR>& W, const uint8_t* slot, 
 }
 
 // 16 tokens of the unfinished block: 16-bit values, tokens behind the last as zeros.  bf16 goes to f16 by a power of two near the
-// largest of the 16 tokens; it is looked for first, and the values are read again (once per sequence and head, from L1).
+// largest of the 16 tokens' K, or V.
 template <int D, bool BF, int NR>
 __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* k, const uint16_t* v, int t0, int len, const int (&place)[NR][2], int window,
                                              float* unit_out, int rows_left, int lane)
@@ -387,18 +387,7 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
     using T = KvTile<D>;
     constexpr int STEPS = D / 16;
     const int g = lane >> 2, c = lane & 3;
-    float scale[2] = {1.f, 1.f};
-    if (BF)
-        for (int which = 0; which < 2; which++) {
-            const uint16_t* const src = which ? v : k;
-            uint32_t amax = 0;
-            for (int i = lane; i < KV_HALF * D / 8; i += 32) {
-                if (t0 + i / (D / 8) >= len) break;
-                amax = max(amax, kv_amax8(*(const uint4*)(src + 8 * i)));
-            }
-            scale[which] = kv_power_below(__reduce_max_sync(0xffffffffu, amax));
-        }
-    const float ki = 1.f / scale[0], vi = 1.f / scale[1];
+    auto amax2 = [](uint32_t a, uint32_t w) { return max(a, max(w << 16 & 0x7fffffffu, w & 0x7fff0000u)); };
     auto narrow = [](uint32_t w, float inv) {
         if (!BF) return w;
         const float2 x = kv_unpack<true>(w);
@@ -407,19 +396,42 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
     float s[1][NR][4], base[NR][2];
 #pragma unroll
     for (int r = 0; r < NR; r++) s[0][r][0] = s[0][r][1] = s[0][r][2] = s[0][r][3] = 0.f;
+    float k_scale = 1.f, v_scale = 1.f;
+    {
+        uint2 lo[STEPS], hi[STEPS];
+        uint32_t amax = 0;
 #pragma unroll
-    for (int i = 0; i < STEPS; i++) {
-        const uint2 lo = t0 + g < len ? *(const uint2*)(k + g * D + T::k_channel(i, c)) : make_uint2(0, 0);
-        const uint2 hi = t0 + 8 + g < len ? *(const uint2*)(k + (8 + g) * D + T::k_channel(i, c)) : make_uint2(0, 0);
+        for (int i = 0; i < STEPS; i++) {
+            lo[i] = t0 + g < len ? *(const uint2*)(k + g * D + T::k_channel(i, c)) : make_uint2(0, 0);
+            hi[i] = t0 + 8 + g < len ? *(const uint2*)(k + (8 + g) * D + T::k_channel(i, c)) : make_uint2(0, 0);
+        }
+        if (BF) {
 #pragma unroll
-        for (int r = 0; r < NR; r++) kv_mma(s[0][r], narrow(lo.x, ki), narrow(hi.x, ki), narrow(lo.y, ki), narrow(hi.y, ki), W.qb[r][i]);
+            for (int i = 0; i < STEPS; i++) amax = amax2(amax2(amax2(amax2(amax, lo[i].x), lo[i].y), hi[i].x), hi[i].y);
+            k_scale = kv_power_below(__reduce_max_sync(0xffffffffu, amax));
+        }
+        const float inv = 1.f / k_scale;
+#pragma unroll
+        for (int i = 0; i < STEPS; i++) {
+            const uint32_t a0 = narrow(lo[i].x, inv), a1 = narrow(hi[i].x, inv), a2 = narrow(lo[i].y, inv), a3 = narrow(hi[i].y, inv);
+#pragma unroll
+            for (int r = 0; r < NR; r++) kv_mma(s[0][r], a0, a1, a2, a3, W.qb[r][i]);
+        }
     }
+    uint32_t w[STEPS][4];                                // V of tokens 2c, 2c+1, 2c+8, 2c+9, two channels each: on their way meanwhile
+#pragma unroll
+    for (int i = 0; i < STEPS; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int t = 2 * c + (j & 1) + (j >> 1) * 8;
+            w[i][j] = t0 + t < len ? *(const uint32_t*)(v + t * D + T::v_channel(g, 2 * i)) : 0u;
+        }
     uint32_t hidden = 0;
 #pragma unroll
     for (int r = 0; r < NR; r++)
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            s[0][r][i] *= scale[0] * W.factor[r][i & 1];
+            s[0][r][i] *= k_scale * W.factor[r][i & 1];
             const int t = t0 + 8 * (i >> 1) + g, at = place[r][i & 1];
             if (t > at || (window > 0 && t <= at - window)) {
                 s[0][r][i] = -KV_INF;
@@ -428,8 +440,14 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
         }
     kv_weigh<D, NR, 1>(W, s, base);
     if (unit_out) kv_note<D, NR, 1>(s, base, 0, 1, unit_out, rows_left, g, c);
-    kv_refer<D, NR>(W, scale[1]);
-    const float vf = scale[1] * W.vinv;
+    if (BF) {
+        uint32_t amax = 0;
+#pragma unroll
+        for (int i = 0; i < STEPS; i++) amax = amax2(amax2(amax2(amax2(amax, w[i][0]), w[i][1]), w[i][2]), w[i][3]);
+        v_scale = kv_power_below(__reduce_max_sync(0xffffffffu, amax));
+    }
+    kv_refer<D, NR>(W, v_scale);
+    const float vf = v_scale * W.vinv, inv = 1.f / v_scale;
     uint32_t pb[NR][2];
 #pragma unroll
     for (int r = 0; r < NR; r++)
@@ -438,15 +456,12 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
             pb[r][up] = kv_transpose(kv_pack<false>(hidden >> (4 * r + 2 * up) & 1 ? 0.f : s[0][r][2 * up] * vf, hidden >> (4 * r + 2 * up + 1) & 1 ? 0.f : s[0][r][2 * up + 1] * vf));
 #pragma unroll
     for (int i = 0; i < STEPS; i++) {
-        uint32_t w[4];
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const int t = 2 * c + (j & 1) + (j >> 1) * 8;
-            w[j] = t0 + t < len ? narrow(*(const uint32_t*)(v + t * D + T::v_channel(g, 2 * i)), vi) : 0u;
-        }
+        for (int j = 0; j < 4; j++) w[i][j] = narrow(w[i][j], inv);
 #pragma unroll
         for (int r = 0; r < NR; r++)
-            kv_mma(W.o[r][i], __byte_perm(w[0], w[1], 0x5410), __byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x5410), __byte_perm(w[2], w[3], 0x7632), pb[r]);
+            kv_mma(W.o[r][i], __byte_perm(w[i][0], w[i][1], 0x5410), __byte_perm(w[i][0], w[i][1], 0x7632), __byte_perm(w[i][2], w[i][3], 0x5410),
+                   __byte_perm(w[i][2], w[i][3], 0x7632), pb[r]);
     }
 }
 
@@ -556,6 +571,12 @@ __global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? 4 : 3) kv_attend_kern
     float* const units = A.unit_l2 ? A.unit_l2 + ((int64_t)seq * S.kv_heads + kh) * A.units * unit_stride + tile_row : nullptr;
     const bool one_unit = S.block_tokens >= KV_TILE;
 
+    // the tail first: its loads pass while the first tiles come
+    const uint16_t* const tail_k = (const uint16_t*)B.tail + (uint64_t)seq * S.tail_values + (uint64_t)kh * 2 * S.block_tokens * D;
+    for (int t0 = max(begin, tail_begin) + KV_HALF * warp; t0 < end; t0 += KV_HALF * KV_WARPS)
+        kv_tail_tile<D, BF, NR>(W, tail_k + (t0 - tail_begin) * D, tail_k + (S.block_tokens + t0 - tail_begin) * D, t0, q.len, place, A.window,
+                                units ? units + (int64_t)(t0 / KV_HALF) * unit_stride : nullptr, rows - tile_row, lane);
+
     uint32_t phase = 0;
     for (int t0 = first; t0 < full_end; t0 += STRIDE) {
         float* const unit_out = units ? units + (int64_t)(t0 / KV_HALF) * unit_stride : nullptr;
@@ -575,11 +596,6 @@ __global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? 4 : 3) kv_attend_kern
             kv_tile<D, E4M3, NR, true>(W, slot, t0, ks, vs, there, place, A.window, unit_out, unit_stride, one_unit, rows - tile_row, lane, k_wait, k_read, v_wait, v_read);
         phase ^= 1;
     }
-    const uint16_t* const tail_k = (const uint16_t*)B.tail + (uint64_t)seq * S.tail_values + (uint64_t)kh * 2 * S.block_tokens * D;
-    for (int t0 = max(begin, tail_begin) + KV_HALF * warp; t0 < end; t0 += KV_HALF * KV_WARPS)
-        kv_tail_tile<D, BF, NR>(W, tail_k + (t0 - tail_begin) * D, tail_k + (S.block_tokens + t0 - tail_begin) * D, t0, q.len, place, A.window,
-                                units ? units + (int64_t)(t0 / KV_HALF) * unit_stride : nullptr, rows - tile_row, lane);
-
     // join the warps, in the tiles' memory
     __syncthreads();
     float (*const sm_o)[ROWS][D + 4] = (float (*)[ROWS][D + 4])kv_smem;

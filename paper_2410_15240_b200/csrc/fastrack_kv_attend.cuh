@@ -468,7 +468,7 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
 // One CTA: 8 NR rows of one kv head of one sequence, one chunk of the tokens they see.  Each of the four warps takes every fourth
 // tile with statistics and an accumulator of its own; they are joined in shared memory at the end.
 template <int D, bool BF, bool E4M3, int NR>
-__global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? 4 : 3) kv_attend_kernel(const KvShape S, const KvBatch B, const KvAttend A,
+__global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? (D == 64 ? 6 : 4) : 3) kv_attend_kernel(const KvShape S, const KvBatch B, const KvAttend A,
                                                                                   const __grid_constant__ CUtensorMap pool)
 {
     using T = KvTile<D>;

@@ -273,9 +273,21 @@ template <int D, int NR> __device__ __forceinline__ void kv_refer(KvState<D, NR>
     }
 }
 
+// Weights of two rows as f16, as the second operand's share of a lane.  FINE (answers of 11 bits, where the rounding of the weights
+// would show as much as that of the answer): what the rounding leaves out as another such number, which gets a product of its own.
+template <bool FINE> __device__ __forceinline__ void kv_weights(float x, float y, uint32_t& hi, uint32_t& lo)
+{
+    hi = kv_pack<false>(x, y);
+    if (FINE) {
+        const float2 z = kv_unpack<false>(hi);
+        lo = kv_transpose(kv_pack<false>(x - z.x, y - z.y));
+    }
+    hi = kv_transpose(hi);
+}
+
 // One tile of full blocks.  RAGGED: some of its tokens are hidden from some rows, or a half is not there; hidden has a bit for each of s.
 // k_wait and v_wait wait for K and V, k_read and v_read are called when they have been read.
-template <int D, bool E4M3, int NR, bool RAGGED, class KWait, class KRead, class VWait, class VRead>
+template <int D, bool FINE, bool E4M3, int NR, bool RAGGED, class KWait, class KRead, class VWait, class VRead>
 __device__ __forceinline__ void kv_tile(KvState<D, NR>& W, const uint8_t* slot, int t0, const float (&ks)[2], const float (&vs)[2], const bool (&there)[2],
                                         const int (&place)[NR][2], int window, float* unit_out, int unit_stride, bool one_unit, int rows_left, int lane,
                                         KWait k_wait, KRead k_read, VWait v_wait, VRead v_read)
@@ -339,7 +351,7 @@ __device__ __forceinline__ void kv_tile(KvState<D, NR>& W, const uint8_t* slot, 
 #pragma unroll
     for (int h = 0; h < 2; h++) {
         const float vf = !fine ? __int_as_float(0x7fffffff) : W.vref > 0.f ? vs[h] * W.vinv : vs[h];     // bytes that never came: NaN
-        uint32_t pb[NR][2];
+        uint32_t pb[NR][2], pl[NR][2];
 #pragma unroll
         for (int r = 0; r < NR; r++)
 #pragma unroll
@@ -349,7 +361,7 @@ __device__ __forceinline__ void kv_tile(KvState<D, NR>& W, const uint8_t* slot, 
                     if (hidden >> (8 * r + 4 * h + 2 * up) & 1) x = 0.f;
                     if (hidden >> (8 * r + 4 * h + 2 * up + 1) & 1) y = 0.f;
                 }
-                pb[r][up] = kv_transpose(kv_pack<false>(x, y));
+                kv_weights<FINE>(x, y, pb[r][up], pl[r][up]);
             }
         uint32_t vw[4][T::VW];
 #pragma unroll
@@ -372,6 +384,10 @@ __device__ __forceinline__ void kv_tile(KvState<D, NR>& W, const uint8_t* slot, 
             for (int r = 0; r < NR; r++) {
                 kv_mma(W.o[r][2 * w], a[0], a[1], b[0], b[1], pb[r]);
                 kv_mma(W.o[r][2 * w + 1], a[2], a[3], b[2], b[3], pb[r]);
+                if (FINE) {
+                    kv_mma(W.o[r][2 * w], a[0], a[1], b[0], b[1], pl[r]);
+                    kv_mma(W.o[r][2 * w + 1], a[2], a[3], b[2], b[3], pl[r]);
+                }
             }
         }
     }
@@ -448,20 +464,24 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
     }
     kv_refer<D, NR>(W, v_scale);
     const float vf = v_scale * W.vinv, inv = 1.f / v_scale;
-    uint32_t pb[NR][2];
+    uint32_t pb[NR][2], pl[NR][2];
 #pragma unroll
     for (int r = 0; r < NR; r++)
 #pragma unroll
         for (int up = 0; up < 2; up++)
-            pb[r][up] = kv_transpose(kv_pack<false>(hidden >> (4 * r + 2 * up) & 1 ? 0.f : s[0][r][2 * up] * vf, hidden >> (4 * r + 2 * up + 1) & 1 ? 0.f : s[0][r][2 * up + 1] * vf));
+            kv_weights<!BF>(hidden >> (4 * r + 2 * up) & 1 ? 0.f : s[0][r][2 * up] * vf, hidden >> (4 * r + 2 * up + 1) & 1 ? 0.f : s[0][r][2 * up + 1] * vf,
+                            pb[r][up], pl[r][up]);
 #pragma unroll
     for (int i = 0; i < STEPS; i++) {
 #pragma unroll
         for (int j = 0; j < 4; j++) w[i][j] = narrow(w[i][j], inv);
+        const uint32_t a0 = __byte_perm(w[i][0], w[i][1], 0x5410), a1 = __byte_perm(w[i][0], w[i][1], 0x7632), a2 = __byte_perm(w[i][2], w[i][3], 0x5410),
+                       a3 = __byte_perm(w[i][2], w[i][3], 0x7632);
 #pragma unroll
-        for (int r = 0; r < NR; r++)
-            kv_mma(W.o[r][i], __byte_perm(w[i][0], w[i][1], 0x5410), __byte_perm(w[i][0], w[i][1], 0x7632), __byte_perm(w[i][2], w[i][3], 0x5410),
-                   __byte_perm(w[i][2], w[i][3], 0x7632), pb[r]);
+        for (int r = 0; r < NR; r++) {
+            kv_mma(W.o[r][i], a0, a1, a2, a3, pb[r]);
+            if (!BF) kv_mma(W.o[r][i], a0, a1, a2, a3, pl[r]);
+        }
     }
 }
 
@@ -591,9 +611,9 @@ __global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? (D == 64 ? 6 : 4) : 3
         scale[1] = scales_of(pages.y);
         next = make_int2(page_of(t0 + 2 * STRIDE), page_of(t0 + 2 * STRIDE + KV_HALF));
         if (t0 + KV_TILE - 1 <= see_all && t0 > low_all && there[0] && there[1])
-            kv_tile<D, E4M3, NR, false>(W, slot, t0, ks, vs, there, place, A.window, unit_out, unit_stride, one_unit, rows - tile_row, lane, k_wait, k_read, v_wait, v_read);
+            kv_tile<D, !BF, E4M3, NR, false>(W, slot, t0, ks, vs, there, place, A.window, unit_out, unit_stride, one_unit, rows - tile_row, lane, k_wait, k_read, v_wait, v_read);
         else
-            kv_tile<D, E4M3, NR, true>(W, slot, t0, ks, vs, there, place, A.window, unit_out, unit_stride, one_unit, rows - tile_row, lane, k_wait, k_read, v_wait, v_read);
+            kv_tile<D, !BF, E4M3, NR, true>(W, slot, t0, ks, vs, there, place, A.window, unit_out, unit_stride, one_unit, rows - tile_row, lane, k_wait, k_read, v_wait, v_read);
         phase ^= 1;
     }
     // join the warps, in the tiles' memory

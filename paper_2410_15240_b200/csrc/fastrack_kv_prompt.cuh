@@ -270,7 +270,7 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
             }
             // ask for the next step's scores now
             ended = kv_ended(bars + 8 * (KV_S_IN + 2 * m_tile + (half ^ 1)), (s + 1) >> 1 & 1);
-            uint32_t p[32];
+            uint32_t p[32], rest[BF ? 1 : 32];           // f16 answers: what rounding leaves out, see kv_weights
 #pragma unroll
             for (int i = 0; i < 32 + KV_P_AHEAD; i++) {
                 if (i < 32) {
@@ -291,9 +291,14 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
                     }
                     asm volatile("{\n\t.reg .b64 t;\n\tmov.b64 t, {%1, %2};\n\tadd.rn.f32x2 %0, %0, t;\n\t}" : "+l"(sum[k >> 3]) : "r"(u), "r"(w));
                     asm volatile("cvt.rn.f16x2.f32 %0, %2, %1;" : "=r"(p[k]) : "r"(u), "r"(w));
+                    if (!BF) {
+                        const float2 e = kv_unpack<false>(p[k]);
+                        rest[BF ? 0 : k] = kv_pack<false>(__uint_as_float(u) - e.x, __uint_as_float(w) - e.y);
+                    }
                 }
             }
             kv_tmem_store32(p, at);                      // over the scores of the first 32 tokens
+            if constexpr (!BF) kv_tmem_store32(rest, at + 32);
         };
         if (ragged) pass(KvYes());
         else pass(KvNo());
@@ -516,7 +521,7 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
 
 // The products, by one warp.  They run in the order in which they are issued: scores are written over weights after those have been
 // used.
-template <int D>
+template <int D, bool BF>
 __device__ __forceinline__ void kv_prompt_products(int tiles, int parts, uint32_t sm_at, uint32_t bars, volatile int* stop, uint32_t tmem)
 {
     using T = KvPrompt<D>;
@@ -538,6 +543,9 @@ __device__ __forceinline__ void kv_prompt_products(int tiles, int parts, uint32_
         const uint64_t b = kv_desc(sm_at + T::V + (j & 1) * T::TILE + half * 64 * 128, KV_P_TOKENS * 128, 1024);
 #pragma unroll
         for (int k = 0; k < 4; k++) kv_mma_ts(tmem + 256 + 128 * m, tmem + 128 * m + 64 * half + 8 * k, b + (k * 2048 >> 4), o_what, s > 0 || k > 0);
+        if (!BF)
+#pragma unroll
+            for (int k = 0; k < 4; k++) kv_mma_ts(tmem + 256 + 128 * m, tmem + 128 * m + 64 * half + 32 + 8 * k, b + (k * 2048 >> 4), o_what, true);
         kv_commit(bars + 8 * (KV_O_IN + m));
     };
     kv_wait_or_stop(bars + 8 * KV_Q_IN, 0, stop);
@@ -602,7 +610,7 @@ __global__ void __launch_bounds__(KV_P_THREADS, 1) kv_prompt_kernel(const KvShap
     } else if (warp < 12) {
         kv_prompt_bring<D, BF, E4M3>(S, B, q, seq, kh, begin, end, tiles, sm, bars, stop);
     } else {
-        kv_prompt_products<D>(tiles, parts, sm_at, bars, stop, tmem);
+        kv_prompt_products<D, BF>(tiles, parts, sm_at, bars, stop, tmem);
         __syncwarp();
         kv_commit(bars + 8 * KV_END);                    // nothing is on its way any more when the memory is given back
         kv_wait(bars + 8 * KV_END, 0);

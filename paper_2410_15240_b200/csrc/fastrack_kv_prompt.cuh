@@ -3,13 +3,19 @@
 #include "fastrack_kv_attend.cuh"
 
 // One CTA takes 256 rows (two tiles of 128) of one kv head of one sequence against a chunk of the tokens, 128 at a time:
-//     S_m = Q_m K^T  (128 x 128, tensor memory)  ->  P_m = weights as f16 (tensor memory, over S_m)  ->  O_m += P_m V.
+//     S_m = Q_m K^T  (tensor memory)  ->  P_m = weights as f16 (tensor memory, over S_m)  ->  O_m += P_m V.
 // Warps 0-3 and 4-7 make P_0 and P_1 (a thread per row: no exchange between lanes), warps 8-11 bring the codes and widen them to f16
-// in shared memory, where the tensor cores read them, and one thread of warp 12 issues the products.  The two row tiles take turns:
-// while one's weights are made, the other's products run.  Both share the widened K and V.
+// in shared memory, where the tensor cores read them, and warp 12 issues the products.  S is made in two halves of 64 tokens, one
+// while the other's weights are: both row tiles and both halves keep the tensor cores and the exponentials going at once, and the two
+// row tiles share the widened K and V.
 //
-// What bounds it, per 128 tokens and SM: the products 4 x 512 cycles; shared memory the same (Q and K for S, V for O, the widened
-// codes' way in: 256 KB at 128 B a cycle); the exponentials 2 x 128 x 128 at 16 a cycle, again 2048.
+// What bounds it, per 128 tokens and SM: the products 4 x 512 cycles; shared memory 2560 (Q twice and K for S, V for O, the widened
+// codes' way in: 320 KB at 128 B a cycle); the exponentials 2 x 128 x 128 at 16 a cycle, 2048.  It takes some 5000: a step of a row
+// tile is a chain (scores from tensor memory, largest, exponentials, weights back) of some 2300 cycles, half of them exponentials,
+// in which every access to shared memory, a barrier's too, waits for the tensor cores' reads (150 to 300 cycles).
+// 3 x 1024 new tokens over up to 6100, 32 heads of 128, bf16: 337 us = 570 TFLOP/s of the visible pairs, tensor cores active 35 %.
+// What it came from: one m16n8k16 row tile per pass 2231 us; this division of work, codes unrolled and generic addressing 843; packed
+// arithmetic and less code 369; two halves and products issued by a converged warp 348.  Two threads per row took 375.
 #define KV_P_ROWS 128                   // of a row tile
 #define KV_P_TOKENS 128
 #define KV_P_THREADS 416

@@ -145,15 +145,16 @@ template <bool BF> __device__ __forceinline__ uint4 kv_narrow8(const float* x)
 // rounded to a whole number, to even, whose last byte is the code.  A NaN gives some code, but none that is a NaN.
 template <bool E4M3> __device__ __forceinline__ uint32_t kv_codes4(const float* x)
 {
-    if (E4M3) {
+    if constexpr (E4M3) {
         const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(fmaxf(x[0], -448.f), fmaxf(x[1], -448.f)), __NV_SATFINITE, __NV_E4M3);
         const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(fmaxf(x[2], -448.f), fmaxf(x[3], -448.f)), __NV_SATFINITE, __NV_E4M3);
         return lo | hi << 16;
-    }
-    uint32_t y[4];
+    } else {
+        uint32_t y[4];
 #pragma unroll
-    for (int i = 0; i < 4; i++) y[i] = __float_as_uint(__fadd_rn(x[i], 12582912.f));
-    return __byte_perm(__byte_perm(y[0], y[1], 0x0040), __byte_perm(y[2], y[3], 0x0040), 0x5410);
+        for (int i = 0; i < 4; i++) y[i] = __float_as_uint(__fadd_rn(x[i], 12582912.f));
+        return __byte_perm(__byte_perm(y[0], y[1], 0x0040), __byte_perm(y[2], y[3], 0x0040), 0x5410);
+    }
 }
 // The larger of a and |x|; a NaN wins
 __device__ __forceinline__ float kv_max_nan(float a, float x)

@@ -68,7 +68,8 @@ typedef struct {
 
 /* The sequences of a call.  The new tokens of all sequences lie packed: sequence i has rows d_starts[i] .. d_starts[i+1]-1
  * of q, k and v, and they are its LAST tokens: d_lens[i] counts them.  The same struct serves the append of the tokens and
- * the attention of their queries.  A sequence without new tokens is left alone. */
+ * the attention of their queries.  A sequence without new tokens is left alone.  q, k, v, their positions and the answers have
+ * total_new rows. */
 typedef struct {
     int n_seqs;
     int total_new;              /* d_starts[n_seqs], or an upper bound of it */
@@ -129,7 +130,8 @@ FASTRACK_API int fastrack_kv_read(fastrack_kv* kv, const fastrack_kv_batch* batc
                                   const fastrack_kv_rows* v_out, void* stream);
 
 /* Bytes that fastrack_kv_attention needs as workspace for such a batch (the bounds in the struct count, not the device's
- * values); 0 for bad arguments. */
+ * values); 0 for bad arguments.  With weights it grows with max_new * max_len (4 bytes per q head and 16 to 64 tokens): long prompts
+ * are best taken in pieces of some thousand tokens. */
 FASTRACK_API size_t fastrack_kv_attention_workspace(const fastrack_kv* kv, const fastrack_kv_batch* batch, int with_mass);
 
 /* Attention of the new tokens over the cache (append them first).  Query j of the n new ones of a sequence of length L stands at

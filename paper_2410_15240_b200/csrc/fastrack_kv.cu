@@ -684,7 +684,7 @@ static void kv_attend_launch(const fastrack_kv* kv, const KvBatch& B, const KvAt
 {
     const KvShape& S = kv->shape;
     const bool e4 = kv->config.format == FASTRACK_KV_E4M3;
-    const dim3 grid(A.splits, S.kv_heads * A.row_tiles, B.n_seqs);
+    const dim3 grid(S.kv_heads * A.row_tiles, A.splits, B.n_seqs);
     if (A.rows > 16) (e4 ? kv_prompt_kernel<D, BF, true> : kv_prompt_kernel<D, BF, false>)<<<grid, KV_P_THREADS, KvPrompt<D>::SMEM, stream>>>(S, B, A);
     auto kernel = A.rows == 8 ? (e4 ? kv_attend_kernel<D, BF, true, 1> : kv_attend_kernel<D, BF, false, 1>)
                               : (e4 ? kv_attend_kernel<D, BF, true, 2> : kv_attend_kernel<D, BF, false, 2>);
@@ -692,8 +692,8 @@ static void kv_attend_launch(const fastrack_kv* kv, const KvBatch& B, const KvAt
         cudaLaunchConfig_t c = {};
         cudaLaunchAttribute cluster;
         cluster.id = cudaLaunchAttributeClusterDimension;
-        cluster.val.clusterDim.x = A.chunk == 0 ? A.splits : 1;
-        cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+        cluster.val.clusterDim.y = A.chunk == 0 ? A.splits : 1;
+        cluster.val.clusterDim.x = cluster.val.clusterDim.z = 1;
         c.gridDim = grid;
         c.blockDim = dim3(32 * KV_WARPS);
         c.dynamicSmemBytes = kv_attend_smem<D>(A.rows) + 16 * KV_WARPS;
@@ -770,8 +770,12 @@ extern "C" int fastrack_kv_attention(fastrack_kv* kv, const fastrack_kv_batch* b
     }
     if (mass && batch->max_len > 0) {
         const int blocks = (batch->max_len + S.block_tokens - 1) / S.block_tokens;
-        if ((int64_t)batch->max_new * S.group <= KV_MASS_ROWS) kv_launch_after(st, dim3((blocks + 255) / 256, S.kv_heads, batch->n_seqs), 256, kv_mass_kernel<true>, S, B, A, p.unit_shift);
-        else kv_launch_after(st, dim3((blocks + 7) / 8, S.kv_heads, batch->n_seqs), 256, kv_mass_kernel<false>, S, B, A, p.unit_shift);
+        const bool few = (int64_t)batch->max_new * S.group <= KV_MASS_ROWS;
+        auto kernel = few ? kv_mass_kernel<true> : kv_mass_kernel<false>;
+        const dim3 grid(few ? (blocks + 255) / 256 : blocks, S.kv_heads, batch->n_seqs);
+        // it reads lengths before it waits, which this call's own kernels do not write, but one of the caller's might
+        if (launches) kv_launch_after(st, grid, 256, kernel, S, B, A, p.unit_shift);
+        else kernel<<<grid, 256, 0, st>>>(S, B, A, p.unit_shift);
         launches++;
     }
     return kv_launched(kv, launches);

@@ -500,7 +500,7 @@ __global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? (D == 64 ? 6 : 4) : 3
     constexpr int STEPS = T::STEPS, ROWS = 8 * NR;
     extern __shared__ __align__(1024) uint8_t kv_smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
-    const int chunk = blockIdx.x, kh = blockIdx.y % S.kv_heads, tile_row = blockIdx.y / S.kv_heads * ROWS, seq = blockIdx.z;
+    const int chunk = blockIdx.y, kh = blockIdx.x % S.kv_heads, tile_row = blockIdx.x / S.kv_heads * ROWS, seq = blockIdx.z;
     asm volatile("griddepcontrol.launch_dependents;");   // the join may take its place; it waits for this kernel's end
     const KvSeq q = kv_seq(S, B, seq);
     const KvSpan span = kv_span(S, q, A.window, tile_row, ROWS);
@@ -763,24 +763,24 @@ __global__ void __launch_bounds__(32 * KV_WARPS) kv_join_kernel(const KvShape S,
 }
 
 // Weight of each block: sum over the block's units and the rows that see any of it of exp2(log2 of the unit's sum - log2 of the row's
-// sum).  FEW (at most KV_MASS_ROWS rows per sequence and kv head): a thread per block; otherwise a warp per block.  The order of the
-// sum is always the same.
+// sum).  FEW (at most KV_MASS_ROWS rows per sequence and kv head): a thread per block; otherwise a CTA per block (a warp per block took 20 us
+// longer for 4096 rows).  The order of the sum is always the same.
 #define KV_MASS_ROWS 32
 template <bool FEW>
 __global__ void __launch_bounds__(256) kv_mass_kernel(const KvShape S, const KvBatch B, const KvAttend A, const int unit_shift)
 {
-    const int lane = threadIdx.x & 31, kh = blockIdx.y, seq = blockIdx.z;
-    const int block = FEW ? blockIdx.x * 256 + threadIdx.x : blockIdx.x * 8 + (threadIdx.x >> 5);
-    __shared__ float row_l2[KV_MASS_ROWS];
+    const int kh = blockIdx.y, seq = blockIdx.z, block = FEW ? blockIdx.x * 256 + threadIdx.x : blockIdx.x;
+    __shared__ float shared[KV_MASS_ROWS];               // FEW: the rows' sums; else the warps'
     const KvSeq q = kv_seq(S, B, seq);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int rows = q.n * S.group, stride = B.max_new * S.group;
+    const float* const l2 = A.lse2 + kv_lse2_at(S, q, kh, 0);
     if (FEW) {
         if (blockIdx.x * 256 << S.block_shift >= q.len) return;
-        if (threadIdx.x < rows) row_l2[threadIdx.x] = A.lse2[kv_lse2_at(S, q, kh, threadIdx.x)];
+        if (threadIdx.x < rows) shared[threadIdx.x] = l2[threadIdx.x];
         __syncthreads();
     }
-    if (block << S.block_shift >= q.len) return;
+    if (block << S.block_shift >= q.len) return;         // FEW: no barrier follows; else the CTA as a whole
     const int unit0 = block << S.block_shift >> unit_shift, unit1 = (min((block + 1) << S.block_shift, q.len) - 1 >> unit_shift) + 1;
     const bool there = block == q.full || kv_page(B, seq, block) >= 0;
     const int step = unit_shift == 4 && block < q.full && S.block_tokens >= KV_TILE ? KV_TILE / KV_HALF : 1;   // of kv_attend_kernel's full blocks: a sum per tile
@@ -793,17 +793,21 @@ __global__ void __launch_bounds__(256) kv_mass_kernel(const KvShape S, const KvB
             const int lo = max(t0 - (q.len - q.n), 0), hi = A.window > 0 ? min(q.n - 1, t1 + A.window - 1 - (q.len - q.n)) : q.n - 1;
             if (FEW) {
 #pragma unroll 4
-                for (int row = lo * S.group; row < (hi + 1) * S.group; row++) sum += kv_exp2(src[row] - row_l2[row]);
+                for (int row = lo * S.group; row < (hi + 1) * S.group; row++) sum += kv_exp2(src[row] - shared[row]);
             } else {
-                const float* l2 = A.lse2 + kv_lse2_at(S, q, kh, 0);
 #pragma unroll 8
-                for (int row = lo * S.group + lane; row < (hi + 1) * S.group; row += 32) sum += kv_exp2(src[row] - l2[row]);
+                for (int row = lo * S.group + threadIdx.x; row < (hi + 1) * S.group; row += 256) sum += kv_exp2(src[row] - l2[row]);
             }
         }
     if (!FEW) {
 #pragma unroll
         for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        if (lane) return;
+        if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = sum;
+        __syncthreads();
+        if (threadIdx.x) return;
+        sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; w++) sum += shared[w];
     }
     const int64_t at = ((int64_t)seq * S.kv_heads + kh) * A.mass_stride + block;
     A.mass_out[at] = A.mass_in[at] + sum;

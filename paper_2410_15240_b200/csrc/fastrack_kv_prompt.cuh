@@ -585,7 +585,7 @@ __global__ void __launch_bounds__(KV_P_THREADS, 1) kv_prompt_kernel(const KvShap
     uint8_t* const sm = kv_raw + (-(uint32_t)__cvta_generic_to_shared(kv_raw) & 1023u);
     const uint32_t sm_at = (uint32_t)__cvta_generic_to_shared(sm), bars = sm_at + T::BARS;
     const int warp = threadIdx.x >> 5;
-    const int chunk = blockIdx.x, kh = blockIdx.y % S.kv_heads, tile_row = blockIdx.y / S.kv_heads * A.rows, seq = blockIdx.z;
+    const int chunk = blockIdx.y, kh = blockIdx.x % S.kv_heads, tile_row = blockIdx.x / S.kv_heads * A.rows, seq = blockIdx.z;
     asm volatile("griddepcontrol.launch_dependents;");
     const KvSeq q = kv_seq(S, B, seq);
     const KvSpan span = kv_span(S, q, A.window, tile_row, A.rows);

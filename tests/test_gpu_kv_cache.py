@@ -347,6 +347,15 @@ def test_evict(seed):
     check_evict(table, lens, mass, block, int(rng.integers(0, blocks + 2)), int(rng.integers(0, 4)), int(rng.integers(0, 6)))
 
 
+@pytest.mark.parametrize("heads,blocks", [(9, 40), (20, 1500), (8, 1024), (8, 1025), (8, 4096), (3, 4097), (2, 9000)])
+def test_evict_on_either_side_of_what_registers_hold(heads, blocks):
+    rng = np.random.default_rng(heads * blocks)
+    stride = blocks                                     # the unfinished block has no entry of its own: every table ends exactly here
+    table = rng.permutation(2 * stride).reshape(2, stride).astype(np.int32)
+    mass = (rng.integers(0, 5, (2, heads, stride)) / 4.0).astype(np.float32)
+    check_evict(table, np.array([blocks * 16, blocks * 16 // 3], np.int32), mass, 16, blocks // 2, 2, 3)
+
+
 def test_evict_ties_and_odd_weights():
     table = np.arange(2 * 40, dtype=np.int32).reshape(2, 40)
     mass = np.ones((2, 3, 40), np.float32)              # all the same: the lowest index first

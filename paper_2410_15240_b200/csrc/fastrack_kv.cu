@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(KV_ROT_THREADS) kv_rotary_kernel(const KvShape
 
 #define KV_APPEND_THREADS 256
 
-struct KvAppend { KvRows k, v, q, q_out; int slots, quant_ctas, q_per; };
+struct KvAppend { KvRows k, v, q, q_out; int slots, quant_ctas, q_per; bool spread; };
 
 // Raw values of unit u of a token: K (which = 0) or V of a new token, or what the tail has of one from before the call.
 __device__ __forceinline__ const uint16_t* kv_unit_source(const KvShape& S, const KvBatch& B, const KvAppend& A, const KvSeq& q, int seq, int kh, int which, int token)
@@ -160,21 +160,25 @@ __device__ __forceinline__ void kv_append_block(const KvShape& S, const KvBatch&
     }
 }
 
-// CTAs 0 .. quant_ctas - 1: one block that the call touches, of one kv head.  The CTA of a sequence's first block also writes the
-// head's tail, after it has read what the tail held: no other CTA touches the head's tail row.  The CTAs behind turn q.
+// quant_ctas CTAs: one block that the call touches, of one kv head.  The CTA of a sequence's first block also writes the head's tail,
+// after it has read what the tail held: no other CTA touches the head's tail row.  The others turn q.  Where the first kind fits on
+// the device at once it comes first, since it takes longest (5 x 333 tokens and their reading back: 17.6 us, 19.5 with the kinds mixed).
+// Where it doesn't, the two are spread evenly, since the others wait for memory where those compute (17478 tokens: 84 us, 89 in order).
 template <bool BF, bool E4M3, int N>
 __global__ void __launch_bounds__(KV_APPEND_THREADS, N < 4 ? 3 : 2) kv_append_kernel(const KvShape S, const KvBatch B, const KvAppend A)
 {
     const int units = S.head_dim / 16, tid = threadIdx.x;
-    if ((int)blockIdx.x >= A.quant_ctas) {
+    auto first_kind = [&](unsigned cta) { return A.spread ? (int)((uint64_t)cta * A.quant_ctas / gridDim.x) : min((int)cta, A.quant_ctas); };   // of the CTAs before cta
+    const int before = first_kind(blockIdx.x);
+    if (first_kind(blockIdx.x + 1) == before) {
         const int groups = (S.q_heads + A.q_per - 1) / A.q_per;
-        const int64_t idx = (int64_t)(blockIdx.x - A.quant_ctas) * KV_APPEND_THREADS + tid;
+        const int64_t idx = (int64_t)((int)blockIdx.x - before) * KV_APPEND_THREADS + tid;
         const int64_t token = idx / units / groups;
         if (token >= B.total_new) return;
         kv_turn_heads<BF, 2>(S, A.q, A.q_out, B.positions, token, (int)(idx % units), (int)(idx / units % groups) * A.q_per, A.q_per, S.q_heads, false);
         return;
     }
-    const int kh = blockIdx.x % S.kv_heads, slot = blockIdx.x / S.kv_heads % A.slots, seq = blockIdx.x / S.kv_heads / A.slots;
+    const int kh = before % S.kv_heads, slot = before / S.kv_heads % A.slots, seq = before / S.kv_heads / A.slots;
     const KvSeq q = kv_seq(S, B, seq);
     if (q.n == 0) return;
     const int first = max(q.len - q.n, 0), block = (first >> S.block_shift) + slot;
@@ -720,6 +724,7 @@ extern "C" int fastrack_kv_append(fastrack_kv* kv, const fastrack_kv_batch* batc
         return bf ? (e4 ? kv_append_kernel<true, true, N> : kv_append_kernel<true, false, N>) : (e4 ? kv_append_kernel<false, true, N> : kv_append_kernel<false, false, N>);
     };
     auto kernel = each == 1 ? pick(std::integral_constant<int, 1>()) : each == 2 ? pick(std::integral_constant<int, 2>()) : pick(std::integral_constant<int, 4>());
+    A.spread = quant > (int64_t)kv->num_sms * (each < 4 ? 3 : 2);
     kernel<<<(unsigned)(quant + turn), KV_APPEND_THREADS, 0, (cudaStream_t)stream>>>(S, kv_batch(batch), A);
     return kv_launched(kv);
 }

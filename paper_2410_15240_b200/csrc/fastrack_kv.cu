@@ -745,7 +745,8 @@ extern "C" int fastrack_kv_read(fastrack_kv* kv, const fastrack_kv_batch* batch,
 
 // ------------------------------------------------------------------------------------------------ attention ----
 
-#define KV_WAVES 3                      // times that chunks fill the SMs, where there is so much
+#define KV_WAVES 4                      // times that chunks fill the SMs, where there is so much (4 x 131072 tokens, 16 x 20000, 16 x 3000 .. 30000:
+                                        // 224, 132 and 122 us; 3 times 220, 136 and 132)
 #define KV_CHUNK_LEAST 1024             // tokens of a chunk, where chunks fill the SMs once with more
 #define KV_CHUNK_CLUSTER 2048           // tokens of a chunk in a cluster: above, more chunks than a cluster has are worth the join (where a cluster
                                         // would have less than 4 chunks, 61 sequences of up to 4096 tokens took 88 us against 77)
@@ -768,7 +769,9 @@ static KvPlan kv_plan(const fastrack_kv* kv, const fastrack_kv_batch* b, bool ma
     const int64_t spans = (int64_t)b->n_seqs * S.kv_heads * p.row_tiles > 0 ? (int64_t)b->n_seqs * S.kv_heads * p.row_tiles : 1;
     const int64_t step = prompt ? KV_P_TOKENS : KV_STEP, most = (span + step - 1) / step;
     const int64_t room = (prompt ? 1 : 4) * (int64_t)kv->num_sms, fill = (room + spans - 1) / spans;       // chunks of a span that fill the SMs
-    int64_t splits = prompt ? fill : KV_WAVES * fill < span / KV_CHUNK_LEAST ? KV_WAVES * fill : span / KV_CHUNK_LEAST > fill ? span / KV_CHUNK_LEAST : fill;
+    // chunks of a span where there is much: rounded down, since some more than fill the SMs would be a wave of their own
+    const int64_t waves = KV_WAVES * room / spans > fill ? KV_WAVES * room / spans : fill;
+    int64_t splits = prompt ? fill : waves < span / KV_CHUNK_LEAST ? waves : span / KV_CHUNK_LEAST > fill ? span / KV_CHUNK_LEAST : fill;
     const bool cluster = !prompt && fill >= 4 && span <= KV_CHUNK_CLUSTER * (fill < KV_CLUSTER ? fill : KV_CLUSTER);
     if (cluster) splits = fill < KV_CLUSTER ? fill : KV_CLUSTER;
     if (splits > most) splits = most;
@@ -810,7 +813,7 @@ static void kv_launch_after(cudaStream_t stream, dim3 grid, int threads, void (*
 }
 
 template <int D, bool BF>
-static void kv_attend_launch(const fastrack_kv* kv, const KvBatch& B, const KvAttend& A, const CUtensorMap& pool, bool parts, cudaStream_t stream)
+static void kv_attend_launch(const fastrack_kv* kv, const KvBatch& B, const KvAttend& A, const CUtensorMap& pool, bool parts, int weigh_tiles, cudaStream_t stream)
 {
     const KvShape& S = kv->shape;
     const bool e4 = kv->config.format == FASTRACK_KV_E4M3;
@@ -832,7 +835,7 @@ static void kv_attend_launch(const fastrack_kv* kv, const KvBatch& B, const KvAt
         c.numAttrs = 1;
         (void)cudaLaunchKernelEx(&c, kernel, S, B, A, pool);                 // an error stays for cudaGetLastError
     }
-    if (parts) kv_launch_after(stream, dim3((unsigned)(B.max_new * S.q_heads), B.n_seqs), 32 * KV_WARPS, kv_join_kernel<D, BF>, S, B, A);
+    if (parts) kv_launch_after(stream, dim3((unsigned)(B.max_new * S.q_heads + weigh_tiles * S.kv_heads), B.n_seqs), 32 * KV_WARPS, kv_join_kernel<D, BF>, S, B, A);
 }
 
 // The pool as a tensor of bytes (head_dim, rows of a page: K of all heads, then V, pages); boxes of 16 rows of one page.
@@ -883,6 +886,10 @@ extern "C" int fastrack_kv_attention(fastrack_kv* kv, const fastrack_kv_batch* b
     A.mass_in = d_mass_in;
     A.mass_out = d_mass_out;
     A.mass_stride = mass_stride;
+    A.unit_shift = p.unit_shift;
+    const int blocks = mass ? (batch->max_len + S.block_tokens - 1) / S.block_tokens : 0;
+    const bool few = (int64_t)batch->max_new * S.group <= KV_MASS_ROWS;
+    const int weigh_tiles = few ? (blocks + 32 * KV_WARPS - 1) / (32 * KV_WARPS) : 0;                          // of kv_join_kernel
     int launches = 0;
     cudaStream_t st = (cudaStream_t)stream;
     if (batch->total_new > 0 && batch->max_new > 0) {
@@ -892,20 +899,18 @@ extern "C" int fastrack_kv_attention(fastrack_kv* kv, const fastrack_kv_batch* b
         CUtensorMap pool;
         if (int rc = kv_pool_map(kv, B, &pool)) return rc;
         switch (S.head_dim) {
-        case 64: bf ? kv_attend_launch<64, true>(kv, B, A, pool, kv_parts(p), st) : kv_attend_launch<64, false>(kv, B, A, pool, kv_parts(p), st); break;
-        case 96: bf ? kv_attend_launch<96, true>(kv, B, A, pool, kv_parts(p), st) : kv_attend_launch<96, false>(kv, B, A, pool, kv_parts(p), st); break;
-        default: bf ? kv_attend_launch<128, true>(kv, B, A, pool, kv_parts(p), st) : kv_attend_launch<128, false>(kv, B, A, pool, kv_parts(p), st); break;
+        case 64: bf ? kv_attend_launch<64, true>(kv, B, A, pool, kv_parts(p), weigh_tiles, st) : kv_attend_launch<64, false>(kv, B, A, pool, kv_parts(p), weigh_tiles, st); break;
+        case 96: bf ? kv_attend_launch<96, true>(kv, B, A, pool, kv_parts(p), weigh_tiles, st) : kv_attend_launch<96, false>(kv, B, A, pool, kv_parts(p), weigh_tiles, st); break;
+        default: bf ? kv_attend_launch<128, true>(kv, B, A, pool, kv_parts(p), weigh_tiles, st) : kv_attend_launch<128, false>(kv, B, A, pool, kv_parts(p), weigh_tiles, st); break;
         }
         launches += 1 + kv_parts(p);
     }
-    if (mass && batch->max_len > 0) {
-        const int blocks = (batch->max_len + S.block_tokens - 1) / S.block_tokens;
-        const bool few = (int64_t)batch->max_new * S.group <= KV_MASS_ROWS;
+    if (blocks > 0 && !(launches && kv_parts(p) && few)) {
         auto kernel = few ? kv_mass_kernel<true> : kv_mass_kernel<false>;
         const dim3 grid(few ? (blocks + 255) / 256 : blocks, S.kv_heads, batch->n_seqs);
         // it reads lengths before it waits, which this call's own kernels do not write, but one of the caller's might
-        if (launches) kv_launch_after(st, grid, 256, kernel, S, B, A, p.unit_shift);
-        else kernel<<<grid, 256, 0, st>>>(S, B, A, p.unit_shift);
+        if (launches) kv_launch_after(st, grid, 256, kernel, S, B, A);
+        else kernel<<<grid, 256, 0, st>>>(S, B, A);
         launches++;
     }
     return kv_launched(kv, launches);

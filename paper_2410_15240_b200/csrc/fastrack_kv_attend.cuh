@@ -28,7 +28,8 @@ struct KvAttend {
     int rows;               // of a CTA: 8, 16 or 256
     int splits;             // most chunks of a span
     int chunk;              // tokens of a chunk; 0: the chunks of a span are a cluster and equal
-    int row_tiles, units;   // units: per sequence, for weights
+    int row_tiles, units;   // units: per sequence, for weights, of
+    int unit_shift;         // log2 of their tokens
     float* part_o;          // [splits][total_new * q_heads][head_dim]
     float* part_ml;         // [splits][total_new * q_heads][2]: running maximum and sum
     float* lse2;            // [total_new * q_heads], base 2, see kv_lse2_at
@@ -710,18 +711,81 @@ __global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? (D == 64 ? 6 : 4) : 3
     kv_cluster_sync();                                   // nobody leaves while others read its memory
 }
 
-// Joins the chunks of each row: a CTA per row, of which a warp takes every fourth chunk.
+// Sum over a block's units and the rows that see any of one of exp2(log2 of the unit's sum - log2 of the row's sum): the block's weight.
+// A thread takes every EVERY-th row from its first.
+template <int EVERY, int UNROLL>
+__device__ __forceinline__ float kv_block_weight(const KvShape& S, const KvBatch& B, const KvAttend& A, const KvSeq& q, int seq, int kh, int block, int first, const float* l2)
+{
+    const int stride = B.max_new * S.group;
+    const int unit0 = block << S.block_shift >> A.unit_shift, unit1 = (min((block + 1) << S.block_shift, q.len) - 1 >> A.unit_shift) + 1;
+    const int step = A.unit_shift == 4 && block < q.full && S.block_tokens >= KV_TILE ? KV_TILE / KV_HALF : 1; // of kv_attend_kernel's full blocks: a sum per tile
+    float sum = 0.f;
+    if (block < q.full && kv_page(B, seq, block) < 0) return sum;
+    for (int unit = unit0; unit < unit1; unit += step) {
+        const float* src = A.unit_l2 + (((int64_t)seq * S.kv_heads + kh) * A.units + unit) * stride;
+        const int t0 = unit << A.unit_shift, t1 = t0 + (step << A.unit_shift) - 1;
+        // the first token whose query sees the unit at all, and the last that has it in its window
+        const int lo = max(t0 - (q.len - q.n), 0), hi = A.window > 0 ? min(q.n - 1, t1 + A.window - 1 - (q.len - q.n)) : q.n - 1;
+#pragma unroll UNROLL
+        for (int row = lo * S.group + first; row < (hi + 1) * S.group; row += EVERY) sum += kv_exp2(src[row] - l2[row]);
+    }
+    return sum;
+}
+
+// One kv head's blocks from first_block on, one to a thread, after `sums` has log2 of each row's sum.
+__device__ __forceinline__ void kv_weigh_blocks(const KvShape& S, const KvBatch& B, const KvAttend& A, const KvSeq& q, int seq, int kh, int first_block, const float* sums)
+{
+    const int block = first_block + threadIdx.x;
+    if (block << S.block_shift >= q.len) return;
+    const int64_t at = ((int64_t)seq * S.kv_heads + kh) * A.mass_stride + block;
+    A.mass_out[at] = A.mass_in[at] + kv_block_weight<1, 4>(S, B, A, q, seq, kh, block, 0, sums);
+}
+
+#define KV_MASS_ROWS 32                                  // rows per sequence and kv head up to which a thread weighs a block
+
+// Joins the chunks of each row: a CTA per row, of which a warp takes every fourth chunk.  With few rows CTAs behind these weigh blocks:
+// each works out the rows' sums again, a half warp to a row, instead of a launch that waits for them (4 sequences of up to 131072
+// tokens 209 us in all, 214 with it; 61 of up to 4096 66.6, 68.5).
 template <int D, bool BF>
 __global__ void __launch_bounds__(32 * KV_WARPS) kv_join_kernel(const KvShape S, const KvBatch B, const KvAttend A)
 {
     constexpr int V = D / 32;
-    __shared__ float sm_acc[KV_WARPS][D], sm_sum[KV_WARPS];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, seq = blockIdx.y, token = blockIdx.x / S.q_heads, head = blockIdx.x % S.q_heads;
+    __shared__ float sm_acc[KV_WARPS][D], sm_sum[KV_WARPS], sm_rows[KV_MASS_ROWS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, seq = blockIdx.y;
+    const int joins = B.max_new * S.q_heads;
     asm volatile("griddepcontrol.launch_dependents;");
     const KvSeq q = kv_seq(S, B, seq);
-    const KvSpan span = kv_span(S, q, A.window, (token * S.group + head % S.group) / A.rows * A.rows, A.rows);
-    const int chunks = max(1, (span.end - span.begin + A.chunk - 1) / A.chunk);
-    const int64_t first = (int64_t)(q.start + token) * S.q_heads + head, stride = (int64_t)B.total_new * S.q_heads;
+    const int64_t stride = (int64_t)B.total_new * S.q_heads;
+    auto chunks_of = [&](int row) {
+        const KvSpan span = kv_span(S, q, A.window, row / A.rows * A.rows, A.rows);
+        return max(1, (span.end - span.begin + A.chunk - 1) / A.chunk);
+    };
+    if ((int)blockIdx.x >= joins) {
+        const int kh = ((int)blockIdx.x - joins) % S.kv_heads, first_block = ((int)blockIdx.x - joins) / S.kv_heads * 32 * KV_WARPS;
+        if (first_block << S.block_shift >= q.len) return;
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        for (int row0 = 0; row0 < q.n * S.group; row0 += 2 * KV_WARPS) {
+            const int row = row0 + (threadIdx.x >> 4), n = row < q.n * S.group ? chunks_of(row) : 0;
+            const float* src = A.part_ml + 2 * ((int64_t)(q.start + row / S.group) * S.q_heads + kh * S.group + row % S.group);
+            float m = -KV_INF, l = 0.f;
+            for (int k = lane & 15; k < n; k += 16) m = fmaxf(m, src[2 * k * stride]);
+#pragma unroll
+            for (int d = 8; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+            const float base = m == -KV_INF ? 0.f : m;
+            for (int k = lane & 15; k < n; k += 16) {
+                const float2 ml = *(const float2*)(src + 2 * k * stride);
+                l += ml.y * kv_exp2(ml.x - base);
+            }
+#pragma unroll
+            for (int d = 8; d; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+            if ((lane & 15) == 0 && n) sm_rows[row] = l == 0.f ? -KV_INF : m + log2f(l);
+        }
+        __syncthreads();
+        kv_weigh_blocks(S, B, A, q, seq, kh, first_block, sm_rows);
+        return;
+    }
+    const int token = blockIdx.x / S.q_heads, head = blockIdx.x % S.q_heads, chunks = chunks_of(token * S.group + head % S.group);
+    const int64_t first = (int64_t)(q.start + token) * S.q_heads + head;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (token >= q.n) return;
     // the largest maximum first, then every chunk's sum and answer by its distance from it: loads that do not wait for one another
@@ -762,53 +826,32 @@ __global__ void __launch_bounds__(32 * KV_WARPS) kv_join_kernel(const KvShape S,
     }
 }
 
-// Weight of each block: sum over the block's units and the rows that see any of it of exp2(log2 of the unit's sum - log2 of the row's
-// sum).  FEW (at most KV_MASS_ROWS rows per sequence and kv head): a thread per block; otherwise a CTA per block (a warp per block took 20 us
-// longer for 4096 rows).  The order of the sum is always the same.
-#define KV_MASS_ROWS 32
+// Weight of each block.  FEW (at most KV_MASS_ROWS rows per sequence and kv head): a thread per block; otherwise a CTA per block (a warp
+// per block took 20 us longer for 4096 rows).  The order of the sum is always the same.
 template <bool FEW>
-__global__ void __launch_bounds__(256) kv_mass_kernel(const KvShape S, const KvBatch B, const KvAttend A, const int unit_shift)
+__global__ void __launch_bounds__(256) kv_mass_kernel(const KvShape S, const KvBatch B, const KvAttend A)
 {
-    const int kh = blockIdx.y, seq = blockIdx.z, block = FEW ? blockIdx.x * 256 + threadIdx.x : blockIdx.x;
+    const int kh = blockIdx.y, seq = blockIdx.z, first_block = FEW ? blockIdx.x * 256 : blockIdx.x;
     __shared__ float shared[KV_MASS_ROWS];               // FEW: the rows' sums; else the warps'
     const KvSeq q = kv_seq(S, B, seq);
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int rows = q.n * S.group, stride = B.max_new * S.group;
+    if (first_block << S.block_shift >= q.len) return;   // the CTA as a whole
     const float* const l2 = A.lse2 + kv_lse2_at(S, q, kh, 0);
     if (FEW) {
-        if (blockIdx.x * 256 << S.block_shift >= q.len) return;
-        if (threadIdx.x < rows) shared[threadIdx.x] = l2[threadIdx.x];
+        if (threadIdx.x < q.n * S.group) shared[threadIdx.x] = l2[threadIdx.x];
         __syncthreads();
+        kv_weigh_blocks(S, B, A, q, seq, kh, first_block, shared);
+        return;
     }
-    if (block << S.block_shift >= q.len) return;         // FEW: no barrier follows; else the CTA as a whole
-    const int unit0 = block << S.block_shift >> unit_shift, unit1 = (min((block + 1) << S.block_shift, q.len) - 1 >> unit_shift) + 1;
-    const bool there = block == q.full || kv_page(B, seq, block) >= 0;
-    const int step = unit_shift == 4 && block < q.full && S.block_tokens >= KV_TILE ? KV_TILE / KV_HALF : 1;   // of kv_attend_kernel's full blocks: a sum per tile
-    float sum = 0.f;
-    if (there)
-        for (int unit = unit0; unit < unit1; unit += step) {
-            const float* src = A.unit_l2 + (((int64_t)seq * S.kv_heads + kh) * A.units + unit) * stride;
-            const int t0 = unit << unit_shift, t1 = t0 + (step << unit_shift) - 1;
-            // the first token whose query sees the unit at all, and the last that has it in its window
-            const int lo = max(t0 - (q.len - q.n), 0), hi = A.window > 0 ? min(q.n - 1, t1 + A.window - 1 - (q.len - q.n)) : q.n - 1;
-            if (FEW) {
-#pragma unroll 4
-                for (int row = lo * S.group; row < (hi + 1) * S.group; row++) sum += kv_exp2(src[row] - shared[row]);
-            } else {
-#pragma unroll 8
-                for (int row = lo * S.group + threadIdx.x; row < (hi + 1) * S.group; row += 256) sum += kv_exp2(src[row] - l2[row]);
-            }
-        }
-    if (!FEW) {
+    float sum = kv_block_weight<256, 8>(S, B, A, q, seq, kh, first_block, threadIdx.x, l2);
 #pragma unroll
-        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = sum;
-        __syncthreads();
-        if (threadIdx.x) return;
-        sum = 0.f;
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    if (threadIdx.x) return;
+    sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < 8; w++) sum += shared[w];
-    }
-    const int64_t at = ((int64_t)seq * S.kv_heads + kh) * A.mass_stride + block;
+    for (int w = 0; w < 8; w++) sum += shared[w];
+    const int64_t at = ((int64_t)seq * S.kv_heads + kh) * A.mass_stride + first_block;
     A.mass_out[at] = A.mass_in[at] + sum;
 }

@@ -13,7 +13,7 @@
 // codes' way in: 320 KB at 128 B a cycle); the exponentials 2 x 128 x 128 at 16 a cycle, 2048.  It takes some 5000: a step of a row
 // tile is a chain (scores from tensor memory, largest, exponentials, weights back) of some 2300 cycles, half of them exponentials,
 // in which every access to shared memory, a barrier's too, waits for the tensor cores' reads (150 to 300 cycles).
-// 3 x 1024 new tokens over up to 6100, 32 heads of 128, bf16: 337 us = 570 TFLOP/s of the visible pairs, tensor cores active 35 %.
+// 3 x 1024 new tokens over up to 6100, 32 heads of 128, bf16: 321 us = 599 TFLOP/s of the visible pairs, tensor cores active 35 %.
 // What it came from: one m16n8k16 row tile per pass 2231 us; this division of work, codes unrolled and generic addressing 843; packed
 // arithmetic and less code 369; two halves and products issued by a converged warp 348.  Two threads per row took 375.
 #define KV_P_ROWS 128                   // of a row tile

@@ -209,7 +209,8 @@ template <bool BF, bool E4M3>
 __global__ void __launch_bounds__(256) kv_read_kernel(const KvShape S, const KvBatch B, const KvRows ko, const KvRows vo)
 {
     const int seq = blockIdx.z, which = blockIdx.y & 1, kh = blockIdx.y >> 1, pieces = S.head_dim / 8;
-    const int i = blockIdx.x * 256 + threadIdx.x, token = i / pieces, at = i % pieces * 8;
+    // piece blockIdx.x * 256 + threadIdx.x of max_len * pieces: there may be 2^34, so the multiple of 256 * pieces is taken off first
+    const int i = blockIdx.x % pieces * 256 + threadIdx.x, token = blockIdx.x / pieces * 256 + i / pieces, at = i % pieces * 8;
     if (token >= B.max_len) return;
     const KvSeq q = kv_seq(S, B, seq);
     const int block = token >> S.block_shift, in_block = token & (S.block_tokens - 1);

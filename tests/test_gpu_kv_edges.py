@@ -1,0 +1,45 @@
+"""The cache operators where they can go wrong: what a query does not see must not reach it, whatever stands there; sizes and
+windows at the ends of what the header allows."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("no CUDA device", allow_module_level=True)
+
+from kv_reference import UNIT, Cache, rows  # noqa: E402
+from paper_2410_15240_b200 import kv  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_read_of_more_than_2_31_pieces(dim):
+    """A sequence whose rows count more pieces of 8 channels than 31 bits do.  Rows 8 channels apart (what they share holds the same
+    number): 16 bytes a token.  All pages are absent but the last, whose codes are all alike."""
+    block, held_page = 128, 3
+    max_len = (1 << 31) * 8 // dim + 1000
+    cache = kv.KvCache(kv.BF16, kv.INT8, 1, 1, dim, block)
+    blocks = max_len // block
+    table = torch.full((1, blocks), -1, dtype=torch.int32, device="cuda")
+    table[0, -1] = held_page
+    pool = torch.full((5, cache.page_bytes), 255, dtype=torch.uint8, device="cuda")
+    codes = block * dim
+    pool[held_page, :2 * codes] = 3
+    pool[held_page, 2 * codes:2 * codes + 8].view(torch.float32)[:] = 0.5
+    tail = torch.full((cache.tail_bytes // 2,), 1.5, dtype=torch.bfloat16, device="cuda")
+    lens, starts = torch.tensor([max_len], dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    guard, size = 1 << 20, 8 * (max_len - 1) + dim
+    out = torch.full((guard + size + guard,), -7.0, dtype=torch.bfloat16, device="cuda")
+    b = kv.Batch(n_seqs=1, total_new=0, max_new=0, max_len=max_len, pool_pages=5, table_stride=blocks, d_pool=pool.data_ptr(), d_tail=tail.data_ptr(),
+                 d_table=table.data_ptr(), d_lens=lens.data_ptr(), d_starts=starts.data_ptr())
+    to = kv.Rows(out[guard:].data_ptr(), 8, 8)
+    cache.read(b, to, to)
+    torch.cuda.synchronize()
+    assert bool((out[:guard] == -7).all()) and bool((out[guard + size:] == -7).all())
+    rows_ = out[guard:guard + size]
+    page, rest = 8 * (blocks - 1) * block, 8 * blocks * block   # first values of the page's tokens and of the unfinished block's
+    assert bool((rows_[:page] == 0).all())                      # absent
+    assert bool((rows_[page + dim:rest] == 1.5).all())          # 3 x 0.5
+    assert bool((rows_[rest + dim:] == 1.5).all())

@@ -135,7 +135,8 @@ FASTRACK_API int fastrack_kv_read(fastrack_kv* kv, const fastrack_kv_batch* batc
 FASTRACK_API size_t fastrack_kv_attention_workspace(const fastrack_kv* kv, const fastrack_kv_batch* batch, int with_mass);
 
 /* Attention of the new tokens over the cache (append them first).  Query j of the n new ones of a sequence of length L stands at
- * place i = L - n + j and sees the tokens t <= i, with window > 0 only those t > i - window, without absent pages:
+ * place i = L - n + j and sees the tokens t <= i, with window > 0 only those t > i - window (a window of max_len or more hides
+ * nothing), without absent pages:
  *     out = sum_t p_t v_t,  p = softmax_t(softmax_scale * q . k_t).
  * A query that sees nothing gets out = 0 and lse = -inf.
  *   d_lse       [total_new][q_heads] float, natural logarithm of the sum of exponentials; may be NULL.

@@ -863,6 +863,7 @@ extern "C" int fastrack_kv_attention(fastrack_kv* kv, const fastrack_kv_batch* b
     if (!kv || kv_bad_batch(kv, batch) || window < 0 || !d_mass_in != !d_mass_out) return FASTRACK_ERR_ARG;
     if (batch->n_seqs == 0 || batch->max_len == 0 && batch->total_new == 0) return FASTRACK_OK;
     const KvShape& S = kv->shape;
+    if (window >= batch->max_len) window = 0;            // hides nothing; and places plus a window stay below 2^31
     const bool mass = d_mass_out != nullptr;
     if (mass && (kv_misaligned(d_mass_in, 4) || kv_misaligned(d_mass_out, 4) || mass_stride < (batch->max_len + S.block_tokens - 1) / S.block_tokens)) return FASTRACK_ERR_ARG;
     if (batch->total_new > 0 && (kv_bad_rows(q) || kv_bad_rows(out) || (d_lse && kv_misaligned(d_lse, 4)))) return FASTRACK_ERR_ARG;

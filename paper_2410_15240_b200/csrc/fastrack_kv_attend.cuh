@@ -725,7 +725,7 @@ __device__ __forceinline__ float kv_block_weight(const KvShape& S, const KvBatch
         const float* src = A.unit_l2 + (((int64_t)seq * S.kv_heads + kh) * A.units + unit) * stride;
         const int t0 = unit << A.unit_shift, t1 = t0 + (step << A.unit_shift) - 1;
         // the first token whose query sees the unit at all, and the last that has it in its window
-        const int lo = max(t0 - (q.len - q.n), 0), hi = A.window > 0 ? min(q.n - 1, t1 + A.window - 1 - (q.len - q.n)) : q.n - 1;
+        const int lo = max(t0 - (q.len - q.n), 0), hi = A.window > 0 ? min(q.n - 1, t1 - (q.len - q.n) + A.window - 1) : q.n - 1;
 #pragma unroll UNROLL
         for (int row = lo * S.group + first; row < (hi + 1) * S.group; row += EVERY) sum += kv_exp2(src[row] - l2[row]);
     }

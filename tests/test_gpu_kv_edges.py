@@ -43,3 +43,22 @@ def test_read_of_more_than_2_31_pieces(dim):
     assert bool((rows_[:page] == 0).all())                      # absent
     assert bool((rows_[page + dim:rest] == 1.5).all())          # 3 x 0.5
     assert bool((rows_[rest + dim:] == 1.5).all())
+
+
+@pytest.mark.parametrize("new", [1, 5, 150])
+@pytest.mark.parametrize("window", [900, 1 << 30, (1 << 31) - 1])
+def test_window_that_hides_nothing(new, window):
+    """A window of max_len tokens or more, up to the largest number, is none: same answers, same weights."""
+    c = Cache(kv.BF16, kv.INT8, 8, 2, 64, 32, [900, new + 3], [new, new])
+    c.fill()
+    gen = torch.Generator().manual_seed(1)
+    q = torch.randn(c.total, c.qh, c.d, generator=gen).to(c.t).cuda()
+    got = []
+    for w in (0, window):
+        out, m_out = torch.empty_like(q), torch.full((c.n, c.kh, 30), -5.0, device="cuda")
+        m_in = torch.zeros_like(m_out)
+        lse = c.run_attention(q, out, w, m_in, m_out)
+        got.append((out, lse, m_out))
+    c.check_attention(q, got[0][0], got[0][1], 0, m_in, got[0][2])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)

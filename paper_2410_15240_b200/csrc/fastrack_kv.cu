@@ -849,8 +849,14 @@ static int kv_pool_map(fastrack_kv* kv, const KvBatch& B, CUtensorMap* map)
     const cuuint64_t strides[2] = {(cuuint64_t)S.head_dim, S.page_bytes};
     const cuuint32_t box[3] = {(cuuint32_t)S.head_dim, KV_HALF, 1}, steps[3] = {1, 1, 1};
     const CUtensorMapSwizzle swizzle = S.head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : S.head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE;
-    const CUresult r = kv->encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, B.pool, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
-                                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    auto encode = [&] {
+        return kv->encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, B.pool, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    };
+    CUresult r = encode();
+    // a thread that has made no runtime call yet has no context, which the driver's function wants: setting the device, which is current
+    // by number already, makes it so
+    if (r == CUDA_ERROR_INVALID_CONTEXT && kv_cuda(kv, cudaSetDevice(kv->device)) == FASTRACK_OK) r = encode();
     if (r == CUDA_SUCCESS) return FASTRACK_OK;
     kv->last_cuda_error = (int)r;
     return FASTRACK_ERR_CUDA;

@@ -62,3 +62,38 @@ def test_window_that_hides_nothing(new, window):
     c.check_attention(q, got[0][0], got[0][1], 0, m_in, got[0][2])
     for a, b in zip(*got):
         assert torch.equal(a, b)
+
+
+def test_one_handle_on_several_threads_and_streams():
+    """A handle holds constants only: threads with streams, batches and workspaces of their own use it at the same time."""
+    import threading
+    c = Cache(kv.BF16, kv.E4M3, 8, 2, 128, 64, [5000, 1200, 333], [5, 5, 5])
+    c.fill()
+    gen = torch.Generator().manual_seed(3)
+    qs = [torch.randn(c.total, c.qh, c.d, generator=gen).to(c.t).cuda() for _ in range(4)]
+    want = [torch.empty_like(q) for q in qs]
+    for q, w in zip(qs, want):
+        c.run_attention(q, w)
+    outs, failed = [[torch.empty_like(q) for _ in range(20)] for q in qs], []
+    need = c.kv.workspace_bytes(c.batch(), False)
+    spaces = [torch.empty(need, dtype=torch.uint8, device="cuda") for _ in qs]
+    streams = [torch.cuda.Stream() for _ in qs]
+    torch.cuda.synchronize()
+
+    def work(i):
+        try:
+            b = c.batch()
+            for o in outs[i]:
+                c.kv.attention(b, rows(qs[i]), rows(o), spaces[i].data_ptr(), need, stream=streams[i].cuda_stream)
+            streams[i].synchronize()
+        except Exception as e:                          # noqa: BLE001
+            failed.append(e)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(qs))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(60)
+    assert not failed and not any(t.is_alive() for t in threads)
+    torch.cuda.synchronize()
+    for w, got in zip(want, outs):
+        assert all(torch.equal(w, o) for o in got)

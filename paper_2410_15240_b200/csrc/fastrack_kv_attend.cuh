@@ -138,6 +138,10 @@ __device__ __forceinline__ float kv_power_below(uint32_t abs_bits)
     return __uint_as_float(e << 23);
 }
 
+// V of the unfinished block is held over a power of two of at least this, which is what a page's smallest values are: a reference of
+// that power still has an inverse, V below it keeps its bits down to 2^-124, and zeros do not take any from pages.
+#define KV_V_LEAST 0x1p-100f
+
 // The largest magnitude of 8 bf16 values, as bits
 __device__ __forceinline__ uint32_t kv_amax8(const uint4& w)
 {
@@ -461,7 +465,8 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
         uint32_t amax = 0;
 #pragma unroll
         for (int i = 0; i < STEPS; i++) amax = amax2(amax2(amax2(amax2(amax, w[i][0]), w[i][1]), w[i][2]), w[i][3]);
-        v_scale = kv_power_below(__reduce_max_sync(0xffffffffu, amax));
+        amax = __reduce_max_sync(0xffffffffu, amax);
+        v_scale = amax == 0 ? KV_V_LEAST : fmaxf(kv_power_below(amax), KV_V_LEAST);
     }
     kv_refer<D, NR>(W, v_scale);
     const float vf = v_scale * W.vinv, inv = 1.f / v_scale;

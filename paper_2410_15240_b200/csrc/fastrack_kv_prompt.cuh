@@ -414,7 +414,9 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
         uint32_t amax = 0;
         for (int i = lane; i < KV_HALF * D / 8; i += 32)
             if (t + i / (D / 8) < q.len) amax = max(amax, kv_amax8(*(const uint4*)(tail + ((uint64_t)which * S.block_tokens + t - tail_begin) * D + 8 * i)));
-        return kv_power_below(__reduce_max_sync(0xffffffffu, amax));
+        amax = __reduce_max_sync(0xffffffffu, amax);
+        const float least = which ? KV_V_LEAST : 0.f;
+        return which && amax == 0 ? least : fmaxf(kv_power_below(amax), least);
     };
     auto store = [&](const uint4 (&w)[2][P], int which, int t0, int2 kind, float2 power, uint8_t* dst) {
 #pragma unroll

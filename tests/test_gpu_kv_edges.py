@@ -97,3 +97,79 @@ def test_one_handle_on_several_threads_and_streams():
     torch.cuda.synchronize()
     for w, got in zip(want, outs):
         assert all(torch.equal(w, o) for o in got)
+
+
+def definition(c, q, window=0):
+    """Attention in 64 bits where values may be infinite or NaN: a token counts for the rows that see it, and for no other.
+    -> out, lse, the sums of |p v| over finite values, the largest |score|."""
+    out, spread = (torch.zeros(c.total, c.qh, c.d, dtype=torch.float64) for _ in range(2))
+    lse, top = torch.full((c.total, c.qh), -math.inf, dtype=torch.float64), torch.zeros(c.total, c.qh, dtype=torch.float64)
+    for i, (L, n) in enumerate(zip(c.lens, c.news)):
+        k, v, there = c.held(i)
+        sl = slice(c.starts[i], c.starts[i + 1])
+        place, token = torch.arange(L - n, L)[:, None], torch.arange(L)[None]
+        sees = (token <= place) & there[None]
+        if window:
+            sees &= token > place - window
+        for h in range(c.qh):
+            a = h // (c.qh // c.kh)
+            s = torch.where(sees, (q[sl, h].double().cpu() @ k[a].T) * c.scale, -math.inf)
+            p = torch.softmax(s, 1)
+            fine = torch.where(torch.isfinite(v[a]), v[a], 0.0)
+            o = p @ fine
+            for t in (~torch.isfinite(v[a])).any(1).nonzero().flatten().tolist():
+                o = torch.where(sees[:, t, None] & ~torch.isfinite(v[a, t])[None], o + v[a, t][None], o)
+            out[sl, h], spread[sl, h] = o, p @ fine.abs()
+            lse[sl, h] = torch.logsumexp(s, 1)
+            top[sl, h] = torch.where(torch.isfinite(s), s.abs(), 0.0).amax(1)
+    return out, lse, spread, top
+
+
+def compare(c, got, lse, want, least=2.0 ** -24):
+    """The bounds of Cache.check_attention, but for its share of the row's largest |p v|; `least`: what the type's smallest step may add.
+    Infinities and NaN have to be where the definition has them."""
+    r_out, r_lse, spread, top = want
+    g, slack = got.double().cpu(), 2.0 ** -17 * (1 + top)
+    assert torch.equal(torch.isnan(g), torch.isnan(r_out)), "NaN"
+    assert torch.equal(torch.isinf(g), torch.isinf(r_out)) and bool((g.sign() == r_out.sign())[torch.isinf(r_out)].all()), "infinite"
+    fine = torch.isfinite(r_out)
+    bound = UNIT[c.dtype] * r_out.abs() + (2.0 ** -10 + 4 * slack)[..., None] * spread + least + 2.0 ** -16 * spread.amax(-1, keepdim=True)
+    bad = ((g - r_out).abs() > bound) & fine
+    assert not bool(bad.any()), (int(bad.sum()), bad.nonzero()[:4].tolist(), float(((g - r_out).abs() / bound)[fine].max()))
+    fine = torch.isfinite(r_lse)
+    assert torch.equal(torch.isnan(lse.double().cpu()), torch.isnan(r_lse))
+    assert bool(((lse.double().cpu() - r_lse).abs() <= slack + 2.0 ** -22 * r_lse.abs())[fine].all())
+
+
+def attend(c, seed=5, scale=2.0, window=0):
+    gen = torch.Generator().manual_seed(seed)
+    q = (scale * torch.randn(c.total, c.qh, c.d, generator=gen)).to(c.t).cuda()
+    out = torch.full_like(q, -7.0)
+    return q, out, c.run_attention(q, out, window)
+
+
+@pytest.mark.parametrize("new", [1, 5, 150])
+@pytest.mark.parametrize("size", [2.0 ** -100, 2.0 ** -119, 1e-37, 1e-40])
+def test_tiny_values_in_the_unfinished_block(new, size):
+    """V far below what a page would hold, alone in the cache and beside pages: small answers, not infinite ones."""
+    c = Cache(kv.BF16, kv.INT8, 4, 2, 128, 64, [new + 40, new + 64 - new % 64 + 9], [new, new])
+    c.fill()
+    c.tail[:, :, 1] *= size
+    if new < 24:
+        c.pool[:, 2 * c.codes:2 * c.codes + 8 * c.kh].view(torch.float32).view(c.pages, c.kh, 2)[..., 1] = 2.0 ** -100
+    q, out, lse = attend(c)
+    # where all of V is small: steps of 2^-133, and 16 bits of f16 at 2^-25 of a page's smallest power
+    compare(c, out, lse, definition(c, q), least=2.0 ** -118 if new < 24 else 2.0 ** -24)
+
+
+@pytest.mark.parametrize("dtype", [kv.BF16])
+@pytest.mark.parametrize("new,group,block", [(1, 4, 64), (5, 1, 16), (5, 8, 32), (150, 2, 64)])
+def test_zeros_in_the_unfinished_block_cost_nothing(dtype, new, group, block):
+    """V of zeros (no matter at what power of two they are held) beside pages with small scales, whose answers keep their bits."""
+    c = Cache(dtype, kv.INT8, 2 * group, 2, 128, block, [new + 6 * block - new % block + 9] * 2, [new] * 2)
+    c.fill(spread=0.3)
+    c.tail[:, :, 1] = 0
+    small = 2.0 ** (-46 if dtype == kv.BF16 else -17)
+    c.pool[:, 2 * c.codes:2 * c.codes + 8 * c.kh].view(torch.float32).view(c.pages, c.kh, 2)[..., 1] *= small
+    q, out, lse = attend(c)
+    compare(c, out, lse, definition(c, q), least=2.0 ** -25 if dtype == kv.F16 else 2.0 ** -90)

@@ -6,11 +6,21 @@
 #define KV_WARPS 4
 #define KV_HALF 16          // tokens that lie inside one block for sure
 #define KV_TILE 32          // tokens of a warp's step: two halves
-#define KV_LAZY 4.0f        // a running maximum is raised only when exceeded by this many powers of two
-// Weights enter the second product as f16, times V's scale over its reference (at most 1), times this: 2^4 * 2^11 stays below
-// f16's largest, and a weight down to 2^-25 of the largest keeps all 11 bits, so that a token of little weight whose values are
-// orders above the others' is not lost.
-#define KV_P_SCALE 2048.0f
+// What a token adds to the answer is exp2(s) * (V's scale) * (V's codes), s its score in base 2.  With y = log2 of V's scale, its weight
+// enters the second product as f16 exp2(s + y - m), m the row's reference: s + y of every token that the row has seen is at most
+// m + KV_P_MOST, which f16 holds.  Where one is above, m is raised to KV_P_BITS below it, and what was added up falls.  So what adds down to
+// 2^-25 of the largest share keeps all 11 bits, whatever the scales of blocks that the row sees and of others.
+// The sum of exponentials wants the weights without V's scale: the sum of every 16 tokens with one scale is multiplied by
+// z = 2^-KV_L_BITS / scale.  The answer's accumulator is in units of 2^m, the sum l in units of 2^(m + KV_L_BITS): for scales from
+// 2^-109 (append's smallest) to 2^121 neither z nor l of 2^30 tokens leaves the range of a float.  (An exponential that ends
+// below 2^-126 is lost to the sum: that takes tokens of one row whose scales are 2^137 apart.)
+#define KV_P_MOST 15.0f
+#define KV_P_BITS 11.0f
+#define KV_L_BITS 27.0f
+#define KV_M_NONE -3.402823466e38f      // the reference of a row that has seen nothing: finite, so that a difference from it is a number
+// The power of two that zeros are taken to be held over, in a page (scale 0) or in the unfinished block: they add nothing to any answer, but their
+// weights count in the sum.  Low enough to leave other blocks' weights their bits, high enough for the sum beside large ones.
+#define KV_V_ZERO 0x1p-72f
 
 // Every span is cut into chunks, a CTA for each.  Where the chunks fill the SMs several times, they are equal pieces of whatever length
 // a sequence has, so that one CTA's start and end pass under the others' loads; they are joined through the workspace by a kernel of its
@@ -31,7 +41,7 @@ struct KvAttend {
     int row_tiles, units;   // units: per sequence, for weights, of
     int unit_shift;         // log2 of their tokens
     float* part_o;          // [splits][total_new * q_heads][head_dim]
-    float* part_ml;         // [splits][total_new * q_heads][2]: running maximum and sum
+    float* part_ml;         // [splits][total_new * q_heads][2]: m and l, see KV_P_MOST
     float* lse2;            // [total_new * q_heads], base 2, see kv_lse2_at
     float* unit_l2;         // [n_seqs][kv_heads][units][max_new * group]: log2 of the sum of exponentials of a unit; NULL without weights
     const float* mass_in;
@@ -142,11 +152,28 @@ __device__ __forceinline__ float kv_power_below(uint32_t abs_bits)
 // that power still has an inverse, V below it keeps its bits down to 2^-124, and zeros do not take any from pages.
 #define KV_V_LEAST 0x1p-100f
 
-// The largest magnitude of 8 bf16 values, as bits
-__device__ __forceinline__ uint32_t kv_amax8(const uint4& w)
+// y and z of a scale of V (see KV_P_MOST); NaN for NaN.  The exponent is taken off the logarithm's argument: y is as exact as its size
+// allows, 2^-21 at most, and the sum sees the weights as the answer does.
+__device__ __forceinline__ float2 kv_v_share(float scale)
 {
-    const uint32_t a = max(max(w.x << 16 & 0x7fffffffu, w.x & 0x7fff0000u), max(w.y << 16 & 0x7fffffffu, w.y & 0x7fff0000u));
-    return max(a, max(max(w.z << 16 & 0x7fffffffu, w.z & 0x7fff0000u), max(w.w << 16 & 0x7fffffffu, w.w & 0x7fff0000u)));
+    const float v = scale < 0x1p-110f ? KV_V_ZERO : scale;
+    const uint32_t bits = __float_as_uint(v);
+    const float exponent = __uint_as_float(0x4b000000u | bits >> 23) - (8388608.f + 127.f);
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(v));
+    return make_float2(fmaf(v, 0.f, exponent + kv_log2(__uint_as_float((bits & 0x7fffffu) | 0x3f800000u))), inv * (1.f / 134217728));
+}
+// What an accumulated answer is multiplied by, for the sum l of its row: 2^-KV_L_BITS / l; 0 where the row saw nothing.
+__device__ __forceinline__ float kv_over_sum(float l)
+{
+    return l == 0.f ? 0.f : l < 1.f ? 1.f / (l * 134217728.f) : 1.f / 134217728 / l;
+}
+
+// The largest magnitude of 8 values, as the bits of a float (bf16) or of an f16: 16-bit magnitudes are in the order of their bits
+template <bool BF> __device__ __forceinline__ uint32_t kv_amax8(const uint4& w)
+{
+    const uint32_t m = 0x7fff7fffu, a = __vmaxu2(__vmaxu2(w.x & m, w.y & m), __vmaxu2(w.z & m, w.w & m)), most = max(a & 0xffffu, a >> 16);
+    return BF ? most << 16 : most;
 }
 
 // Where a row's sum stands in lse2: the rows of a sequence and kv head are neighbours.
@@ -196,17 +223,16 @@ template <int D> __host__ __device__ constexpr int kv_attend_smem(int rows)
 template <int D, int NR> struct KvState {
     uint32_t qb[NR][D / 16][2];                          // queries as f16: row 8 r + g
     float factor[NR][2];                                 // of the scores of rows 8 r + 2 c + e
-    float m[NR][2], l[NR][2];
-    float o[NR][D / 16][4];
-    float vref, vinv;                                    // power of two that V's scales are measured by (o is in its units), KV_P_SCALE over it
+    float m[NR][2], l[NR][2];                            // see KV_P_MOST
+    float o[NR][D / 16][4];                              // in units of 2^m
 };
 
-// Scores in base 2 and times their scales, -inf where hidden: raises the running maxima where one is exceeded by far, turns the
-// scores into weights (unrounded; their sums go to l) and leaves the rows' bases.
+// s + y of scores and V's scales, -inf where hidden: raises the rows' references where one is exceeded and turns them into weights (unrounded).
 template <int D, int NR, int HALVES>
-__device__ __forceinline__ void kv_weigh(KvState<D, NR>& W, float (&s)[HALVES][NR][4], float (&base)[NR][2])
+__device__ __forceinline__ void kv_weigh(KvState<D, NR>& W, float (&s)[HALVES][NR][4])
 {
     bool higher = false;
+    float base[NR][2];
 #pragma unroll
     for (int r = 0; r < NR; r++)
 #pragma unroll
@@ -214,7 +240,7 @@ __device__ __forceinline__ void kv_weigh(KvState<D, NR>& W, float (&s)[HALVES][N
             float top = fmaxf(s[0][r][e], s[0][r][2 + e]);
             if (HALVES == 2) top = fmaxf(top, fmaxf(s[HALVES - 1][r][e], s[HALVES - 1][r][2 + e]));
             base[r][e] = top;
-            higher |= top > W.m[r][e] + KV_LAZY;
+            higher |= top - W.m[r][e] > KV_P_MOST;       // exact, however large the two are
         }
     if (__any_sync(0xffffffffu, higher)) {
 #pragma unroll
@@ -224,8 +250,8 @@ __device__ __forceinline__ void kv_weigh(KvState<D, NR>& W, float (&s)[HALVES][N
                 float top = base[r][e];
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                top = fmaxf(W.m[r][e], top);
-                const float f = top == -KV_INF ? 1.f : kv_exp2(W.m[r][e] - top);
+                top = fmaxf(W.m[r][e], __fadd_ru(top, -KV_P_BITS));          // up: what is rounded away would be above KV_P_MOST
+                const float f = kv_exp2(W.m[r][e] - top);
                 W.m[r][e] = top;
                 W.l[r][e] *= f;
 #pragma unroll
@@ -235,20 +261,22 @@ __device__ __forceinline__ void kv_weigh(KvState<D, NR>& W, float (&s)[HALVES][N
 #pragma unroll
     for (int r = 0; r < NR; r++)
 #pragma unroll
-        for (int e = 0; e < 2; e++) {
-            base[r][e] = W.m[r][e] == -KV_INF ? 0.f : W.m[r][e];
+        for (int e = 0; e < 2; e++)
 #pragma unroll
             for (int h = 0; h < HALVES; h++) {
-                s[h][r][e] = kv_exp2(s[h][r][e] - base[r][e]);
-                s[h][r][2 + e] = kv_exp2(s[h][r][2 + e] - base[r][e]);
-                W.l[r][e] += s[h][r][e] + s[h][r][2 + e];
+                s[h][r][e] = kv_exp2(s[h][r][e] - W.m[r][e]);
+                s[h][r][2 + e] = kv_exp2(s[h][r][2 + e] - W.m[r][e]);
             }
-        }
 }
 
-// log2 of the rows' sums of the weights of halves h0 .. h1 - 1, to out[row]
-template <int D, int NR, int HALVES>
-__device__ __forceinline__ void kv_note(const float (&s)[HALVES][NR][4], const float (&base)[NR][2], int h0, int h1, float* out, int rows_left, int g, int c)
+// log2 of a row's sum of exponentials, and of a unit's of weights, made once per tile, in one instruction: off by at most 2^-22 of the
+// logarithm, which adds some 10 to m (exact for powers of two, as the other).
+__device__ __forceinline__ float kv_sum_log2(float l, float m) { return l == 0.f ? -KV_INF : m + (KV_L_BITS + log2f(l)); }
+__device__ __forceinline__ float kv_unit_log2(float l, float m) { return m + (KV_L_BITS + kv_log2(l)); }
+
+// log2 of the rows' sums of exponentials of halves h0 .. h1 - 1, from the lanes' parts of l, to out[row]
+template <int NR, int HALVES>
+__device__ __forceinline__ void kv_note(const float (&part)[HALVES][NR][2], const float (&m)[NR][2], int h0, int h1, float* out, int rows_left, int g, int c)
 {
 #pragma unroll
     for (int r = 0; r < NR; r++)
@@ -257,25 +285,12 @@ __device__ __forceinline__ void kv_note(const float (&s)[HALVES][NR][4], const f
             float sum = 0.f;
 #pragma unroll
             for (int h = 0; h < HALVES; h++)
-                if (h >= h0 && h < h1) sum += s[h][r][e] + s[h][r][2 + e];
+                if (h >= h0 && h < h1) sum += part[h][r][e];
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
             const int at = 8 * r + 2 * c + e;
-            if (g == 0 && at < rows_left) out[at] = kv_log2(sum) + base[r][e];
+            if (g == 0 && at < rows_left) out[at] = kv_unit_log2(sum, m[r][e]);
         }
-}
-
-template <int D, int NR> __device__ __forceinline__ void kv_refer(KvState<D, NR>& W, float vs)
-{
-    if (vs > W.vref) {                                   // the warp as a whole
-        const float next = 4.f * kv_power_below(__float_as_uint(vs)), f = W.vref / next;
-#pragma unroll
-        for (int r = 0; r < NR; r++)
-#pragma unroll
-            for (int i = 0; i < D / 16; i++) { W.o[r][i][0] *= f; W.o[r][i][1] *= f; W.o[r][i][2] *= f; W.o[r][i][3] *= f; }
-        W.vref = next;
-        W.vinv = KV_P_SCALE / next;
-    }
 }
 
 // Weights of two rows as f16, as the second operand's share of a lane.  FINE (answers of 11 bits, where the rounding of the weights
@@ -290,7 +305,7 @@ template <bool FINE> __device__ __forceinline__ void kv_weights(float x, float y
     hi = kv_transpose(hi);
 }
 
-// One tile of full blocks.  RAGGED: some of its tokens are hidden from some rows, or a half is not there; hidden has a bit for each of s.
+// One tile of full blocks.  RAGGED: some of its tokens are hidden from some rows, or a half is not there.
 // k_wait and v_wait wait for K and V, k_read and v_read are called when they have been read.
 template <int D, bool FINE, bool E4M3, int NR, bool RAGGED, class KWait, class KRead, class VWait, class VRead>
 __device__ __forceinline__ void kv_tile(KvState<D, NR>& W, const uint8_t* slot, int t0, const float (&ks)[2], const float (&vs)[2], const bool (&there)[2],
@@ -326,48 +341,50 @@ __device__ __forceinline__ void kv_tile(KvState<D, NR>& W, const uint8_t* slot, 
             }
         }
     k_read();
-    uint32_t hidden = 0;
+    const float2 share[2] = {kv_v_share(vs[0]), kv_v_share(vs[1])};
 #pragma unroll
     for (int h = 0; h < 2; h++)
 #pragma unroll
         for (int r = 0; r < NR; r++)
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-                s[h][r][i] *= ks[h] * W.factor[r][i & 1];
-                if (RAGGED) {
+                s[h][r][i] = fmaf(s[h][r][i], ks[h] * W.factor[r][i & 1], share[h].x);
+                if (RAGGED) {                            // a masked token's scales, whatever they are, do not count
                     const int t = t0 + KV_HALF * h + 8 * (i >> 1) + token, at = place[r][i & 1];
-                    if (t > at || (window > 0 && t <= at - window) || !there[h]) {
-                        s[h][r][i] = -KV_INF;
-                        hidden |= 1u << (8 * r + 4 * h + i);
-                    }
+                    if (t > at || (window > 0 && t <= at - window) || !there[h]) s[h][r][i] = -KV_INF;
                 }
             }
-    float base[NR][2];
-    kv_weigh<D, NR, 2>(W, s, base);
+    float part[2][NR][2];
+    kv_weigh<D, NR, 2>(W, s);
+#pragma unroll
+    for (int r = 0; r < NR; r++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const float sum = s[h][r][e] + s[h][r][2 + e];
+                part[h][r][e] = RAGGED && sum == 0.f ? 0.f : sum * share[h].y;
+            }
+            W.l[r][e] += part[0][r][e] + part[1][r][e];
+        }
     if (unit_out) {
-        if (one_unit) kv_note<D, NR, 2>(s, base, 0, 2, unit_out, rows_left, g, c);
+        if (one_unit) kv_note<NR, 2>(part, W.m, 0, 2, unit_out, rows_left, g, c);
         else {
-            kv_note<D, NR, 2>(s, base, 0, 1, unit_out, rows_left, g, c);
-            if (there[1]) kv_note<D, NR, 2>(s, base, 1, 2, unit_out + unit_stride, rows_left, g, c);
+            kv_note<NR, 2>(part, W.m, 0, 1, unit_out, rows_left, g, c);
+            if (there[1]) kv_note<NR, 2>(part, W.m, 1, 2, unit_out + unit_stride, rows_left, g, c);
         }
     }
-    kv_refer<D, NR>(W, fmaxf(vs[0], vs[1]));
     fine = v_wait() && fine;
+    if (!fine)                                           // bytes that never came: NaN answers
+#pragma unroll
+        for (int r = 0; r < NR; r++) W.l[r][0] = W.l[r][1] = __int_as_float(0x7fffffff);
 #pragma unroll
     for (int h = 0; h < 2; h++) {
-        const float vf = !fine ? __int_as_float(0x7fffffff) : W.vref > 0.f ? vs[h] * W.vinv : vs[h];     // bytes that never came: NaN
         uint32_t pb[NR][2], pl[NR][2];
 #pragma unroll
         for (int r = 0; r < NR; r++)
 #pragma unroll
-            for (int up = 0; up < 2; up++) {
-                float x = s[h][r][2 * up] * vf, y = s[h][r][2 * up + 1] * vf;
-                if (RAGGED) {                            // a masked token's scale, whatever it is, does not count
-                    if (hidden >> (8 * r + 4 * h + 2 * up) & 1) x = 0.f;
-                    if (hidden >> (8 * r + 4 * h + 2 * up + 1) & 1) y = 0.f;
-                }
-                kv_weights<FINE>(x, y, pb[r][up], pl[r][up]);
-            }
+            for (int up = 0; up < 2; up++) kv_weights<FINE>(s[h][r][2 * up], s[h][r][2 * up + 1], pb[r][up], pl[r][up]);
         uint32_t vw[4][T::VW];
 #pragma unroll
         for (int j = 0; j < 4; j++) {
@@ -414,7 +431,7 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
         const float2 x = kv_unpack<true>(w);
         return kv_pack<false>(x.x * inv, x.y * inv);
     };
-    float s[1][NR][4], base[NR][2];
+    float s[1][NR][4];
 #pragma unroll
     for (int r = 0; r < NR; r++) s[0][r][0] = s[0][r][1] = s[0][r][2] = s[0][r][3] = 0.f;
     float k_scale = 1.f, v_scale = 1.f;
@@ -447,36 +464,39 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
             const int t = 2 * c + (j & 1) + (j >> 1) * 8;
             w[i][j] = t0 + t < len ? *(const uint32_t*)(v + t * D + T::v_channel(g, 2 * i)) : 0u;
         }
-    uint32_t hidden = 0;
-#pragma unroll
-    for (int r = 0; r < NR; r++)
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            s[0][r][i] *= k_scale * W.factor[r][i & 1];
-            const int t = t0 + 8 * (i >> 1) + g, at = place[r][i & 1];
-            if (t > at || (window > 0 && t <= at - window)) {
-                s[0][r][i] = -KV_INF;
-                hidden |= 1u << (4 * r + i);
-            }
-        }
-    kv_weigh<D, NR, 1>(W, s, base);
-    if (unit_out) kv_note<D, NR, 1>(s, base, 0, 1, unit_out, rows_left, g, c);
     if (BF) {
         uint32_t amax = 0;
 #pragma unroll
         for (int i = 0; i < STEPS; i++) amax = amax2(amax2(amax2(amax2(amax, w[i][0]), w[i][1]), w[i][2]), w[i][3]);
         amax = __reduce_max_sync(0xffffffffu, amax);
-        v_scale = amax == 0 ? KV_V_LEAST : fmaxf(kv_power_below(amax), KV_V_LEAST);
+        v_scale = amax == 0 ? KV_V_ZERO : fmaxf(kv_power_below(amax), KV_V_LEAST);
     }
-    kv_refer<D, NR>(W, v_scale);
-    const float vf = v_scale * W.vinv, inv = 1.f / v_scale;
+    const float2 share = kv_v_share(v_scale);
+    const float inv = 1.f / v_scale;
+#pragma unroll
+    for (int r = 0; r < NR; r++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            s[0][r][i] = fmaf(s[0][r][i], k_scale * W.factor[r][i & 1], share.x);
+            const int t = t0 + 8 * (i >> 1) + g, at = place[r][i & 1];
+            if (t > at || (window > 0 && t <= at - window)) s[0][r][i] = -KV_INF;
+        }
+    kv_weigh<D, NR, 1>(W, s);
+    float part[1][NR][2];
+#pragma unroll
+    for (int r = 0; r < NR; r++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+            part[0][r][e] = (s[0][r][e] + s[0][r][2 + e]) * share.y;
+            W.l[r][e] += part[0][r][e];
+        }
+    if (unit_out) kv_note<NR, 1>(part, W.m, 0, 1, unit_out, rows_left, g, c);
     uint32_t pb[NR][2], pl[NR][2];
 #pragma unroll
     for (int r = 0; r < NR; r++)
 #pragma unroll
         for (int up = 0; up < 2; up++)
-            kv_weights<!BF>(hidden >> (4 * r + 2 * up) & 1 ? 0.f : s[0][r][2 * up] * vf, hidden >> (4 * r + 2 * up + 1) & 1 ? 0.f : s[0][r][2 * up + 1] * vf,
-                            pb[r][up], pl[r][up]);
+            kv_weights<!BF>(s[0][r][2 * up], s[0][r][2 * up + 1], pb[r][up], pl[r][up]);
 #pragma unroll
     for (int i = 0; i < STEPS; i++) {
 #pragma unroll
@@ -588,13 +608,12 @@ __global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? (D == 64 ? 6 : 4) : 3
             const int mine = tile_row + 8 * r + 2 * c + e;
             W.factor[r][e] = S.scale_log2 * __shfl_sync(0xffffffffu, p, 4 * (2 * c + e));
             place[r][e] = mine < rows ? q.len - q.n + mine / S.group : -1;
-            W.m[r][e] = -KV_INF;
+            W.m[r][e] = KV_M_NONE;
             W.l[r][e] = 0.f;
         }
 #pragma unroll
         for (int i = 0; i < STEPS; i++) W.o[r][i][0] = W.o[r][i][1] = W.o[r][i][2] = W.o[r][i][3] = 0.f;
     }
-    W.vref = W.vinv = 0.f;
     const int last_row = min(tile_row + ROWS, rows) - 1;
     const int see_all = q.len - q.n + tile_row / S.group;                    // tokens up to here are seen by every row (without a window)
     const int low_all = A.window > 0 ? q.len - q.n + last_row / S.group - A.window : -1;   // tokens behind here are in every row's window
@@ -632,7 +651,6 @@ __global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? (D == 64 ? 6 : 4) : 3
     float (*const sm_o)[ROWS][D + 4] = (float (*)[ROWS][D + 4])kv_smem;
     float (*const sm_m)[ROWS] = (float (*)[ROWS])(kv_smem + KV_WARPS * ROWS * (D + 4) * 4);
     float (*const sm_l)[ROWS] = sm_m + KV_WARPS;
-    const float unit = W.vref > 0.f ? W.vref / KV_P_SCALE : 1.f;             // without a reference o is 0 or NaN
 #pragma unroll
     for (int r = 0; r < NR; r++)
 #pragma unroll
@@ -643,8 +661,8 @@ __global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? (D == 64 ? 6 : 4) : 3
             if (g == 0) { sm_m[warp][row] = W.m[r][e]; sm_l[warp][row] = W.l[r][e]; }
 #pragma unroll
             for (int i = 0; i < STEPS; i++) {
-                sm_o[warp][row][T::v_channel(g, 2 * i)] = W.o[r][i][e] * unit;
-                sm_o[warp][row][T::v_channel(g, 2 * i + 1)] = W.o[r][i][2 + e] * unit;
+                sm_o[warp][row][T::v_channel(g, 2 * i)] = W.o[r][i][e];
+                sm_o[warp][row][T::v_channel(g, 2 * i + 1)] = W.o[r][i][2 + e];
             }
         }
     __syncthreads();
@@ -653,10 +671,10 @@ __global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? (D == 64 ? 6 : 4) : 3
     auto answer = [&](int row, int ch, float top, float sum, float x, float y) {
         const int all = tile_row + row, head = kh * S.group + all % S.group;
         const int64_t token = q.start + all / S.group;
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const float inv = kv_over_sum(sum);
         *(uint32_t*)((uint16_t*)A.out.data + token * A.out.token_stride + head * A.out.head_stride + ch) = kv_pack<BF>(x * inv, y * inv);
         if (ch == 0) {
-            const float l2 = sum == 0.f ? -KV_INF : top + log2f(sum);
+            const float l2 = kv_sum_log2(sum, top);
             if (A.lse) A.lse[token * S.q_heads + head] = l2 * 0.6931471805599453f;
             A.lse2[kv_lse2_at(S, q, kh, all)] = l2;
         }
@@ -664,14 +682,13 @@ __global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? (D == 64 ? 6 : 4) : 3
     for (int idx = threadIdx.x; idx < ROWS * (D / 2); idx += 32 * KV_WARPS) {
         const int row = idx / (D / 2), ch = idx % (D / 2) * 2, all = tile_row + row;
         if (all >= rows) break;
-        float top = -KV_INF;
+        float top = sm_m[0][row];
 #pragma unroll
-        for (int w = 0; w < KV_WARPS; w++) top = fmaxf(top, sm_m[w][row]);
-        const float base = top == -KV_INF ? 0.f : top;
+        for (int w = 1; w < KV_WARPS; w++) top = fmaxf(top, sm_m[w][row]);
         float x = 0.f, y = 0.f, sum = 0.f;
 #pragma unroll
         for (int w = 0; w < KV_WARPS; w++) {
-            const float f = kv_exp2(sm_m[w][row] - base);
+            const float f = kv_exp2(sm_m[w][row] - top);
             sum += f * sm_l[w][row];
             x += f * sm_o[w][row][ch];
             y += f * sm_o[w][row][ch + 1];
@@ -702,11 +719,10 @@ __global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? (D == 64 ? 6 : 4) : 3
         }
 #pragma unroll
         for (int k = 0; k < KV_CLUSTER; k++) top = fmaxf(top, ml[k].x);
-        const float base = top == -KV_INF ? 0.f : top;
         float x = 0.f, y = 0.f, sum = 0.f;
 #pragma unroll
         for (int k = 0; k < KV_CLUSTER; k++) {
-            const float f = kv_exp2(ml[k].x - base);
+            const float f = kv_exp2(ml[k].x - top);
             sum += f * ml[k].y;
             x += f * o[k].x;
             y += f * o[k].y;
@@ -776,14 +792,13 @@ __global__ void __launch_bounds__(32 * KV_WARPS) kv_join_kernel(const KvShape S,
             for (int k = lane & 15; k < n; k += 16) m = fmaxf(m, src[2 * k * stride]);
 #pragma unroll
             for (int d = 8; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-            const float base = m == -KV_INF ? 0.f : m;
             for (int k = lane & 15; k < n; k += 16) {
                 const float2 ml = *(const float2*)(src + 2 * k * stride);
-                l += ml.y * kv_exp2(ml.x - base);
+                l += ml.y * kv_exp2(ml.x - m);
             }
 #pragma unroll
             for (int d = 8; d; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-            if ((lane & 15) == 0 && n) sm_rows[row] = l == 0.f ? -KV_INF : m + log2f(l);
+            if ((lane & 15) == 0 && n) sm_rows[row] = kv_sum_log2(l, m);
         }
         __syncthreads();
         kv_weigh_blocks(S, B, A, q, seq, kh, first_block, sm_rows);
@@ -798,14 +813,13 @@ __global__ void __launch_bounds__(32 * KV_WARPS) kv_join_kernel(const KvShape S,
     for (int k = lane; k < chunks; k += 32) m = fmaxf(m, A.part_ml[2 * (first + k * stride)]);
 #pragma unroll
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    const float base = m == -KV_INF ? 0.f : m;
 #pragma unroll
     for (int i = 0; i < V; i++) acc[i] = 0.f;
 #pragma unroll 8
     for (int k = warp; k < chunks; k += KV_WARPS) {
         const float2 ml = *(const float2*)(A.part_ml + 2 * (first + k * stride));
         const float* src = A.part_o + (first + k * stride) * D + lane;
-        const float h = kv_exp2(ml.x - base);
+        const float h = kv_exp2(ml.x - m);
         l += ml.y * h;
 #pragma unroll
         for (int i = 0; i < V; i++) acc[i] += src[32 * i] * h;
@@ -817,7 +831,7 @@ __global__ void __launch_bounds__(32 * KV_WARPS) kv_join_kernel(const KvShape S,
     l = 0.f;
 #pragma unroll
     for (int w = 0; w < KV_WARPS; w++) l += sm_sum[w];
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = kv_over_sum(l);
     if (threadIdx.x < D / 2) {
         float2 x = make_float2(0.f, 0.f);
 #pragma unroll
@@ -825,7 +839,7 @@ __global__ void __launch_bounds__(32 * KV_WARPS) kv_join_kernel(const KvShape S,
         *(uint32_t*)((uint16_t*)A.out.data + (q.start + token) * A.out.token_stride + head * A.out.head_stride + 2 * threadIdx.x) = kv_pack<BF>(x.x * inv, x.y * inv);
     }
     if (threadIdx.x == 0) {
-        const float l2 = l == 0.f ? -KV_INF : m + log2f(l);
+        const float l2 = kv_sum_log2(l, m);
         if (A.lse) A.lse[first] = l2 * 0.6931471805599453f;
         A.lse2[kv_lse2_at(S, q, head / S.group, token * S.group + head % S.group)] = l2;
     }

@@ -1,5 +1,6 @@
 // fastrack_kv_prompt.cuh -- attention of many query rows over the 8-bit cache, on the 5th-generation tensor cores.
 #pragma once
+#include <type_traits>
 #include "fastrack_kv_attend.cuh"
 
 // One CTA takes 256 rows (two tiles of 128) of one kv head of one sequence against a chunk of the tokens, 128 at a time:
@@ -21,7 +22,6 @@
 #define KV_P_THREADS 416
 #define KV_P_GROUPS (KV_P_TOKENS / KV_HALF)
 #define KV_P_AHEAD 4                   // pairs of values between an exponential and the use of its result
-#define KV_P_LEAST 0x1p-40f             // a block's V scale counts for at least this share of the reference (below it V is lost to 11 bits anyway)
 
 template <int D> struct KvPrompt {
     static constexpr int HALVES = (D + 63) / 64;                             // runs of 64 channels: 128-byte rows, swizzled by the row's number
@@ -105,9 +105,6 @@ __device__ __forceinline__ uint64_t kv_add2(uint64_t a, uint64_t b)
     return d;
 }
 
-struct KvYes { static constexpr bool value = true; };
-struct KvNo { static constexpr bool value = false; };
-
 // Bounded wait that also ends when another warp has given up.
 __device__ __forceinline__ bool kv_wait_or_stop(uint32_t bar, uint32_t parity, volatile int* stop)
 {
@@ -154,12 +151,13 @@ template <bool E4M3> __device__ __forceinline__ void kv_widen16(const uint4& w, 
 // S_IN and P_IN: [row tile][half of the tile's tokens]; O_IN: an answer product of the row tile is done.
 enum { KV_K_IN = 0, KV_K_OUT = 4, KV_V_IN = 6, KV_V_OUT = 8, KV_S_IN = 10, KV_P_IN = 14, KV_O_IN = 18, KV_Q_IN = 20, KV_TAIL = 21, KV_END = 22, KV_BARS = 23 };
 
-// What a tile's slot of T::SCALES holds: per 16 tokens {K's scale, log2 of V's scale over the reference, one over that share, whether the
-// tokens are there}; the tile's change of the reference and the reference itself stand behind the groups.
-struct KvSlot { float4 group[KV_P_GROUPS]; float step, unit, pad[2]; };
+// What a tile's slot of T::SCALES holds: per 16 tokens {K's scale, y and z of V's (see KV_P_MOST), whether the tokens are there}; and of each half
+// the largest scale of K, infinite for the unfinished block, negative where some tokens are not there.
+struct KvSlot { float4 group[KV_P_GROUPS]; float k_most[2], pad[2]; };
+enum { KV_TILE_WHOLE, KV_TILE_RAGGED, KV_TILE_LARGE };
 
-// log2 of 128 (query, head) rows' weights, made tile by tile by 128 threads, a row each; see the head of this file.
-template <int D, bool BF>
+// 128 (query, head) rows' weights, made tile by tile by 128 threads, a row each; see the head of this file.
+template <int D, bool BF, bool E4M3>
 __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& B, const KvAttend& A, const KvSeq& q, int seq, int kh, int tile_row, int m_tile,
                                                int chunk, int begin, int end, int tiles, uint8_t* sm, uint32_t bars, volatile int* stop, uint32_t tmem)
 {
@@ -170,19 +168,23 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
     const int head = kh * S.group + row % S.group, place = valid ? q.len - q.n + row / S.group : -1;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21, s_at = tmem + lanes + 128 * m_tile, o_at = tmem + lanes + 256 + 128 * m_tile;
     const KvSlot* const slots = (const KvSlot*)(sm + T::SCALES);
-    float factor = S.scale_log2;
+    float factor = S.scale_log2, score_most;
     {
         // the row of Q, as f16 (bf16: over a power of two near its largest), to shared memory
         const uint16_t* src = (const uint16_t*)A.q.data + token * A.q.token_stride + head * A.q.head_stride;
-        float inv = 1.f;
-        if (BF) {
-            uint32_t amax = 0;
+        float inv = 1.f, most = 2.f;                     // most: no value of the row, as f16, is larger
+        uint32_t amax = 0;
 #pragma unroll 4
-            for (int i = 0; i < D / 8; i++) amax = max(amax, valid ? kv_amax8(*(const uint4*)(src + 8 * i)) : 0u);
+        for (int i = 0; i < D / 8; i++) amax = max(amax, valid ? kv_amax8<BF>(*(const uint4*)(src + 8 * i)) : 0u);
+        if (BF) {
             const float p = kv_power_below(amax);
             factor *= p;
             inv = 1.f / p;
+        } else {
+            most = __half2float(__ushort_as_half((unsigned short)amax));
         }
+        // no score of the warp's rows is larger than this times K's scale
+        score_most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(factor * most))) * (D * (E4M3 ? 448.f : 127.f));
 #pragma unroll 4
         for (int i = 0; i < D / 8; i++) {
             uint4 w = valid ? *(const uint4*)(src + 8 * i) : make_uint4(0, 0, 0, 0);
@@ -205,7 +207,7 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
     const int unit_stride = B.max_new * S.group;        // units of weights: 64 tokens, or smaller blocks
     float* const units = A.unit_l2 && valid ? A.unit_l2 + ((int64_t)seq * S.kv_heads + kh) * A.units * unit_stride + row : nullptr;
     const bool small_units = units && S.block_tokens < 64;
-    float m = -KV_INF, l = 0.f, unit = 1.f;
+    float m = KV_M_NONE, l = 0.f;                        // see KV_P_MOST
     bool fine = true;
     // Steps of 64 tokens: while this one's weights are made, the next one's scores are (in the other half of S).
     uint32_t ended = 0;                                  // whether this step's scores are known to be there
@@ -220,17 +222,21 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
         if (!__all_sync(0xffffffffu, ended)) fine = kv_warp_wait(bars + 8 * (KV_S_IN + 2 * m_tile + half), j & 1, stop) && fine;
         if (!fine) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const bool ragged = slot.pad[0] != 0.f || t0 + 63 > see_all || t0 <= low_all;
-        float step = half ? 1.f : slot.step;             // of O: it is in units of V's reference, l is not
-        unit = slot.unit;
-        float base = 0.f, z[4];
+        const float k_most = slot.k_most[half];
+        const bool ragged = __float_as_int(k_most) < 0 || t0 + 63 > see_all || t0 <= low_all;
+        float fall = 1.f, z[4];                          // fall: what l and O are multiplied by
         uint64_t sum[4] = {0, 0, 0, 0};                  // of 16 tokens' weights each
-        auto pass = [&](auto some_hidden) {
-            constexpr bool RAGGED = decltype(some_hidden)::value;
+        // LARGE: where a score may be so large that y - m would be rounded to steps of a quarter or more, s + y is formed first, for the largest
+        // and for the weights alike.
+        auto pass = [&](auto kind) {
+            constexpr bool LARGE = decltype(kind)::value == KV_TILE_LARGE, RAGGED = LARGE || decltype(kind)::value == KV_TILE_RAGGED;
             uint32_t seen[2] = {0xffffffffu, 0xffffffffu};                   // which of 32 tokens the row sees
-            float f[4];
+            float f[4], y[4];
 #pragma unroll
-            for (int g = 0; g < 4; g++) f[g] = sc[g].x * factor;
+            for (int g = 0; g < 4; g++) {
+                f[g] = LARGE ? 1.f : sc[g].x * factor;
+                y[g] = LARGE ? 0.f : sc[g].y;
+            }
             if (RAGGED)
 #pragma unroll
                 for (int b = 0; b < 2; b++) {
@@ -241,10 +247,13 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
                 }
             uint32_t x[64];
             kv_tmem_load64(x, at);
-            // the largest score; a scale is not negative, so that of 16 tokens with one scale the largest product is the largest score
+            // the largest s + y; a scale is not negative, so that of 16 tokens with one scale the largest product is the largest score
             float top = -KV_INF;
 #pragma unroll
             for (int g = 0; g < 4; g++) {
+                if (LARGE)
+#pragma unroll
+                    for (int i = 16 * g; i < 16 * g + 16; i++) x[i] = __float_as_uint(fmaf(__uint_as_float(x[i]) * sc[g].x, factor, sc[g].y));
                 if (RAGGED)
 #pragma unroll
                     for (int i = 16 * g; i < 16 * g + 16; i++) x[i] = seen[g >> 1] >> (i & 31) & 1 ? x[i] : 0xff800000u;
@@ -256,22 +265,20 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
                 u = fmaxf(fmaxf(u, __uint_as_float(x[o + 10])), __uint_as_float(x[o + 11]));
                 w = fmaxf(fmaxf(w, __uint_as_float(x[o + 12])), __uint_as_float(x[o + 13]));
                 u = fmaxf(fmaxf(u, __uint_as_float(x[o + 14])), __uint_as_float(x[o + 15]));
-                top = fmaxf(top, fmaxf(u, w) * f[g]);    // a NaN (0 times -inf where 16 hidden tokens have a scale of 0) does not count
+                top = fmaxf(top, fmaf(fmaxf(u, w), f[g], y[g]));                  // a NaN (0 times -inf where 16 hidden tokens have a scale of 0) does not count
             }
             // without a branch, behind which the compiler might leave the rows apart: the tensor memory's instructions want the warp whole
-            const bool higher = top > m + KV_LAZY;
-            const float fall = higher ? kv_exp2(m - top) : 1.f;
+            const bool higher = LARGE ? top - m > KV_P_MOST : top > m + KV_P_MOST;
+            top = LARGE ? __fadd_ru(top, -KV_P_BITS) : top - KV_P_BITS;      // up: what is rounded away would be above KV_P_MOST
+            fall = higher ? kv_exp2(m - top) : 1.f;
             l *= fall;
-            step *= fall;
             m = higher ? top : m;
-            // weights times V's share of the reference: the share's logarithm goes into the exponent, and out of the sum again by its
-            // inverse.  A pair of values takes three steps, some pairs apart: an exponential's result comes after some 40 cycles, and the
-            // unit takes one of a warp every 8, between which there is room for the other steps.
-            base = m == -KV_INF ? 0.f : m;
+            // A pair of values takes three steps, some pairs apart: an exponential's result comes after some 40 cycles, and the unit takes one
+            // of a warp every 8, between which there is room for the other steps.
             float up[4];
 #pragma unroll
             for (int g = 0; g < 4; g++) {
-                up[g] = sc[g].y - base;
+                up[g] = y[g] - m;
                 z[g] = sc[g].z;
             }
             // ask for the next step's scores now
@@ -306,9 +313,10 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
             kv_tmem_store32(p, at);                      // over the scores of the first 32 tokens
             if constexpr (!BF) kv_tmem_store32(rest, at + 32);
         };
-        if (ragged) pass(KvYes());
-        else pass(KvNo());
-        if (s > 0 && __any_sync(0xffffffffu, step != 1.f)) {
+        if (!(fabsf(k_most) * score_most < 0x1p22f)) pass(std::integral_constant<int, KV_TILE_LARGE>());
+        else if (ragged) pass(std::integral_constant<int, KV_TILE_RAGGED>());
+        else pass(std::integral_constant<int, KV_TILE_WHOLE>());
+        if (s > 0 && __any_sync(0xffffffffu, fall != 1.f)) {
             // behind the product of the step before, the last that has been issued
             fine = kv_warp_wait(bars + 8 * (KV_O_IN + m_tile), (s - 1) & 1, stop);
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -317,7 +325,7 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
                 uint32_t y[32];
                 kv_tmem_load32(y, o_at + 32 * b);
 #pragma unroll
-                for (int i = 0; i < 32; i++) y[i] = __float_as_uint(__uint_as_float(y[i]) * step);
+                for (int i = 0; i < 32; i++) y[i] = __float_as_uint(__uint_as_float(y[i]) * fall);
                 kv_tmem_store32(y, o_at + 32 * b);
             }
         }
@@ -335,20 +343,19 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
         const float total = (w[0] + w[1]) + (w[2] + w[3]);
         l += total;
         if (units && !small_units) {
-            if (t0 < end) units[(int64_t)(t0 >> 6) * unit_stride] = kv_log2(total) + base;
+            if (t0 < end) units[(int64_t)(t0 >> 6) * unit_stride] = kv_unit_log2(total, m);
         } else if (units) {
 #pragma unroll
             for (int g = 0; g < 4; g++) {
                 const int t = t0 + KV_HALF * g;
                 if (t < end && (S.block_tokens == 16 || !(g & 1)))
-                    units[(int64_t)(t >> S.block_shift) * unit_stride] = kv_log2(S.block_tokens == 16 ? w[g] : w[g] + w[g | 1]) + base;
+                    units[(int64_t)(t >> S.block_shift) * unit_stride] = kv_unit_log2(S.block_tokens == 16 ? w[g] : w[g] + w[g | 1], m);
             }
         }
     }
     if (fine && tiles > 0) fine = kv_warp_wait(bars + 8 * (KV_S_IN + 2 * m_tile), tiles & 1, stop);     // all products
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const float nan = __int_as_float(0x7fffffff), inv = !fine ? nan : l == 0.f ? 0.f : 1.f / l;
-    const float out_factor = A.splits == 1 ? inv * unit : fine ? unit : nan;
+    const float out_factor = !fine ? __int_as_float(0x7fffffff) : A.splits == 1 ? kv_over_sum(l) : 1.f;
 #pragma unroll
     for (int b = 0; b < D / 32; b++) {
         uint32_t x[32];
@@ -374,7 +381,7 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
     }
     if (!valid) return;
     if (A.splits == 1) {
-        const float l2 = l == 0.f ? -KV_INF : m + log2f(l);
+        const float l2 = kv_sum_log2(l, m);
         if (A.lse) A.lse[token * S.q_heads + head] = l2 * 0.6931471805599453f;
         A.lse2[kv_lse2_at(S, q, kh, row)] = l2;
     } else {
@@ -413,10 +420,9 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
     auto tail_power = [&](int which, int t) {
         uint32_t amax = 0;
         for (int i = lane; i < KV_HALF * D / 8; i += 32)
-            if (t + i / (D / 8) < q.len) amax = max(amax, kv_amax8(*(const uint4*)(tail + ((uint64_t)which * S.block_tokens + t - tail_begin) * D + 8 * i)));
+            if (t + i / (D / 8) < q.len) amax = max(amax, kv_amax8<true>(*(const uint4*)(tail + ((uint64_t)which * S.block_tokens + t - tail_begin) * D + 8 * i)));
         amax = __reduce_max_sync(0xffffffffu, amax);
-        const float least = which ? KV_V_LEAST : 0.f;
-        return which && amax == 0 ? least : fmaxf(kv_power_below(amax), least);
+        return which ? amax == 0 ? KV_V_ZERO : fmaxf(kv_power_below(amax), KV_V_LEAST) : kv_power_below(amax);
     };
     auto store = [&](const uint4 (&w)[2][P], int which, int t0, int2 kind, float2 power, uint8_t* dst) {
 #pragma unroll
@@ -456,7 +462,6 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
             }
         }
     };
-    float vref = 0.f, vinv = 0.f;                        // by the first warp's lanes
     uint4 kw[2][P], vw[2][P];
     int t0 = begin + 32 * warp;
     int2 kind = make_int2(kind_of(t0), kind_of(t0 + KV_HALF));
@@ -495,24 +500,13 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
             scale_page = scale_next;
             scale = scale_of(scale_page);
             scale_next = kind_of(tile0 + 2 * KV_P_TOKENS + KV_HALF * (lane & 7));
-            float most = vs;
-#pragma unroll
-            for (int d = 1; d < 8; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-            float step = 1.f;
-            if (most > vref) {
-                const float higher = 4.f * kv_power_below(__float_as_uint(most));
-                step = vref / higher;
-                vref = higher;
-                vinv = 1.f / higher;
-            }
-            const float share = vref > 0.f ? fmaxf(vs * vinv, KV_P_LEAST) * KV_P_SCALE : 1.f;
-            const bool some_absent = __any_sync(0xffffffffu, page == -1);
-            if (lane < 8) slot.group[lane] = make_float4(ks, vs == vs ? kv_log2(share) : vs, 1.f / share, page == -1 ? 0.f : 1.f);
-            if (lane == 0) {
-                slot.step = step;
-                slot.unit = vref > 0.f ? vref / KV_P_SCALE : 1.f;
-                slot.pad[0] = some_absent ? 1.f : 0.f;
-            }
+            const float2 share = kv_v_share(vs);
+            const uint32_t absent = __ballot_sync(0xffffffffu, page == -1), open = __ballot_sync(0xffffffffu, page == -2);
+            float k_most = ks;
+            k_most = fmaxf(k_most, __shfl_xor_sync(0xffffffffu, k_most, 1));
+            k_most = fmaxf(k_most, __shfl_xor_sync(0xffffffffu, k_most, 2));
+            if (lane < 8) slot.group[lane] = make_float4(ks, share.x, share.y, page == -1 ? 0.f : 1.f);
+            if (lane < 8 && (lane & 3) == 0) slot.k_most[lane >> 2] = copysignf(open >> lane & 15 ? KV_INF : k_most, absent >> lane & 15 ? -1.f : 1.f);
         }
         store(kw, 0, t0, kind, kp, sm + T::K + (j & 1) * T::TILE);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -614,7 +608,7 @@ __global__ void __launch_bounds__(KV_P_THREADS, 1) kv_prompt_kernel(const KvShap
     const uint32_t tmem = *(volatile uint32_t*)tmem_at;  // S_0, S_1, O_0, O_1: 128 columns each
 
     if (warp < 8) {
-        if (warp < 4 * parts) kv_prompt_rows<D, BF>(S, B, A, q, seq, kh, tile_row, warp >> 2, chunk, begin, end, tiles, sm, bars, stop, tmem);
+        if (warp < 4 * parts) kv_prompt_rows<D, BF, E4M3>(S, B, A, q, seq, kh, tile_row, warp >> 2, chunk, begin, end, tiles, sm, bars, stop, tmem);
     } else if (warp < 12) {
         kv_prompt_bring<D, BF, E4M3>(S, B, q, seq, kh, begin, end, tiles, sm, bars, stop);
     } else {

@@ -173,3 +173,47 @@ def test_zeros_in_the_unfinished_block_cost_nothing(dtype, new, group, block):
     c.pool[:, 2 * c.codes:2 * c.codes + 8 * c.kh].view(torch.float32).view(c.pages, c.kh, 2)[..., 1] *= small
     q, out, lse = attend(c)
     compare(c, out, lse, definition(c, q), least=2.0 ** -25 if dtype == kv.F16 else 2.0 ** -90)
+
+
+@pytest.mark.parametrize("dtype,ratio", [(kv.BF16, 2.0 ** 45), (kv.BF16, 2.0 ** 80), (kv.F16, 2.0 ** 24)])
+@pytest.mark.parametrize("fmt", [kv.INT8, kv.E4M3])
+@pytest.mark.parametrize("new,group,window", [(5, 1, 100), (16, 1, 100), (5, 3, 100), (8, 8, 100), (150, 2, 0), (150, 2, 100), (300, 1, 0)])
+def test_a_page_that_some_rows_do_not_see(dtype, ratio, fmt, new, group, window):
+    """One page's V is larger than all others' by orders of magnitude: rows that do not see it answer as without it."""
+    block = 16
+    L = 320 + new
+    first = L - new                                     # place of the first new token
+    # the page is at the first row's window's edge (its last token is seen by the first row only), or full of new tokens
+    big = (first - window + 1) // block if window else (first + new // 2) // block
+    if window:
+        L += (big * block + block - 1) - (first - window + 1)
+    c = Cache(dtype, fmt, 2 * group, 2, 64, block, [L, L], [new] * 2, seed=4)
+    c.fill(spread=0.3)
+    scales = c.pool[:, 2 * c.codes:2 * c.codes + 8 * c.kh].view(torch.float32).view(c.pages, c.kh, 2)
+    scales[..., 1] *= 2.0 ** -14 if dtype == kv.F16 else 2.0 ** -20
+    scales[int(c.table[0, big]), :, 1] *= ratio
+    q, out, lse = attend(c, window=window)
+    want = definition(c, q, window)
+    block_seen = want[2].amax((1, 2))[:new] > 2 * want[2].amax((1, 2))[new:].max()
+    assert bool(block_seen.any()) and not bool(block_seen.all())         # the case is what it says
+    got = out
+    if dtype == kv.F16:                                 # what the type cannot hold
+        over = want[0].abs() > 60000
+        got = torch.where(over.cuda(), want[0].cuda(), out.double())
+    compare(c, got, lse, want, least=2.0 ** -25 if dtype == kv.F16 else 2.0 ** -90)
+
+
+@pytest.mark.parametrize("new", [1, 5, 150])
+def test_a_page_of_large_values_and_little_weight(new):
+    """One page's V is larger by 2^60, and its tokens' weights are smaller by more than that."""
+    c = Cache(kv.BF16, kv.E4M3, 4, 2, 64, 16, [new + 300] * 2, [new] * 2, seed=6)
+    c.fill(spread=0.3)
+    q = torch.ones(c.total, c.qh, c.d, dtype=c.t, device="cuda")
+    page, scales = int(c.table[0, 5]), c.pool[:, 2 * c.codes:2 * c.codes + 8 * c.kh].view(torch.float32).view(c.pages, c.kh, 2)
+    scales[page, :, 1] *= 2.0 ** 60
+    scales[page, :, 0] = 1.0
+    codes = torch.full((c.codes,), -8.0).to(torch.float8_e4m3fn)         # scores of -64 (the others': within a few of 0)
+    c.pool[page, :c.codes] = codes.view(torch.uint8).cuda()
+    out = torch.full_like(q, -7.0)
+    lse = c.run_attention(q, out)
+    compare(c, out, lse, definition(c, q), least=2.0 ** -90)

@@ -416,8 +416,8 @@ __device__ __forceinline__ void kv_tile(KvState<D, NR>& W, const uint8_t* slot, 
     v_read();
 }
 
-// 16 tokens of the unfinished block: 16-bit values, tokens behind the last as zeros.  bf16 goes to f16 by a power of two near the
-// largest of the 16 tokens' K, or V.
+// 16 tokens of the unfinished block: 16-bit values, tokens behind the last as zeros.  bf16 goes to f16 by a power of two: K by one near the
+// token's largest value, so that no token's K, whatever it is, reaches another's score; V by one near the 16 tokens' largest.
 template <int D, bool BF, int NR>
 __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* k, const uint16_t* v, int t0, int len, const int (&place)[NR][2], int window,
                                              float* unit_out, int rows_left, int lane)
@@ -434,10 +434,10 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
     float s[1][NR][4];
 #pragma unroll
     for (int r = 0; r < NR; r++) s[0][r][0] = s[0][r][1] = s[0][r][2] = s[0][r][3] = 0.f;
-    float k_scale = 1.f, v_scale = 1.f;
+    float k_scale[2] = {1.f, 1.f}, v_scale = 1.f;        // of tokens g and g + 8
     {
         uint2 lo[STEPS], hi[STEPS];
-        uint32_t amax = 0;
+        uint32_t amax[2] = {0, 0};
 #pragma unroll
         for (int i = 0; i < STEPS; i++) {
             lo[i] = t0 + g < len ? *(const uint2*)(k + g * D + T::k_channel(i, c)) : make_uint2(0, 0);
@@ -445,13 +445,21 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
         }
         if (BF) {
 #pragma unroll
-            for (int i = 0; i < STEPS; i++) amax = amax2(amax2(amax2(amax2(amax, lo[i].x), lo[i].y), hi[i].x), hi[i].y);
-            k_scale = kv_power_below(__reduce_max_sync(0xffffffffu, amax));
+            for (int i = 0; i < STEPS; i++) {
+                amax[0] = amax2(amax2(amax[0], lo[i].x), lo[i].y);
+                amax[1] = amax2(amax2(amax[1], hi[i].x), hi[i].y);
+            }
+#pragma unroll
+            for (int up = 0; up < 2; up++) {
+                amax[up] = max(amax[up], __shfl_xor_sync(0xffffffffu, amax[up], 1));
+                amax[up] = max(amax[up], __shfl_xor_sync(0xffffffffu, amax[up], 2));
+                k_scale[up] = kv_power_below(amax[up]);
+            }
         }
-        const float inv = 1.f / k_scale;
+        const float inv[2] = {1.f / k_scale[0], 1.f / k_scale[1]};
 #pragma unroll
         for (int i = 0; i < STEPS; i++) {
-            const uint32_t a0 = narrow(lo[i].x, inv), a1 = narrow(hi[i].x, inv), a2 = narrow(lo[i].y, inv), a3 = narrow(hi[i].y, inv);
+            const uint32_t a0 = narrow(lo[i].x, inv[0]), a1 = narrow(hi[i].x, inv[1]), a2 = narrow(lo[i].y, inv[0]), a3 = narrow(hi[i].y, inv[1]);
 #pragma unroll
             for (int r = 0; r < NR; r++) kv_mma(s[0][r], a0, a1, a2, a3, W.qb[r][i]);
         }
@@ -477,7 +485,7 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
     for (int r = 0; r < NR; r++)
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            s[0][r][i] = fmaf(s[0][r][i], k_scale * W.factor[r][i & 1], share.x);
+            s[0][r][i] = fmaf(s[0][r][i] * k_scale[i >> 1], W.factor[r][i & 1], share.x);
             const int t = t0 + 8 * (i >> 1) + g, at = place[r][i & 1];
             if (t > at || (window > 0 && t <= at - window)) s[0][r][i] = -KV_INF;
         }

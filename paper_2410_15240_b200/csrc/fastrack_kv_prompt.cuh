@@ -152,14 +152,15 @@ template <bool E4M3> __device__ __forceinline__ void kv_widen16(const uint4& w, 
 enum { KV_K_IN = 0, KV_K_OUT = 4, KV_V_IN = 6, KV_V_OUT = 8, KV_S_IN = 10, KV_P_IN = 14, KV_O_IN = 18, KV_Q_IN = 20, KV_TAIL = 21, KV_END = 22, KV_BARS = 23 };
 
 // What a tile's slot of T::SCALES holds: per 16 tokens {K's scale, y and z of V's (see KV_P_MOST), whether the tokens are there}; and of each half
-// the largest scale of K, infinite for the unfinished block, negative where some tokens are not there.
+// the largest scale of K, negative where some tokens are not there.
 struct KvSlot { float4 group[KV_P_GROUPS]; float k_most[2], pad[2]; };
 enum { KV_TILE_WHOLE, KV_TILE_RAGGED, KV_TILE_LARGE };
 
-// 128 (query, head) rows' weights, made tile by tile by 128 threads, a row each; see the head of this file.
+// 128 (query, head) rows' weights, made tile by tile by 128 threads, a row each, and their answers; see the head of this file.
 template <int D, bool BF, bool E4M3>
 __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& B, const KvAttend& A, const KvSeq& q, int seq, int kh, int tile_row, int m_tile,
-                                               int chunk, int begin, int end, int tiles, uint8_t* sm, uint32_t bars, volatile int* stop, uint32_t tmem)
+                                               int chunk, int begin, int end, int tiles, uint8_t* sm, uint32_t bars, volatile int* stop, const volatile uint32_t* apart,
+                                               uint32_t tmem)
 {
     using T = KvPrompt<D>;
     const int warp = threadIdx.x >> 5, r = threadIdx.x & 127, rows = q.n * S.group, row = tile_row + KV_P_ROWS * m_tile + r;
@@ -355,10 +356,46 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
     }
     if (fine && tiles > 0) fine = kv_warp_wait(bars + 8 * (KV_S_IN + 2 * m_tile), tiles & 1, stop);     // all products
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    // Tokens of the unfinished block that the products left out, in 32 bits: the sum first, then with every 32 channels of the answer.
+    float lost = 1.f;                                    // what O is multiplied by for a new m
+    const uint32_t left_out = *apart;
+    const int tail_begin = q.full << S.block_shift, tail_tile = begin + (tail_begin - begin) / KV_P_TOKENS * KV_P_TOKENS;
+    const uint16_t* const tail = (const uint16_t*)B.tail + (uint64_t)seq * S.tail_values + (uint64_t)kh * 2 * S.block_tokens * D;
+    auto for_apart = [&](auto use) {                     // use(token's place in the tail, score in base 2)
+        for (int t = tail_begin; t < end; t++) {
+            if (!(left_out >> ((t - tail_tile) / KV_HALF) & 1) || t > place || (A.window > 0 && t <= place - A.window)) continue;
+            const uint16_t *qs = (const uint16_t*)A.q.data + token * A.q.token_stride + head * A.q.head_stride, *ks = tail + (int64_t)(t - tail_begin) * D;
+            float dot = 0.f;
+#pragma unroll 1
+            for (int ch = 0; ch < D; ch += 8) {
+                float a[8], b[8];
+                kv_widen8<BF>(*(const uint4*)(qs + ch), a);
+                kv_widen8<BF>(*(const uint4*)(ks + ch), b);
+#pragma unroll
+                for (int e = 0; e < 8; e++) dot = fmaf(a[e], b[e], dot);
+            }
+            use(t - tail_begin, dot * S.scale_log2);
+        }
+    };
+    if (left_out && valid) {
+        for_apart([&](int, float x) {
+            const float next = fmaxf(m, x), f = kv_exp2(m - next);
+            l = l * f + kv_exp2(x - next) * (1.f / 134217728);
+            lost *= f;
+            m = next;
+        });
+        if (units)
+            for_apart([&](int t, float x) {              // a unit's weight, token by token
+                float& unit = units[(int64_t)((tail_begin + t) >> A.unit_shift) * unit_stride];
+                const float most = fmaxf(unit, x);
+                unit = x == -KV_INF ? unit : most + kv_log2(kv_exp2(unit - most) + kv_exp2(x - most));
+            });
+    }
     const float out_factor = !fine ? __int_as_float(0x7fffffff) : A.splits == 1 ? kv_over_sum(l) : 1.f;
 #pragma unroll
     for (int b = 0; b < D / 32; b++) {
         uint32_t x[32];
+        __syncwarp();
         if (tiles > 0) {
             kv_tmem_load32(x, o_at + 32 * b);
         } else {
@@ -368,7 +405,24 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
         if (!valid) continue;
         float y[32];
 #pragma unroll
-        for (int i = 0; i < 32; i++) y[i] = l == 0.f && fine ? 0.f : __uint_as_float(x[i]) * out_factor;
+        for (int i = 0; i < 32; i++) y[i] = __uint_as_float(x[i]);
+        if (left_out) {
+#pragma unroll
+            for (int i = 0; i < 32; i++) y[i] *= lost;
+            for_apart([&](int t, float score) {
+                const float weight = kv_exp2(score - m);
+                const uint16_t* const vs = tail + ((int64_t)S.block_tokens + t) * D + 32 * b;
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) {
+                    float v[8];
+                    kv_widen8<BF>(*(const uint4*)(vs + i), v);
+#pragma unroll
+                    for (int e = 0; e < 8; e++) y[i + e] = fabsf(v[e]) < KV_INF ? fmaf(weight, v[e], y[i + e]) : y[i + e] + v[e];
+                }
+            });
+        }
+#pragma unroll
+        for (int i = 0; i < 32; i++) y[i] = l == 0.f && fine ? 0.f : y[i] * out_factor;
         if (A.splits == 1) {
             uint16_t* dst = (uint16_t*)A.out.data + token * A.out.token_stride + head * A.out.head_stride + 32 * b;
 #pragma unroll
@@ -392,7 +446,7 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
 // K and V of the tiles, widened to f16: 128 threads, of which warp w has tokens 32 w .. 32 w + 31 of a tile.
 template <int D, bool BF, bool E4M3>
 __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch& B, const KvSeq& q, int seq, int kh, int begin, int end, int tiles, uint8_t* sm,
-                                                uint32_t bars, volatile int* stop)
+                                                uint32_t bars, volatile int* stop, uint32_t* apart)
 {
     using T = KvPrompt<D>;
     // A lane's share of 16 tokens, P pieces of 16 channels.  Eight rows by four pieces of 64 channels at a time: eight lanes then write
@@ -416,14 +470,25 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
             for (int i = 0; i < P; i++) w[h][i] = page >= 0 ? __ldg((const uint4*)(src + row_of(lane, i) * D + channel_of(lane, i))) : make_uint4(0, 0, 0, 0);
         }
     };
-    // the largest magnitude of 16 tail tokens from t on, as a power of two not above it
-    auto tail_power = [&](int which, int t) {
-        uint32_t amax = 0;
-        for (int i = lane; i < KV_HALF * D / 8; i += 32)
-            if (t + i / (D / 8) < q.len) amax = max(amax, kv_amax8<true>(*(const uint4*)(tail + ((uint64_t)which * S.block_tokens + t - tail_begin) * D + 8 * i)));
-        amax = __reduce_max_sync(0xffffffffu, amax);
-        return which ? amax == 0 ? KV_V_ZERO : fmaxf(kv_power_below(amax), KV_V_LEAST) : kv_power_below(amax);
+    // Of the 16 tail tokens from t on, the largest values of K or V, as kv_amax8: the largest of them and the least that is not zero
+    auto tail_sizes = [&](int which, int t) {
+        constexpr int LANES = D == 64 ? 8 : 16, ROWS = 32 / LANES;           // lanes of a row (of 96 channels, 12 take part)
+        const int ch = lane % LANES * 8;
+        uint32_t most = 0, least = 0xffffffffu;
+#pragma unroll 4
+        for (int i = lane / LANES; i < KV_HALF; i += ROWS) {
+            uint32_t amax = t + i < q.len && ch < D ? kv_amax8<BF>(*(const uint4*)(tail + ((int64_t)which * S.block_tokens + t + i - tail_begin) * D + ch)) : 0u;
+#pragma unroll
+            for (int d = 1; d < LANES; d <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, d));
+            most = max(most, amax);
+            least = min(least, amax - 1u);               // zero counts as the largest
+        }
+        most = __reduce_max_sync(0xffffffffu, most);
+        least = __reduce_min_sync(0xffffffffu, least) + 1u;
+        return BF ? make_float2(__uint_as_float(most), __uint_as_float(least)) : make_float2(__half2float(__ushort_as_half(most)), __half2float(__ushort_as_half(least)));
     };
+    // What one power of two would not hold: what is not finite, and tokens whose largest values are 2^8 apart
+    auto wide = [&](float2 sizes) { return !(sizes.x < KV_INF) || (BF && sizes.x > 256.f * sizes.y); };
     auto store = [&](const uint4 (&w)[2][P], int which, int t0, int2 kind, float2 power, uint8_t* dst) {
 #pragma unroll
         for (int h = 0; h < 2; h++) {
@@ -476,37 +541,45 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
         KvSlot& slot = slots[j & 3];
         const int tile0 = begin + KV_P_TOKENS * j;
         if (!kv_warp_wait(bars + 8 * (KV_K_OUT + (j & 1)), (j >> 1 & 1) ^ 1, stop)) return;
-        if (BF && tile0 + KV_P_TOKENS > tail_begin && tail_begin < end) {
-            // the tail's powers of two go through the slot: y K's, z V's
-            if (kind.x == -2) { kp.x = tail_power(0, t0); vp.x = tail_power(1, t0); }
-            if (kind.y == -2) { kp.y = tail_power(0, t0 + KV_HALF); vp.y = tail_power(1, t0 + KV_HALF); }
-            if (lane == 0) {
-                slot.group[2 * warp].y = kp.x;
-                slot.group[2 * warp].z = vp.x;
-                slot.group[2 * warp + 1].y = kp.y;
-                slot.group[2 * warp + 1].z = vp.y;
+        if (tile0 + KV_P_TOKENS > tail_begin && tail_begin < end) {
+            // Once: the tail lies in one tile.  Its powers of two go through the slot: x and y for K and V, or 0 where the 16 tokens are left to the
+            // rows, which take them apart at the end.
+#pragma unroll 1
+            for (int h = 0; h < 2; h++) {
+                if ((h ? kind.y : kind.x) != -2) continue;
+                const float2 k = tail_sizes(0, t0 + KV_HALF * h), v = tail_sizes(1, t0 + KV_HALF * h);
+                const bool out = BF && wide(k);
+                float2 p = make_float2(kv_power_below(__float_as_uint(k.x)), !BF ? 1.f : v.x == 0.f ? KV_V_ZERO : fmaxf(kv_power_below(__float_as_uint(v.x)), KV_V_LEAST));
+                if (h) { kp.y = p.x; vp.y = p.y; } else { kp.x = p.x; vp.x = p.y; }
+                if (out) { if (h) kind.y = -1; else kind.x = -1; }
+                if (lane == 0) {
+                    slot.group[2 * warp + h].x = out ? 0.f : p.x;
+                    slot.group[2 * warp + h].y = p.y;
+                    if (out) atomicOr(apart, 1u << (2 * warp + h));
+                }
             }
             kv_warp_arrive(bars + 8 * KV_TAIL);
-            if (warp == 0 && !kv_warp_wait(bars + 8 * KV_TAIL, 0, stop)) return;   // once: the tail lies in one tile
+            if (warp == 0 && !kv_warp_wait(bars + 8 * KV_TAIL, 0, stop)) return;
         }
         if (warp == 0) {
             // lane g < 8: 16 tokens' scales, asked for a tile ahead
-            float ks = kv_finite(scale.x), vs = kv_finite(scale.y);
-            const int page = scale_page;
+            float ks = kv_finite(scale.x), vs = kv_finite(scale.y), k_most = ks;
+            int page = scale_page;
             if (page == -2) {
-                ks = BF ? slot.group[lane & 7].y : 1.f;
-                vs = BF ? slot.group[lane & 7].z : 1.f;
+                k_most = slot.group[lane & 7].x;
+                vs = slot.group[lane & 7].y;
+                ks = BF ? k_most : 1.f;
+                if (k_most == 0.f) page = -1;
             }
             scale_page = scale_next;
             scale = scale_of(scale_page);
             scale_next = kind_of(tile0 + 2 * KV_P_TOKENS + KV_HALF * (lane & 7));
             const float2 share = kv_v_share(vs);
-            const uint32_t absent = __ballot_sync(0xffffffffu, page == -1), open = __ballot_sync(0xffffffffu, page == -2);
-            float k_most = ks;
+            const uint32_t absent = __ballot_sync(0xffffffffu, page == -1);
             k_most = fmaxf(k_most, __shfl_xor_sync(0xffffffffu, k_most, 1));
             k_most = fmaxf(k_most, __shfl_xor_sync(0xffffffffu, k_most, 2));
             if (lane < 8) slot.group[lane] = make_float4(ks, share.x, share.y, page == -1 ? 0.f : 1.f);
-            if (lane < 8 && (lane & 3) == 0) slot.k_most[lane >> 2] = copysignf(open >> lane & 15 ? KV_INF : k_most, absent >> lane & 15 ? -1.f : 1.f);
+            if (lane < 8 && (lane & 3) == 0) slot.k_most[lane >> 2] = copysignf(k_most, absent >> lane & 15 ? -1.f : 1.f);
         }
         store(kw, 0, t0, kind, kp, sm + T::K + (j & 1) * T::TILE);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -592,7 +665,7 @@ __global__ void __launch_bounds__(KV_P_THREADS, 1) kv_prompt_kernel(const KvShap
     const int tiles = max((end - begin + KV_P_TOKENS - 1) / KV_P_TOKENS, 0), parts = tile_row + KV_P_ROWS < rows ? 2 : 1;
 
     volatile int* const stop = (volatile int*)(sm + T::BARS + 8 * KV_BARS);
-    uint32_t* const tmem_at = (uint32_t*)(sm + T::BARS + 8 * KV_BARS + 4);
+    uint32_t *const tmem_at = (uint32_t*)(sm + T::BARS + 8 * KV_BARS + 4), *const apart = tmem_at + 1;
     if (threadIdx.x == 0) {
         for (int i = 0; i < KV_BARS; i++) {
             const int count = i < KV_K_OUT || i == KV_V_IN || i == KV_V_IN + 1 || (i >= KV_P_IN && i < KV_O_IN) ? 4 : i == KV_Q_IN ? 4 * parts : i == KV_TAIL ? 4 : 1;
@@ -600,6 +673,7 @@ __global__ void __launch_bounds__(KV_P_THREADS, 1) kv_prompt_kernel(const KvShap
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *stop = 0;
+        *apart = 0;
     }
     if (warp == 12) asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"((uint32_t)__cvta_generic_to_shared(tmem_at)) : "memory");
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -608,9 +682,9 @@ __global__ void __launch_bounds__(KV_P_THREADS, 1) kv_prompt_kernel(const KvShap
     const uint32_t tmem = *(volatile uint32_t*)tmem_at;  // S_0, S_1, O_0, O_1: 128 columns each
 
     if (warp < 8) {
-        if (warp < 4 * parts) kv_prompt_rows<D, BF, E4M3>(S, B, A, q, seq, kh, tile_row, warp >> 2, chunk, begin, end, tiles, sm, bars, stop, tmem);
+        if (warp < 4 * parts) kv_prompt_rows<D, BF, E4M3>(S, B, A, q, seq, kh, tile_row, warp >> 2, chunk, begin, end, tiles, sm, bars, stop, apart, tmem);
     } else if (warp < 12) {
-        kv_prompt_bring<D, BF, E4M3>(S, B, q, seq, kh, begin, end, tiles, sm, bars, stop);
+        kv_prompt_bring<D, BF, E4M3>(S, B, q, seq, kh, begin, end, tiles, sm, bars, stop, apart);
     } else {
         kv_prompt_products<D, BF>(tiles, parts, sm_at, bars, stop, tmem);
         __syncwarp();

@@ -217,3 +217,42 @@ def test_a_page_of_large_values_and_little_weight(new):
     out = torch.full_like(q, -7.0)
     lse = c.run_attention(q, out)
     compare(c, out, lse, definition(c, q), least=2.0 ** -90)
+
+
+SPOIL = [math.nan, math.inf, -math.inf, 2.0 ** 60]
+
+
+@pytest.mark.parametrize("dtype", [kv.BF16, kv.F16])
+@pytest.mark.parametrize("value", SPOIL)
+@pytest.mark.parametrize("new,group,block", [(5, 1, 64), (3, 5, 16), (5, 8, 64), (150, 2, 128), (100, 1, 128)])
+def test_k_of_later_tokens(dtype, value, new, group, block):
+    """An infinite, NaN or huge K of the last new token reaches no query that does not see it."""
+    if dtype == kv.F16 and value == 2.0 ** 60:
+        value = 65504.0
+    c = Cache(dtype, kv.E4M3, 2 * group, 2, 64, block, [3 * block + block - 1, max(new, block + 7)], [new, new])
+    c.fill()
+    for i, L in enumerate(c.lens):
+        c.tail[i, :, 0, L % block - 1] = value
+    q, out, lse = attend(c)
+    want = definition(c, q)
+    last = torch.tensor([s - 1 for s in c.starts[1:]])
+    keep = torch.ones(c.total, dtype=torch.bool)
+    keep[last] = False
+    assert bool(torch.isfinite(want[0][keep]).all())
+    sub = tuple(x[keep] for x in want)
+    compare(c, out[keep.cuda()], lse[keep.cuda()], sub)
+    if math.isnan(value):
+        assert bool(torch.isnan(out[last.cuda()]).all())
+
+
+@pytest.mark.parametrize("dtype", [kv.BF16, kv.F16])
+@pytest.mark.parametrize("new,group", [(1, 4), (5, 8), (150, 1)])
+def test_a_score_of_minus_infinity(dtype, new, group):
+    """A seen token whose score is -infinity has no weight, and the others have the weights that they have without it."""
+    c = Cache(dtype, kv.INT8, 2 * group, 2, 64, 64, [64 + 40 + new - new % 64 if new > 24 else 104, 20 + new], [new, new])
+    c.fill()
+    q = torch.full((c.total, c.qh, c.d), 0.25, dtype=c.t, device="cuda")
+    c.tail[:, :, 0, 3, 5] = -math.inf
+    out = torch.full_like(q, -7.0)
+    lse = c.run_attention(q, out)
+    compare(c, out, lse, definition(c, q))

@@ -166,8 +166,19 @@ __device__ __forceinline__ float2 kv_v_share(float scale)
 // What an accumulated answer is multiplied by, for the sum l of its row: 2^-KV_L_BITS / l; 0 where the row saw nothing.
 __device__ __forceinline__ float kv_over_sum(float l)
 {
-    return l == 0.f ? 0.f : l < 1.f ? 1.f / (l * 134217728.f) : 1.f / 134217728 / l;
+    const float inv = 1.f / (l < 1.f ? l * 134217728.f : l);                 // of a sum whose inverse is a float
+    return l == 0.f ? 0.f : l < 1.f ? inv : inv * (1.f / 134217728);
 }
+
+// Of a power of two that one of these gave: its inverse, and y and z of V held over it
+__device__ __forceinline__ float kv_power_inverse(float p) { return __uint_as_float(0x7f000000u - __float_as_uint(p)); }
+__device__ __forceinline__ float2 kv_power_share(float p)
+{
+    return make_float2((float)((int)(__float_as_uint(p) >> 23) - 127), kv_power_inverse(p) * (1.f / 134217728));
+}
+
+// The power of two that V is held over, for values of at most this size (finite)
+__device__ __forceinline__ float kv_v_power(float amax) { return amax == 0.f ? KV_V_ZERO : fmaxf(kv_power_below(__float_as_uint(amax)), KV_V_LEAST); }
 
 // The largest magnitude of 8 values, as the bits of a float (bf16) or of an f16: 16-bit magnitudes are in the order of their bits
 template <bool BF> __device__ __forceinline__ uint32_t kv_amax8(const uint4& w)
@@ -416,8 +427,9 @@ __device__ __forceinline__ void kv_tile(KvState<D, NR>& W, const uint8_t* slot, 
     v_read();
 }
 
-// 16 tokens of the unfinished block: 16-bit values, tokens behind the last as zeros.  bf16 goes to f16 by a power of two: K by one near the
-// token's largest value, so that no token's K, whatever it is, reaches another's score; V by one near the 16 tokens' largest.
+// 16 tokens of the unfinished block: 16-bit values, tokens behind the last as zeros.  V, and bf16 K, go to f16 over a power of two near the token's
+// largest value, so that no token, whatever it holds, reaches a row that does not see it.  What is not finite in V stays out of the product (a
+// weight of 0 would not hide it there) and is added for the rows that see the token.
 template <int D, bool BF, int NR>
 __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* k, const uint16_t* v, int t0, int len, const int (&place)[NR][2], int window,
                                              float* unit_out, int rows_left, int lane)
@@ -434,7 +446,7 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
     float s[1][NR][4];
 #pragma unroll
     for (int r = 0; r < NR; r++) s[0][r][0] = s[0][r][1] = s[0][r][2] = s[0][r][3] = 0.f;
-    float k_scale[2] = {1.f, 1.f}, v_scale = 1.f;        // of tokens g and g + 8
+    float k_scale[2] = {1.f, 1.f};                       // of tokens g and g + 8
     {
         uint2 lo[STEPS], hi[STEPS];
         uint32_t amax[2] = {0, 0};
@@ -456,7 +468,7 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
                 k_scale[up] = kv_power_below(amax[up]);
             }
         }
-        const float inv[2] = {1.f / k_scale[0], 1.f / k_scale[1]};
+        const float inv[2] = {kv_power_inverse(k_scale[0]), kv_power_inverse(k_scale[1])};
 #pragma unroll
         for (int i = 0; i < STEPS; i++) {
             const uint32_t a0 = narrow(lo[i].x, inv[0]), a1 = narrow(hi[i].x, inv[1]), a2 = narrow(lo[i].y, inv[0]), a3 = narrow(hi[i].y, inv[1]);
@@ -472,20 +484,51 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
             const int t = 2 * c + (j & 1) + (j >> 1) * 8;
             w[i][j] = t0 + t < len ? *(const uint32_t*)(v + t * D + T::v_channel(g, 2 * i)) : 0u;
         }
-    if (BF) {
-        uint32_t amax = 0;
+    // the tokens' largest magnitudes as 16 bits: low and high half of sizes[u] of tokens 8 u + 2 c and 8 u + 2 c + 1
+    constexpr uint32_t INFINITE = BF ? 0x7f80u : 0x7c00u;
+    uint32_t sizes[2], odd = 0;                          // odd: tokens with values that are not finite
+    auto measure = [&] {
 #pragma unroll
-        for (int i = 0; i < STEPS; i++) amax = amax2(amax2(amax2(amax2(amax, w[i][0]), w[i][1]), w[i][2]), w[i][3]);
-        amax = __reduce_max_sync(0xffffffffu, amax);
-        v_scale = amax == 0 ? KV_V_ZERO : fmaxf(kv_power_below(amax), KV_V_LEAST);
+        for (int u = 0; u < 2; u++) {
+            uint32_t a[2] = {0, 0};
+#pragma unroll
+            for (int i = 0; i < STEPS; i++)
+#pragma unroll
+                for (int k = 0; k < 2; k++) a[k] = __vmaxu2(a[k], w[i][2 * u + k] & 0x7fff7fffu);
+            sizes[u] = max(a[0] & 0xffffu, a[0] >> 16) | max(a[1] & 0xffffu, a[1] >> 16) << 16;
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) sizes[u] = __vmaxu2(sizes[u], __shfl_xor_sync(0xffffffffu, sizes[u], d));
+        }
+    };
+    measure();
+#pragma unroll
+    for (int u = 0; u < 2; u++) odd |= ((sizes[u] & 0xffffu) >= INFINITE ? 1u : 0u) << (8 * u + 2 * c) | (sizes[u] >> 16 >= INFINITE ? 2u : 0u) << (8 * u + 2 * c);
+    odd = __reduce_or_sync(0xffffffffu, odd);
+    if (odd) {
+#pragma unroll
+        for (int i = 0; i < STEPS; i++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                if ((w[i][j] & 0x7fffu) >= INFINITE) w[i][j] &= 0xffff0000u;
+                if ((w[i][j] >> 16 & 0x7fffu) >= INFINITE) w[i][j] &= 0xffffu;
+            }
+        measure();
     }
-    const float2 share = kv_v_share(v_scale);
-    const float inv = 1.f / v_scale;
+    auto power = [](uint32_t size) { return kv_v_power(BF ? __uint_as_float(size << 16) : __half2float(__ushort_as_half((unsigned short)size))); };
+    float2 share[2];                                     // of tokens g and g + 8
+    float inv[4];                                        // of the tokens of w
+#pragma unroll
+    for (int u = 0; u < 2; u++) {
+        const uint32_t two = __shfl_sync(0xffffffffu, sizes[u], g >> 1);
+        share[u] = kv_power_share(power(g & 1 ? two >> 16 : two & 0xffffu));
+        inv[2 * u] = kv_power_inverse(power(sizes[u] & 0xffffu));
+        inv[2 * u + 1] = kv_power_inverse(power(sizes[u] >> 16));
+    }
 #pragma unroll
     for (int r = 0; r < NR; r++)
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            s[0][r][i] = fmaf(s[0][r][i] * k_scale[i >> 1], W.factor[r][i & 1], share.x);
+            s[0][r][i] = fmaf(s[0][r][i] * k_scale[i >> 1], W.factor[r][i & 1], share[i >> 1].x);
             const int t = t0 + 8 * (i >> 1) + g, at = place[r][i & 1];
             if (t > at || (window > 0 && t <= at - window)) s[0][r][i] = -KV_INF;
         }
@@ -495,7 +538,7 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
     for (int r = 0; r < NR; r++)
 #pragma unroll
         for (int e = 0; e < 2; e++) {
-            part[0][r][e] = (s[0][r][e] + s[0][r][2 + e]) * share.y;
+            part[0][r][e] = s[0][r][e] * share[0].y + s[0][r][2 + e] * share[1].y;
             W.l[r][e] += part[0][r][e];
         }
     if (unit_out) kv_note<NR, 1>(part, W.m, 0, 1, unit_out, rows_left, g, c);
@@ -508,13 +551,34 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
 #pragma unroll
     for (int i = 0; i < STEPS; i++) {
 #pragma unroll
-        for (int j = 0; j < 4; j++) w[i][j] = narrow(w[i][j], inv);
+        for (int j = 0; j < 4; j++) {
+            const float2 x = kv_unpack<BF>(w[i][j]);
+            w[i][j] = kv_pack<false>(x.x * inv[j], x.y * inv[j]);
+        }
         const uint32_t a0 = __byte_perm(w[i][0], w[i][1], 0x5410), a1 = __byte_perm(w[i][0], w[i][1], 0x7632), a2 = __byte_perm(w[i][2], w[i][3], 0x5410),
                        a3 = __byte_perm(w[i][2], w[i][3], 0x7632);
 #pragma unroll
         for (int r = 0; r < NR; r++) {
             kv_mma(W.o[r][i], a0, a1, a2, a3, pb[r]);
             if (!BF) kv_mma(W.o[r][i], a0, a1, a2, a3, pl[r]);
+        }
+    }
+    if (odd == 0) return;
+    auto not_finite = [](float x) { return fabsf(x) < KV_INF ? 0.f : x; };
+#pragma unroll 1
+    for (int t = 0; t < KV_HALF; t++) {
+        if (!(odd >> t & 1)) continue;
+#pragma unroll
+        for (int i = 0; i < STEPS; i++) {
+            const float2 x = kv_unpack<BF>(*(const uint32_t*)(v + t * D + T::v_channel(g, 2 * i)));
+#pragma unroll
+            for (int r = 0; r < NR; r++)
+#pragma unroll
+                for (int e = 0; e < 2; e++)
+                    if (t0 + t <= place[r][e] && (window == 0 || t0 + t > place[r][e] - window)) {
+                        W.o[r][i][e] += not_finite(x.x);
+                        W.o[r][i][2 + e] += not_finite(x.y);
+                    }
         }
     }
 }
@@ -602,7 +666,7 @@ __global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? (D == 64 ? 6 : 4) : 3
             amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
             amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
             p = kv_power_below(amax);
-            const float inv = 1.f / p;
+            const float inv = kv_power_inverse(p);
 #pragma unroll
             for (int s = 0; s < STEPS; s++)
 #pragma unroll

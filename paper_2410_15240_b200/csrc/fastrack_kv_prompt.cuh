@@ -26,7 +26,8 @@
 template <int D> struct KvPrompt {
     static constexpr int HALVES = (D + 63) / 64;                             // runs of 64 channels: 128-byte rows, swizzled by the row's number
     static constexpr int TILE = HALVES * KV_P_TOKENS * 128;                  // bytes of a tile of 128 rows as f16
-    static constexpr int Q = 0, K = 2 * TILE, V = 4 * TILE, SCALES = 6 * TILE, BARS = SCALES + 4 * (KV_P_GROUPS + 1) * 16, END = BARS + 256;
+    static constexpr int Q = 0, K = 2 * TILE, V = 4 * TILE, SCALES = 6 * TILE, POWERS = SCALES + 4 * (KV_P_GROUPS + 1) * 16,
+                         BARS = POWERS + KV_P_GROUPS * 8, END = BARS + 256;
     static constexpr int SMEM = END + 1024;                                  // the base is rounded up to 1024
     // byte of the 16-byte piece that holds channels ch .. ch + 7 of a row
     __device__ static int at(int row, int ch) { return (ch >> 6) * KV_P_TOKENS * 128 + row * 128 + (((ch >> 3 & 7) ^ (row & 7)) << 4); }
@@ -156,10 +157,34 @@ enum { KV_K_IN = 0, KV_K_OUT = 4, KV_V_IN = 6, KV_V_OUT = 8, KV_S_IN = 10, KV_P_
 struct KvSlot { float4 group[KV_P_GROUPS]; float k_most[2], pad[2]; };
 enum { KV_TILE_WHOLE, KV_TILE_RAGGED, KV_TILE_LARGE };
 
+// Of up to 16 tokens of the unfinished block, from src on, the largest values' magnitudes: the largest of them and the least that is not zero.  For a warp.
+template <int D, bool BF> __device__ __forceinline__ float2 kv_prompt_sizes(const uint16_t* src, int there)
+{
+    constexpr int LANES = D == 64 ? 8 : 16, ROWS = 32 / LANES, STEPS = KV_HALF / ROWS;       // lanes of a row (of 96 channels, 12 take part)
+    const int lane = threadIdx.x & 31, ch = lane % LANES * 8;
+    uint32_t amax[STEPS], most = 0, least = 0xffffffffu;
+#pragma unroll
+    for (int i = 0; i < STEPS; i++) {
+        const int row = i * ROWS + lane / LANES;
+        amax[i] = row < there && ch < D ? kv_amax8<BF>(*(const uint4*)(src + row * D + ch)) : 0u;
+    }
+#pragma unroll
+    for (int i = 0; i < STEPS; i++) {
+#pragma unroll
+        for (int d = 1; d < LANES; d <<= 1) amax[i] = max(amax[i], __shfl_xor_sync(0xffffffffu, amax[i], d));
+        most = max(most, amax[i]);
+        least = min(least, amax[i] - 1u);                // zero counts as the largest
+    }
+    most = __reduce_max_sync(0xffffffffu, most);
+    least = __reduce_min_sync(0xffffffffu, least) + 1u;
+    return BF ? make_float2(__uint_as_float(most), __uint_as_float(least))
+              : make_float2(__half2float(__ushort_as_half((unsigned short)most)), __half2float(__ushort_as_half((unsigned short)least)));
+}
+
 // 128 (query, head) rows' weights, made tile by tile by 128 threads, a row each, and their answers; see the head of this file.
 template <int D, bool BF, bool E4M3>
 __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& B, const KvAttend& A, const KvSeq& q, int seq, int kh, int tile_row, int m_tile,
-                                               int chunk, int begin, int end, int tiles, uint8_t* sm, uint32_t bars, volatile int* stop, const volatile uint32_t* apart,
+                                               int chunk, int begin, int end, int tiles, uint8_t* sm, uint32_t bars, volatile int* stop, uint32_t* apart,
                                                uint32_t tmem)
 {
     using T = KvPrompt<D>;
@@ -169,6 +194,7 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
     const int head = kh * S.group + row % S.group, place = valid ? q.len - q.n + row / S.group : -1;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21, s_at = tmem + lanes + 128 * m_tile, o_at = tmem + lanes + 256 + 128 * m_tile;
     const KvSlot* const slots = (const KvSlot*)(sm + T::SCALES);
+    const int warps = tile_row + KV_P_ROWS < rows ? 8 : 4;                   // that do this
     float factor = S.scale_log2, score_most;
     {
         // the row of Q, as f16 (bf16: over a power of two near its largest), to shared memory
@@ -180,7 +206,7 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
         if (BF) {
             const float p = kv_power_below(amax);
             factor *= p;
-            inv = 1.f / p;
+            inv = kv_power_inverse(p);
         } else {
             most = __half2float(__ushort_as_half((unsigned short)amax));
         }
@@ -200,6 +226,23 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         kv_warp_arrive(bars + 8 * KV_Q_IN);
+    }
+    // Powers of two for the unfinished block, 16 tokens at a time, while the first codes come.  What one power would not hold (values that are not
+    // finite, tokens whose largest values are 2^8 apart; f16 K needs none) stays out of the products: the rows take it apart at the end.
+    const int tail_begin = q.full << S.block_shift, tail_tile = begin + (tail_begin - begin) / KV_P_TOKENS * KV_P_TOKENS;
+    const uint16_t* const tail = (const uint16_t*)B.tail + (uint64_t)seq * S.tail_values + (uint64_t)kh * 2 * S.block_tokens * D;
+    if (tail_begin < end) {
+        for (int g = warp; g < KV_P_GROUPS; g += warps) {
+            const int t = tail_tile + KV_HALF * g, there = min(KV_HALF, q.len - t);
+            if (t < tail_begin || t >= end) continue;
+            const float2 k = kv_prompt_sizes<D, BF>(tail + (int64_t)(t - tail_begin) * D, there), v = kv_prompt_sizes<D, BF>(tail + ((int64_t)S.block_tokens + t - tail_begin) * D, there);
+            auto wide = [](float2 sizes) { return !(sizes.x < KV_INF) || sizes.x > 256.f * sizes.y; };
+            if ((threadIdx.x & 31) == 0) {
+                ((float2*)(sm + T::POWERS))[g] = make_float2(kv_power_below(__float_as_uint(k.x)), kv_v_power(v.x));
+                if ((BF && wide(k)) || wide(v)) atomicOr(apart, 1u << g);
+            }
+        }
+        kv_warp_arrive(bars + 8 * KV_TAIL);
     }
     // rows of this warp: tokens up to see_all are seen by all of them, tokens behind low_all are in every one's window
     const int first_row = tile_row + KV_P_ROWS * m_tile + 32 * (warp & 3), last_row = min(first_row + 31, rows - 1);
@@ -358,9 +401,7 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     // Tokens of the unfinished block that the products left out, in 32 bits: the sum first, then with every 32 channels of the answer.
     float lost = 1.f;                                    // what O is multiplied by for a new m
-    const uint32_t left_out = *apart;
-    const int tail_begin = q.full << S.block_shift, tail_tile = begin + (tail_begin - begin) / KV_P_TOKENS * KV_P_TOKENS;
-    const uint16_t* const tail = (const uint16_t*)B.tail + (uint64_t)seq * S.tail_values + (uint64_t)kh * 2 * S.block_tokens * D;
+    const uint32_t left_out = *(volatile uint32_t*)apart;
     auto for_apart = [&](auto use) {                     // use(token's place in the tail, score in base 2)
         for (int t = tail_begin; t < end; t++) {
             if (!(left_out >> ((t - tail_tile) / KV_HALF) & 1) || t > place || (A.window > 0 && t <= place - A.window)) continue;
@@ -446,7 +487,7 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
 // K and V of the tiles, widened to f16: 128 threads, of which warp w has tokens 32 w .. 32 w + 31 of a tile.
 template <int D, bool BF, bool E4M3>
 __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch& B, const KvSeq& q, int seq, int kh, int begin, int end, int tiles, uint8_t* sm,
-                                                uint32_t bars, volatile int* stop, uint32_t* apart)
+                                                uint32_t bars, volatile int* stop, const volatile uint32_t* apart)
 {
     using T = KvPrompt<D>;
     // A lane's share of 16 tokens, P pieces of 16 channels.  Eight rows by four pieces of 64 channels at a time: eight lanes then write
@@ -470,26 +511,8 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
             for (int i = 0; i < P; i++) w[h][i] = page >= 0 ? __ldg((const uint4*)(src + row_of(lane, i) * D + channel_of(lane, i))) : make_uint4(0, 0, 0, 0);
         }
     };
-    // Of the 16 tail tokens from t on, the largest values of K or V, as kv_amax8: the largest of them and the least that is not zero
-    auto tail_sizes = [&](int which, int t) {
-        constexpr int LANES = D == 64 ? 8 : 16, ROWS = 32 / LANES;           // lanes of a row (of 96 channels, 12 take part)
-        const int ch = lane % LANES * 8;
-        uint32_t most = 0, least = 0xffffffffu;
-#pragma unroll 4
-        for (int i = lane / LANES; i < KV_HALF; i += ROWS) {
-            uint32_t amax = t + i < q.len && ch < D ? kv_amax8<BF>(*(const uint4*)(tail + ((int64_t)which * S.block_tokens + t + i - tail_begin) * D + ch)) : 0u;
-#pragma unroll
-            for (int d = 1; d < LANES; d <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, d));
-            most = max(most, amax);
-            least = min(least, amax - 1u);               // zero counts as the largest
-        }
-        most = __reduce_max_sync(0xffffffffu, most);
-        least = __reduce_min_sync(0xffffffffu, least) + 1u;
-        return BF ? make_float2(__uint_as_float(most), __uint_as_float(least)) : make_float2(__half2float(__ushort_as_half(most)), __half2float(__ushort_as_half(least)));
-    };
-    // What one power of two would not hold: what is not finite, and tokens whose largest values are 2^8 apart
-    auto wide = [&](float2 sizes) { return !(sizes.x < KV_INF) || (BF && sizes.x > 256.f * sizes.y); };
-    auto store = [&](const uint4 (&w)[2][P], int which, int t0, int2 kind, float2 power, uint8_t* dst) {
+    const volatile float2* const powers = (const volatile float2*)(sm + T::POWERS);
+    auto store = [&](const uint4 (&w)[2][P], int which, int t0, int2 kind, uint8_t* dst) {
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             if ((h ? kind.y : kind.x) != -2) {
@@ -503,7 +526,7 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
                 }
                 continue;
             }
-            const float inv = 1.f / (h ? power.y : power.x);
+            const float inv = kv_power_inverse(which ? powers[2 * warp + h].y : powers[2 * warp + h].x);
 #pragma unroll 1
             for (int i = 0; i < P; i++) {
                 const int row = KV_HALF * h + row_of(lane, i), ch = channel_of(lane, i);
@@ -512,11 +535,11 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
                     const uint4* src = (const uint4*)(tail + ((uint64_t)which * S.block_tokens + t0 + row - tail_begin) * D + ch);
                     v[0] = src[0];
                     v[1] = src[1];
-                    if (BF)
+                    if (BF || which)
 #pragma unroll
                         for (int k = 0; k < 2; k++) {
                             float x[8];
-                            kv_widen8<true>(v[k], x);
+                            kv_widen8<BF>(v[k], x);
 #pragma unroll
                             for (int e = 0; e < 8; e++) x[e] *= inv;
                             v[k] = kv_narrow8<false>(x);
@@ -537,39 +560,24 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
     float2 scale = scale_of(scale_page);
     for (int j = 0; j < tiles; j++, t0 += KV_P_TOKENS) {
         const int2 next = make_int2(kind_of(t0 + KV_P_TOKENS), kind_of(t0 + KV_P_TOKENS + KV_HALF));
-        float2 kp = make_float2(1.f, 1.f), vp = kp;
         KvSlot& slot = slots[j & 3];
         const int tile0 = begin + KV_P_TOKENS * j;
         if (!kv_warp_wait(bars + 8 * (KV_K_OUT + (j & 1)), (j >> 1 & 1) ^ 1, stop)) return;
         if (tile0 + KV_P_TOKENS > tail_begin && tail_begin < end) {
-            // Once: the tail lies in one tile.  Its powers of two go through the slot: x and y for K and V, or 0 where the 16 tokens are left to the
-            // rows, which take them apart at the end.
-#pragma unroll 1
-            for (int h = 0; h < 2; h++) {
-                if ((h ? kind.y : kind.x) != -2) continue;
-                const float2 k = tail_sizes(0, t0 + KV_HALF * h), v = tail_sizes(1, t0 + KV_HALF * h);
-                const bool out = BF && wide(k);
-                float2 p = make_float2(kv_power_below(__float_as_uint(k.x)), !BF ? 1.f : v.x == 0.f ? KV_V_ZERO : fmaxf(kv_power_below(__float_as_uint(v.x)), KV_V_LEAST));
-                if (h) { kp.y = p.x; vp.y = p.y; } else { kp.x = p.x; vp.x = p.y; }
-                if (out) { if (h) kind.y = -1; else kind.x = -1; }
-                if (lane == 0) {
-                    slot.group[2 * warp + h].x = out ? 0.f : p.x;
-                    slot.group[2 * warp + h].y = p.y;
-                    if (out) atomicOr(apart, 1u << (2 * warp + h));
-                }
-            }
-            kv_warp_arrive(bars + 8 * KV_TAIL);
-            if (warp == 0 && !kv_warp_wait(bars + 8 * KV_TAIL, 0, stop)) return;
+            // once: the tail lies in one tile
+            if (!kv_warp_wait(bars + 8 * KV_TAIL, 0, stop)) return;
+            if (*apart >> 2 * warp & 1) kind.x = -1;
+            if (*apart >> 2 * warp & 2) kind.y = -1;
         }
         if (warp == 0) {
             // lane g < 8: 16 tokens' scales, asked for a tile ahead
             float ks = kv_finite(scale.x), vs = kv_finite(scale.y), k_most = ks;
             int page = scale_page;
             if (page == -2) {
-                k_most = slot.group[lane & 7].x;
-                vs = slot.group[lane & 7].y;
+                k_most = powers[lane & 7].x;
+                vs = powers[lane & 7].y;
                 ks = BF ? k_most : 1.f;
-                if (k_most == 0.f) page = -1;
+                if (*apart >> (lane & 7) & 1) page = -1;
             }
             scale_page = scale_next;
             scale = scale_of(scale_page);
@@ -581,12 +589,12 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
             if (lane < 8) slot.group[lane] = make_float4(ks, share.x, share.y, page == -1 ? 0.f : 1.f);
             if (lane < 8 && (lane & 3) == 0) slot.k_most[lane >> 2] = copysignf(k_most, absent >> lane & 15 ? -1.f : 1.f);
         }
-        store(kw, 0, t0, kind, kp, sm + T::K + (j & 1) * T::TILE);
+        store(kw, 0, t0, kind, sm + T::K + (j & 1) * T::TILE);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         kv_warp_arrive(bars + 8 * (KV_K_IN + (j & 3)));
         codes(kw, 0, t0 + KV_P_TOKENS, next);
         if (!kv_warp_wait(bars + 8 * (KV_V_OUT + (j & 1)), (j >> 1 & 1) ^ 1, stop)) return;
-        store(vw, 1, t0, kind, vp, sm + T::V + (j & 1) * T::TILE);
+        store(vw, 1, t0, kind, sm + T::V + (j & 1) * T::TILE);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         kv_warp_arrive(bars + 8 * (KV_V_IN + (j & 1)));
         codes(vw, 1, t0 + KV_P_TOKENS, next);
@@ -668,7 +676,7 @@ __global__ void __launch_bounds__(KV_P_THREADS, 1) kv_prompt_kernel(const KvShap
     uint32_t *const tmem_at = (uint32_t*)(sm + T::BARS + 8 * KV_BARS + 4), *const apart = tmem_at + 1;
     if (threadIdx.x == 0) {
         for (int i = 0; i < KV_BARS; i++) {
-            const int count = i < KV_K_OUT || i == KV_V_IN || i == KV_V_IN + 1 || (i >= KV_P_IN && i < KV_O_IN) ? 4 : i == KV_Q_IN ? 4 * parts : i == KV_TAIL ? 4 : 1;
+            const int count = i < KV_K_OUT || i == KV_V_IN || i == KV_V_IN + 1 || (i >= KV_P_IN && i < KV_O_IN) ? 4 : i == KV_Q_IN ? 4 * parts : i == KV_TAIL ? 4 * parts : 1;
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bars + 8 * i), "r"(count) : "memory");
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");

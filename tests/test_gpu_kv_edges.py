@@ -162,7 +162,7 @@ def test_tiny_values_in_the_unfinished_block(new, size):
     compare(c, out, lse, definition(c, q), least=2.0 ** -118 if new < 24 else 2.0 ** -24)
 
 
-@pytest.mark.parametrize("dtype", [kv.BF16])
+@pytest.mark.parametrize("dtype", [kv.BF16, kv.F16])
 @pytest.mark.parametrize("new,group,block", [(1, 4, 64), (5, 1, 16), (5, 8, 32), (150, 2, 64)])
 def test_zeros_in_the_unfinished_block_cost_nothing(dtype, new, group, block):
     """V of zeros (no matter at what power of two they are held) beside pages with small scales, whose answers keep their bits."""
@@ -255,4 +255,45 @@ def test_a_score_of_minus_infinity(dtype, new, group):
     c.tail[:, :, 0, 3, 5] = -math.inf
     out = torch.full_like(q, -7.0)
     lse = c.run_attention(q, out)
+    compare(c, out, lse, definition(c, q))
+
+
+@pytest.mark.parametrize("dtype", [kv.BF16, kv.F16])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf, 2.0 ** 100])
+@pytest.mark.parametrize("new,group,block", [(1, 4, 64), (5, 1, 64), (3, 5, 16), (5, 8, 64), (150, 2, 128), (100, 1, 128)])
+def test_v_of_later_tokens(dtype, value, new, group, block):
+    """An infinite, NaN or huge V of the last new token reaches no query that does not see it, and shows in those that do, in its
+    channels."""
+    if dtype == kv.F16 and value == 2.0 ** 100:
+        value = 65504.0
+    c = Cache(dtype, kv.E4M3, 2 * group, 2, 64, block, [3 * block + block - 1, max(new, block + 7)], [new, new])
+    c.fill()
+    for i, L in enumerate(c.lens):
+        c.tail[i, :, 1, L % block - 1, 3:50] = value
+    q, out, lse = attend(c)
+    compare(c, out, lse, definition(c, q))
+
+
+@pytest.mark.parametrize("new,group", [(5, 2), (150, 1)])
+def test_infinities_of_both_signs(new, group):
+    """Where a query sees both, NaN; where it sees one, that one."""
+    c = Cache(kv.F16, kv.INT8, 2 * group, 2, 96, 32, [new + 96 - new % 32 + 20] * 2, [new, new])
+    c.fill()
+    rest = c.lens[0] % 32
+    c.tail[:, :, 1, rest - 3, 7] = math.inf
+    c.tail[:, :, 1, rest - 2, 7] = -math.inf
+    c.tail[:, :, 1, rest - 2, 90] = -math.inf
+    c.tail[1, :, 1, 0, 33] = math.nan
+    q, out, lse = attend(c)
+    compare(c, out, lse, definition(c, q))
+
+
+@pytest.mark.parametrize("new,group,block", [(1, 4, 64), (5, 8, 128), (150, 2, 128)])
+def test_values_of_very_different_sizes(new, group, block):
+    """V of tokens that a query does not see may be larger by any power."""
+    c = Cache(kv.BF16, kv.INT8, 2 * group, 2, 64, block, [block + block - 3, max(new, block - 2)], [new, new], seed=9)
+    c.fill()
+    power = torch.exp2(torch.arange(block, device="cuda").float() * 0.5)[:, None]      # later ones larger, up to 2^63
+    c.tail[:, :, 1] = torch.where(torch.isnan(c.tail[:, :, 1]), c.tail[:, :, 1], c.tail[:, :, 1] * power)
+    q, out, lse = attend(c)
     compare(c, out, lse, definition(c, q))

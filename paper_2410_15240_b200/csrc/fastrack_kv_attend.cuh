@@ -180,10 +180,17 @@ __device__ __forceinline__ float2 kv_power_share(float p)
 // The power of two that V is held over, for values of at most this size (finite)
 __device__ __forceinline__ float kv_v_power(float amax) { return amax == 0.f ? KV_V_ZERO : fmaxf(kv_power_below(__float_as_uint(amax)), KV_V_LEAST); }
 
+// The larger of two 16-bit numbers, twice
+__device__ __forceinline__ uint32_t kv_max2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
 // The largest magnitude of 8 values, as the bits of a float (bf16) or of an f16: 16-bit magnitudes are in the order of their bits
 template <bool BF> __device__ __forceinline__ uint32_t kv_amax8(const uint4& w)
 {
-    const uint32_t m = 0x7fff7fffu, a = __vmaxu2(__vmaxu2(w.x & m, w.y & m), __vmaxu2(w.z & m, w.w & m)), most = max(a & 0xffffu, a >> 16);
+    const uint32_t m = 0x7fff7fffu, a = kv_max2(kv_max2(w.x & m, w.y & m), kv_max2(w.z & m, w.w & m)), most = max(a & 0xffffu, a >> 16);
     return BF ? most << 16 : most;
 }
 
@@ -494,17 +501,18 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
 #pragma unroll
             for (int i = 0; i < STEPS; i++)
 #pragma unroll
-                for (int k = 0; k < 2; k++) a[k] = __vmaxu2(a[k], w[i][2 * u + k] & 0x7fff7fffu);
+                for (int k = 0; k < 2; k++) a[k] = kv_max2(a[k], w[i][2 * u + k] & 0x7fff7fffu);
             sizes[u] = max(a[0] & 0xffffu, a[0] >> 16) | max(a[1] & 0xffffu, a[1] >> 16) << 16;
 #pragma unroll
-            for (int d = 4; d < 32; d <<= 1) sizes[u] = __vmaxu2(sizes[u], __shfl_xor_sync(0xffffffffu, sizes[u], d));
+            for (int d = 4; d < 32; d <<= 1) sizes[u] = kv_max2(sizes[u], __shfl_xor_sync(0xffffffffu, sizes[u], d));
         }
     };
     measure();
+    const uint32_t both = kv_max2(sizes[0], sizes[1]);
+    if (__any_sync(0xffffffffu, (both & 0xffffu) >= INFINITE || both >> 16 >= INFINITE)) {
 #pragma unroll
-    for (int u = 0; u < 2; u++) odd |= ((sizes[u] & 0xffffu) >= INFINITE ? 1u : 0u) << (8 * u + 2 * c) | (sizes[u] >> 16 >= INFINITE ? 2u : 0u) << (8 * u + 2 * c);
-    odd = __reduce_or_sync(0xffffffffu, odd);
-    if (odd) {
+        for (int u = 0; u < 2; u++) odd |= ((sizes[u] & 0xffffu) >= INFINITE ? 1u : 0u) << (8 * u + 2 * c) | (sizes[u] >> 16 >= INFINITE ? 2u : 0u) << (8 * u + 2 * c);
+        odd = __reduce_or_sync(0xffffffffu, odd);
 #pragma unroll
         for (int i = 0; i < STEPS; i++)
 #pragma unroll

@@ -21,6 +21,7 @@
 #define KV_P_TOKENS 128
 #define KV_P_THREADS 416
 #define KV_P_GROUPS (KV_P_TOKENS / KV_HALF)
+#define KV_P_LARGE 0x1p22f              // bound of a score from which on tokens are taken apart
 #define KV_P_AHEAD 4                   // pairs of values between an exponential and the use of its result
 
 template <int D> struct KvPrompt {
@@ -155,7 +156,20 @@ enum { KV_K_IN = 0, KV_K_OUT = 4, KV_V_IN = 6, KV_V_OUT = 8, KV_S_IN = 10, KV_P_
 // What a tile's slot of T::SCALES holds: per 16 tokens {K's scale, y and z of V's (see KV_P_MOST), whether the tokens are there}; and of each half
 // the largest scale of K, negative where some tokens are not there.
 struct KvSlot { float4 group[KV_P_GROUPS]; float k_most[2], pad[2]; };
-enum { KV_TILE_WHOLE, KV_TILE_RAGGED, KV_TILE_LARGE };
+
+// 8 channels of K (which = 0) or V (1) of a kv head's token, from the sequence's tail (page -2) or a page, as 32-bit numbers
+template <bool BF, bool E4M3>
+__device__ __forceinline__ void kv_held8(const KvShape& S, const KvBatch& B, const uint16_t* tail, int kh, int which, int page, int at, int ch, float* x)
+{
+    if (page == -2) {
+        kv_widen8<BF>(*(const uint4*)(tail + ((int64_t)which * S.block_tokens + at) * S.head_dim + ch), x);
+    } else {
+        const float scale = kv_finite(kv_scales(S, B, page)[2 * kh + which]);
+        const uint2 codes = *(const uint2*)(B.pool + (uint64_t)page * S.page_bytes + (uint64_t)which * S.codes_bytes + ((uint64_t)kh * S.block_tokens + at) * S.head_dim + ch);
+        kv_decode4<E4M3>(codes.x, scale, x);
+        kv_decode4<E4M3>(codes.y, scale, x + 4);
+    }
+}
 
 // Of up to 16 tokens of the unfinished block, from src on, the largest values' magnitudes: the largest of them and the least that is not zero.  For a warp.
 template <int D, bool BF> __device__ __forceinline__ float2 kv_prompt_sizes(const uint16_t* src, int there)
@@ -201,17 +215,13 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
         const uint16_t* src = (const uint16_t*)A.q.data + token * A.q.token_stride + head * A.q.head_stride;
         float inv = 1.f, most = 2.f;                     // most: no value of the row, as f16, is larger
         uint32_t amax = 0;
-#pragma unroll 4
-        for (int i = 0; i < D / 8; i++) amax = max(amax, valid ? kv_amax8<BF>(*(const uint4*)(src + 8 * i)) : 0u);
         if (BF) {
+#pragma unroll 4
+            for (int i = 0; i < D / 8; i++) amax = max(amax, valid ? kv_amax8<true>(*(const uint4*)(src + 8 * i)) : 0u);
             const float p = kv_power_below(amax);
             factor *= p;
             inv = kv_power_inverse(p);
-        } else {
-            most = __half2float(__ushort_as_half((unsigned short)amax));
         }
-        // no score of the warp's rows is larger than this times K's scale
-        score_most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(factor * most))) * (D * (E4M3 ? 448.f : 127.f));
 #pragma unroll 4
         for (int i = 0; i < D / 8; i++) {
             uint4 w = valid ? *(const uint4*)(src + 8 * i) : make_uint4(0, 0, 0, 0);
@@ -221,11 +231,16 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
 #pragma unroll
                 for (int e = 0; e < 8; e++) x[e] *= inv;
                 w = kv_narrow8<false>(x);
+            } else {
+                amax = max(amax, kv_amax8<false>(w));
             }
             *(uint4*)(sm + T::Q + m_tile * T::TILE + T::at(r, 8 * i)) = w;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         kv_warp_arrive(bars + 8 * KV_Q_IN);
+        if (!BF) most = __half2float(__ushort_as_half((unsigned short)amax));
+        // no score of the warp's rows is larger than this times K's scale
+        score_most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(factor * most))) * (D * (E4M3 ? 448.f : 127.f));
     }
     // Powers of two for the unfinished block, 16 tokens at a time, while the first codes come.  What one power would not hold (values that are not
     // finite, tokens whose largest values are 2^8 apart; f16 K needs none) stays out of the products: the rows take it apart at the end.
@@ -252,7 +267,7 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
     float* const units = A.unit_l2 && valid ? A.unit_l2 + ((int64_t)seq * S.kv_heads + kh) * A.units * unit_stride + row : nullptr;
     const bool small_units = units && S.block_tokens < 64;
     float m = KV_M_NONE, l = 0.f;                        // see KV_P_MOST
-    bool fine = true;
+    bool fine = true, some_large = false;
     // Steps of 64 tokens: while this one's weights are made, the next one's scores are (in the other half of S).
     uint32_t ended = 0;                                  // whether this step's scores are known to be there
     for (int s = 0; s < 2 * tiles && fine; s++) {
@@ -270,21 +285,20 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
         const bool ragged = __float_as_int(k_most) < 0 || t0 + 63 > see_all || t0 <= low_all;
         float fall = 1.f, z[4];                          // fall: what l and O are multiplied by
         uint64_t sum[4] = {0, 0, 0, 0};                  // of 16 tokens' weights each
-        // LARGE: where a score may be so large that y - m would be rounded to steps of a quarter or more, s + y is formed first, for the largest
-        // and for the weights alike.
-        auto pass = [&](auto kind) {
-            constexpr bool LARGE = decltype(kind)::value == KV_TILE_LARGE, RAGGED = LARGE || decltype(kind)::value == KV_TILE_RAGGED;
+        // Scores may be so large that y - m would be rounded to steps of a quarter or more: these rows see nothing here, and take the tokens apart at
+        // the end.
+        const bool large = !(fabsf(k_most) * score_most < KV_P_LARGE);
+        some_large |= large;
+        auto pass = [&](auto some_hidden) {
+            constexpr bool RAGGED = decltype(some_hidden)::value;
             uint32_t seen[2] = {0xffffffffu, 0xffffffffu};                   // which of 32 tokens the row sees
-            float f[4], y[4];
+            float f[4];
 #pragma unroll
-            for (int g = 0; g < 4; g++) {
-                f[g] = LARGE ? 1.f : sc[g].x * factor;
-                y[g] = LARGE ? 0.f : sc[g].y;
-            }
+            for (int g = 0; g < 4; g++) f[g] = sc[g].x * factor;
             if (RAGGED)
 #pragma unroll
                 for (int b = 0; b < 2; b++) {
-                    const int t = t0 + 32 * b, upto = min(max(place - t + 1, 0), 32), from = A.window > 0 ? min(max(place - A.window + 1 - t, 0), 32) : 0;
+                    const int t = t0 + 32 * b, upto = large ? 0 : min(max(place - t + 1, 0), 32), from = A.window > 0 ? min(max(place - A.window + 1 - t, 0), 32) : 0;
                     seen[b] = (uint32_t)(((uint64_t)1 << upto) - 1) & ~(uint32_t)(((uint64_t)1 << from) - 1);
                     if (sc[2 * b].w == 0.f) seen[b] &= 0xffff0000u;
                     if (sc[2 * b + 1].w == 0.f) seen[b] &= 0x0000ffffu;
@@ -295,9 +309,6 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
             float top = -KV_INF;
 #pragma unroll
             for (int g = 0; g < 4; g++) {
-                if (LARGE)
-#pragma unroll
-                    for (int i = 16 * g; i < 16 * g + 16; i++) x[i] = __float_as_uint(fmaf(__uint_as_float(x[i]) * sc[g].x, factor, sc[g].y));
                 if (RAGGED)
 #pragma unroll
                     for (int i = 16 * g; i < 16 * g + 16; i++) x[i] = seen[g >> 1] >> (i & 31) & 1 ? x[i] : 0xff800000u;
@@ -309,11 +320,11 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
                 u = fmaxf(fmaxf(u, __uint_as_float(x[o + 10])), __uint_as_float(x[o + 11]));
                 w = fmaxf(fmaxf(w, __uint_as_float(x[o + 12])), __uint_as_float(x[o + 13]));
                 u = fmaxf(fmaxf(u, __uint_as_float(x[o + 14])), __uint_as_float(x[o + 15]));
-                top = fmaxf(top, fmaf(fmaxf(u, w), f[g], y[g]));                  // a NaN (0 times -inf where 16 hidden tokens have a scale of 0) does not count
+                top = fmaxf(top, fmaf(fmaxf(u, w), f[g], sc[g].y));                  // a NaN (0 times -inf where 16 hidden tokens have a scale of 0) does not count
             }
             // without a branch, behind which the compiler might leave the rows apart: the tensor memory's instructions want the warp whole
-            const bool higher = LARGE ? top - m > KV_P_MOST : top > m + KV_P_MOST;
-            top = LARGE ? __fadd_ru(top, -KV_P_BITS) : top - KV_P_BITS;      // up: what is rounded away would be above KV_P_MOST
+            const bool higher = top > m + KV_P_MOST;
+            top -= KV_P_BITS;
             fall = higher ? kv_exp2(m - top) : 1.f;
             l *= fall;
             m = higher ? top : m;
@@ -322,7 +333,7 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
             float up[4];
 #pragma unroll
             for (int g = 0; g < 4; g++) {
-                up[g] = y[g] - m;
+                up[g] = sc[g].y - m;
                 z[g] = sc[g].z;
             }
             // ask for the next step's scores now
@@ -357,9 +368,8 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
             kv_tmem_store32(p, at);                      // over the scores of the first 32 tokens
             if constexpr (!BF) kv_tmem_store32(rest, at + 32);
         };
-        if (!(fabsf(k_most) * score_most < 0x1p22f)) pass(std::integral_constant<int, KV_TILE_LARGE>());
-        else if (ragged) pass(std::integral_constant<int, KV_TILE_RAGGED>());
-        else pass(std::integral_constant<int, KV_TILE_WHOLE>());
+        if (ragged || large) pass(std::true_type());
+        else pass(std::false_type());
         if (s > 0 && __any_sync(0xffffffffu, fall != 1.f)) {
             // behind the product of the step before, the last that has been issued
             fine = kv_warp_wait(bars + 8 * (KV_O_IN + m_tile), (s - 1) & 1, stop);
@@ -399,35 +409,48 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
     }
     if (fine && tiles > 0) fine = kv_warp_wait(bars + 8 * (KV_S_IN + 2 * m_tile), tiles & 1, stop);     // all products
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    // Tokens of the unfinished block that the products left out, in 32 bits: the sum first, then with every 32 channels of the answer.
+    // Tokens that the products left out, in 32 bits: the sum first, then with every 32 channels of the answer.
     float lost = 1.f;                                    // what O is multiplied by for a new m
     const uint32_t left_out = *(volatile uint32_t*)apart;
-    auto for_apart = [&](auto use) {                     // use(token's place in the tail, score in base 2)
-        for (int t = tail_begin; t < end; t++) {
-            if (!(left_out >> ((t - tail_tile) / KV_HALF) & 1) || t > place || (A.window > 0 && t <= place - A.window)) continue;
-            const uint16_t *qs = (const uint16_t*)A.q.data + token * A.q.token_stride + head * A.q.head_stride, *ks = tail + (int64_t)(t - tail_begin) * D;
-            float dot = 0.f;
-#pragma unroll 1
-            for (int ch = 0; ch < D; ch += 8) {
-                float a[8], b[8];
-                kv_widen8<BF>(*(const uint4*)(qs + ch), a);
-                kv_widen8<BF>(*(const uint4*)(ks + ch), b);
-#pragma unroll
-                for (int e = 0; e < 8; e++) dot = fmaf(a[e], b[e], dot);
+    const bool by_hand = left_out || some_large;
+    auto for_apart = [&](auto use) {                     // use(place of the token's page, or -2; its place in it or in the tail; score in base 2)
+        for (int t0 = some_large ? begin : tail_tile; t0 < end; t0 += 64) {
+            float k_most = 0.f;
+            for (int t = t0; t < min(t0 + 64, end) && some_large; t += KV_HALF) {
+                const int page = t < tail_begin ? kv_page(B, seq, t >> S.block_shift) : -1;
+                const float ks = t >= tail_begin ? ((const float2*)(sm + T::POWERS))[(t - tail_tile) / KV_HALF].x : page < 0 ? 0.f : kv_finite(kv_scales(S, B, page)[2 * kh]);
+                if (t < tail_begin || !(left_out >> ((t - tail_tile) / KV_HALF) & 1)) k_most = fmaxf(k_most, ks);
             }
-            use(t - tail_begin, dot * S.scale_log2);
+            const bool large = !(k_most * score_most < KV_P_LARGE);
+            for (int t = t0; t < min(t0 + 64, end); t++) {
+                const bool in_tail = t >= tail_begin;
+                if (t > place || (A.window > 0 && t <= place - A.window) || !(large || (in_tail && left_out >> ((t - tail_tile) / KV_HALF) & 1))) continue;
+                const int page = in_tail ? -2 : kv_page(B, seq, t >> S.block_shift), at = in_tail ? t - tail_begin : t & (S.block_tokens - 1);
+                if (page == -1) continue;
+                const uint16_t* const qs = (const uint16_t*)A.q.data + token * A.q.token_stride + head * A.q.head_stride;
+                float dot = 0.f;
+#pragma unroll 1
+                for (int ch = 0; ch < D; ch += 8) {
+                    float a[8], b[8];
+                    kv_widen8<BF>(*(const uint4*)(qs + ch), a);
+                    kv_held8<BF, E4M3>(S, B, tail, kh, 0, page, at, ch, b);
+#pragma unroll
+                    for (int e = 0; e < 8; e++) dot = fmaf(a[e], b[e], dot);
+                }
+                use(page, at, t, __fmul_rn(dot, S.scale_log2));          // rounded, for the largest and for the weights alike
+            }
         }
     };
-    if (left_out && valid) {
-        for_apart([&](int, float x) {
+    if (by_hand && valid) {
+        for_apart([&](int, int, int, float x) {
             const float next = fmaxf(m, x), f = kv_exp2(m - next);
             l = l * f + kv_exp2(x - next) * (1.f / 134217728);
             lost *= f;
             m = next;
         });
         if (units)
-            for_apart([&](int t, float x) {              // a unit's weight, token by token
-                float& unit = units[(int64_t)((tail_begin + t) >> A.unit_shift) * unit_stride];
+            for_apart([&](int, int, int t, float x) {    // a unit's weight, token by token
+                float& unit = units[(int64_t)(t >> A.unit_shift) * unit_stride];
                 const float most = fmaxf(unit, x);
                 unit = x == -KV_INF ? unit : most + kv_log2(kv_exp2(unit - most) + kv_exp2(x - most));
             });
@@ -447,16 +470,15 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
         float y[32];
 #pragma unroll
         for (int i = 0; i < 32; i++) y[i] = __uint_as_float(x[i]);
-        if (left_out) {
+        if (by_hand) {
 #pragma unroll
             for (int i = 0; i < 32; i++) y[i] *= lost;
-            for_apart([&](int t, float score) {
+            for_apart([&](int page, int at, int, float score) {
                 const float weight = kv_exp2(score - m);
-                const uint16_t* const vs = tail + ((int64_t)S.block_tokens + t) * D + 32 * b;
 #pragma unroll
                 for (int i = 0; i < 32; i += 8) {
                     float v[8];
-                    kv_widen8<BF>(*(const uint4*)(vs + i), v);
+                    kv_held8<BF, E4M3>(S, B, tail, kh, 1, page, at, 32 * b + i, v);
 #pragma unroll
                     for (int e = 0; e < 8; e++) y[i + e] = fabsf(v[e]) < KV_INF ? fmaf(weight, v[e], y[i + e]) : y[i + e] + v[e];
                 }
@@ -577,7 +599,10 @@ __device__ __forceinline__ void kv_prompt_bring(const KvShape& S, const KvBatch&
                 k_most = powers[lane & 7].x;
                 vs = powers[lane & 7].y;
                 ks = BF ? k_most : 1.f;
-                if (*apart >> (lane & 7) & 1) page = -1;
+                if (*apart >> (lane & 7) & 1) {
+                    page = -1;
+                    k_most = 0.f;
+                }
             }
             scale_page = scale_next;
             scale = scale_of(scale_page);

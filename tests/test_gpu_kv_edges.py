@@ -297,3 +297,35 @@ def test_values_of_very_different_sizes(new, group, block):
     c.tail[:, :, 1] = torch.where(torch.isnan(c.tail[:, :, 1]), c.tail[:, :, 1], c.tail[:, :, 1] * power)
     q, out, lse = attend(c)
     compare(c, out, lse, definition(c, q))
+
+
+@pytest.mark.parametrize("dtype", [kv.BF16, kv.F16])
+@pytest.mark.parametrize("new,group,block,window", [(1, 4, 64, 0), (5, 2, 16, 0), (150, 2, 128, 0), (150, 1, 64, 0), (100, 3, 16, 0), (140, 1, 32, 90)])
+def test_weights_beside_tokens_of_very_different_sizes(dtype, new, group, block, window):
+    """Answers, sums and block weights where the unfinished block's tokens differ by up to 2^12 in K and in V."""
+    c = Cache(dtype, kv.E4M3, 2 * group, 2, 64, block, [3 * block + new - new % block + block - 2, max(new, block - 1)], [new, new], seed=12)
+    c.fill()
+    gen = torch.Generator().manual_seed(2)
+    for which in range(2):
+        power = torch.exp2(-torch.randint(0, 13, (c.n, 1, block, 1), generator=gen).float()).cuda()
+        c.tail[:, :, which] *= power
+    q = torch.randn(c.total, c.qh, c.d, generator=gen).to(c.t).cuda()
+    out, stride = torch.full_like(q, -7.0), -(-c.max_len // block) + 1
+    m_in = torch.rand(c.n, c.kh, stride, device="cuda")
+    m_out = torch.full_like(m_in, -5.0)
+    lse = c.run_attention(q, out, window, m_in, m_out)
+    c.check_attention(q, out, lse, window, m_in, m_out)
+
+
+@pytest.mark.parametrize("new,window", [(1, 0), (140, 0), (140, 200)])
+def test_scores_beyond_the_last_whole_number(new, window):
+    """Scores up to 2^28, where a float's steps are whole numbers: one token takes all, and no weight leaves f16's range."""
+    c = Cache(kv.BF16, kv.INT8, 4, 2, 128, 32, [800, 333], [new, new], scale=3.0, seed=3)
+    c.fill(spread=4.0)
+    gen = torch.Generator().manual_seed(2)
+    q = (3 * torch.randn(c.total, c.qh, c.d, generator=gen)).to(c.t).cuda()
+    out = torch.full_like(q, -7.0)
+    m_in = torch.rand(c.n, c.kh, 26, device="cuda")
+    m_out = torch.full_like(m_in, -5.0)
+    lse = c.run_attention(q, out, window, m_in, m_out)
+    c.check_attention(q, out, lse, window, m_in, m_out)

@@ -82,7 +82,7 @@ class KvCache:
     def __init__(self, dtype: int, format: int, q_heads: int, kv_heads: int, head_dim: int, block_tokens: int, rotary: int = ROTARY_NONE,
                  frequencies=None, rotary_gain: float = 1.0, softmax_scale: float = 0.0):
         self.handle = None
-        frequencies = list(frequencies or ())
+        frequencies = [] if frequencies is None else [float(f) for f in frequencies]     # any sequence, arrays and tensors among them
         table = (ctypes.c_double * max(1, len(frequencies)))(*frequencies)
         config = Config(dtype, format, q_heads, kv_heads, head_dim, block_tokens, rotary, 2 * len(frequencies), table, rotary_gain, softmax_scale)
         handle = _vp()

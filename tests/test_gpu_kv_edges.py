@@ -329,3 +329,38 @@ def test_scores_beyond_the_last_whole_number(new, window):
     m_out = torch.full_like(m_in, -5.0)
     lse = c.run_attention(q, out, window, m_in, m_out)
     c.check_attention(q, out, lse, window, m_in, m_out)
+
+
+@pytest.mark.parametrize("new,lens,window", [(1, [70000, 65000], 0), (1, [30000], 2000), (5, [3000, 2500], 0), (150, [2000], 0), (150, [900, 800], 300)])
+def test_graph_capture_with_joins_and_weights(new, lens, window):
+    """The paths whose later launches start under the earlier ones, replayed in a graph behind kernels that change their input."""
+    c = Cache(kv.BF16, kv.INT8, 8, 1, 128, 64, lens, [new] * len(lens))
+    c.fill()
+    gen = torch.Generator().manual_seed(3)
+    inputs = [torch.randn(c.total, c.qh, c.d, generator=gen).to(c.t).cuda() for _ in range(2)]
+    q, out, lse = inputs[0].clone(), torch.empty_like(inputs[0]), torch.empty(c.total, c.qh, device="cuda")
+    stride = -(-c.max_len // c.bt)
+    m_in, m_out = torch.rand(c.n, c.kh, stride, device="cuda"), torch.empty(c.n, c.kh, stride, device="cuda")
+    b = c.batch()
+    ws = torch.empty(c.kv.workspace_bytes(b, True), dtype=torch.uint8, device="cuda")
+    plain = []
+    for x in inputs:
+        o, m = torch.empty_like(out), torch.full_like(m_out, -5.0)
+        plain.append((o, c.run_attention(x, o, window, m_in, m), m))
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph, fresh = torch.cuda.CUDAGraph(), torch.empty_like(q)
+    with torch.cuda.stream(stream):
+        with torch.cuda.graph(graph, stream=stream):
+            q.copy_(fresh)
+            c.kv.attention(b, rows(q), rows(out), ws.data_ptr(), ws.numel(), d_lse=lse.data_ptr(), window=window, d_mass_in=m_in.data_ptr(),
+                           d_mass_out=m_out.data_ptr(), mass_stride=stride, stream=stream.cuda_stream)
+            kept = [x.clone() for x in (out, lse, m_out)]
+    for k in (0, 1, 0, 1):
+        fresh.copy_(inputs[k])
+        m_out.fill_(-5.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, w in zip(kept, plain[k]):
+            assert torch.equal(a, w)

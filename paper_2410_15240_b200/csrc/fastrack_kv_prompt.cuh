@@ -213,9 +213,9 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
     {
         // the row of Q, as f16 (bf16: over a power of two near its largest), to shared memory
         const uint16_t* src = (const uint16_t*)A.q.data + token * A.q.token_stride + head * A.q.head_stride;
-        float inv = 1.f, most = 2.f;                     // most: no value of the row, as f16, is larger
-        uint32_t amax = 0;
+        float inv = 1.f, size = 0.f;                     // size: of the row's values as f16, the sum of magnitudes
         if (BF) {
+            uint32_t amax = 0;
 #pragma unroll 4
             for (int i = 0; i < D / 8; i++) amax = max(amax, valid ? kv_amax8<true>(*(const uint4*)(src + 8 * i)) : 0u);
             const float p = kv_power_below(amax);
@@ -225,22 +225,20 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
 #pragma unroll 4
         for (int i = 0; i < D / 8; i++) {
             uint4 w = valid ? *(const uint4*)(src + 8 * i) : make_uint4(0, 0, 0, 0);
-            if (BF) {
-                float x[8];
-                kv_widen8<true>(w, x);
+            float x[8];
+            kv_widen8<BF>(w, x);
 #pragma unroll
-                for (int e = 0; e < 8; e++) x[e] *= inv;
-                w = kv_narrow8<false>(x);
-            } else {
-                amax = max(amax, kv_amax8<false>(w));
+            for (int e = 0; e < 8; e++) {
+                x[e] *= inv;
+                size += fabsf(x[e]);
             }
+            if (BF) w = kv_narrow8<false>(x);
             *(uint4*)(sm + T::Q + m_tile * T::TILE + T::at(r, 8 * i)) = w;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         kv_warp_arrive(bars + 8 * KV_Q_IN);
-        if (!BF) most = __half2float(__ushort_as_half((unsigned short)amax));
-        // no score of the warp's rows is larger than this times K's scale
-        score_most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(factor * most))) * (D * (E4M3 ? 448.f : 127.f));
+        // no score of the warp's rows is larger than this times K's scale (a row with infinities or NaN has no answers to be careful of)
+        score_most = __uint_as_float(__reduce_max_sync(0xffffffffu, size < KV_INF ? __float_as_uint(factor * size) : 0u)) * (E4M3 ? 448.f : 127.f);
     }
     // Powers of two for the unfinished block, 16 tokens at a time, while the first codes come.  What one power would not hold (values that are not
     // finite, tokens whose largest values are 2^8 apart; f16 K needs none) stays out of the products: the rows take it apart at the end.

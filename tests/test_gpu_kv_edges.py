@@ -364,3 +364,32 @@ def test_graph_capture_with_joins_and_weights(new, lens, window):
         torch.cuda.synchronize()
         for a, w in zip(kept, plain[k]):
             assert torch.equal(a, w)
+
+
+@pytest.mark.parametrize("new", [3, 150])
+def test_no_tokens_at_all(new):
+    """max_len 0: nothing is held, every query sees nothing."""
+    c = Cache(kv.F16, kv.INT8, 4, 2, 64, 16, [0, 0], [new, new])
+    q, out, lse = attend(c)
+    assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+
+
+@pytest.mark.parametrize("dtype", [kv.BF16, kv.F16])
+@pytest.mark.parametrize("value", [math.nan, math.inf, 2.0 ** 100])
+@pytest.mark.parametrize("new,group", [(5, 2), (150, 1)])
+def test_a_query_that_is_not_finite(dtype, value, new, group):
+    """It is NaN (or huge) for itself: the other rows' bits stay."""
+    c = Cache(dtype, kv.INT8, 2 * group, 2, 128, 64, [300 + new, new], [new, new])
+    c.fill()
+    q, out, lse = attend(c)
+    bad = c.total - 2
+    q[bad, 1] = value if dtype == kv.BF16 or not math.isfinite(value) else 60000.0
+    again = torch.full_like(q, -7.0)
+    lse2 = c.run_attention(q, again)
+    keep = torch.ones(c.total, c.qh, dtype=torch.bool, device="cuda")
+    keep[bad, 1] = False
+    if math.isfinite(value):                            # beside a huge one, others may go another way to the same answer
+        compare(c, torch.where(keep[..., None], again, 0), torch.where(keep, lse2, 0.0), tuple(torch.where(keep.cpu()[..., None] if x.dim() == 3 else keep.cpu(), x, 0.0) for x in definition(c, q)))
+    else:
+        assert torch.equal(out[keep], again[keep]) and torch.equal(lse[keep], lse2[keep])
+        assert bool(torch.isnan(again[bad, 1]).all())

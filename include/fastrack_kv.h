@@ -112,7 +112,8 @@ FASTRACK_API int fastrack_rotary_frequencies(int rotary_dim, double base, int sc
 
 /* Rotary positions: pair (a, b) of a token at position p becomes gain * (a cos w - b sin w, b cos w + a sin w), w = p * frequency.
  * inverse != 0 turns by -w (the gain stays): that is the gradient of the input from the gradient of the output.
- * The angle is formed modulo one turn in 64-bit fixed point, so that it is as exact at position 2^40 as at 1.
+ * The angle is formed modulo one turn in 64-bit fixed point: at position p it is off by at most 2^-32 + |p| 2^-63 of a turn (for
+ * frequencies up to a turn per position), which is 2^-31 up to p = 2^31 and 2^-23 at 2^40.
  * Channels from rotary_dim on are copied.  in == out (same strides) is allowed; other overlap is not checked.
  * `heads` need not be the configuration's.  tokens == 0 or heads == 0: nothing is done. */
 FASTRACK_API int fastrack_rotary(fastrack_kv* kv, int64_t tokens, int heads, const fastrack_kv_rows* in, const fastrack_kv_rows* out,

@@ -98,7 +98,7 @@ __device__ __forceinline__ void kv_sincos(uint32_t phase, float& s, float& c)
 }
 
 // cos and sin of the unit's 8 angles times the gain.  The angle in turns is position * turns mod 1: the top 32 bits of a 64-bit product
-// that wraps.
+// that wraps.  What the table's numbers lack below 2^-64 counts once per position: 2^-63 of a turn with their own rounding.
 __device__ __forceinline__ void kv_angles(const KvShape& S, int u, int64_t position, bool inverse, float* cs, float* sn)
 {
     const float gain = inverse ? -S.rotary_gain : S.rotary_gain;

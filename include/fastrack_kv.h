@@ -20,7 +20,8 @@
  * fraction bits (FASTRACK_KV_E4M3).  scale = amax / 127 or amax / 448, amax the largest magnitude of the block and head;
  * a block with amax < 2^-100 is held as zeros with scale 0.  A NaN or infinity in a block makes that block's scale (head
  * and K or V) NaN or infinite, and every answer that weighs the block NaN: it does not pass unseen.
- * Row of the tail buffer (fastrack_kv_tail_bytes): [kv_heads][2: K, V][block_tokens][head_dim] 16-bit values.
+ * Row of the tail buffer (fastrack_kv_tail_bytes): [kv_heads][2: K, V][block_tokens][head_dim] 16-bit values.  There a NaN or infinity
+ * counts for the queries that see its token: K's makes their scores what it makes them, V's shows in its channels.
  *
  * Conventions are those of fastrack.h: int results (FASTRACK_OK or FASTRACK_ERR_*), nothing throws or prints, device
  * pointers d_*, work is asynchronous on `stream`, calls are refused with FASTRACK_ERR_ARG unless the handle's device is
@@ -71,9 +72,9 @@ typedef struct {
  * the attention of their queries.  A sequence without new tokens is left alone.  q, k, v, their positions and the answers have
  * total_new rows. */
 typedef struct {
-    int n_seqs;
-    int total_new;              /* d_starts[n_seqs], or an upper bound of it */
-    int max_new;                /* upper bound of the new tokens of a sequence */
+    int n_seqs;                 /* at most 65535 */
+    int total_new;              /* d_starts[n_seqs], or an upper bound of it; times q_heads below 2^31 */
+    int max_new;                /* upper bound of the new tokens of a sequence; at most total_new; times q_heads at most 2^30 */
     int max_len;                /* upper bound of d_lens; at most 2^30 */
     int pool_pages;             /* pages in d_pool; a table entry outside 0 .. pool_pages - 1 is an absent page: what is appended to
                                    it is dropped, and attention passes over its tokens */
@@ -139,7 +140,9 @@ FASTRACK_API size_t fastrack_kv_attention_workspace(const fastrack_kv* kv, const
  * place i = L - n + j and sees the tokens t <= i, with window > 0 only those t > i - window (a window of max_len or more hides
  * nothing), without absent pages:
  *     out = sum_t p_t v_t,  p = softmax_t(softmax_scale * q . k_t).
- * A query that sees nothing gets out = 0 and lse = -inf.
+ * A query that sees nothing gets out = 0 and lse = -inf.  What a query does not see has no part in its answer, whatever stands there.  What it
+ * sees counts by its share of the answer: the weights, of 11 bits (bf16) or 22 (f16), are held down to 2^-25 of the largest weight times
+ * scale of V.
  *   d_lse       [total_new][q_heads] float, natural logarithm of the sum of exponentials; may be NULL.
  *   d_mass_in, d_mass_out  [n_seqs][kv_heads][mass_stride] float; both NULL, or both set (they may be the same).  For every block of a
  *               sequence, the unfinished one included: out = in + the sum of p over the block's tokens, the sequence's new

@@ -746,11 +746,11 @@ extern "C" int fastrack_kv_read(fastrack_kv* kv, const fastrack_kv_batch* batch,
 
 // ------------------------------------------------------------------------------------------------ attention ----
 
-#define KV_WAVES 4                      // times that chunks fill the SMs, where there is so much (4 x 131072 tokens, 16 x 20000, 16 x 3000 .. 30000:
-                                        // 224, 132 and 122 us; 3 times 220, 136 and 132)
+#define KV_WAVES 4                      // times that chunks fill the SMs, where there is so much (61 sequences of up to 4096 tokens with weights, 4 x 131072,
+                                        // 16 x 20000, 16 x 3000 .. 30000: 67, 177, 117 and 104 us; 3 times 70, 175, 116 and 107)
 #define KV_CHUNK_LEAST 1024             // tokens of a chunk, where chunks fill the SMs once with more
 #define KV_CHUNK_CLUSTER 2048           // tokens of a chunk in a cluster: above, more chunks than a cluster has are worth the join (where a cluster
-                                        // would have less than 4 chunks, 61 sequences of up to 4096 tokens took 88 us against 77)
+                                        // would have less than 4 chunks, 61 sequences of up to 4096 tokens took 75 us against 67)
 
 struct KvPlan { int rows, splits, chunk, row_tiles, units, unit_shift; size_t ml, lse2, unit_l2, total; };   // byte offsets in the workspace, part_o at 0
 

@@ -25,8 +25,8 @@
 // Every span is cut into chunks, a CTA for each.  Where the chunks fill the SMs several times, they are equal pieces of whatever length
 // a sequence has, so that one CTA's start and end pass under the others' loads; they are joined through the workspace by a kernel of its
 // own.  Where there is less than the SMs hold, a span is cut into up to KV_CLUSTER equal chunks, whose CTAs are a cluster and join
-// their answers through each other's shared memory.  (One sequence of 700 tokens: 12.3 us in a cluster, 14.3 us with the join's
-// launch; 61 sequences of up to 4096: 103 and 77 us, because the CTAs of short sequences wait for nothing in a cluster's place.
+// their answers through each other's shared memory.  (One sequence of 700 tokens: 9.2 us in a cluster, 10.4 us with the join's
+// launch; 61 sequences of up to 4096: 75 and 67 us, because the CTAs of short sequences wait for nothing in a cluster's place.
 // Tried instead: CTAs that stay and take equal runs of one line of all work; all of them start and end at the same time, 148 us.)
 #define KV_CLUSTER 8
 #define KV_STEP (KV_TILE * KV_WARPS)
@@ -287,10 +287,10 @@ __device__ __forceinline__ void kv_weigh(KvState<D, NR>& W, float (&s)[HALVES][N
             }
 }
 
-// log2 of a row's sum of exponentials, and of a unit's of weights, made once per tile, in one instruction: off by at most 2^-22 of the
-// logarithm, which adds some 10 to m (exact for powers of two, as the other).
+// log2 of a row's sum of exponentials; and of a unit's, made for every tile, by the unit's instruction, which is off by at most 2^-22 of a
+// logarithm of some 10 (the library's function took 15 us of the 315 of 3 x 1024 new tokens, 3 of the 67 of 61 single ones).
 __device__ __forceinline__ float kv_sum_log2(float l, float m) { return l == 0.f ? -KV_INF : m + (KV_L_BITS + log2f(l)); }
-__device__ __forceinline__ float kv_unit_log2(float l, float m) { return m + (KV_L_BITS + kv_log2(l)); }
+__device__ __forceinline__ float kv_unit_log2(float l, float m) { return m + (KV_L_BITS - 16.f + kv_log2(l * 65536.f)); }    // no part of l is a denormal number then
 
 // log2 of the rows' sums of exponentials of halves h0 .. h1 - 1, from the lanes' parts of l, to out[row]
 template <int NR, int HALVES>
@@ -313,6 +313,8 @@ __device__ __forceinline__ void kv_note(const float (&part)[HALVES][NR][2], cons
 
 // Weights of two rows as f16, as the second operand's share of a lane.  FINE (answers of 11 bits, where the rounding of the weights
 // would show as much as that of the answer): what the rounding leaves out as another such number, which gets a product of its own.
+// Answers of 8 bits do without: a weight's rounding, 2^-12 and of either sign, is an eighth of the answer's own even before it averages out
+// over the tokens (error against 64 bits 0.0017 of the answer, as that of 32-bit weights).
 template <bool FINE> __device__ __forceinline__ void kv_weights(float x, float y, uint32_t& hi, uint32_t& lo)
 {
     hi = kv_pack<false>(x, y);
@@ -593,11 +595,11 @@ __device__ __forceinline__ void kv_tail_tile(KvState<D, NR>& W, const uint16_t* 
 
 // One CTA: 8 NR rows of one kv head of one sequence, one chunk of the tokens they see.  Each of the four warps takes every fourth
 // tile with statistics and an accumulator of its own; they are joined in shared memory at the end.
-// Bound by the codes' way from memory: 4 sequences of up to 131072 tokens (int8, 913 MB) in 158 us with bf16 queries, 5.8 TB/s, and
-// 174 us with f16 ones and their second product; next to it stands the widening (55 % of the ALU's cycles, 0.6 instructions a cycle
-// and scheduler).  What it came from: codes loaded straight to registers by a warp, rows on the 16-wide side of the instruction
-// 372 us; copies lane by lane into a ring 342; K and V on the 16-wide side 236; 32 tokens a step and a path without masks 211;
-// tensor copies, which free the lanes of addresses and waits, 160.
+// Bound by the codes' way from memory: 4 sequences of up to 131072 tokens (int8, f16 queries with their second product, 913 MB) in 159 us,
+// 5.8 TB/s; next to it stands the widening (56 % of the ALU's cycles, 0.65 instructions a cycle and scheduler).  What it came from, with
+// bf16 queries: codes loaded straight to registers by a warp, rows on the 16-wide side of the instruction 372 us; copies lane by lane
+// into a ring 342; K and V on the 16-wide side 236; 32 tokens a step and a path without masks 211; tensor copies, which free the lanes of
+// addresses and waits, 160.  A reference for V's scales apart from the maximum of the scores took f16 queries 176 us.
 template <int D, bool BF, bool E4M3, int NR>
 __global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? (D == 64 ? 6 : 4) : 3) kv_attend_kernel(const KvShape S, const KvBatch B, const KvAttend A,
                                                                                   const __grid_constant__ CUtensorMap pool)
@@ -846,7 +848,7 @@ __device__ __forceinline__ void kv_weigh_blocks(const KvShape& S, const KvBatch&
 
 // Joins the chunks of each row: a CTA per row, of which a warp takes every fourth chunk.  With few rows CTAs behind these weigh blocks:
 // each works out the rows' sums again, a half warp to a row, instead of a launch that waits for them (4 sequences of up to 131072
-// tokens 209 us in all, 214 with it; 61 of up to 4096 66.6, 68.5).
+// tokens 180.4 us in all, 181.6 with it; 61 of up to 4096 67.0, 68.1).
 template <int D, bool BF>
 __global__ void __launch_bounds__(32 * KV_WARPS) kv_join_kernel(const KvShape S, const KvBatch B, const KvAttend A)
 {

@@ -14,15 +14,20 @@
 // codes' way in: 320 KB at 128 B a cycle); the exponentials 2 x 128 x 128 at 16 a cycle, 2048.  It takes some 5000: a step of a row
 // tile is a chain (scores from tensor memory, largest, exponentials, weights back) of some 2300 cycles, half of them exponentials,
 // in which every access to shared memory, a barrier's too, waits for the tensor cores' reads (150 to 300 cycles).
-// 3 x 1024 new tokens over up to 6100, 32 heads of 128, bf16: 321 us = 599 TFLOP/s of the visible pairs, tensor cores active 35 %.
+// 3 x 1024 new tokens over up to 6100, 32 heads of 128, bf16: 315 us = 610 TFLOP/s of the visible pairs, tensor cores active 35 %.
 // What it came from: one m16n8k16 row tile per pass 2231 us; this division of work, codes unrolled and generic addressing 843; packed
 // arithmetic and less code 369; two halves and products issued by a converged warp 348.  Two threads per row took 375.
+//
+// What f16 operands or these steps would not hold right is taken apart at the end, token by token in 32 bits by the rows that see it: 16 tokens
+// of the unfinished block with a value that is not finite or with sizes 2^8 apart, and 64 tokens whose scores may pass KV_P_LARGE, where
+// y - m (see KV_P_MOST) would be rounded to steps of a quarter or more.  Both are rare; a third kind of step for them cost all others 3 to 20 %
+// in registers.
+#define KV_P_LARGE 0x1p22f
 #define KV_P_ROWS 128                   // of a row tile
 #define KV_P_TOKENS 128
 #define KV_P_THREADS 416
 #define KV_P_GROUPS (KV_P_TOKENS / KV_HALF)
-#define KV_P_LARGE 0x1p22f              // bound of a score from which on tokens are taken apart
-#define KV_P_AHEAD 4                   // pairs of values between an exponential and the use of its result
+#define KV_P_AHEAD 4                    // pairs of values between an exponential and the use of its result
 
 template <int D> struct KvPrompt {
     static constexpr int HALVES = (D + 63) / 64;                             // runs of 64 channels: 128-byte rows, swizzled by the row's number
@@ -150,7 +155,16 @@ template <bool E4M3> __device__ __forceinline__ void kv_widen16(const uint4& w, 
 
 // Barriers, 8 bytes each from T::BARS on.  K_IN has four phases in turn because the scales beside K stay until the weights are made; by
 // the time that a tile's K comes in, the weights of the fourth tile before it are done.
-// S_IN and P_IN: [row tile][half of the tile's tokens]; O_IN: an answer product of the row tile is done.
+// S_IN and P_IN: [row tile][half of the tile's tokens]; O_IN: an answer product of the row tile is done.  TAIL: the unfinished block's powers are there.
+// What the places that are used again rest on (step s: half s & 1 of tile s >> 1):
+//   Slot j & 3 of the scales is written for tile j + 4 behind K_OUT of tile j + 2, whose scores were issued behind P_IN of both halves of tile
+//   j + 1: every row is past tile j.  A row may read a slot from K_IN of its tile on (before, it holds the fourth tile before), and not
+//   after P_IN of its second half.
+//   A half of S is written by scores(s + 2) behind answers(s), in the order of issue, and answers(s) behind P_IN(s): the rows have
+//   read their scores and written their weights.
+//   O_IN has a phase for every step, of which a row asks for s - 1, and only where O has to be multiplied: it may never have asked for
+//   others.  The parity tells phase s - 1 from s - 2 because s - 2 is over: answers(s - 2) and its commit were issued before scores(s) and its
+//   commit, whose end, S_IN(s), the row has seen.  And O rests meanwhile: answers(s) wait for the row's P_IN(s).
 enum { KV_K_IN = 0, KV_K_OUT = 4, KV_V_IN = 6, KV_V_OUT = 8, KV_S_IN = 10, KV_P_IN = 14, KV_O_IN = 18, KV_Q_IN = 20, KV_TAIL = 21, KV_END = 22, KV_BARS = 23 };
 
 // What a tile's slot of T::SCALES holds: per 16 tokens {K's scale, y and z of V's (see KV_P_MOST), whether the tokens are there}; and of each half

@@ -279,7 +279,7 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
     float* const units = A.unit_l2 && valid ? A.unit_l2 + ((int64_t)seq * S.kv_heads + kh) * A.units * unit_stride + row : nullptr;
     const bool small_units = units && S.block_tokens < 64;
     float m = KV_M_NONE, l = 0.f;                        // see KV_P_MOST
-    bool fine = true, some_large = false;
+    bool fine = true;
     // Steps of 64 tokens: while this one's weights are made, the next one's scores are (in the other half of S).
     uint32_t ended = 0;                                  // whether this step's scores are known to be there
     for (int s = 0; s < 2 * tiles && fine; s++) {
@@ -295,12 +295,12 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const float k_most = slot.k_most[half];
         const bool ragged = __float_as_int(k_most) < 0 || t0 + 63 > see_all || t0 <= low_all;
-        float fall = 1.f, z[4];                          // fall: what l and O are multiplied by
+        float fall = 1.f, z[4];                          // fall: what l and O are multiplied by for a new m
         uint64_t sum[4] = {0, 0, 0, 0};                  // of 16 tokens' weights each
         // Scores may be so large that y - m would be rounded to steps of a quarter or more: these rows see nothing here, and take the tokens apart at
         // the end.
         const bool large = !(fabsf(k_most) * score_most < KV_P_LARGE);
-        some_large |= large;
+        if (large && (threadIdx.x & 31) == 0) atomicOr(apart, 256u << warp);
         auto pass = [&](auto some_hidden) {
             constexpr bool RAGGED = decltype(some_hidden)::value;
             uint32_t seen[2] = {0xffffffffu, 0xffffffffu};                   // which of 32 tokens the row sees
@@ -421,52 +421,83 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
     }
     if (fine && tiles > 0) fine = kv_warp_wait(bars + 8 * (KV_S_IN + 2 * m_tile), tiles & 1, stop);     // all products
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    // Tokens that the products left out, in 32 bits: the sum first, then with every 32 channels of the answer.
-    float lost = 1.f;                                    // what O is multiplied by for a new m
-    const uint32_t left_out = *(volatile uint32_t*)apart;
-    const bool by_hand = left_out || some_large;
-    auto for_apart = [&](auto use) {                     // use(place of the token's page, or -2; its place in it or in the tail; score in base 2)
-        for (int t0 = some_large ? begin : tail_tile; t0 < end; t0 += 64) {
-            float k_most = 0.f;
-            for (int t = t0; t < min(t0 + 64, end) && some_large; t += KV_HALF) {
-                const int page = t < tail_begin ? kv_page(B, seq, t >> S.block_shift) : -1;
-                const float ks = t >= tail_begin ? ((const float2*)(sm + T::POWERS))[(t - tail_tile) / KV_HALF].x : page < 0 ? 0.f : kv_finite(kv_scales(S, B, page)[2 * kh]);
-                if (t < tail_begin || !(left_out >> ((t - tail_tile) / KV_HALF) & 1)) k_most = fmaxf(k_most, ks);
-            }
-            const bool large = !(k_most * score_most < KV_P_LARGE);
-            for (int t = t0; t < min(t0 + 64, end); t++) {
-                const bool in_tail = t >= tail_begin;
-                if (t > place || (A.window > 0 && t <= place - A.window) || !(large || (in_tail && left_out >> ((t - tail_tile) / KV_HALF) & 1))) continue;
-                const int page = in_tail ? -2 : kv_page(B, seq, t >> S.block_shift), at = in_tail ? t - tail_begin : t & (S.block_tokens - 1);
-                if (page == -1) continue;
-                const uint16_t* const qs = (const uint16_t*)A.q.data + token * A.q.token_stride + head * A.q.head_stride;
-                float dot = 0.f;
+    // Tokens that the products left out, 16 at a time in 32 bits: their scores from the staged Q, then every 32 channels of O through registers.
+    // The warp stays together for the tensor memory's instructions; a row that does not see a token has a weight of 0 for it.
+    __syncwarp();
+    const uint32_t left_out = *(volatile uint32_t*)apart & 255u;
+    const bool some_large = *(volatile uint32_t*)apart >> 8 >> warp & 1;
+    for (int t0 = some_large ? begin : tail_tile; t0 < end && (left_out || some_large); t0 += 64) {
+        float k_most = 0.f;                              // as in the slot
+        for (int t = t0; t < min(t0 + 64, end) && some_large; t += KV_HALF) {
+            const int page = t < tail_begin ? kv_page(B, seq, t >> S.block_shift) : -1, group = (t - tail_tile) / KV_HALF;
+            const float ks = page >= 0 ? kv_finite(kv_scales(S, B, page)[2 * kh]) : t >= tail_begin && !(left_out >> group & 1) ? ((const float2*)(sm + T::POWERS))[group].x : 0.f;
+            k_most = fmaxf(k_most, ks);
+        }
+        const bool large = !(k_most * score_most < KV_P_LARGE);
 #pragma unroll 1
+        for (int t = t0; t < min(t0 + 64, end); t += KV_HALF) {
+            const bool in_tail = t >= tail_begin;
+            const int page = in_tail ? -2 : kv_page(B, seq, t >> S.block_shift), at = in_tail ? t - tail_begin : t & (S.block_tokens - 1);
+            if (page == -1 || !(large || (in_tail && left_out >> ((t - tail_tile) / KV_HALF) & 1))) continue;
+            float w[KV_HALF], top = m, sum = 0.f;
+            uint32_t sees = 0;
+#pragma unroll 1
+            for (int i = 0; i < KV_HALF; i++) {
+                w[i] = -KV_INF;
+                if (t + i > place || t + i >= end || (A.window > 0 && t + i <= place - A.window)) continue;
+                float dot = 0.f;
+#pragma unroll 2
                 for (int ch = 0; ch < D; ch += 8) {
                     float a[8], b[8];
-                    kv_widen8<BF>(*(const uint4*)(qs + ch), a);
-                    kv_held8<BF, E4M3>(S, B, tail, kh, 0, page, at, ch, b);
+                    kv_widen8<false>(*(const uint4*)(sm + T::Q + m_tile * T::TILE + T::at(r, ch)), a);
+                    kv_held8<BF, E4M3>(S, B, tail, kh, 0, page, at + i, ch, b);
 #pragma unroll
                     for (int e = 0; e < 8; e++) dot = fmaf(a[e], b[e], dot);
                 }
-                use(page, at, t, __fmul_rn(dot, S.scale_log2));          // rounded, for the largest and for the weights alike
+                w[i] = __fmul_rn(dot, factor);           // rounded, for the largest and for the weights alike
+                top = fmaxf(top, w[i]);
+                sees |= 1u << i;
             }
-        }
-    };
-    if (by_hand && valid) {
-        for_apart([&](int, int, int, float x) {
-            const float next = fmaxf(m, x), f = kv_exp2(m - next);
-            l = l * f + kv_exp2(x - next) * (1.f / 134217728);
-            lost *= f;
-            m = next;
-        });
-        if (units)
-            for_apart([&](int, int, int t, float x) {    // a unit's weight, token by token
+            __syncwarp();
+            const float fall = kv_exp2(m - top);
+            m = top;
+#pragma unroll 1
+            for (int i = 0; i < KV_HALF; i++) sum += w[i] = kv_exp2(w[i] - m);
+            l = l * fall + sum * (1.f / 134217728);
+            if (units && sees) {                         // the sum was made without them: -inf, or other tokens'
                 float& unit = units[(int64_t)(t >> A.unit_shift) * unit_stride];
-                const float most = fmaxf(unit, x);
-                unit = x == -KV_INF ? unit : most + kv_log2(kv_exp2(unit - most) + kv_exp2(x - most));
-            });
+                const float of_these = m + kv_log2(sum), most = fmaxf(unit, of_these);
+                unit = sum == 0.f ? unit : most + kv_log2(kv_exp2(unit - most) + kv_exp2(of_these - most));
+            }
+#pragma unroll 1
+            for (int b = 0; b < D / 32; b++) {
+                uint32_t x[32];
+                __syncwarp();
+                kv_tmem_load32(x, o_at + 32 * b);
+#pragma unroll
+                for (int e = 0; e < 32; e++) x[e] = __float_as_uint(__uint_as_float(x[e]) * fall);
+#pragma unroll 1
+                for (int i = 0; i < KV_HALF && t + i < end; i++) {
+                    const float weight = w[i];
+                    const bool seen = sees >> i & 1;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        float v[8];
+                        kv_held8<BF, E4M3>(S, B, tail, kh, 1, page, at + i, 32 * b + e, v);
+#pragma unroll
+                        for (int k = 0; k < 8; k++) {
+                            const float y = __uint_as_float(x[e + k]);
+                            x[e + k] = __float_as_uint(fabsf(v[k]) < KV_INF ? fmaf(weight, v[k], y) : seen ? y + v[k] : y);
+                        }
+                    }
+                }
+                __syncwarp();
+                kv_tmem_store32(x, o_at + 32 * b);
+            }
+            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        }
     }
+    __syncwarp();
     const float out_factor = !fine ? __int_as_float(0x7fffffff) : A.splits == 1 ? kv_over_sum(l) : 1.f;
 #pragma unroll
     for (int b = 0; b < D / 32; b++) {
@@ -481,23 +512,7 @@ __device__ __forceinline__ void kv_prompt_rows(const KvShape& S, const KvBatch& 
         if (!valid) continue;
         float y[32];
 #pragma unroll
-        for (int i = 0; i < 32; i++) y[i] = __uint_as_float(x[i]);
-        if (by_hand) {
-#pragma unroll
-            for (int i = 0; i < 32; i++) y[i] *= lost;
-            for_apart([&](int page, int at, int, float score) {
-                const float weight = kv_exp2(score - m);
-#pragma unroll
-                for (int i = 0; i < 32; i += 8) {
-                    float v[8];
-                    kv_held8<BF, E4M3>(S, B, tail, kh, 1, page, at, 32 * b + i, v);
-#pragma unroll
-                    for (int e = 0; e < 8; e++) y[i + e] = fabsf(v[e]) < KV_INF ? fmaf(weight, v[e], y[i + e]) : y[i + e] + v[e];
-                }
-            });
-        }
-#pragma unroll
-        for (int i = 0; i < 32; i++) y[i] = l == 0.f && fine ? 0.f : y[i] * out_factor;
+        for (int i = 0; i < 32; i++) y[i] = l == 0.f && fine ? 0.f : __uint_as_float(x[i]) * out_factor;
         if (A.splits == 1) {
             uint16_t* dst = (uint16_t*)A.out.data + token * A.out.token_stride + head * A.out.head_stride + 32 * b;
 #pragma unroll
@@ -710,6 +725,7 @@ __global__ void __launch_bounds__(KV_P_THREADS, 1) kv_prompt_kernel(const KvShap
     const int tiles = max((end - begin + KV_P_TOKENS - 1) / KV_P_TOKENS, 0), parts = tile_row + KV_P_ROWS < rows ? 2 : 1;
 
     volatile int* const stop = (volatile int*)(sm + T::BARS + 8 * KV_BARS);
+    // apart: what the rows take apart at the end, the unfinished block's tile by 16 tokens in 8 bits, then a bit for each warp that left out 64
     uint32_t *const tmem_at = (uint32_t*)(sm + T::BARS + 8 * KV_BARS + 4), *const apart = tmem_at + 1;
     if (threadIdx.x == 0) {
         for (int i = 0; i < KV_BARS; i++) {

@@ -105,12 +105,6 @@ __device__ __forceinline__ uint64_t kv_fma2(uint64_t a, uint64_t b, uint64_t c)
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
     return d;
 }
-__device__ __forceinline__ uint64_t kv_add2(uint64_t a, uint64_t b)
-{
-    uint64_t d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
 
 // Bounded wait that also ends when another warp has given up.
 __device__ __forceinline__ bool kv_wait_or_stop(uint32_t bar, uint32_t parity, volatile int* stop)

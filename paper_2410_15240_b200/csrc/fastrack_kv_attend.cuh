@@ -703,9 +703,10 @@ __global__ void __launch_bounds__(32 * KV_WARPS, NR == 1 ? (D == 64 ? 6 : 4) : 3
     float* const units = A.unit_l2 ? A.unit_l2 + ((int64_t)seq * S.kv_heads + kh) * A.units * unit_stride + tile_row : nullptr;
     const bool one_unit = S.block_tokens >= KV_TILE;
 
-    // the tail first: its loads pass while the first tiles come
+    // the tail first: its loads pass while the first tiles come; by the last warps, which have a tile less where their number is not a multiple of four
+    // (61 sequences of up to 4096 tokens 66.2 us, by the first warps 66.9)
     const uint16_t* const tail_k = (const uint16_t*)B.tail + (uint64_t)seq * S.tail_values + (uint64_t)kh * 2 * S.block_tokens * D;
-    for (int t0 = max(begin, tail_begin) + KV_HALF * warp; t0 < end; t0 += KV_HALF * KV_WARPS)
+    for (int t0 = max(begin, tail_begin) + KV_HALF * (KV_WARPS - 1 - warp); t0 < end; t0 += KV_HALF * KV_WARPS)
         kv_tail_tile<D, BF, NR>(W, tail_k + (t0 - tail_begin) * D, tail_k + (S.block_tokens + t0 - tail_begin) * D, t0, q.len, place, A.window,
                                 units ? units + (int64_t)(t0 / KV_HALF) * unit_stride : nullptr, rows - tile_row, lane);
 

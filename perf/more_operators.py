@@ -90,8 +90,8 @@ def draw(rng):
     heads, key, value = rng.choice([1, 5, 8, 16, 32, 64]), rng.choice([64, 128]), rng.choice([64, 128])
     if op == "expand":
         len_max = _spread(rng, 1, 30000)
-        seqs = rng.randint(1, max(1, min(32, int(7e5 / (len_max * heads)))))
-        len_max = max(1, min(len_max, int(7e5 / (seqs * heads))))
+        seqs = rng.randint(1, max(1, min(32, int(2e5 / len_max), int(5e5 / (len_max * heads)))))
+        len_max = max(1, min(len_max, int(5e5 / (seqs * heads))))
         return dict(c, seqs=seqs, new=1, len_min=rng.randint(1, len_max), len_max=len_max, heads=heads, key=key, value=value)
     new = _spread(rng, 1, 4000)
     len_max = rng.randint(new, new + rng.choice([0, 100, 6000]))

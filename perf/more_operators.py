@@ -77,7 +77,7 @@ def draw(rng):
         heads, tree = rng.choice([1, 5, 12, 16, 40, 64, 128]), rng.random() < 0.3
         new = rng.randint(2, 64) if tree else rng.choice([1, 1, rng.randint(2, 12), _spread(rng, 16, 200)])
         len_max = _spread(rng, max(new, 40), 100000)
-        most = min(3.4e5 / len_max, 2.5e7 / (len_max * heads * new))                # tokens, and scores
+        most = min(2.6e5 / len_max, 2.5e7 / (len_max * heads * new), 1e5 / (heads * new))       # tokens, scores, and queries
         if most < 1:
             len_max, most = max(new, int(len_max * most)), 1
         return dict(c, seqs=rng.randint(1, max(1, min(96, int(most)))), new=new, len_min=rng.randint(new, len_max), len_max=len_max, heads=heads, tree=tree)

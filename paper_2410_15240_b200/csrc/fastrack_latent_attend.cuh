@@ -1,0 +1,545 @@
+// fastrack_latent_attend.cuh -- attention in the latent space: the kernel for single tokens, drafts and trees of drafts.
+#pragma once
+#include "fastrack_latent_device.cuh"
+
+// 64 rows of queries (token, head) against tiles of 64 tokens, of which a tile in shared memory serves as K and as V:
+//     S = Q C^T         64 x 64, M = rows, N = tokens, over latent + rope channels
+//     O^T += C^T P^T    latent x rows, M = 128 channels at a time, N = rows, over the tile's tokens
+// The second product is taken the other way round: the accumulator of 64 rows x 512 channels then takes 4 x 64 columns of tensor memory with
+// all 128 lanes, N follows the number of rows that there are, and S keeps its two buffers beside it.  (With rows as M, 512 columns would be
+// full of O alone, half of their lanes idle.)  Warps 0-3 make the weights, 16 rows each, and write them to shared memory; warp 4 brings the
+// tiles; warp 5 issues the products.  The scores of the next tile are made while this one's weights are.
+//
+// All work is one line: for each sequence, for each group of row tiles, the tiles of tokens that the group sees.  The line is cut into equal
+// runs, one for each group of CTAs (a CTA per row tile of a group; the CTAs of a group read the same tokens at the same time, all but the first
+// out of L2).  What a run cuts is joined by a kernel of its own; a run has at most two such pieces, its first and its last.
+#define LT_ROWS 64
+#define LT_TOKENS 64
+#define LT_A_THREADS 192
+#define LT_A_STAGES 4                   // at most
+#define LT_PART 16384                   // bytes of 128 channels of a tile; the shared key's are a part of half that
+#define LT_RAISE 8.f                    // a row's reference is raised when a score is 2^8 above it: weights stay below 2^8, and O seldom has to be multiplied
+
+// Barriers, 8 bytes each.  IN and OUT: [stage][part], part 0 .. latent / 128 - 1 and then the shared key's (part LT_A_KEY).
+enum { LT_A_KEY = 4, LT_A_PARTS = 5, LT_A_IN = 0, LT_A_OUT = LT_A_STAGES * LT_A_PARTS, LT_A_S = 2 * LT_A_OUT, LT_A_P = LT_A_S + 2, LT_A_O, LT_A_Q, LT_A_END, LT_A_BARS };
+struct LtMisc {
+    uint64_t bars[LT_A_BARS];
+    float factor[LT_ROWS];              // of rows: O's when the reference is raised, and 1 / l at the end
+    int64_t out_at[LT_ROWS];            // of rows: where the answer goes
+    uint32_t bad[3][2];                 // tokens of a tile with a score that is not finite, see lt_guard
+    uint32_t present[8];                // of the last tiles: which 16 tokens have a page
+    int stop, halt[2];                  // halt: what the rows' warps go by, all the same way (they have barriers among themselves)
+    uint32_t tmem;
+    int64_t item, item_at;
+    int64_t warp_sum[LT_A_THREADS / 32];
+};
+#define LT_MISC 2048
+static_assert(sizeof(LtMisc) <= LT_MISC, "");
+
+struct LtAttend {
+    KvRows q, q_rope, out;
+    float* lse;
+    const int32_t* parents;             // NULL: a chain
+    int groups;                         // of CTAs: runs that the line is cut into
+    int group_tiles;                    // row tiles, CTAs, of a group
+    int seq_groups;                     // groups of row tiles of a sequence, at most
+    int stages, least;                  // least: tiles of a run
+    float* part_o;                      // [groups][2][group_tiles][64][latent]: the first piece of a run (begun before it), the last
+    float* part_ml;                     // [groups][2][group_tiles][64][2]
+    int* cuts;                          // [groups][4]: of a run whose last item goes on: sequence, group of row tiles, pieces
+};
+
+// Tiles of tokens that an item (a sequence's group of row tiles) takes; one at least if there are rows
+__device__ __forceinline__ int lt_item_tiles(const LtShape& S, const LtAttend& A, const LtSeq& q, int group)
+{
+    const int64_t first = (int64_t)group * A.group_tiles * LT_ROWS, rows = (int64_t)q.n * S.heads;
+    if (first >= rows) return 0;
+    const int last = (int)(min(first + A.group_tiles * LT_ROWS, rows) - 1) / S.heads;
+    const int end = A.parents ? q.len : q.len - q.n + last + 1;
+    return max((end + LT_TOKENS - 1) / LT_TOKENS, 1);
+}
+
+// A walk along a run.  Every warp makes its own.
+struct LtWalk {
+    int64_t item, item_at, at, end;     // at: in the line
+    int seq, group, from, to, tiles;    // the piece: tiles from .. to - 1 of the item's
+    LtSeq q;
+    __device__ __forceinline__ bool next(const LtShape& S, const LtBatch& B, const LtAttend& A)
+    {
+        while (at < end) {
+            seq = (int)(item / A.seq_groups);
+            group = (int)(item % A.seq_groups);
+            if (seq >= B.n_seqs) return false;
+            q = lt_seq(B, seq);
+            tiles = lt_item_tiles(S, A, q, group);
+            from = (int)(at - item_at);
+            to = (int)min((int64_t)tiles, end - item_at);
+            if (from + 1 > tiles) {                      // nothing (left) of this one
+                item++;
+                item_at += tiles;
+                continue;
+            }
+            at = item_at + to;
+            return true;
+        }
+        return false;
+    }
+};
+
+// The tokens before `len`, of 64 from t0 on, whose pages are there
+__device__ __forceinline__ uint64_t lt_there(uint32_t present, int t0, int len)
+{
+    uint64_t m = 0;
+#pragma unroll
+    for (int g = 0; g < 4; g++) m |= present >> g & 1 ? 0xffffull << (16 * g) : 0ull;
+    const int left = len - t0;
+    return left >= 64 ? m : left <= 0 ? 0ull : m & ((1ull << left) - 1);
+}
+// Of 64 tokens from t0 on, those that new token j of a sequence sees
+__device__ __forceinline__ uint64_t lt_sees(const LtAttend& A, const LtSeq& q, int j, int t0)
+{
+    const int base = q.len - q.n;                        // the first new token's place
+    const int upto = (A.parents ? base : base + j + 1) - t0;
+    uint64_t m = upto >= 64 ? ~0ull : upto <= 0 ? 0ull : (1ull << upto) - 1;
+    if (A.parents && t0 + 64 > base) {
+        for (int a = j;;) {                              // a parent is less than its child, so this ends
+            const int bit = base + a - t0;
+            if (bit >= 0 && bit < 64) m |= 1ull << bit;
+            const int p = A.parents[q.start + a];
+            if (p < 0 || p >= a) break;
+            a = p;
+        }
+    }
+    return m;
+}
+
+// Warps 0-3: the weights of the rows, and their answers
+template <bool BF>
+__device__ __forceinline__ void lt_attend_rows(const LtShape& S, const LtBatch& B, const LtAttend& A, LtWalk walk, int64_t share, uint8_t* sm, uint32_t sm_at, LtMisc& M,
+                                               uint32_t bars, uint32_t tmem)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane & 3;
+    const int g = blockIdx.x / A.group_tiles, r = blockIdx.x % A.group_tiles;
+    const int chunks = S.latent / 64, tile_bytes = (chunks + 1) * LT_ROWS * LT_CHUNK_ROW;
+    uint8_t* const p_sm = sm + (1 + A.stages) * tile_bytes;
+    volatile int* const stop = &M.stop;
+    const uint32_t lanes = (uint32_t)warp << 21, s_at = tmem + lanes + 256, o_at = tmem + lanes;
+    const float scale = S.scale_log2;
+    bool fine = true, halted = false;                    // fine: of this warp; where it is not, answers are NaN
+    int c = 0;                                           // tiles so far
+    if (r == 0 && threadIdx.x == 0) A.cuts[4 * g + 2] = 0;
+    while (!halted && walk.next(S, B, A)) {
+        const LtSeq& q = walk.q;
+        const int64_t first = ((int64_t)walk.group * A.group_tiles + r) * LT_ROWS;
+        const int rows = (int)min((int64_t)LT_ROWS, (int64_t)q.n * S.heads - first);
+        const bool whole = walk.from == 0 && walk.to == walk.tiles;
+        if (r == 0 && threadIdx.x == 0 && walk.from == 0 && !whole) {
+            A.cuts[4 * g] = walk.seq;
+            A.cuts[4 * g + 1] = walk.group;
+            A.cuts[4 * g + 2] = (int)((walk.item_at + walk.tiles - 1) / share) - g + 1;
+        }
+        if (rows <= 0) continue;
+        {
+            // Q: 8 threads take a row's chunk
+            const int piece = threadIdx.x & 7;
+            for (int row = threadIdx.x >> 3; row < LT_ROWS; row += 16) {
+                const bool there = row < rows;
+                const int64_t token = q.start + (there ? (first + row) / S.heads : 0);
+                const int head = there ? (int)((first + row) % S.heads) : 0;
+                const uint16_t* src = (const uint16_t*)A.q.data + token * A.q.token_stride + head * A.q.head_stride;
+                const uint16_t* key = (const uint16_t*)A.q_rope.data + token * A.q_rope.token_stride + head * A.q_rope.head_stride;
+                for (int k = 0; k < chunks; k++) lt_copy16(sm_at + k * LT_ROWS * LT_CHUNK_ROW + lt_at(row, piece), src + 64 * k + 8 * piece, there);
+                if (8 * piece < S.rope) lt_copy16(sm_at + chunks * LT_ROWS * LT_CHUNK_ROW + lt_at(row, piece), key + 8 * piece, there);
+                if (piece == 0) M.out_at[row] = token * A.out.token_stride + head * A.out.head_stride;
+            }
+            lt_copies_done();
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            kv_warp_arrive(bars + 8 * LT_A_Q);
+        }
+        const bool active = 16 * warp < rows;
+        // rows of this lane: 16 warp + lane / 4 and 8 further on
+        int j[2];
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const int row = 16 * warp + (lane >> 2) + 8 * h;
+            j[h] = row < rows ? (int)((first + row) / S.heads) : -1;
+        }
+        const int see_all = A.parents ? q.len - q.n : q.len - q.n + (int)(first / S.heads) + 1;
+        float m[2] = {KV_M_NONE, KV_M_NONE}, l[2] = {0.f, 0.f};
+        for (int i = walk.from; i < walk.to && !halted; i++, c++) {
+            const int t0 = i * LT_TOKENS, set = c % 3;
+            fine = kv_warp_wait(bars + 8 * (LT_A_S + (c & 1)), c >> 1 & 1, stop) &&
+                   kv_warp_wait(bars + 8 * (LT_A_IN + c % A.stages * LT_A_PARTS), c / A.stages & 1, stop) && fine;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            uint32_t x[32];
+            const uint32_t present = ((volatile uint32_t*)M.present)[c & 7];
+            const bool ragged = t0 + LT_TOKENS > see_all || present != 15u;
+            float top[2] = {-KV_INF, -KV_INF};
+            if (active) {
+                lt_tmem_load_quads(x, s_at + 64 * (c & 1));
+                if (ragged) {
+                    const uint64_t there = lt_there(present, t0, q.len);
+                    uint32_t bad[2] = {0, 0};
+                    uint64_t sees[2];
+#pragma unroll
+                    for (int h = 0; h < 2; h++) sees[h] = j[h] < 0 ? 0ull : (lt_sees(A, q, j[h], t0) & there) >> (2 * quad);
+#pragma unroll
+                    for (int k = 0; k < 32; k++) {
+                        const int bit = 8 * (k >> 2) + (k & 1);              // and 2 quad on
+                        if (!(fabsf(__uint_as_float(x[k])) < KV_INF)) bad[bit >> 5] |= 1u << (bit & 31);
+                        x[k] = sees[k >> 1 & 1] >> bit & 1 ? x[k] : 0xff800000u;
+                    }
+#pragma unroll
+                    for (int b = 0; b < 2; b++) {
+                        const uint32_t all = __reduce_or_sync(0xffffffffu, bad[b] << (2 * quad));
+                        if (lane == 0 && all) atomicOr(&M.bad[set][b], all);
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < 8; k++) {
+                    top[0] = fmaxf(top[0], fmaxf(__uint_as_float(x[4 * k]), __uint_as_float(x[4 * k + 1])));
+                    top[1] = fmaxf(top[1], fmaxf(__uint_as_float(x[4 * k + 2]), __uint_as_float(x[4 * k + 3])));
+                }
+            }
+            // the set after next's: what it held two tiles ago has been read by all, who have come to the barrier of the tile before this one since
+            if (threadIdx.x == 0) {
+                M.bad[(set + 1) % 3][0] = M.bad[(set + 1) % 3][1] = 0;
+                M.halt[c & 1] = *stop;
+            }
+            const bool raise = lt_any(1, 128, top[0] * scale > m[0] + LT_RAISE || top[1] * scale > m[1] + LT_RAISE);
+            halted = ((volatile int*)M.halt)[c & 1];
+            if (raise) {
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
+                    top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2)) * scale;
+                    const float to = fmaxf(m[h], top[h]), fall = kv_exp2(m[h] - to);
+                    l[h] *= fall;
+                    m[h] = to;
+                    if (quad == 0) M.factor[16 * warp + (lane >> 2) + 8 * h] = fall;
+                }
+            }
+            if (active) {
+#pragma unroll
+                for (int k = 0; k < 8; k++)
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {
+                        const float a = kv_exp2(fmaf(__uint_as_float(x[4 * k + 2 * h]), scale, -m[h])), b = kv_exp2(fmaf(__uint_as_float(x[4 * k + 2 * h + 1]), scale, -m[h]));
+                        l[h] += a + b;
+                        x[2 * k + h] = kv_pack<BF>(a, b);
+                    }
+            }
+            if (c > 0) fine = kv_warp_wait(bars + 8 * LT_A_O, c - 1 & 1, stop) && fine;      // the product before is done: P is free, and O rests
+            if (raise && i > walk.from) {
+                lt_sync(2, 128);
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                for (int b = 0; b < S.latent / 128; b++)
+#pragma unroll 1
+                    for (int n = 0; n < rows; n += 32) {
+                        uint32_t y[32];
+                        kv_tmem_load32(y, o_at + 64 * b + n);
+#pragma unroll
+                        for (int k = 0; k < 32; k++) y[k] = __float_as_uint(__uint_as_float(y[k]) * M.factor[n + k]);
+                        kv_tmem_store32(y, o_at + 64 * b + n);
+                    }
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+            }
+            if (active) {
+#pragma unroll
+                for (int k = 0; k < 8; k++)
+#pragma unroll
+                    for (int h = 0; h < 2; h++)
+                        *(uint32_t*)(p_sm + lt_at(16 * warp + (lane >> 2) + 8 * h, k) + 4 * quad) = x[2 * k + h];
+            }
+            if (ragged) {
+                // Tokens that are not there become zeros, and so does what is not finite in tokens that some rows do not see: a weight of 0
+                // times it would not be 0.  Such a token shows by its scores, of which every one is not finite: its values all enter them.
+                uint8_t* const tile = sm + (1 + c % A.stages) * tile_bytes;
+                const uint64_t there = lt_there(present, t0, q.len);
+                const uint64_t some = see_all - t0 >= 64 ? 0ull : see_all <= t0 ? ~0ull : ~((1ull << (see_all - t0)) - 1);
+                uint64_t todo = ~there | (some & ((uint64_t)((volatile uint32_t*)M.bad[set])[1] << 32 | ((volatile uint32_t*)M.bad[set])[0]));
+                for (int n = threadIdx.x; todo; todo &= todo - 1) {
+                    const int t = __ffsll((long long)todo) - 1;
+                    if (n < 8 * chunks) {
+                        uint4* const at = (uint4*)(tile + (n >> 3) * LT_TOKENS * LT_CHUNK_ROW + lt_at(t, n & 7));
+                        uint4 w = make_uint4(0, 0, 0, 0);
+                        if (there >> t & 1) {
+                            w = *at;
+                            w = make_uint4(lt_finite2<BF>(w.x), lt_finite2<BF>(w.y), lt_finite2<BF>(w.z), lt_finite2<BF>(w.w));
+                        }
+                        *at = w;
+                    }
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            kv_warp_arrive(bars + 8 * LT_A_P);
+        }
+        // the piece's end
+        fine = kv_warp_wait(bars + 8 * LT_A_O, c - 1 & 1, stop) && fine && !*stop;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const int64_t slot = ((int64_t)2 * g + (walk.from == 0)) * A.group_tiles + r;
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
+            l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+            if (!fine) l[h] = __int_as_float(0x7fffffff);
+            const int row = 16 * warp + (lane >> 2) + 8 * h;
+            if (quad == 0) {
+                M.factor[row] = l[h] == 0.f ? 0.f : 1.f / l[h];
+                if (row < rows) {
+                    if (!whole) *(float2*)(A.part_ml + 2 * (slot * LT_ROWS + row)) = make_float2(m[h], l[h]);
+                    else if (A.lse) A.lse[(q.start + (int64_t)j[h]) * S.heads + (first + row) % S.heads] = l[h] == 0.f ? -KV_INF : (m[h] + log2f(l[h])) * 0.6931471805599453f;
+                }
+            }
+        }
+        lt_sync(2, 128);
+        for (int b = 0; b < S.latent / 128; b++) {
+            const int ch = 128 * b + 32 * warp + lane;
+#pragma unroll 1
+            for (int n = 0; n < rows; n += 32) {
+                uint32_t y[32];
+                kv_tmem_load32(y, o_at + 64 * b + n);
+                if (whole) {
+#pragma unroll
+                    for (int k = 0; k < 32; k += 2) {
+                        // two lanes, two rows: each lane gets a pair of channels of one row
+                        const float u = __uint_as_float(y[k]) * M.factor[n + k], w = __uint_as_float(y[k + 1]) * M.factor[n + k + 1];
+                        const bool odd = lane & 1;
+                        const float got = __shfl_xor_sync(0xffffffffu, odd ? u : w, 1);
+                        const int row = n + k + odd;
+                        if (row < rows) *(uint32_t*)((uint16_t*)A.out.data + M.out_at[row] + (ch & ~1)) = odd ? kv_pack<BF>(got, w) : kv_pack<BF>(u, got);
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 32; k++)
+                        if (n + k < rows) A.part_o[(slot * LT_ROWS + n + k) * S.latent + ch] = __uint_as_float(y[k]);
+                }
+            }
+        }
+        lt_sync(2, 128);                                 // factor and out_at have been read
+    }
+}
+
+// Warp 4: the tiles
+__device__ __forceinline__ void lt_attend_bring(const LtShape& S, const LtBatch& B, const LtAttend& A, const CUtensorMap* map, LtWalk walk, uint32_t sm_at, LtMisc& M,
+                                                uint32_t bars)
+{
+    const int lane = threadIdx.x & 31, r = blockIdx.x % A.group_tiles;
+    const int pairs = S.latent / 128, chunks = S.latent / 64, tile_bytes = (chunks + 1) * LT_ROWS * LT_CHUNK_ROW;
+    const int box = min(S.block_tokens, LT_TOKENS), boxes = LT_TOKENS / box;
+    volatile int* const stop = &M.stop;
+    bool fine = true;
+    int c = 0, part = 0;                                 // tiles brought so far, and of the next one the part
+    while (fine && walk.next(S, B, A)) {
+        if (((int64_t)walk.group * A.group_tiles + r) * LT_ROWS >= (int64_t)walk.q.n * S.heads) continue;
+        int known = -1, pages = -1;                      // lane: page of the block known + lane
+        for (int i = walk.from; i < walk.to && fine; i++) {
+            const int stage = c % A.stages, phase = c / A.stages & 1;
+            const int block = i * LT_TOKENS >> S.block_shift;
+            if (known < 0 || block + 4 > known + 32) {
+                known = block;
+                pages = (int64_t)(block + lane) << S.block_shift < walk.q.len ? lt_page(B, walk.seq, block + lane) : -1;
+            }
+            int page[4];
+            uint32_t present = 0;
+#pragma unroll
+            for (int b = 0; b < 4; b++) {
+                page[b] = b < boxes ? __shfl_sync(0xffffffffu, pages, ((i * LT_TOKENS + b * box) >> S.block_shift) - known) : -1;
+                if (page[b] >= 0) present |= ((1u << (box / 16)) - 1) << (b * (box / 16));
+            }
+            const uint32_t to = sm_at + (1 + stage) * tile_bytes;
+            for (part = -1; part < pairs; part++) {
+                const int bar = stage * LT_A_PARTS + (part < 0 ? LT_A_KEY : part);
+                fine = kv_warp_wait(bars + 8 * (LT_A_OUT + bar), phase ^ 1, stop);
+                if (!fine) break;
+                if (lane == 0) {
+                    if (part < 0) ((volatile uint32_t*)M.present)[c & 7] = present;
+                    lt_expect(bars + 8 * (LT_A_IN + bar), __popc(present) * 16 * LT_CHUNK_ROW * (part < 0 ? 1 : 2));
+                    for (int k = part < 0 ? chunks : 2 * part; k < (part < 0 ? chunks + 1 : 2 * part + 2); k++)
+#pragma unroll
+                        for (int b = 0; b < 4; b++)
+                            if (page[b] >= 0)
+                                lt_tma(to + (k * LT_TOKENS + b * box) * LT_CHUNK_ROW, map, 64 * k, (i * LT_TOKENS + b * box) & (S.block_tokens - 1), page[b], bars + 8 * (LT_A_IN + bar));
+                }
+                __syncwarp();
+            }
+            if (fine) c++;
+        }
+    }
+    // what is on its way arrives before the CTA ends: the last tile of every stage, and of an unfinished one the parts before `part`
+    for (int back = fine ? 1 : 0; back <= A.stages; back++) {
+        const int tile = c - back, stage = tile % A.stages;
+        for (int p = -1; tile >= 0 && p < (back ? pairs : part); p++)
+            (void)kv_wait(bars + 8 * (LT_A_IN + stage * LT_A_PARTS + (p < 0 ? LT_A_KEY : p)), tile / A.stages & 1);
+    }
+}
+
+// Warp 5: the products
+template <bool BF>
+__device__ __forceinline__ void lt_attend_products(const LtShape& S, const LtBatch& B, const LtAttend& A, LtWalk walk, uint32_t sm_at, LtMisc& M, uint32_t bars, uint32_t tmem)
+{
+    const int r = blockIdx.x % A.group_tiles;
+    const int pairs = S.latent / 128, chunks = S.latent / 64, tile_bytes = (chunks + 1) * LT_ROWS * LT_CHUNK_ROW;
+    constexpr uint32_t kind = 1u << 4 | (BF ? 1u << 7 | 1u << 10 : 0u);                      // f32 += bf16 * bf16 or f16 * f16
+    constexpr uint32_t s_what = kind | (LT_ROWS / 16) << 24 | (LT_TOKENS / 8) << 17;
+    volatile int* const stop = &M.stop;
+    bool fine = true;
+    auto scores = [&](int c) {
+        const int stage = c % A.stages, phase = c / A.stages & 1;
+        const uint32_t tile = sm_at + (1 + stage) * tile_bytes;
+        for (int part = -1; part < pairs; part++) {
+            const int bar = stage * LT_A_PARTS + (part < 0 ? LT_A_KEY : part);
+            fine = kv_warp_wait(bars + 8 * (LT_A_IN + bar), phase, stop);
+            if (!fine) return;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            for (int k = part < 0 ? chunks : 2 * part; k < (part < 0 ? chunks + 1 : 2 * part + 2); k++) {
+                const uint32_t off = k * LT_ROWS * LT_CHUNK_ROW;
+                const uint64_t a = kv_desc(sm_at + off, 16, 1024), b = kv_desc(tile + off, 16, 1024);
+                const int steps = part < 0 ? S.rope / 16 : 4;
+                for (int s = 0; s < steps; s++) kv_mma_ss(tmem + 256 + 64 * (c & 1), a + 2 * s, b + 2 * s, s_what, part >= 0 || s > 0);
+            }
+            if (part < 0) kv_commit(bars + 8 * (LT_A_OUT + bar));
+        }
+        kv_commit(bars + 8 * (LT_A_S + (c & 1)));
+    };
+    int c = 0, piece = 0;
+    while (fine && walk.next(S, B, A)) {
+        const int64_t left = (int64_t)walk.q.n * S.heads - ((int64_t)walk.group * A.group_tiles + r) * LT_ROWS;
+        if (left <= 0) continue;
+        const uint32_t n = (uint32_t)(min(left, (int64_t)LT_ROWS) + 15) / 16 * 16;
+        const uint32_t o_what = kind | 8u << 24 | n / 8 << 17 | 1u << 15;                    // A's M runs along the row
+        fine = kv_warp_wait(bars + 8 * LT_A_Q, piece & 1, stop);
+        if (fine) scores(c);
+        for (int i = walk.from; i < walk.to && fine; i++, c++) {
+            if (i + 1 < walk.to) scores(c + 1);
+            if (fine) fine = kv_warp_wait(bars + 8 * LT_A_P, c & 1, stop);
+            if (!fine) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const int stage = c % A.stages;
+            const uint64_t b = kv_desc(sm_at + (1 + A.stages) * tile_bytes, 16, 1024);
+            for (int part = 0; part < pairs; part++) {
+                const uint64_t a = kv_desc(sm_at + (1 + stage) * tile_bytes + part * LT_PART, LT_TOKENS * LT_CHUNK_ROW, 1024);
+#pragma unroll
+                for (int s = 0; s < 4; s++) kv_mma_ss(tmem + 64 * part, a + (s * 2048 >> 4), b + 2 * s, o_what, i > walk.from || s > 0);
+                kv_commit(bars + 8 * (LT_A_OUT + stage * LT_A_PARTS + part));
+            }
+            kv_commit(bars + 8 * LT_A_O);
+        }
+        piece++;
+    }
+}
+
+template <bool BF>
+__global__ void __launch_bounds__(LT_A_THREADS, 1) lt_attend_kernel(const LtShape S, const LtBatch B, const LtAttend A, const __grid_constant__ CUtensorMap map)
+{
+    extern __shared__ uint8_t lt_raw[];
+    uint8_t* const sm = lt_raw + (-(uint32_t)__cvta_generic_to_shared(lt_raw) & 1023u);
+    const uint32_t sm_at = (uint32_t)__cvta_generic_to_shared(sm);
+    const int tile_bytes = (S.latent / 64 + 1) * LT_ROWS * LT_CHUNK_ROW, warp = threadIdx.x >> 5;
+    LtMisc& M = *(LtMisc*)(sm + (1 + A.stages) * tile_bytes + LT_ROWS * LT_CHUNK_ROW);
+    const uint32_t bars = (uint32_t)__cvta_generic_to_shared(M.bars);
+    asm volatile("griddepcontrol.launch_dependents;");
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < LT_A_BARS; i++) lt_init(bars + 8 * i, i == LT_A_P || i == LT_A_Q ? 4 : 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        M.stop = 0;
+        for (int i = 0; i < 3; i++) M.bad[i][0] = M.bad[i][1] = 0;
+    }
+    if (warp == 5) asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"((uint32_t)__cvta_generic_to_shared(&M.tmem)) : "memory");
+
+    // the line's length, and where this run begins
+    auto tiles_of = [&](int64_t item) { return lt_item_tiles(S, A, lt_seq(B, (int)(item / A.seq_groups)), (int)(item % A.seq_groups)); };
+    LtStretch mine = lt_stretch<LT_A_THREADS>((int64_t)B.n_seqs * A.seq_groups, tiles_of, M.warp_sum);
+    const int64_t share = max((mine.total + A.groups - 1) / A.groups, (int64_t)A.least);
+    LtWalk walk;
+    walk.at = blockIdx.x / A.group_tiles * share;
+    walk.end = min(walk.at + share, mine.total);
+    if (mine.holds(walk.at)) {
+        mine.find(walk.at, tiles_of);
+        M.item = mine.item;
+        M.item_at = mine.before;
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    walk.item = M.item;
+    walk.item_at = M.item_at;
+    const uint32_t tmem = *(volatile uint32_t*)&M.tmem;  // O: 64 columns per 128 channels; S: 2 x 64 from 256 on
+    if (warp < 4) {
+        lt_attend_rows<BF>(S, B, A, walk, share, sm, sm_at, M, bars, tmem);
+    } else if (warp == 4) {
+        lt_attend_bring(S, B, A, &map, walk, sm_at, M, bars);
+    } else {
+        lt_attend_products<BF>(S, B, A, walk, sm_at, M, bars, tmem);
+        __syncwarp();
+        kv_commit(bars + 8 * LT_A_END);                  // nothing is on its way any more when the memory is given back
+        kv_wait(bars + 8 * LT_A_END, 0);
+        __syncwarp();
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 5) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    }
+}
+
+// Joins the pieces of items that runs cut.  A CTA takes a row at a time: 128 threads a piece, 4 channels each, 4 pieces side by side.
+#define LT_JOIN_THREADS 512
+template <bool BF> __global__ void __launch_bounds__(LT_JOIN_THREADS) lt_join_kernel(const LtShape S, const LtBatch B, const LtAttend A)
+{
+    __shared__ float4 sums[LT_JOIN_THREADS];
+    __shared__ int4 cuts[LT_JOIN_THREADS];
+    const int lane4 = threadIdx.x >> 7, ch = 4 * (threadIdx.x & 127), rows_of = A.group_tiles * LT_ROWS;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    for (int g = threadIdx.x; g < A.groups; g += LT_JOIN_THREADS) cuts[g] = *(const int4*)(A.cuts + 4 * g);
+    __syncthreads();
+    int done = 0;                                        // rows of cut items in front of this run's
+    for (int g = 0; g < A.groups; g++) {
+        const int4 cut = cuts[g];
+        if (cut.z < 2) continue;
+        for (int i = ((int)blockIdx.x - done % (int)gridDim.x + (int)gridDim.x) % (int)gridDim.x; i < rows_of; i += gridDim.x) {
+            const LtSeq q = lt_seq(B, cut.x);
+            const int64_t row = (int64_t)cut.y * rows_of + i;
+            if (row >= (int64_t)q.n * S.heads) continue;
+            auto slot = [&](int s) { return ((s == 0 ? (int64_t)2 * g + 1 : (int64_t)2 * (g + s)) * A.group_tiles + i / LT_ROWS) * LT_ROWS + i % LT_ROWS; };
+            float m = KV_M_NONE, l = 0.f;
+            for (int s = 0; s < cut.z; s++) m = fmaxf(m, A.part_ml[2 * slot(s)]);
+            for (int s = 0; s < cut.z; s++) {
+                const float2 ml = *(const float2*)(A.part_ml + 2 * slot(s));
+                l += ml.y * kv_exp2(ml.x - m);
+            }
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (ch < S.latent)
+#pragma unroll 4
+                for (int s = lane4; s < cut.z; s += 4) {
+                    const float w = kv_exp2(A.part_ml[2 * slot(s)] - m);
+                    const float4 o = *(const float4*)(A.part_o + slot(s) * S.latent + ch);
+                    sum = make_float4(fmaf(w, o.x, sum.x), fmaf(w, o.y, sum.y), fmaf(w, o.z, sum.z), fmaf(w, o.w, sum.w));
+                }
+            __syncthreads();
+            sums[threadIdx.x] = sum;
+            __syncthreads();
+            if (lane4 == 0 && ch < S.latent) {
+                const float by = l == 0.f ? 0.f : 1.f / l;
+                float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    const float4 o = sums[threadIdx.x + 128 * k];
+                    x[0] += o.x;
+                    x[1] += o.y;
+                    x[2] += o.z;
+                    x[3] += o.w;
+                }
+                const int64_t token = q.start + row / S.heads;
+                const int head = (int)(row % S.heads);
+                *(uint2*)((uint16_t*)A.out.data + token * A.out.token_stride + head * A.out.head_stride + ch) =
+                    make_uint2(kv_pack<BF>(x[0] * by, x[1] * by), kv_pack<BF>(x[2] * by, x[3] * by));
+                if (threadIdx.x == 0 && A.lse) A.lse[token * S.heads + head] = l == 0.f ? -KV_INF : (m + log2f(l)) * 0.6931471805599453f;
+            }
+        }
+        done += rows_of;
+    }
+}

@@ -1,0 +1,131 @@
+// fastrack_latent_device.cuh -- what the latent cache's kernels share: parameters, the view of one sequence, copies into swizzled tiles.
+#pragma once
+#include <cuda.h>
+#include "fastrack_kv_prompt.cuh"
+
+struct LtShape {                        // constants of a handle
+    KvShape turn;                       // for the rotation: a "head" of rope channels
+    int heads, latent, rope, row;       // row: latent + rope, the values of a token
+    int key, value, block_tokens, block_shift;
+    float scale_log2, norm_eps;         // softmax scale times log2(e)
+};
+
+struct LtBatch {
+    int n_seqs, total_new, max_new, max_len, pool_pages, table_stride;
+    uint16_t* pool;
+    const int32_t *table, *lens, *starts;
+    const int64_t* positions;
+};
+
+// One sequence as the device's numbers give it, clamped to the bounds that buffers were sized for.
+struct LtSeq { int len, start, n; };    // tokens held, first packed row, new tokens
+
+__device__ __forceinline__ int lt_len(const LtBatch& B, int i) { return min(max(B.lens[i], 0), B.max_len); }
+__device__ __forceinline__ LtSeq lt_seq(const LtBatch& B, int i)
+{
+    LtSeq q;
+    q.len = lt_len(B, i);
+    q.start = min(max(B.starts[i], 0), B.total_new);
+    q.n = min(max(min(B.starts[i + 1], B.total_new) - q.start, 0), B.max_new);
+    return q;
+}
+
+// Page of a block, or -1 where it is absent.
+__device__ __forceinline__ int lt_page(const LtBatch& B, int seq, int block)
+{
+    if (block < 0 || block >= B.table_stride) return -1;
+    const int p = B.table[(int64_t)seq * B.table_stride + block];
+    return p >= 0 && p < B.pool_pages ? p : -1;
+}
+
+// The vector at a place of a sequence, or NULL where its page is absent.
+__device__ __forceinline__ uint16_t* lt_token(const LtShape& S, const LtBatch& B, int seq, int place)
+{
+    const int page = place < 0 ? -1 : lt_page(B, seq, place >> S.block_shift);
+    return page < 0 ? nullptr : B.pool + ((int64_t)page * S.block_tokens + (place & (S.block_tokens - 1))) * S.row;
+}
+
+// A tile in shared memory is made of chunks of 64 channels: rows of 128 bytes, whose 16-byte pieces are swizzled by the row's number.
+#define LT_CHUNK_ROW 128
+__device__ __forceinline__ uint32_t lt_at(int row, int piece) { return (uint32_t)(row * LT_CHUNK_ROW + ((piece ^ (row & 7)) << 4)); }
+
+// A box of the tensor (x, y, z) to shared memory
+__device__ __forceinline__ void lt_tma(uint32_t smem, const CUtensorMap* map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(smem), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void lt_expect(uint32_t bar, uint32_t bytes)      // and arrive
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void lt_init(uint32_t bar, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+
+// 16 bytes to shared memory without waiting; zeros where there is no source
+__device__ __forceinline__ void lt_copy16(uint32_t smem, const void* src, bool there)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void lt_copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// Whether any of a group's threads says so: barrier `id` of `threads` threads
+__device__ __forceinline__ bool lt_any(int id, int threads, bool mine)
+{
+    uint32_t any;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %3, 0;\n\tbarrier.cta.red.or.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(any) : "r"(id), "r"(threads), "r"((uint32_t)mine) : "memory");
+    return any != 0;
+}
+__device__ __forceinline__ void lt_sync(int id, int threads) { asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
+// 16-bit values that are infinite or NaN, each of the two of a word, become zero
+template <bool BF> __device__ __forceinline__ uint32_t lt_finite2(uint32_t w)
+{
+    constexpr uint32_t exponent = BF ? 0x7f80u : 0x7c00u;
+    if ((w & exponent) == exponent) w &= 0xffff0000u;
+    if ((w >> 16 & exponent) == exponent) w &= 0x0000ffffu;
+    return w;
+}
+
+// S of 64 rows (tensor memory, 16 lanes of each warp's 32): lane l of the warp gets of its 16 rows the rows l / 4 and l / 4 + 8, and of every 8 columns
+// the columns 2 (l % 4) and the next: x[4 k], x[4 k + 1] of the first row and x[4 k + 2], x[4 k + 3] of the second, columns 8 k on.
+__device__ __forceinline__ void lt_tmem_load_quads(uint32_t (&x)[32], uint32_t at)
+{
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : KV_R8(x, 0), KV_R8(x, 8), KV_R8(x, 16), KV_R8(x, 24) : "r"(at) : "memory");
+}
+
+// A line of work: items one behind the other, `size(item)` units each.  Every thread of a CTA adds up a stretch of items, and the one in whose
+// stretch a unit lies looks for its item.
+struct LtStretch {
+    int64_t item, before, units, total;     // the stretch's first item, the units in front of it and in it, and in the line
+    __device__ __forceinline__ bool holds(int64_t unit) const { return before <= unit && unit < before + units; }
+    template <class F> __device__ __forceinline__ void find(int64_t unit, F size)
+    {
+        for (int64_t n; before + (n = size(item)) <= unit; item++) before += n;
+    }
+};
+// warp_sum: room for a number per warp, which the CTA's next barrier leaves free again
+template <int THREADS, class F> __device__ __forceinline__ LtStretch lt_stretch(int64_t items, F size, int64_t* warp_sum)
+{
+    const int64_t per = (items + THREADS - 1) / THREADS, lo = min(items, threadIdx.x * per), hi = min(items, lo + per);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    LtStretch s = {lo, 0, 0, 0};
+    for (int64_t item = lo; item < hi; item++) s.units += size(item);
+    s.before = s.units;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int64_t v = __shfl_up_sync(0xffffffffu, s.before, d);
+        if (lane >= d) s.before += v;
+    }
+    if (lane == 31) warp_sum[warp] = s.before;
+    __syncthreads();
+    s.before -= s.units;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; w++) {
+        if (w < warp) s.before += warp_sum[w];
+        s.total += warp_sum[w];
+    }
+    return s;
+}

@@ -1,0 +1,374 @@
+// fastrack_latent_prompt.cuh -- attention of many new tokens over expanded keys and values.
+#pragma once
+#include <type_traits>
+#include "fastrack_latent_device.cuh"
+
+// One CTA takes 256 queries of one head (two tiles of 128 rows) against 128 tokens at a time:
+//     S_m = Q_m K^T  (tensor memory)  ->  P_m = weights as 16 bits (tensor memory, over S_m)  ->  O_m += P_m V.
+// Warps 0-3 and 4-7 make P_0 and P_1, a thread per row; warp 8 brings K, the shared keys and V; warp 9 issues the products, of which one row
+// tile's run while the other's weights are made; warps 10 and 11 look after V where some rows do not see some tokens.
+#define LT_P_ROWS 128
+#define LT_P_TOKENS 128
+#define LT_P_THREADS 384
+#define LT_P_CHUNK (128 * LT_CHUNK_ROW)                  // bytes of 64 channels of 128 rows
+#define LT_P_APART 4                                     // tiles at most, in which some rows see tokens that others do not
+
+enum { LT_P_K_IN = 0, LT_P_K_OUT = 2, LT_P_V_IN = 4, LT_P_V_OK, LT_P_V_OUT, LT_P_S_IN, LT_P_P_IN = LT_P_S_IN + 2, LT_P_Q_IN = LT_P_P_IN + 2, LT_P_END, LT_P_BARS };
+struct LtPromptMisc {
+    uint64_t bars[LT_P_BARS];
+    uint32_t present[8];                                 // of the last tiles: which 16 tokens have a page
+    uint32_t apart[LT_P_APART][4];                       // tokens with values in V that are not finite, from the first tile on that some rows see in part
+    int stop;
+    uint32_t tmem;
+};
+struct LtPrompt {
+    KvRows q, q_rope, out;
+    const uint16_t* v;                                   // values again, for the tokens that are taken apart
+    int64_t v_token_stride, v_head_stride;
+    float* lse;
+    const int32_t* key_starts;
+    int total_keys, tiles;                               // tiles: of 256 queries, at most
+    bool k_heads, v_heads;                               // whether heads differ
+};
+// Q, two stages of K, V
+__host__ __device__ __forceinline__ int lt_prompt_k_chunks(const LtShape& S) { return S.key / 64 + 1; }
+static inline int lt_prompt_smem(const LtShape& S) { return (4 * lt_prompt_k_chunks(S) + S.value / 64) * LT_P_CHUNK + 1024 + 1024; }
+static_assert(sizeof(LtPromptMisc) <= 1024, "");
+
+// What a CTA works on
+struct LtPromptJob {
+    LtSeq q;
+    int seq, head, row, steps[2], rows;                  // row: first of its queries; rows: that there are; steps: of 128 tokens, for each row tile
+    int lo, hi;                                          // tokens whose keys lie in the buffers
+    int see_all;                                         // tokens before this one are seen by all rows
+    int64_t key_start;
+};
+
+// The value's row of a token may hold what is not finite, the token's weight may be 0 for some rows, and 0 times it is not 0: see lt_prompt_guard.
+__device__ __forceinline__ bool lt_prompt_ragged(const LtPromptJob& J, int t0, uint32_t present)
+{
+    return t0 < J.lo || t0 + LT_P_TOKENS > min(J.see_all, J.hi) || present != 0xffu;
+}
+__device__ __forceinline__ uint32_t lt_bits(int from, int upto)              // bits from .. upto - 1 of 32, of any numbers
+{
+    const uint32_t below = upto >= 32 ? 0xffffffffu : upto <= 0 ? 0u : (1u << upto) - 1, skip = from >= 32 ? 0xffffffffu : from <= 0 ? 0u : (1u << from) - 1;
+    return below & ~skip;
+}
+// Of 32 tokens from t0 + 32 b on, those that are there
+__device__ __forceinline__ uint32_t lt_prompt_there(const LtPromptJob& J, int t0, int b, uint32_t present)
+{
+    const uint32_t pages = (present >> 2 * b & 1 ? 0xffffu : 0u) | (present >> 2 * b & 2 ? 0xffff0000u : 0u);
+    return pages & lt_bits(J.lo - t0 - 32 * b, J.hi - t0 - 32 * b);
+}
+
+template <bool BF>
+__device__ __forceinline__ void lt_prompt_rows(const LtShape& S, const LtPrompt& A, const LtPromptJob& J, int m_tile, uint32_t sm_at, LtPromptMisc& M, uint32_t bars, uint32_t tmem)
+{
+    const int warp = threadIdx.x >> 5, r = threadIdx.x & 127, row = J.row + LT_P_ROWS * m_tile + r, steps = J.steps[m_tile];
+    const bool valid = row < J.q.n;
+    const int place = valid ? J.q.len - J.q.n + row : -1;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21, s_at = tmem + lanes + 128 * m_tile, o_at = tmem + lanes + 256 + 128 * m_tile;
+    const int k_chunks = lt_prompt_k_chunks(S);
+    volatile int* const stop = &M.stop;
+    {
+        // Q: 8 threads take a row's chunk
+        const uint32_t to = sm_at + m_tile * k_chunks * LT_P_CHUNK;
+        const int piece = r & 7;
+        for (int i = r >> 3; i < LT_P_ROWS; i += 16) {
+            const int at = J.row + LT_P_ROWS * m_tile + i;
+            const bool there = at < J.q.n;
+            const int64_t token = J.q.start + (there ? at : 0);
+            const uint16_t* src = (const uint16_t*)A.q.data + token * A.q.token_stride + J.head * A.q.head_stride;
+            const uint16_t* key = (const uint16_t*)A.q_rope.data + token * A.q_rope.token_stride + J.head * A.q_rope.head_stride;
+            for (int k = 0; k < k_chunks - 1; k++) lt_copy16(to + k * LT_P_CHUNK + lt_at(i, piece), src + 64 * k + 8 * piece, there);
+            if (8 * piece < S.rope) lt_copy16(to + (k_chunks - 1) * LT_P_CHUNK + lt_at(i, piece), key + 8 * piece, there);
+        }
+        lt_copies_done();
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        kv_warp_arrive(bars + 8 * LT_P_Q_IN);
+    }
+    const int first_place = J.q.len - J.q.n + J.row + LT_P_ROWS * m_tile + 32 * (warp & 3);  // of this warp's rows
+    const float scale = S.scale_log2;
+    float m = KV_M_NONE, l = 0.f;
+    bool fine = true;
+    for (int s = 0; s < steps && fine; s++) {
+        const int t0 = LT_P_TOKENS * s;
+        fine = kv_warp_wait(bars + 8 * (LT_P_S_IN + m_tile), s & 1, stop);
+        if (!fine) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t present = ((volatile uint32_t*)M.present)[s & 7];
+        const bool ragged = t0 < J.lo || t0 + LT_P_TOKENS > min(first_place + 1, J.hi) || present != 0xffu;
+        uint32_t x[64], z[64];
+        kv_tmem_load64(x, s_at);
+        kv_tmem_load64(z, s_at + 64);
+        if (ragged) {
+#pragma unroll
+            for (int b = 0; b < 4; b++) {
+                const uint32_t sees = lt_prompt_there(J, t0, b, present) & lt_bits(0, place + 1 - t0 - 32 * b);
+#pragma unroll
+                for (int i = 0; i < 32; i++) {
+                    uint32_t& y = b < 2 ? x[32 * (b & 1) + i] : z[32 * (b & 1) + i];
+                    y = sees >> i & 1 ? y : 0xff800000u;
+                }
+            }
+        }
+        float top = -KV_INF;
+#pragma unroll
+        for (int i = 0; i < 64; i += 2) {
+            top = fmaxf(fmaxf(top, __uint_as_float(x[i])), __uint_as_float(x[i + 1]));
+            top = fmaxf(fmaxf(top, __uint_as_float(z[i])), __uint_as_float(z[i + 1]));
+        }
+        top *= scale;
+        const bool higher = top > m + 8.f;               // weights stay below 2^8, and O seldom has to be multiplied
+        const float fall = higher ? kv_exp2(m - top) : 1.f;
+        m = higher ? top : m;
+        l *= fall;
+        uint32_t p[32];
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; i++) {
+            const float a = kv_exp2(fmaf(__uint_as_float(x[2 * i]), scale, -m)), b = kv_exp2(fmaf(__uint_as_float(x[2 * i + 1]), scale, -m));
+            sum += a + b;
+            p[i] = kv_pack<BF>(a, b);
+        }
+        kv_tmem_store32(p, s_at);
+#pragma unroll
+        for (int i = 0; i < 32; i++) {
+            const float a = kv_exp2(fmaf(__uint_as_float(z[2 * i]), scale, -m)), b = kv_exp2(fmaf(__uint_as_float(z[2 * i + 1]), scale, -m));
+            sum += a + b;
+            p[i] = kv_pack<BF>(a, b);
+        }
+        kv_tmem_store32(p, s_at + 32);
+        l += sum;
+        // The row tile's last product was issued before these scores were: it is done, and O rests.
+        if (s > 0 && __any_sync(0xffffffffu, higher)) {
+#pragma unroll 1
+            for (int b = 0; b < S.value; b += 32) {
+                uint32_t y[32];
+                kv_tmem_load32(y, o_at + b);
+#pragma unroll
+                for (int i = 0; i < 32; i++) y[i] = __float_as_uint(__uint_as_float(y[i]) * fall);
+                kv_tmem_store32(y, o_at + b);
+            }
+        }
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        kv_warp_arrive(bars + 8 * (LT_P_P_IN + m_tile));
+    }
+    fine = kv_warp_wait(bars + 8 * LT_P_END, 0, stop) && fine && !*stop;
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const float by = !fine ? __int_as_float(0x7fffffff) : l == 0.f ? 0.f : 1.f / l;
+    const int64_t token = J.q.start + (int64_t)row;
+    if (valid && A.lse) A.lse[token * S.heads + J.head] = !fine ? by : l == 0.f ? -KV_INF : (m + log2f(l)) * 0.6931471805599453f;
+    const int apart_tile = min(J.see_all, J.hi) / LT_P_TOKENS;
+#pragma unroll 1
+    for (int b = 0; b < S.value; b += 32) {
+        uint32_t x[32];
+        __syncwarp();
+        if (steps > 0) {
+            kv_tmem_load32(x, o_at + b);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; i++) x[i] = 0u;
+        }
+        if (!valid) continue;
+        float y[32];
+#pragma unroll
+        for (int i = 0; i < 32; i++) y[i] = l == 0.f && fine ? 0.f : __uint_as_float(x[i]) * by;
+        // what the guard took out of V, for rows that see the token
+#pragma unroll 1
+        for (int w = 0; w < 4 * LT_P_APART; w++)
+            for (uint32_t bits = ((volatile uint32_t*)M.apart)[w]; bits; bits &= bits - 1) {
+                const int t = apart_tile * LT_P_TOKENS + 32 * w + __ffs(bits) - 1;
+                if (t > place) continue;
+                const uint16_t* v = A.v + (J.key_start + t) * A.v_token_stride + J.head * A.v_head_stride + b;
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) {
+                    float e[8];
+                    kv_widen8<BF>(*(const uint4*)(v + i), e);
+#pragma unroll
+                    for (int k = 0; k < 8; k++)
+                        if (!(fabsf(e[k]) < KV_INF)) y[i + k] += e[k];
+                }
+            }
+        uint16_t* dst = (uint16_t*)A.out.data + token * A.out.token_stride + J.head * A.out.head_stride + b;
+#pragma unroll
+        for (int i = 0; i < 4; i++) *(uint4*)(dst + 8 * i) = kv_narrow8<BF>(y + 8 * i);
+    }
+}
+
+// Warp 8
+__device__ __forceinline__ void lt_prompt_bring(const LtShape& S, const LtBatch& B, const LtPrompt& A, const LtPromptJob& J, int steps, const CUtensorMap* pool,
+                                                const CUtensorMap* k_map, const CUtensorMap* v_map, uint32_t sm_at, LtPromptMisc& M, uint32_t bars)
+{
+    const int lane = threadIdx.x & 31, k_chunks = lt_prompt_k_chunks(S), v_chunks = S.value / 64, box = min(S.block_tokens, 64), boxes = LT_P_TOKENS / box;
+    const uint32_t k_at = sm_at + 2 * k_chunks * LT_P_CHUNK, v_at = k_at + 2 * k_chunks * LT_P_CHUNK;
+    volatile int* const stop = &M.stop;
+    int s = 0;
+    bool k_out = false;
+    for (; s < steps; s++) {
+        // lane: a box of the tile's shared keys
+        const int t0 = LT_P_TOKENS * s, t = t0 + lane * box;
+        const int page = lane < boxes && t < J.hi ? lt_page(B, J.seq, t >> S.block_shift) : -1;
+        const uint32_t some = __ballot_sync(0xffffffffu, page >= 0);
+        uint32_t present = 0;
+        for (int b = 0; b < boxes; b++)
+            if (some >> b & 1) present |= ((1u << (box / 16)) - 1) << (b * (box / 16));
+        k_out = false;
+        if (!kv_warp_wait(bars + 8 * (LT_P_K_OUT + (s & 1)), (s >> 1 & 1) ^ 1, stop)) break;
+        const uint32_t bar = bars + 8 * (LT_P_K_IN + (s & 1)), to = k_at + (s & 1) * k_chunks * LT_P_CHUNK;
+        if (lane == 0) {
+            ((volatile uint32_t*)M.present)[s & 7] = present;
+            lt_expect(bar, (k_chunks - 1) * LT_P_CHUNK + __popc(some) * box * LT_CHUNK_ROW);
+            for (int k = 0; k < k_chunks - 1; k++) lt_tma(to + k * LT_P_CHUNK, k_map, 64 * k, (int)J.key_start + t0, A.k_heads ? J.head : 0, bar);
+        }
+        __syncwarp();
+        if (page >= 0) lt_tma(to + (k_chunks - 1) * LT_P_CHUNK + lane * box * LT_CHUNK_ROW, pool, S.latent, t & (S.block_tokens - 1), page, bar);
+        k_out = true;
+        __syncwarp();
+        if (!kv_warp_wait(bars + 8 * LT_P_V_OUT, (s & 1) ^ 1, stop)) break;
+        if (lane == 0) {
+            lt_expect(bars + 8 * LT_P_V_IN, v_chunks * LT_P_CHUNK);
+            for (int k = 0; k < v_chunks; k++) lt_tma(v_at + k * LT_P_CHUNK, v_map, 64 * k, (int)J.key_start + t0, A.v_heads ? J.head : 0, bars + 8 * LT_P_V_IN);
+        }
+        __syncwarp();
+    }
+    // what is on its way arrives before the CTA ends
+    const int brought = s + (s < steps && k_out);
+    for (int back = 1; back <= 2 && back <= brought; back++) (void)kv_wait(bars + 8 * (LT_P_K_IN + (brought - back & 1)), brought - back >> 1 & 1);
+    if (s > 0) (void)kv_wait(bars + 8 * LT_P_V_IN, s - 1 & 1);
+}
+
+// Warp 9
+template <bool BF>
+__device__ __forceinline__ void lt_prompt_products(const LtShape& S, const LtPromptJob& J, int steps, int parts, uint32_t sm_at, LtPromptMisc& M, uint32_t bars, uint32_t tmem)
+{
+    const int k_chunks = lt_prompt_k_chunks(S);
+    const uint32_t k_at = sm_at + 2 * k_chunks * LT_P_CHUNK, v_at = k_at + 2 * k_chunks * LT_P_CHUNK;
+    constexpr uint32_t kind = 1u << 4 | (BF ? 1u << 7 | 1u << 10 : 0u) | (LT_P_ROWS / 16) << 24;
+    constexpr uint32_t s_what = kind | (LT_P_TOKENS / 8) << 17;
+    const uint32_t o_what = kind | (uint32_t)S.value / 8 << 17 | 1u << 16;                   // V is the operand whose N runs along the row
+    volatile int* const stop = &M.stop;
+    auto scores = [&](int s, int m) {
+        for (int k = 0; k < k_chunks; k++) {
+            const uint64_t a = kv_desc(sm_at + (m * k_chunks + k) * LT_P_CHUNK, 16, 1024), b = kv_desc(k_at + ((s & 1) * k_chunks + k) * LT_P_CHUNK, 16, 1024);
+            const int n = k < k_chunks - 1 ? 4 : S.rope / 16;
+            for (int i = 0; i < n; i++) kv_mma_ss(tmem + 128 * m, a + 2 * i, b + 2 * i, s_what, k > 0 || i > 0);
+        }
+        kv_commit(bars + 8 * (LT_P_S_IN + m));
+    };
+    if (!kv_warp_wait(bars + 8 * LT_P_Q_IN, 0, stop)) return;
+    // step s of a row tile: its answers when its weights are made, and then the scores of step s + 1 in the weights' place
+    for (int s = -1; s < steps; s++) {
+        if (s + 1 < steps && !kv_warp_wait(bars + 8 * (LT_P_K_IN + (s + 1 & 1)), s + 1 >> 1 & 1, stop)) return;
+        if (s >= 0 && !kv_warp_wait(bars + 8 * LT_P_V_OK, s & 1, stop)) return;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        for (int m = 0; m < parts; m++) {
+            if (s >= 0 && s < J.steps[m]) {
+                if (!kv_warp_wait(bars + 8 * (LT_P_P_IN + m), s & 1, stop)) return;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint64_t b = kv_desc(v_at, LT_P_CHUNK, 1024);
+#pragma unroll
+                for (int k = 0; k < 8; k++) kv_mma_ts(tmem + 256 + 128 * m, tmem + 128 * m + 8 * k, b + (k * 2048 >> 4), o_what, s > 0 || k > 0);
+            }
+            if (s + 1 < J.steps[m]) scores(s + 1, m);
+        }
+        if (s >= 0) kv_commit(bars + 8 * LT_P_V_OUT);
+        if (s + 1 < steps) kv_commit(bars + 8 * (LT_P_K_OUT + (s + 1 & 1)));
+    }
+}
+
+// Warps 10 and 11: V of tokens that are not there becomes zeros.  Where some rows do not see a token, what is not finite in its V becomes 0
+// too (a weight of 0 times it would not be 0), and is noted down: rows that see it add it at the end.
+template <bool BF>
+__device__ __forceinline__ void lt_prompt_guard(const LtShape& S, const LtPromptJob& J, int steps, uint8_t* v_sm, LtPromptMisc& M, uint32_t bars)
+{
+    const int n = threadIdx.x - 320;
+    volatile int* const stop = &M.stop;
+    const int see_all = min(J.see_all, J.hi), apart_tile = see_all / LT_P_TOKENS;
+    for (int s = 0; s < steps; s++) {
+        if (!kv_warp_wait(bars + 8 * LT_P_V_IN, s & 1, stop)) return;
+        // the shared keys came in front of V; who waits here for both may read what was noted beside them
+        if (!kv_warp_wait(bars + 8 * (LT_P_K_IN + (s & 1)), s >> 1 & 1, stop)) return;
+        const int t0 = LT_P_TOKENS * s;
+        const uint32_t present = ((volatile uint32_t*)M.present)[s & 7];
+        if (lt_prompt_ragged(J, t0, present)) {
+            for (int i = n; i < LT_P_TOKENS * (S.value / 8); i += 64) {
+                const int t = i & 127, piece = i >> 7;
+                uint4* const at = (uint4*)(v_sm + (piece >> 3) * LT_P_CHUNK + lt_at(t, piece & 7));
+                const bool there = lt_prompt_there(J, t0, t >> 5, present) >> (t & 31) & 1;
+                if (there && t0 + t < see_all) continue;
+                const uint4 w = *at;
+                uint4 f = make_uint4(0, 0, 0, 0);
+                if (there) f = make_uint4(lt_finite2<BF>(w.x), lt_finite2<BF>(w.y), lt_finite2<BF>(w.z), lt_finite2<BF>(w.w));
+                if (f.x != w.x || f.y != w.y || f.z != w.z || f.w != w.w) {
+                    *at = f;
+                    if (there && s - apart_tile < LT_P_APART) atomicOr(&M.apart[s - apart_tile][t >> 5], 1u << (t & 31));
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+        kv_warp_arrive(bars + 8 * LT_P_V_OK);
+    }
+}
+
+template <bool BF>
+__global__ void __launch_bounds__(LT_P_THREADS, 1) lt_prompt_kernel(const LtShape S, const LtBatch B, const LtPrompt A, const __grid_constant__ CUtensorMap pool,
+                                                                    const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
+{
+    extern __shared__ uint8_t lt_raw[];
+    uint8_t* const sm = lt_raw + (-(uint32_t)__cvta_generic_to_shared(lt_raw) & 1023u);
+    const uint32_t sm_at = (uint32_t)__cvta_generic_to_shared(sm);
+    const int warp = threadIdx.x >> 5, k_chunks = lt_prompt_k_chunks(S);
+    LtPromptMisc& M = *(LtPromptMisc*)(sm + (4 * k_chunks + S.value / 64) * LT_P_CHUNK);
+    const uint32_t bars = (uint32_t)__cvta_generic_to_shared(M.bars);
+    LtPromptJob J;
+    J.seq = blockIdx.z;
+    J.head = blockIdx.x / A.tiles;
+    J.row = (A.tiles - 1 - (int)blockIdx.x % A.tiles) * 2 * LT_P_ROWS;       // those that see most first
+    J.q = lt_seq(B, J.seq);
+    if (J.row >= J.q.n) return;
+    J.rows = min(J.q.n - J.row, 2 * LT_P_ROWS);
+    const int parts = J.rows > LT_P_ROWS ? 2 : 1;
+    J.key_start = A.key_starts[J.seq];
+    J.lo = (int)min(max(-J.key_start, (int64_t)0), (int64_t)J.q.len);
+    J.hi = (int)min(max((int64_t)A.total_keys - J.key_start, (int64_t)0), (int64_t)J.q.len);
+    J.see_all = max(J.q.len - J.q.n + J.row + 1, 0);
+    for (int m = 0; m < 2; m++) {
+        const int end = min(J.q.len - J.q.n + J.row + min(J.rows, LT_P_ROWS * (m + 1)), J.hi);
+        J.steps[m] = m < parts && end > J.lo ? (end + LT_P_TOKENS - 1) / LT_P_TOKENS : 0;
+    }
+    const int steps = max(J.steps[0], J.steps[1]);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < LT_P_BARS; i++)
+            lt_init(bars + 8 * i, i == LT_P_V_OK ? 2 : i == LT_P_P_IN || i == LT_P_P_IN + 1 ? 4 : i == LT_P_Q_IN ? 4 * parts : 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        M.stop = 0;
+        for (int i = 0; i < 4 * LT_P_APART; i++) M.apart[0][i] = 0;
+    }
+    if (warp == 9) asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"((uint32_t)__cvta_generic_to_shared(&M.tmem)) : "memory");
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = *(volatile uint32_t*)&M.tmem;  // S_0, S_1, O_0, O_1: 128 columns each
+    if (warp < 8) {
+        if (warp < 4 * parts) lt_prompt_rows<BF>(S, A, J, warp >> 2, sm_at, M, bars, tmem);
+    } else if (warp == 8) {
+        lt_prompt_bring(S, B, A, J, steps, &pool, &k_map, &v_map, sm_at, M, bars);
+    } else if (warp == 9) {
+        lt_prompt_products<BF>(S, J, steps, parts, sm_at, M, bars, tmem);
+        __syncwarp();
+        kv_commit(bars + 8 * LT_P_END);                  // the answers are there, and nothing is on its way any more when the memory is given back
+        kv_wait(bars + 8 * LT_P_END, 0);
+        __syncwarp();
+    } else {
+        lt_prompt_guard<BF>(S, J, steps, sm + 4 * k_chunks * LT_P_CHUNK, M, bars);
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 9) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    }
+}

@@ -175,6 +175,15 @@ static bool lt_bad_rows(const fastrack_kv_rows* r) { return !r || lt_misaligned(
 static KvRows lt_rows(const fastrack_kv_rows* r) { return {r->data, r->token_stride, r->head_stride}; }
 static int lt_log2i(int x) { int s = 0; while ((1 << s) < x) s++; return s; }
 
+using LtAttendKernel = void (*)(LtShape, LtBatch, LtAttend, CUtensorMap, CUtensorMap);
+struct LtAttendKind { LtAttendKernel kernel; int smem; };
+static const LtAttendKind lt_attend_kinds[8] = {          // [latent / 128 - 1][bf16]
+    {(LtAttendKernel)lt_attend_kernel<1, false>, LtTile<1>::SMEM}, {(LtAttendKernel)lt_attend_kernel<1, true>, LtTile<1>::SMEM},
+    {(LtAttendKernel)lt_attend_kernel<2, false>, LtTile<2>::SMEM}, {(LtAttendKernel)lt_attend_kernel<2, true>, LtTile<2>::SMEM},
+    {(LtAttendKernel)lt_attend_kernel<3, false>, LtTile<3>::SMEM}, {(LtAttendKernel)lt_attend_kernel<3, true>, LtTile<3>::SMEM},
+    {(LtAttendKernel)lt_attend_kernel<4, false>, LtTile<4>::SMEM}, {(LtAttendKernel)lt_attend_kernel<4, true>, LtTile<4>::SMEM}};
+static_assert(LtTile<4>::SMEM <= 232448 && LtTile<2>::SMEM <= 232448, "");
+
 // news: whether the call is about new tokens
 static bool lt_bad_batch(const fastrack_latent* lt, const fastrack_latent_batch* b, bool news = true)
 {
@@ -191,8 +200,6 @@ static LtBatch lt_batch(const fastrack_latent_batch* b)
             b->d_positions};
 }
 
-// Shared memory of the attention kernel: Q, the stages, P, the rest and room to round the base up
-static int lt_attend_smem(const LtShape& S, int stages) { return (1 + stages) * (S.latent / 64 + 1) * LT_ROWS * LT_CHUNK_ROW + LT_ROWS * LT_CHUNK_ROW + LT_MISC + 1024; }
 #define LT_SMEM_MOST 232448
 
 extern "C" int fastrack_latent_create(const fastrack_latent_config* c, fastrack_latent** out)
@@ -244,8 +251,7 @@ extern "C" int fastrack_latent_create(const fastrack_latent_config* c, fastrack_
     if (e == cudaSuccess) e = cudaMalloc(&lt->d_turns, sizeof turns);
     if (e == cudaSuccess) e = cudaMemcpy(lt->d_turns, turns, sizeof turns, cudaMemcpyHostToDevice);
     auto ask = [&](const void* kernel, int bytes) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); };
-    ask((const void*)lt_attend_kernel<true>, LT_SMEM_MOST);
-    ask((const void*)lt_attend_kernel<false>, LT_SMEM_MOST);
+    for (const LtAttendKind& kind : lt_attend_kinds) ask((const void*)kind.kernel, kind.smem);
     ask((const void*)lt_expand_kernel<true>, LT_SMEM_MOST);
     ask((const void*)lt_expand_kernel<false>, LT_SMEM_MOST);
     ask((const void*)lt_prompt_kernel<true>, LT_SMEM_MOST);
@@ -318,7 +324,7 @@ extern "C" int fastrack_latent_accept(fastrack_latent* lt, const fastrack_latent
 
 // ------------------------------------------------------------------------------------------------ attention ----
 
-struct LtPlan { int groups, group_tiles, seq_groups, stages; size_t ml, cuts, total; };      // byte offsets in the workspace, part_o at 0
+struct LtPlan { int groups, group_tiles, seq_groups; size_t ml, cuts, total; };      // byte offsets in the workspace, part_o at 0
 
 // CTAs that read the same tokens side by side, one per row tile: all row tiles of a sequence up to 8 (an SM in 148 / 8 may be left over),
 // and beyond that the number between 5 and 8 that wastes the fewest CTAs on row tiles that are not there or SMs that are left.
@@ -327,7 +333,7 @@ static LtPlan lt_plan(const fastrack_latent* lt, const fastrack_latent_batch* b)
     const LtShape& S = lt->shape;
     LtPlan p;
     const int64_t rows = (int64_t)b->max_new * S.heads, row_tiles = rows > LT_ROWS ? (rows + LT_ROWS - 1) / LT_ROWS : 1;
-    const int sms = lt->num_sms < LT_JOIN_THREADS ? lt->num_sms : LT_JOIN_THREADS;
+    const int sms = lt->num_sms < LT_JOIN_CUTS ? lt->num_sms : LT_JOIN_CUTS;
     p.group_tiles = (int)(row_tiles < 8 ? row_tiles : 8);
     if (row_tiles > 8) {
         double best = 0;
@@ -342,7 +348,6 @@ static LtPlan lt_plan(const fastrack_latent* lt, const fastrack_latent_batch* b)
     if (p.group_tiles > sms) p.group_tiles = sms;
     p.groups = sms / p.group_tiles;
     p.seq_groups = (int)((row_tiles + p.group_tiles - 1) / p.group_tiles);
-    for (p.stages = LT_A_STAGES; lt_attend_smem(S, p.stages) > LT_SMEM_MOST;) p.stages--;
     const size_t slots = (size_t)p.groups * 2 * p.group_tiles * LT_ROWS;
     p.ml = slots * S.latent * 4;
     p.cuts = p.ml + slots * 8;
@@ -356,13 +361,14 @@ extern "C" size_t fastrack_latent_attention_workspace(const fastrack_latent* lt,
     return lt_plan(lt, batch).total;
 }
 
-// A tensor map of 16-bit values (x: row's values, y: rows, z), whose boxes are 64 values wide
-static int lt_map(fastrack_latent* lt, CUtensorMap* map, void* data, int64_t width, int64_t y, int64_t z, int64_t y_bytes, int64_t z_bytes, int box_y)
+// A tensor map of 16-bit values (x: row's values, y: rows, z, and w if there is one), whose boxes are 64 values wide
+static int lt_map(fastrack_latent* lt, CUtensorMap* map, void* data, int64_t width, int64_t y, int64_t z, int64_t y_bytes, int64_t z_bytes, int box_y, int64_t w = 0,
+                  int64_t w_bytes = 0, int box_z = 1)
 {
-    const cuuint64_t dims[3] = {(cuuint64_t)width, (cuuint64_t)y, (cuuint64_t)z}, strides[2] = {(cuuint64_t)y_bytes, (cuuint64_t)z_bytes};
-    const cuuint32_t box[3] = {64, (cuuint32_t)box_y, 1}, steps[3] = {1, 1, 1};
+    const cuuint64_t dims[4] = {(cuuint64_t)width, (cuuint64_t)y, (cuuint64_t)z, (cuuint64_t)w}, strides[3] = {(cuuint64_t)y_bytes, (cuuint64_t)z_bytes, (cuuint64_t)w_bytes};
+    const cuuint32_t box[4] = {64, (cuuint32_t)box_y, (cuuint32_t)box_z, 1}, steps[4] = {1, 1, 1, 1};
     auto encode = [&] {
-        return lt->encode(map, lt->config.dtype == FASTRACK_KV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, data, dims, strides, box, steps,
+        return lt->encode(map, lt->config.dtype == FASTRACK_KV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, w ? 4 : 3, data, dims, strides, box, steps,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     };
     CUresult r = encode();
@@ -380,6 +386,15 @@ static int lt_pool_map(fastrack_latent* lt, const LtBatch& B, CUtensorMap* map)
     memset(map, 0, sizeof *map);
     if (B.pool_pages == 0) return FASTRACK_OK;           // every page is absent
     return lt_map(lt, map, B.pool, S.row, S.block_tokens, B.pool_pages, 2 * S.row, (int64_t)2 * S.row * S.block_tokens, S.block_tokens < LT_TOKENS ? S.block_tokens : LT_TOKENS);
+}
+
+// The pool's latents by 64 channels: channels, rows of a page, which 64, pages; boxes of 64 tokens and all channels (blocks of 64 tokens or more)
+static int lt_pairs_map(fastrack_latent* lt, const LtBatch& B, CUtensorMap* map)
+{
+    const LtShape& S = lt->shape;
+    memset(map, 0, sizeof *map);
+    if (B.pool_pages == 0 || S.block_tokens < LT_TOKENS) return FASTRACK_OK;
+    return lt_map(lt, map, B.pool, 64, S.block_tokens, S.latent / 64, 2 * S.row, 128, LT_TOKENS, B.pool_pages, (int64_t)2 * S.row * S.block_tokens, S.latent / 64);
 }
 
 extern "C" int fastrack_latent_attention(fastrack_latent* lt, const fastrack_latent_batch* batch, const fastrack_kv_rows* q, const fastrack_kv_rows* q_rope,
@@ -404,22 +419,23 @@ extern "C" int fastrack_latent_attention(fastrack_latent* lt, const fastrack_lat
     A.groups = p.groups;
     A.group_tiles = p.group_tiles;
     A.seq_groups = p.seq_groups;
-    A.stages = p.stages;
     A.least = 2;
     A.part_o = (float*)ws;
     A.part_ml = (float*)(ws + p.ml);
     A.cuts = (int*)(ws + p.cuts);
-    CUtensorMap pool;
+    CUtensorMap pool, pairs;
     if (int rc = lt_pool_map(lt, B, &pool)) return rc;
+    if (int rc = lt_pairs_map(lt, B, &pairs)) return rc;
     const bool bf = lt->config.dtype == FASTRACK_KV_BF16;
     const cudaStream_t st = (cudaStream_t)stream;
-    (bf ? lt_attend_kernel<true> : lt_attend_kernel<false>)<<<p.groups * p.group_tiles, LT_A_THREADS, lt_attend_smem(S, p.stages), st>>>(S, B, A, pool);
+    const LtAttendKind& kind = lt_attend_kinds[2 * (S.latent / 128 - 1) + bf];
+    kind.kernel<<<p.groups * p.group_tiles, LT_A_THREADS, kind.smem, st>>>(S, B, A, pool, pairs);
     // its start may overlap the end of the kernel before it; it waits (griddepcontrol.wait) before it reads anything
     cudaLaunchConfig_t c = {};
     cudaLaunchAttribute overlap;
     overlap.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     overlap.val.programmaticStreamSerializationAllowed = 1;
-    c.gridDim = dim3(2 * lt->num_sms);
+    c.gridDim = dim3(8 * lt->num_sms);
     c.blockDim = dim3(LT_JOIN_THREADS);
     c.stream = st;
     c.attrs = &overlap;

@@ -17,11 +17,17 @@
 #define LT_TOKENS 64
 #define LT_A_THREADS 192
 #define LT_A_STAGES 4                   // at most
-#define LT_PART 16384                   // bytes of 128 channels of a tile; the shared key's are a part of half that
+// PAIRS: of 64 channels of the latent
+template <int PAIRS> struct LtTile {
+    static constexpr int CHUNKS = 2 * PAIRS + 1, BYTES = CHUNKS * 64 * LT_CHUNK_ROW, STAGES = PAIRS > 2 ? 2 : 4;
+    static constexpr int P = (1 + STAGES) * BYTES, MISC = P + 64 * LT_CHUNK_ROW, SMEM = MISC + 2048 + 1024;    // after Q and the stages; room to round the base up
+};
+#define LT_PART 16384                   // bytes of 128 channels of a tile
 #define LT_RAISE 8.f                    // a row's reference is raised when a score is 2^8 above it: weights stay below 2^8, and O seldom has to be multiplied
 
-// Barriers, 8 bytes each.  IN and OUT: [stage][part], part 0 .. latent / 128 - 1 and then the shared key's (part LT_A_KEY).
-enum { LT_A_KEY = 4, LT_A_PARTS = 5, LT_A_IN = 0, LT_A_OUT = LT_A_STAGES * LT_A_PARTS, LT_A_S = 2 * LT_A_OUT, LT_A_P = LT_A_S + 2, LT_A_O, LT_A_Q, LT_A_END, LT_A_BARS };
+// Barriers, 8 bytes each.  IN and OUT: of a stage.  (While the tensor cores read their operands, an access to shared memory takes some 240
+// cycles, a barrier's that has long been there too: one for each 128 channels cost a tile's scores 1000 cycles.)
+enum { LT_A_IN = 0, LT_A_OUT = LT_A_STAGES, LT_A_S = 2 * LT_A_OUT, LT_A_P = LT_A_S + 2, LT_A_O, LT_A_Q, LT_A_END, LT_A_BARS };
 struct LtMisc {
     uint64_t bars[LT_A_BARS];
     float factor[LT_ROWS];              // of rows: O's when the reference is raised, and 1 / l at the end
@@ -33,8 +39,7 @@ struct LtMisc {
     int64_t item, item_at;
     int64_t warp_sum[LT_A_THREADS / 32];
 };
-#define LT_MISC 2048
-static_assert(sizeof(LtMisc) <= LT_MISC, "");
+static_assert(sizeof(LtMisc) <= 2048, "");
 
 struct LtAttend {
     KvRows q, q_rope, out;
@@ -43,7 +48,7 @@ struct LtAttend {
     int groups;                         // of CTAs: runs that the line is cut into
     int group_tiles;                    // row tiles, CTAs, of a group
     int seq_groups;                     // groups of row tiles of a sequence, at most
-    int stages, least;                  // least: tiles of a run
+    int least;                          // tiles of a run
     float* part_o;                      // [groups][2][group_tiles][64][latent]: the first piece of a run (begun before it), the last
     float* part_ml;                     // [groups][2][group_tiles][64][2]
     int* cuts;                          // [groups][4]: of a run whose last item goes on: sequence, group of row tiles, pieces
@@ -114,14 +119,15 @@ __device__ __forceinline__ uint64_t lt_sees(const LtAttend& A, const LtSeq& q, i
 }
 
 // Warps 0-3: the weights of the rows, and their answers
-template <bool BF>
+template <int PAIRS, bool BF>
 __device__ __forceinline__ void lt_attend_rows(const LtShape& S, const LtBatch& B, const LtAttend& A, LtWalk walk, int64_t share, uint8_t* sm, uint32_t sm_at, LtMisc& M,
                                                uint32_t bars, uint32_t tmem)
 {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane & 3;
     const int g = blockIdx.x / A.group_tiles, r = blockIdx.x % A.group_tiles;
-    const int chunks = S.latent / 64, tile_bytes = (chunks + 1) * LT_ROWS * LT_CHUNK_ROW;
-    uint8_t* const p_sm = sm + (1 + A.stages) * tile_bytes;
+    using T = LtTile<PAIRS>;
+    constexpr int chunks = 2 * PAIRS, latent = 128 * PAIRS;
+    uint8_t* const p_sm = sm + T::P;
     volatile int* const stop = &M.stop;
     const uint32_t lanes = (uint32_t)warp << 21, s_at = tmem + lanes + 256, o_at = tmem + lanes;
     const float scale = S.scale_log2;
@@ -148,6 +154,7 @@ __device__ __forceinline__ void lt_attend_rows(const LtShape& S, const LtBatch& 
                 const int head = there ? (int)((first + row) % S.heads) : 0;
                 const uint16_t* src = (const uint16_t*)A.q.data + token * A.q.token_stride + head * A.q.head_stride;
                 const uint16_t* key = (const uint16_t*)A.q_rope.data + token * A.q_rope.token_stride + head * A.q_rope.head_stride;
+#pragma unroll
                 for (int k = 0; k < chunks; k++) lt_copy16(sm_at + k * LT_ROWS * LT_CHUNK_ROW + lt_at(row, piece), src + 64 * k + 8 * piece, there);
                 if (8 * piece < S.rope) lt_copy16(sm_at + chunks * LT_ROWS * LT_CHUNK_ROW + lt_at(row, piece), key + 8 * piece, there);
                 if (piece == 0) M.out_at[row] = token * A.out.token_stride + head * A.out.head_stride;
@@ -168,11 +175,12 @@ __device__ __forceinline__ void lt_attend_rows(const LtShape& S, const LtBatch& 
         float m[2] = {KV_M_NONE, KV_M_NONE}, l[2] = {0.f, 0.f};
         for (int i = walk.from; i < walk.to && !halted; i++, c++) {
             const int t0 = i * LT_TOKENS, set = c % 3;
-            fine = kv_warp_wait(bars + 8 * (LT_A_S + (c & 1)), c >> 1 & 1, stop) &&
-                   kv_warp_wait(bars + 8 * (LT_A_IN + c % A.stages * LT_A_PARTS), c / A.stages & 1, stop) && fine;
+            // what is known of the tile first, while its scores are made
+            fine = kv_warp_wait(bars + 8 * (LT_A_IN + c % T::STAGES), c / T::STAGES & 1, stop) && fine;
+            const uint32_t present = ((volatile uint32_t*)M.present)[c & 7];
+            fine = kv_warp_wait(bars + 8 * (LT_A_S + (c & 1)), c >> 1 & 1, stop) && fine;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             uint32_t x[32];
-            const uint32_t present = ((volatile uint32_t*)M.present)[c & 7];
             const bool ragged = t0 + LT_TOKENS > see_all || present != 15u;
             float top[2] = {-KV_INF, -KV_INF};
             if (active) {
@@ -208,6 +216,7 @@ __device__ __forceinline__ void lt_attend_rows(const LtShape& S, const LtBatch& 
             }
             const bool raise = lt_any(1, 128, top[0] * scale > m[0] + LT_RAISE || top[1] * scale > m[1] + LT_RAISE);
             halted = ((volatile int*)M.halt)[c & 1];
+            const uint32_t p_free = kv_ended(bars + 8 * LT_A_O, c + 1 & 1);  // asked early, needed late
             if (raise) {
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
@@ -229,11 +238,12 @@ __device__ __forceinline__ void lt_attend_rows(const LtShape& S, const LtBatch& 
                         x[2 * k + h] = kv_pack<BF>(a, b);
                     }
             }
-            if (c > 0) fine = kv_warp_wait(bars + 8 * LT_A_O, c - 1 & 1, stop) && fine;      // the product before is done: P is free, and O rests
+            // the product before is done: P is free, and O rests
+            if (!__all_sync(0xffffffffu, p_free)) fine = kv_warp_wait(bars + 8 * LT_A_O, c + 1 & 1, stop) && fine;
             if (raise && i > walk.from) {
                 lt_sync(2, 128);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                for (int b = 0; b < S.latent / 128; b++)
+                for (int b = 0; b < PAIRS; b++)
 #pragma unroll 1
                     for (int n = 0; n < rows; n += 32) {
                         uint32_t y[32];
@@ -254,7 +264,7 @@ __device__ __forceinline__ void lt_attend_rows(const LtShape& S, const LtBatch& 
             if (ragged) {
                 // Tokens that are not there become zeros, and so does what is not finite in tokens that some rows do not see: a weight of 0
                 // times it would not be 0.  Such a token shows by its scores, of which every one is not finite: its values all enter them.
-                uint8_t* const tile = sm + (1 + c % A.stages) * tile_bytes;
+                uint8_t* const tile = sm + (1 + c % T::STAGES) * T::BYTES;
                 const uint64_t there = lt_there(present, t0, q.len);
                 const uint64_t some = see_all - t0 >= 64 ? 0ull : see_all <= t0 ? ~0ull : ~((1ull << (see_all - t0)) - 1);
                 uint64_t todo = ~there | (some & ((uint64_t)((volatile uint32_t*)M.bad[set])[1] << 32 | ((volatile uint32_t*)M.bad[set])[0]));
@@ -294,7 +304,7 @@ __device__ __forceinline__ void lt_attend_rows(const LtShape& S, const LtBatch& 
             }
         }
         lt_sync(2, 128);
-        for (int b = 0; b < S.latent / 128; b++) {
+        for (int b = 0; b < PAIRS; b++) {
             const int ch = 128 * b + 32 * warp + lane;
 #pragma unroll 1
             for (int n = 0; n < rows; n += 32) {
@@ -313,7 +323,7 @@ __device__ __forceinline__ void lt_attend_rows(const LtShape& S, const LtBatch& 
                 } else {
 #pragma unroll
                     for (int k = 0; k < 32; k++)
-                        if (n + k < rows) A.part_o[(slot * LT_ROWS + n + k) * S.latent + ch] = __uint_as_float(y[k]);
+                        if (n + k < rows) A.part_o[(slot * LT_ROWS + n + k) * latent + ch] = __uint_as_float(y[k]);
                 }
             }
         }
@@ -321,86 +331,87 @@ __device__ __forceinline__ void lt_attend_rows(const LtShape& S, const LtBatch& 
     }
 }
 
-// Warp 4: the tiles
-__device__ __forceinline__ void lt_attend_bring(const LtShape& S, const LtBatch& B, const LtAttend& A, const CUtensorMap* map, LtWalk walk, uint32_t sm_at, LtMisc& M,
-                                                uint32_t bars)
+// Warp 4: the tiles.  It and warp 5 are one chain of instructions each, of which every one counts: no divisions, addresses known early.
+template <int PAIRS>
+__device__ __forceinline__ void lt_attend_bring(const LtShape& S, const LtBatch& B, const LtAttend& A, const CUtensorMap* map, const CUtensorMap* pairs_map, LtWalk walk,
+                                                uint32_t sm_at, LtMisc& M, uint32_t bars)
 {
+    using T = LtTile<PAIRS>;
     const int lane = threadIdx.x & 31, r = blockIdx.x % A.group_tiles;
-    const int pairs = S.latent / 128, chunks = S.latent / 64, tile_bytes = (chunks + 1) * LT_ROWS * LT_CHUNK_ROW;
-    const int box = min(S.block_tokens, LT_TOKENS), boxes = LT_TOKENS / box;
+    const int box_shift = min(S.block_shift, 6), box = 1 << box_shift;
+    const uint32_t box_bits = (1u << (box / 16)) - 1;
     volatile int* const stop = &M.stop;
     bool fine = true;
-    int c = 0, part = 0;                                 // tiles brought so far, and of the next one the part
+    int c = 0;                                           // tiles so far
     while (fine && walk.next(S, B, A)) {
         if (((int64_t)walk.group * A.group_tiles + r) * LT_ROWS >= (int64_t)walk.q.n * S.heads) continue;
         int known = -1, pages = -1;                      // lane: page of the block known + lane
         for (int i = walk.from; i < walk.to && fine; i++) {
-            const int stage = c % A.stages, phase = c / A.stages & 1;
-            const int block = i * LT_TOKENS >> S.block_shift;
+            const uint32_t stage = c % T::STAGES, in = bars + 8 * (LT_A_IN + stage), to = sm_at + (1 + stage) * T::BYTES;
+            const int block = i * LT_TOKENS >> S.block_shift, y = i * LT_TOKENS & (S.block_tokens - 1);
             if (known < 0 || block + 4 > known + 32) {
                 known = block;
                 pages = (int64_t)(block + lane) << S.block_shift < walk.q.len ? lt_page(B, walk.seq, block + lane) : -1;
             }
-            int page[4];
             uint32_t present = 0;
+            int page[4];
+            if (box_shift == 6) {
+                page[0] = lt_uniform(pages, block - known);
+                present = page[0] >= 0 ? 15u : 0u;
+            } else {
 #pragma unroll
-            for (int b = 0; b < 4; b++) {
-                page[b] = b < boxes ? __shfl_sync(0xffffffffu, pages, ((i * LT_TOKENS + b * box) >> S.block_shift) - known) : -1;
-                if (page[b] >= 0) present |= ((1u << (box / 16)) - 1) << (b * (box / 16));
-            }
-            const uint32_t to = sm_at + (1 + stage) * tile_bytes;
-            for (part = -1; part < pairs; part++) {
-                const int bar = stage * LT_A_PARTS + (part < 0 ? LT_A_KEY : part);
-                fine = kv_warp_wait(bars + 8 * (LT_A_OUT + bar), phase ^ 1, stop);
-                if (!fine) break;
-                if (lane == 0) {
-                    if (part < 0) ((volatile uint32_t*)M.present)[c & 7] = present;
-                    lt_expect(bars + 8 * (LT_A_IN + bar), __popc(present) * 16 * LT_CHUNK_ROW * (part < 0 ? 1 : 2));
-                    for (int k = part < 0 ? chunks : 2 * part; k < (part < 0 ? chunks + 1 : 2 * part + 2); k++)
-#pragma unroll
-                        for (int b = 0; b < 4; b++)
-                            if (page[b] >= 0)
-                                lt_tma(to + (k * LT_TOKENS + b * box) * LT_CHUNK_ROW, map, 64 * k, (i * LT_TOKENS + b * box) & (S.block_tokens - 1), page[b], bars + 8 * (LT_A_IN + bar));
+                for (int b = 0; b < 4; b++) {
+                    page[b] = b << box_shift < LT_TOKENS ? lt_uniform(pages, block + b - known) : -1;
+                    if (page[b] >= 0) present |= box_bits << (b << box_shift >> 4);
                 }
-                __syncwarp();
             }
-            if (fine) c++;
+            fine = kv_warp_wait(bars + 8 * (LT_A_OUT + stage), (c / T::STAGES & 1) ^ 1, stop);
+            if (!fine) break;
+            if (lane == 0) ((volatile uint32_t*)M.present)[c & 7] = present;
+            __syncwarp();
+            lt_expect(in, __popc(present) * 16 * LT_CHUNK_ROW * T::CHUNKS);
+            if (box_shift == 6) {
+                if (present) {
+                    lt_tma(to + 2 * PAIRS * LT_TOKENS * LT_CHUNK_ROW, map, 128 * PAIRS, y, page[0], in);
+                    lt_tma(to, pairs_map, 0, y, 0, page[0], in);
+                }
+            } else {
+#pragma unroll 1
+                for (int k = 0; k < T::CHUNKS; k++)
+#pragma unroll
+                    for (int b = 0; b < 4; b++)
+                        if (page[b] >= 0) lt_tma(to + (k * LT_TOKENS + (b << box_shift)) * LT_CHUNK_ROW, map, 64 * k, 0, page[b], in);
+            }
+            c++;
         }
     }
-    // what is on its way arrives before the CTA ends: the last tile of every stage, and of an unfinished one the parts before `part`
-    for (int back = fine ? 1 : 0; back <= A.stages; back++) {
-        const int tile = c - back, stage = tile % A.stages;
-        for (int p = -1; tile >= 0 && p < (back ? pairs : part); p++)
-            (void)kv_wait(bars + 8 * (LT_A_IN + stage * LT_A_PARTS + (p < 0 ? LT_A_KEY : p)), tile / A.stages & 1);
-    }
+    // what is on its way arrives before the CTA ends
+    for (int back = 1; back <= T::STAGES && back <= c; back++) (void)kv_wait(bars + 8 * (LT_A_IN + (c - back) % T::STAGES), (c - back) / T::STAGES & 1);
 }
 
 // Warp 5: the products
-template <bool BF>
+template <int PAIRS, bool BF>
 __device__ __forceinline__ void lt_attend_products(const LtShape& S, const LtBatch& B, const LtAttend& A, LtWalk walk, uint32_t sm_at, LtMisc& M, uint32_t bars, uint32_t tmem)
 {
+    using T = LtTile<PAIRS>;
     const int r = blockIdx.x % A.group_tiles;
-    const int pairs = S.latent / 128, chunks = S.latent / 64, tile_bytes = (chunks + 1) * LT_ROWS * LT_CHUNK_ROW;
     constexpr uint32_t kind = 1u << 4 | (BF ? 1u << 7 | 1u << 10 : 0u);                      // f32 += bf16 * bf16 or f16 * f16
     constexpr uint32_t s_what = kind | (LT_ROWS / 16) << 24 | (LT_TOKENS / 8) << 17;
+    constexpr uint32_t CHUNK = 64 * LT_CHUNK_ROW >> 4;   // in descriptors
     volatile int* const stop = &M.stop;
+    const uint64_t q_desc = kv_desc(sm_at, 16, 1024), k_desc = kv_desc(sm_at + T::BYTES, 16, 1024), v_desc = kv_desc(sm_at + T::BYTES, LT_TOKENS * LT_CHUNK_ROW, 1024),
+                   p_desc = kv_desc(sm_at + T::P, 16, 1024);
     bool fine = true;
     auto scores = [&](int c) {
-        const int stage = c % A.stages, phase = c / A.stages & 1;
-        const uint32_t tile = sm_at + (1 + stage) * tile_bytes;
-        for (int part = -1; part < pairs; part++) {
-            const int bar = stage * LT_A_PARTS + (part < 0 ? LT_A_KEY : part);
-            fine = kv_warp_wait(bars + 8 * (LT_A_IN + bar), phase, stop);
-            if (!fine) return;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            for (int k = part < 0 ? chunks : 2 * part; k < (part < 0 ? chunks + 1 : 2 * part + 2); k++) {
-                const uint32_t off = k * LT_ROWS * LT_CHUNK_ROW;
-                const uint64_t a = kv_desc(sm_at + off, 16, 1024), b = kv_desc(tile + off, 16, 1024);
-                const int steps = part < 0 ? S.rope / 16 : 4;
-                for (int s = 0; s < steps; s++) kv_mma_ss(tmem + 256 + 64 * (c & 1), a + 2 * s, b + 2 * s, s_what, part >= 0 || s > 0);
-            }
-            if (part < 0) kv_commit(bars + 8 * (LT_A_OUT + bar));
-        }
+        const uint32_t stage = c % T::STAGES, s_at = tmem + 256 + 64 * (c & 1);
+        const uint64_t k = k_desc + stage * (T::BYTES >> 4);
+        fine = kv_warp_wait(bars + 8 * (LT_A_IN + stage), c / T::STAGES & 1, stop);
+        if (!fine) return;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+        for (int n = 0; n < 2 * PAIRS; n++) lt_mma_ss<4, 2, 2>(s_at, q_desc + n * CHUNK, k + n * CHUNK, s_what, n > 0);
+        lt_mma_ss<2, 2, 2>(s_at, q_desc + 2 * PAIRS * CHUNK, k + 2 * PAIRS * CHUNK, s_what, true);
+        if (S.rope == 64) lt_mma_ss<2, 2, 2>(s_at, q_desc + 2 * PAIRS * CHUNK + 4, k + 2 * PAIRS * CHUNK + 4, s_what, true);
         kv_commit(bars + 8 * (LT_A_S + (c & 1)));
     };
     int c = 0, piece = 0;
@@ -412,32 +423,43 @@ __device__ __forceinline__ void lt_attend_products(const LtShape& S, const LtBat
         fine = kv_warp_wait(bars + 8 * LT_A_Q, piece & 1, stop);
         if (fine) scores(c);
         for (int i = walk.from; i < walk.to && fine; i++, c++) {
-            if (i + 1 < walk.to) scores(c + 1);
+            // The next tile's scores first, if it is there before this one's weights are: where memory is the bound it is not, and this one's
+            // answers must not wait for it (they free the place that the tile after it comes to).
+            bool next = i + 1 < walk.to;
+            const uint32_t next_in = bars + 8 * (LT_A_IN + (c + 1) % T::STAGES);
+            for (int turn = 0; next && fine && turn < 1 << 18; turn++) {
+                if (__all_sync(0xffffffffu, kv_ended(next_in, (c + 1) / T::STAGES & 1))) {
+                    scores(c + 1);
+                    next = false;
+                } else if (__all_sync(0xffffffffu, kv_ended(bars + 8 * LT_A_P, c & 1)) || *stop) {
+                    break;
+                }
+            }
             if (fine) fine = kv_warp_wait(bars + 8 * LT_A_P, c & 1, stop);
             if (!fine) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const int stage = c % A.stages;
-            const uint64_t b = kv_desc(sm_at + (1 + A.stages) * tile_bytes, 16, 1024);
-            for (int part = 0; part < pairs; part++) {
-                const uint64_t a = kv_desc(sm_at + (1 + stage) * tile_bytes + part * LT_PART, LT_TOKENS * LT_CHUNK_ROW, 1024);
+            const uint32_t stage = c % T::STAGES;
+            const uint64_t v = v_desc + stage * (T::BYTES >> 4);
+            const bool add = i > walk.from;
 #pragma unroll
-                for (int s = 0; s < 4; s++) kv_mma_ss(tmem + 64 * part, a + (s * 2048 >> 4), b + 2 * s, o_what, i > walk.from || s > 0);
-                kv_commit(bars + 8 * (LT_A_OUT + stage * LT_A_PARTS + part));
-            }
+            for (int p = 0; p < PAIRS; p++) lt_mma_ss<4, 2048 / 16, 2>(tmem + 64 * p, v + p * (LT_PART >> 4), p_desc, o_what, add);
+            kv_commit(bars + 8 * (LT_A_OUT + stage));
             kv_commit(bars + 8 * LT_A_O);
+            if (next) scores(c + 1);
         }
         piece++;
     }
 }
 
-template <bool BF>
-__global__ void __launch_bounds__(LT_A_THREADS, 1) lt_attend_kernel(const LtShape S, const LtBatch B, const LtAttend A, const __grid_constant__ CUtensorMap map)
+template <int PAIRS, bool BF>
+__global__ void __launch_bounds__(LT_A_THREADS, 1) lt_attend_kernel(const LtShape S, const LtBatch B, const LtAttend A, const __grid_constant__ CUtensorMap map,
+                                                                    const __grid_constant__ CUtensorMap pairs_map)
 {
     extern __shared__ uint8_t lt_raw[];
     uint8_t* const sm = lt_raw + (-(uint32_t)__cvta_generic_to_shared(lt_raw) & 1023u);
     const uint32_t sm_at = (uint32_t)__cvta_generic_to_shared(sm);
-    const int tile_bytes = (S.latent / 64 + 1) * LT_ROWS * LT_CHUNK_ROW, warp = threadIdx.x >> 5;
-    LtMisc& M = *(LtMisc*)(sm + (1 + A.stages) * tile_bytes + LT_ROWS * LT_CHUNK_ROW);
+    const int warp = threadIdx.x >> 5;
+    LtMisc& M = *(LtMisc*)(sm + LtTile<PAIRS>::MISC);
     const uint32_t bars = (uint32_t)__cvta_generic_to_shared(M.bars);
     asm volatile("griddepcontrol.launch_dependents;");
     if (threadIdx.x == 0) {
@@ -467,11 +489,11 @@ __global__ void __launch_bounds__(LT_A_THREADS, 1) lt_attend_kernel(const LtShap
     walk.item_at = M.item_at;
     const uint32_t tmem = *(volatile uint32_t*)&M.tmem;  // O: 64 columns per 128 channels; S: 2 x 64 from 256 on
     if (warp < 4) {
-        lt_attend_rows<BF>(S, B, A, walk, share, sm, sm_at, M, bars, tmem);
+        lt_attend_rows<PAIRS, BF>(S, B, A, walk, share, sm, sm_at, M, bars, tmem);
     } else if (warp == 4) {
-        lt_attend_bring(S, B, A, &map, walk, sm_at, M, bars);
+        lt_attend_bring<PAIRS>(S, B, A, &map, &pairs_map, walk, sm_at, M, bars);
     } else {
-        lt_attend_products<BF>(S, B, A, walk, sm_at, M, bars, tmem);
+        lt_attend_products<PAIRS, BF>(S, B, A, walk, sm_at, M, bars, tmem);
         __syncwarp();
         kv_commit(bars + 8 * LT_A_END);                  // nothing is on its way any more when the memory is given back
         kv_wait(bars + 8 * LT_A_END, 0);
@@ -486,60 +508,70 @@ __global__ void __launch_bounds__(LT_A_THREADS, 1) lt_attend_kernel(const LtShap
     }
 }
 
-// Joins the pieces of items that runs cut.  A CTA takes a row at a time: 128 threads a piece, 4 channels each, 4 pieces side by side.
-#define LT_JOIN_THREADS 512
+// Joins the pieces of items that runs cut.  A warp takes 128 channels of a row, 4 channels a lane, and asks for 8 pieces at a time; the pieces'
+// references and sums it has in its lanes, 32 at a time.
+#define LT_JOIN_THREADS 128
+#define LT_JOIN_CUTS 1024               // most groups of CTAs
 template <bool BF> __global__ void __launch_bounds__(LT_JOIN_THREADS) lt_join_kernel(const LtShape S, const LtBatch B, const LtAttend A)
 {
-    __shared__ float4 sums[LT_JOIN_THREADS];
-    __shared__ int4 cuts[LT_JOIN_THREADS];
-    const int lane4 = threadIdx.x >> 7, ch = 4 * (threadIdx.x & 127), rows_of = A.group_tiles * LT_ROWS;
+    __shared__ int cut_runs[LT_JOIN_CUTS], cut_count;
+    const int lane = threadIdx.x & 31, pairs = S.latent / 128, rows_of = A.group_tiles * LT_ROWS;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    for (int g = threadIdx.x; g < A.groups; g += LT_JOIN_THREADS) cuts[g] = *(const int4*)(A.cuts + 4 * g);
-    __syncthreads();
-    int done = 0;                                        // rows of cut items in front of this run's
-    for (int g = 0; g < A.groups; g++) {
-        const int4 cut = cuts[g];
-        if (cut.z < 2) continue;
-        for (int i = ((int)blockIdx.x - done % (int)gridDim.x + (int)gridDim.x) % (int)gridDim.x; i < rows_of; i += gridDim.x) {
-            const LtSeq q = lt_seq(B, cut.x);
-            const int64_t row = (int64_t)cut.y * rows_of + i;
-            if (row >= (int64_t)q.n * S.heads) continue;
-            auto slot = [&](int s) { return ((s == 0 ? (int64_t)2 * g + 1 : (int64_t)2 * (g + s)) * A.group_tiles + i / LT_ROWS) * LT_ROWS + i % LT_ROWS; };
-            float m = KV_M_NONE, l = 0.f;
-            for (int s = 0; s < cut.z; s++) m = fmaxf(m, A.part_ml[2 * slot(s)]);
-            for (int s = 0; s < cut.z; s++) {
-                const float2 ml = *(const float2*)(A.part_ml + 2 * slot(s));
-                l += ml.y * kv_exp2(ml.x - m);
-            }
-            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (ch < S.latent)
-#pragma unroll 4
-                for (int s = lane4; s < cut.z; s += 4) {
-                    const float w = kv_exp2(A.part_ml[2 * slot(s)] - m);
-                    const float4 o = *(const float4*)(A.part_o + slot(s) * S.latent + ch);
-                    sum = make_float4(fmaf(w, o.x, sum.x), fmaf(w, o.y, sum.y), fmaf(w, o.z, sum.z), fmaf(w, o.w, sum.w));
-                }
-            __syncthreads();
-            sums[threadIdx.x] = sum;
-            __syncthreads();
-            if (lane4 == 0 && ch < S.latent) {
-                const float by = l == 0.f ? 0.f : 1.f / l;
-                float x[4] = {0.f, 0.f, 0.f, 0.f};
+    if (threadIdx.x < 32) {
+        // the runs whose last item goes on, in order: every CTA has the same list
+        int n = 0;
+        for (int g0 = 0; g0 < A.groups; g0 += 5 * 32) {
+            bool cut[5];
 #pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    const float4 o = sums[threadIdx.x + 128 * k];
-                    x[0] += o.x;
-                    x[1] += o.y;
-                    x[2] += o.z;
-                    x[3] += o.w;
-                }
-                const int64_t token = q.start + row / S.heads;
-                const int head = (int)(row % S.heads);
-                *(uint2*)((uint16_t*)A.out.data + token * A.out.token_stride + head * A.out.head_stride + ch) =
-                    make_uint2(kv_pack<BF>(x[0] * by, x[1] * by), kv_pack<BF>(x[2] * by, x[3] * by));
-                if (threadIdx.x == 0 && A.lse) A.lse[token * S.heads + head] = l == 0.f ? -KV_INF : (m + log2f(l)) * 0.6931471805599453f;
+            for (int k = 0; k < 5; k++) cut[k] = g0 + 32 * k + lane < A.groups && A.cuts[4 * (g0 + 32 * k + lane) + 2] > 1;
+#pragma unroll
+            for (int k = 0; k < 5; k++) {
+                const uint32_t some = __ballot_sync(0xffffffffu, cut[k]);
+                if (cut[k]) cut_runs[n + __popc(some & ((1u << lane) - 1))] = g0 + 32 * k + lane;
+                n += __popc(some);
             }
         }
-        done += rows_of;
+        if (lane == 0) cut_count = n;
+    }
+    __syncthreads();
+    const int64_t work = (int64_t)cut_count * rows_of * pairs, step = (int64_t)gridDim.x * (LT_JOIN_THREADS / 32);
+    for (int64_t w = (int64_t)blockIdx.x * (LT_JOIN_THREADS / 32) + (threadIdx.x >> 5); w < work; w += step) {
+        const int g = cut_runs[w / (rows_of * pairs)], at = (int)(w % (rows_of * pairs)), i = at / pairs, ch = at % pairs * 128 + 4 * lane;
+        const int4 cut = *(const int4*)(A.cuts + 4 * g);
+        const LtSeq q = lt_seq(B, cut.x);
+        const int64_t row = (int64_t)cut.y * rows_of + i;
+        if (row >= (int64_t)q.n * S.heads) continue;
+        auto slot = [&](int s) { return ((s == 0 ? (int64_t)2 * g + 1 : (int64_t)2 * (g + s)) * A.group_tiles + i / LT_ROWS) * LT_ROWS + i % LT_ROWS; };
+        float m = KV_M_NONE, l = 0.f;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s0 = 0; s0 < cut.z; s0 += 32) {
+            const float2 ml = s0 + lane < cut.z ? *(const float2*)(A.part_ml + 2 * slot(s0 + lane)) : make_float2(KV_M_NONE, 0.f);
+            float top = ml.x;
+#pragma unroll
+            for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            top = fmaxf(top, m);
+            const float fall = kv_exp2(m - top), weight = kv_exp2(ml.x - top);
+            m = top;
+            float part = ml.y * weight;
+#pragma unroll
+            for (int d = 16; d; d >>= 1) part += __shfl_xor_sync(0xffffffffu, part, d);
+            l = l * fall + part;
+            sum = make_float4(sum.x * fall, sum.y * fall, sum.z * fall, sum.w * fall);
+            for (int s = 0; s < 32 && s0 + s < cut.z; s += 8) {
+                float4 o[8];
+#pragma unroll
+                for (int k = 0; k < 8; k++) o[k] = s0 + s + k < cut.z ? *(const float4*)(A.part_o + slot(s0 + s + k) * S.latent + ch) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int k = 0; k < 8; k++) {
+                    const float by = __shfl_sync(0xffffffffu, weight, s + k);
+                    if (s0 + s + k < cut.z) sum = make_float4(fmaf(by, o[k].x, sum.x), fmaf(by, o[k].y, sum.y), fmaf(by, o[k].z, sum.z), fmaf(by, o[k].w, sum.w));
+                }
+            }
+        }
+        const float by = l == 0.f ? 0.f : 1.f / l;
+        const int64_t token = q.start + row / S.heads;
+        const int head = (int)(row % S.heads);
+        *(uint2*)((uint16_t*)A.out.data + token * A.out.token_stride + head * A.out.head_stride + ch) = make_uint2(kv_pack<BF>(sum.x * by, sum.y * by), kv_pack<BF>(sum.z * by, sum.w * by));
+        if (ch == 0 && A.lse) A.lse[token * S.heads + head] = l == 0.f ? -KV_INF : (m + log2f(l)) * 0.6931471805599453f;
     }
 }

@@ -49,15 +49,47 @@ __device__ __forceinline__ uint16_t* lt_token(const LtShape& S, const LtBatch& B
 #define LT_CHUNK_ROW 128
 __device__ __forceinline__ uint32_t lt_at(int row, int piece) { return (uint32_t)(row * LT_CHUNK_ROW + ((piece ^ (row & 7)) << 4)); }
 
+// A warp as a whole comes to the copies and products below, and one thread of it issues them: the operands then are where the compiler knows them
+// to be the same for all lanes, in the registers that these instructions want.  (Issued by `if (lane == 0)`, a copy held up its warp for 800
+// cycles and a product for 500.)  So must be what the operands come from: a page number goes through lt_uniform.
+__device__ __forceinline__ int lt_uniform(int x, int lane)                   // lane's x; not below -1
+{
+    return (int)__reduce_max_sync(0xffffffffu, (threadIdx.x & 31) == (unsigned)lane ? (unsigned)(x + 1) : 0u) - 1;
+}
 // A box of the tensor (x, y, z) to shared memory
 __device__ __forceinline__ void lt_tma(uint32_t smem, const CUtensorMap* map, int x, int y, int z, uint32_t bar)
 {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+    asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+                 "@e cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n\t}"
                  ::"r"(smem), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void lt_tma(uint32_t smem, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar)
+{
+    asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+                 "@e cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}"
+                 ::"r"(smem), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void lt_expect(uint32_t bar, uint32_t bytes)      // and arrive
 {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+    asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t@e mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar), "r"(bytes) : "memory");
+}
+// N products of 16 channels or tokens each, D += A B, from shared memory; SA, SB: steps of the descriptors
+template <int N, int SA, int SB> __device__ __forceinline__ void lt_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add)
+{
+    asm volatile("{\n\t.reg .pred p, e, t;\n\t.reg .b64 a, b;\n\telect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.eq.u32 t, 0, 0;\n\t"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t"
+                 "add.u64 a, %1, %5;\n\tadd.u64 b, %2, %6;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(what), "r"((uint32_t)add), "n"(SA), "n"(SB) : "memory");
+    if constexpr (N > 2) lt_mma_ss<N - 2, SA, SB>(d, a + 2 * SA, b + 2 * SB, what, true);
+}
+// The same with A in tensor memory, 8 columns a step
+template <int N, int SB> __device__ __forceinline__ void lt_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add)
+{
+    asm volatile("{\n\t.reg .pred p, e, t;\n\t.reg .b32 a;\n\t.reg .b64 b;\n\telect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.eq.u32 t, 0, 0;\n\t"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+                 "add.u32 a, %1, 8;\n\tadd.u64 b, %2, %5;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(what), "r"((uint32_t)add), "n"(SB) : "memory");
+    if constexpr (N > 2) lt_mma_ts<N - 2, SB>(d, a + 16, b + 2 * SB, what, true);
 }
 __device__ __forceinline__ void lt_init(uint32_t bar, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 

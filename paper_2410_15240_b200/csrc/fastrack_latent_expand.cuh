@@ -107,23 +107,22 @@ __device__ __forceinline__ void lt_expand_bring(const LtShape& S, const LtBatch&
         const int boxes = __popc(__ballot_sync(0xffffffffu, page >= 0));
         fine = kv_warp_wait(bars + 8 * LT_E_A_OUT, (pieces & 1) ^ 1, stop);
         if (!fine) break;
-        if (lane == 0) lt_expect(bars + 8 * LT_E_A_IN, boxes * box * LT_CHUNK_ROW * chunks);
-        __syncwarp();
-        if (page >= 0)
-            for (int k = 0; k < chunks; k++) lt_tma(sm_at + k * LT_E_CHUNK + lane * box * LT_CHUNK_ROW, pool, 64 * k, t & (S.block_tokens - 1), page, bars + 8 * LT_E_A_IN);
+        lt_expect(bars + 8 * LT_E_A_IN, boxes * box * LT_CHUNK_ROW * chunks);
+        for (int b = 0; b < LT_E_TOKENS / box; b++) {
+            const int from = lt_uniform(page, b);
+            if (from >= 0)
+                for (int k = 0; k < chunks; k++)
+                    lt_tma(sm_at + k * LT_E_CHUNK + b * box * LT_CHUNK_ROW, pool, 64 * k, (walk.tile * LT_E_TOKENS + b * box) & (S.block_tokens - 1), from, bars + 8 * LT_E_A_IN);
+        }
         pieces++;
-        __syncwarp();
         for (int u = walk.from; u < walk.to && fine; u++) {
             const int width = u & 1 ? S.value : S.key;
             for (int k = 0; k < chunks; k++, c++) {
                 const int s = c % LT_E_STAGES;
                 fine = kv_warp_wait(bars + 8 * (LT_E_B_OUT + s), (c / LT_E_STAGES & 1) ^ 1, stop);
                 if (!fine) break;
-                if (lane == 0) {
-                    lt_expect(bars + 8 * (LT_E_B_IN + s), width * LT_CHUNK_ROW);
-                    lt_tma(weights_at + s * LT_E_CHUNK, u & 1 ? v_weights : k_weights, 64 * k, 0, u >> 1, bars + 8 * (LT_E_B_IN + s));
-                }
-                __syncwarp();
+                lt_expect(bars + 8 * (LT_E_B_IN + s), width * LT_CHUNK_ROW);
+                lt_tma(weights_at + s * LT_E_CHUNK, u & 1 ? v_weights : k_weights, 64 * k, 0, u >> 1, bars + 8 * (LT_E_B_IN + s));
             }
         }
     }
@@ -149,8 +148,7 @@ __device__ __forceinline__ void lt_expand_products(const LtShape& S, const LtBat
                 if (!kv_warp_wait(bars + 8 * (LT_E_B_IN + s), c / LT_E_STAGES & 1, stop)) return;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint64_t a = kv_desc(sm_at + k * LT_E_CHUNK, 16, 1024), b = kv_desc(sm_at + (chunks + s) * LT_E_CHUNK, 16, 1024);
-#pragma unroll
-                for (int i = 0; i < 4; i++) kv_mma_ss(tmem + 128 * (units & 1), a + 2 * i, b + 2 * i, what, k > 0 || i > 0);
+                lt_mma_ss<4, 2, 2>(tmem + 128 * (units & 1), a, b, what, k > 0);
                 kv_commit(bars + 8 * (LT_E_B_OUT + s));
             }
             kv_commit(bars + 8 * (LT_E_D_IN + (units & 1)));

@@ -217,21 +217,18 @@ __device__ __forceinline__ void lt_prompt_bring(const LtShape& S, const LtBatch&
         k_out = false;
         if (!kv_warp_wait(bars + 8 * (LT_P_K_OUT + (s & 1)), (s >> 1 & 1) ^ 1, stop)) break;
         const uint32_t bar = bars + 8 * (LT_P_K_IN + (s & 1)), to = k_at + (s & 1) * k_chunks * LT_P_CHUNK;
-        if (lane == 0) {
-            ((volatile uint32_t*)M.present)[s & 7] = present;
-            lt_expect(bar, (k_chunks - 1) * LT_P_CHUNK + __popc(some) * box * LT_CHUNK_ROW);
-            for (int k = 0; k < k_chunks - 1; k++) lt_tma(to + k * LT_P_CHUNK, k_map, 64 * k, (int)J.key_start + t0, A.k_heads ? J.head : 0, bar);
-        }
+        if (lane == 0) ((volatile uint32_t*)M.present)[s & 7] = present;
         __syncwarp();
-        if (page >= 0) lt_tma(to + (k_chunks - 1) * LT_P_CHUNK + lane * box * LT_CHUNK_ROW, pool, S.latent, t & (S.block_tokens - 1), page, bar);
+        lt_expect(bar, (k_chunks - 1) * LT_P_CHUNK + __popc(some) * box * LT_CHUNK_ROW);
+        for (int k = 0; k < k_chunks - 1; k++) lt_tma(to + k * LT_P_CHUNK, k_map, 64 * k, (int)J.key_start + t0, A.k_heads ? J.head : 0, bar);
+        for (int b = 0; b < boxes; b++) {
+            const int from = lt_uniform(page, b);
+            if (from >= 0) lt_tma(to + (k_chunks - 1) * LT_P_CHUNK + b * box * LT_CHUNK_ROW, pool, S.latent, (t0 + b * box) & (S.block_tokens - 1), from, bar);
+        }
         k_out = true;
-        __syncwarp();
         if (!kv_warp_wait(bars + 8 * LT_P_V_OUT, (s & 1) ^ 1, stop)) break;
-        if (lane == 0) {
-            lt_expect(bars + 8 * LT_P_V_IN, v_chunks * LT_P_CHUNK);
-            for (int k = 0; k < v_chunks; k++) lt_tma(v_at + k * LT_P_CHUNK, v_map, 64 * k, (int)J.key_start + t0, A.v_heads ? J.head : 0, bars + 8 * LT_P_V_IN);
-        }
-        __syncwarp();
+        lt_expect(bars + 8 * LT_P_V_IN, v_chunks * LT_P_CHUNK);
+        for (int k = 0; k < v_chunks; k++) lt_tma(v_at + k * LT_P_CHUNK, v_map, 64 * k, (int)J.key_start + t0, A.v_heads ? J.head : 0, bars + 8 * LT_P_V_IN);
     }
     // what is on its way arrives before the CTA ends
     const int brought = s + (s < steps && k_out);
@@ -252,8 +249,8 @@ __device__ __forceinline__ void lt_prompt_products(const LtShape& S, const LtPro
     auto scores = [&](int s, int m) {
         for (int k = 0; k < k_chunks; k++) {
             const uint64_t a = kv_desc(sm_at + (m * k_chunks + k) * LT_P_CHUNK, 16, 1024), b = kv_desc(k_at + ((s & 1) * k_chunks + k) * LT_P_CHUNK, 16, 1024);
-            const int n = k < k_chunks - 1 ? 4 : S.rope / 16;
-            for (int i = 0; i < n; i++) kv_mma_ss(tmem + 128 * m, a + 2 * i, b + 2 * i, s_what, k > 0 || i > 0);
+            if (k == k_chunks - 1 && S.rope == 32) lt_mma_ss<2, 2, 2>(tmem + 128 * m, a, b, s_what, true);
+            else lt_mma_ss<4, 2, 2>(tmem + 128 * m, a, b, s_what, k > 0);
         }
         kv_commit(bars + 8 * (LT_P_S_IN + m));
     };
@@ -268,8 +265,7 @@ __device__ __forceinline__ void lt_prompt_products(const LtShape& S, const LtPro
                 if (!kv_warp_wait(bars + 8 * (LT_P_P_IN + m), s & 1, stop)) return;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint64_t b = kv_desc(v_at, LT_P_CHUNK, 1024);
-#pragma unroll
-                for (int k = 0; k < 8; k++) kv_mma_ts(tmem + 256 + 128 * m, tmem + 128 * m + 8 * k, b + (k * 2048 >> 4), o_what, s > 0 || k > 0);
+                lt_mma_ts<8, 2048 / 16>(tmem + 256 + 128 * m, tmem + 128 * m, b, o_what, s > 0);
             }
             if (s + 1 < J.steps[m]) scores(s + 1, m);
         }

@@ -388,13 +388,13 @@ static int lt_pool_map(fastrack_latent* lt, const LtBatch& B, CUtensorMap* map)
     return lt_map(lt, map, B.pool, S.row, S.block_tokens, B.pool_pages, 2 * S.row, (int64_t)2 * S.row * S.block_tokens, S.block_tokens < LT_TOKENS ? S.block_tokens : LT_TOKENS);
 }
 
-// The pool's latents by 64 channels: channels, rows of a page, which 64, pages; boxes of 64 tokens and all channels (blocks of 64 tokens or more)
+// The pool's latents by 64 channels: channels, rows of a page, which 64, pages; boxes of 64 tokens and 128 channels (blocks of 64 tokens or more)
 static int lt_pairs_map(fastrack_latent* lt, const LtBatch& B, CUtensorMap* map)
 {
     const LtShape& S = lt->shape;
     memset(map, 0, sizeof *map);
     if (B.pool_pages == 0 || S.block_tokens < LT_TOKENS) return FASTRACK_OK;
-    return lt_map(lt, map, B.pool, 64, S.block_tokens, S.latent / 64, 2 * S.row, 128, LT_TOKENS, B.pool_pages, (int64_t)2 * S.row * S.block_tokens, S.latent / 64);
+    return lt_map(lt, map, B.pool, 64, S.block_tokens, S.latent / 64, 2 * S.row, 128, LT_TOKENS, B.pool_pages, (int64_t)2 * S.row * S.block_tokens, 2);
 }
 
 extern "C" int fastrack_latent_attention(fastrack_latent* lt, const fastrack_latent_batch* batch, const fastrack_kv_rows* q, const fastrack_kv_rows* q_rope,
@@ -435,7 +435,7 @@ extern "C" int fastrack_latent_attention(fastrack_latent* lt, const fastrack_lat
     cudaLaunchAttribute overlap;
     overlap.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     overlap.val.programmaticStreamSerializationAllowed = 1;
-    c.gridDim = dim3(8 * lt->num_sms);
+    c.gridDim = dim3(16 * lt->num_sms);
     c.blockDim = dim3(LT_JOIN_THREADS);
     c.stream = st;
     c.attrs = &overlap;

@@ -7,40 +7,30 @@
 //     O^T += C^T P^T    latent x rows, M = 128 channels at a time, N = rows, over the tile's tokens
 // The second product is taken the other way round: the accumulator of 64 rows x 512 channels then takes 4 x 64 columns of tensor memory with
 // all 128 lanes, N follows the number of rows that there are, and S keeps its two buffers beside it.  (With rows as M, 512 columns would be
-// full of O alone, half of their lanes idle.)  Warps 0-3 make the weights, 16 rows each, and write them to shared memory; warp 4 brings the
-// tiles; warp 5 issues the products.  The scores of the next tile are made while this one's weights are.
+// full of O alone, half of their lanes idle.)  Warps 0-7 make the weights and write them to shared memory; warp 8 brings the
+// tiles; warp 9 issues the products.  The scores of the next tile are made while this one's weights are.
 //
 // All work is one line: for each sequence, for each group of row tiles, the tiles of tokens that the group sees.  The line is cut into equal
 // runs, one for each group of CTAs (a CTA per row tile of a group; the CTAs of a group read the same tokens at the same time, all but the first
 // out of L2).  What a run cuts is joined by a kernel of its own; a run has at most two such pieces, its first and its last.
 #define LT_ROWS 64
 #define LT_TOKENS 64
-#define LT_A_THREADS 192
+#define LT_A_THREADS 320
 #define LT_A_STAGES 4                   // at most
 // PAIRS: of 64 channels of the latent
 template <int PAIRS> struct LtTile {
     static constexpr int CHUNKS = 2 * PAIRS + 1, BYTES = CHUNKS * 64 * LT_CHUNK_ROW, STAGES = PAIRS > 2 ? 2 : 4;
+    static constexpr int FIRST = PAIRS > 1 ? PAIRS / 2 : 1;                  // pairs of a tile's first part; the second has the rest and the shared key
     static constexpr int P = (1 + STAGES) * BYTES, MISC = P + 64 * LT_CHUNK_ROW, SMEM = MISC + 2048 + 1024;    // after Q and the stages; room to round the base up
 };
+#define LT_A_AHEAD 4                    // tiles that are brought to L2 in advance
 #define LT_PART 16384                   // bytes of 128 channels of a tile
 #define LT_RAISE 8.f                    // a row's reference is raised when a score is 2^8 above it: weights stay below 2^8, and O seldom has to be multiplied
 
-// Barriers, 8 bytes each.  IN and OUT: of a stage.  (While the tensor cores read their operands, an access to shared memory takes some 240
-// cycles, a barrier's that has long been there too: one for each 128 channels cost a tile's scores 1000 cycles.)
-enum { LT_A_IN = 0, LT_A_OUT = LT_A_STAGES, LT_A_S = 2 * LT_A_OUT, LT_A_P = LT_A_S + 2, LT_A_O, LT_A_Q, LT_A_END, LT_A_BARS };
-struct LtMisc {
-    uint64_t bars[LT_A_BARS];
-    float factor[LT_ROWS];              // of rows: O's when the reference is raised, and 1 / l at the end
-    int64_t out_at[LT_ROWS];            // of rows: where the answer goes
-    uint32_t bad[3][2];                 // tokens of a tile with a score that is not finite, see lt_guard
-    uint32_t present[8];                // of the last tiles: which 16 tokens have a page
-    int stop, halt[2];                  // halt: what the rows' warps go by, all the same way (they have barriers among themselves)
-    uint32_t tmem;
-    int64_t item, item_at;
-    int64_t warp_sum[LT_A_THREADS / 32];
-};
-static_assert(sizeof(LtMisc) <= 2048, "");
-
+// Barriers, 8 bytes each.  IN and OUT: of a stage's two parts.  A part is filled again while the other is still used, and scores begin with the first.
+// (While the tensor cores read their operands, an access to shared memory takes some 240 cycles, a barrier's that has long been there too, so
+// that more parts cost more than they bring, and barriers are asked before the answer is needed.)
+enum { LT_A_IN = 0, LT_A_OUT = 2 * LT_A_STAGES, LT_A_S = 2 * LT_A_OUT, LT_A_P = LT_A_S + 2, LT_A_O, LT_A_Q, LT_A_END, LT_A_BARS };
 struct LtAttend {
     KvRows q, q_rope, out;
     float* lse;
@@ -51,45 +41,59 @@ struct LtAttend {
     int least;                          // tiles of a run
     float* part_o;                      // [groups][2][group_tiles][64][latent]: the first piece of a run (begun before it), the last
     float* part_ml;                     // [groups][2][group_tiles][64][2]
-    int* cuts;                          // [groups][4]: of a run whose last item goes on: sequence, group of row tiles, pieces
+    int* cuts;                          // [groups][4]: of a run whose last item goes on: first packed row of the sequence, the item's first row, pieces, rows of the sequence
 };
 
-// Tiles of tokens that an item (a sequence's group of row tiles) takes; one at least if there are rows
+// Tiles of tokens that an item (a sequence's group of row tiles) takes; one at least if there are rows.  (Rows of a sequence: at most 2^30.)
 __device__ __forceinline__ int lt_item_tiles(const LtShape& S, const LtAttend& A, const LtSeq& q, int group)
 {
-    const int64_t first = (int64_t)group * A.group_tiles * LT_ROWS, rows = (int64_t)q.n * S.heads;
+    const int rows_of = A.group_tiles * LT_ROWS, first = group * rows_of, rows = q.n * S.heads;
     if (first >= rows) return 0;
-    const int last = (int)(min(first + A.group_tiles * LT_ROWS, rows) - 1) / S.heads;
+    const int last = (int)((uint32_t)(min(first + rows_of, rows) - 1) / (uint32_t)S.heads);
     const int end = A.parents ? q.len : q.len - q.n + last + 1;
     return max((end + LT_TOKENS - 1) / LT_TOKENS, 1);
 }
 
-// A walk along a run.  Every warp makes its own.
+// A walk along a run.  Every warp makes its own; whoever looked for the run's first item has left it in `q` and `tiles`.
 struct LtWalk {
-    int64_t item, item_at, at, end;     // at: in the line
+    int64_t item_at, at, end;           // in the line: where the item begins, where the walk is, where the run ends
     int seq, group, from, to, tiles;    // the piece: tiles from .. to - 1 of the item's
     LtSeq q;
     __device__ __forceinline__ bool next(const LtShape& S, const LtBatch& B, const LtAttend& A)
     {
         while (at < end) {
-            seq = (int)(item / A.seq_groups);
-            group = (int)(item % A.seq_groups);
-            if (seq >= B.n_seqs) return false;
-            q = lt_seq(B, seq);
-            tiles = lt_item_tiles(S, A, q, group);
-            from = (int)(at - item_at);
-            to = (int)min((int64_t)tiles, end - item_at);
-            if (from + 1 > tiles) {                      // nothing (left) of this one
-                item++;
-                item_at += tiles;
+            if (at == item_at + tiles) {                 // nothing left of this item
+                item_at = at;
+                if (++group == A.seq_groups) {
+                    group = 0;
+                    if (++seq >= B.n_seqs) return false;
+                    q = lt_seq(B, seq);
+                }
+                tiles = lt_item_tiles(S, A, q, group);
                 continue;
             }
+            from = (int)(at - item_at);
+            to = (int)min((int64_t)tiles, end - item_at);
             at = item_at + to;
             return true;
         }
         return false;
     }
 };
+
+struct LtMisc {
+    uint64_t bars[LT_A_BARS];
+    float factor[LT_ROWS];              // of rows: O's when the reference is raised, and 1 / l at the end
+    int64_t out_at[LT_ROWS];            // of rows: where the answer goes
+    uint32_t bad[3][2];                 // tokens of a tile with a score that is not finite, see lt_guard
+    uint32_t present[8];                // of the last tiles: which 16 tokens have a page
+    int stop, halt[2];                  // halt: what the rows' warps go by, all the same way (they have barriers among themselves)
+    uint32_t tmem;
+    LtWalk walk;                        // at the run's begin
+    float of_half[2][LT_ROWS];          // of rows over half of the tokens: a tile's largest scores, and at the end the sums of weights
+    int64_t warp_sum[LT_A_THREADS / 32];
+};
+static_assert(sizeof(LtMisc) <= 2048, "");
 
 // The tokens before `len`, of 64 from t0 on, whose pages are there
 __device__ __forceinline__ uint64_t lt_there(uint32_t present, int t0, int len)
@@ -118,45 +122,49 @@ __device__ __forceinline__ uint64_t lt_sees(const LtAttend& A, const LtSeq& q, i
     return m;
 }
 
-// Warps 0-3: the weights of the rows, and their answers
+// Warps 0-7: the weights of the rows, and their answers.  Warps w and w + 4 have the same 16 rows, 32 tokens of a tile each.
+#define LT_A_ROW_THREADS 256
 template <int PAIRS, bool BF>
 __device__ __forceinline__ void lt_attend_rows(const LtShape& S, const LtBatch& B, const LtAttend& A, LtWalk walk, int64_t share, uint8_t* sm, uint32_t sm_at, LtMisc& M,
                                                uint32_t bars, uint32_t tmem)
 {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane & 3;
-    const int g = blockIdx.x / A.group_tiles, r = blockIdx.x % A.group_tiles;
     using T = LtTile<PAIRS>;
     constexpr int chunks = 2 * PAIRS, latent = 128 * PAIRS;
+    const int warp = threadIdx.x >> 5 & 3, half = threadIdx.x >> 7, lane = threadIdx.x & 31, quad = lane & 3;
+    const int g = blockIdx.x / A.group_tiles, r = blockIdx.x % A.group_tiles;
     uint8_t* const p_sm = sm + T::P;
     volatile int* const stop = &M.stop;
-    const uint32_t lanes = (uint32_t)warp << 21, s_at = tmem + lanes + 256, o_at = tmem + lanes;
+    const uint32_t lanes = (uint32_t)warp << 21, s_at = tmem + lanes + 256 + 32 * half, o_at = tmem + lanes;
     const float scale = S.scale_log2;
+    const uint32_t heads = S.heads;
     bool fine = true, halted = false;                    // fine: of this warp; where it is not, answers are NaN
     int c = 0;                                           // tiles so far
     if (r == 0 && threadIdx.x == 0) A.cuts[4 * g + 2] = 0;
     while (!halted && walk.next(S, B, A)) {
         const LtSeq& q = walk.q;
-        const int64_t first = ((int64_t)walk.group * A.group_tiles + r) * LT_ROWS;
-        const int rows = (int)min((int64_t)LT_ROWS, (int64_t)q.n * S.heads - first);
+        const int first = (walk.group * A.group_tiles + r) * LT_ROWS, rows = min(LT_ROWS, q.n * (int)heads - first);
         const bool whole = walk.from == 0 && walk.to == walk.tiles;
         if (r == 0 && threadIdx.x == 0 && walk.from == 0 && !whole) {
-            A.cuts[4 * g] = walk.seq;
-            A.cuts[4 * g + 1] = walk.group;
+            A.cuts[4 * g] = q.start;
+            A.cuts[4 * g + 1] = first;
             A.cuts[4 * g + 2] = (int)((walk.item_at + walk.tiles - 1) / share) - g + 1;
+            A.cuts[4 * g + 3] = q.n * (int)heads;
         }
         if (rows <= 0) continue;
         {
             // Q: 8 threads take a row's chunk
             const int piece = threadIdx.x & 7;
-            for (int row = threadIdx.x >> 3; row < LT_ROWS; row += 16) {
-                const bool there = row < rows;
-                const int64_t token = q.start + (there ? (first + row) / S.heads : 0);
-                const int head = there ? (int)((first + row) % S.heads) : 0;
-                const uint16_t* src = (const uint16_t*)A.q.data + token * A.q.token_stride + head * A.q.head_stride;
-                const uint16_t* key = (const uint16_t*)A.q_rope.data + token * A.q_rope.token_stride + head * A.q_rope.head_stride;
 #pragma unroll
-                for (int k = 0; k < chunks; k++) lt_copy16(sm_at + k * LT_ROWS * LT_CHUNK_ROW + lt_at(row, piece), src + 64 * k + 8 * piece, there);
-                if (8 * piece < S.rope) lt_copy16(sm_at + chunks * LT_ROWS * LT_CHUNK_ROW + lt_at(row, piece), key + 8 * piece, there);
+            for (int k2 = 0; k2 < LT_ROWS * 8 / LT_A_ROW_THREADS; k2++) {
+                const int row = (threadIdx.x >> 3) + LT_A_ROW_THREADS / 8 * k2;
+                const bool there = row < rows;
+                const uint32_t at = there ? first + row : 0, j = at / heads, head = at - j * heads;
+                const int64_t token = q.start + (int64_t)j;
+                const uint16_t* src = (const uint16_t*)A.q.data + token * A.q.token_stride + head * A.q.head_stride + 8 * piece;
+                const uint16_t* key = (const uint16_t*)A.q_rope.data + token * A.q_rope.token_stride + head * A.q_rope.head_stride + 8 * piece;
+#pragma unroll
+                for (int k = 0; k < chunks; k++) lt_copy16(sm_at + k * LT_ROWS * LT_CHUNK_ROW + lt_at(row, piece), src + 64 * k, there);
+                if (8 * piece < S.rope) lt_copy16(sm_at + chunks * LT_ROWS * LT_CHUNK_ROW + lt_at(row, piece), key, there);
                 if (piece == 0) M.out_at[row] = token * A.out.token_stride + head * A.out.head_stride;
             }
             lt_copies_done();
@@ -165,46 +173,40 @@ __device__ __forceinline__ void lt_attend_rows(const LtShape& S, const LtBatch& 
         }
         const bool active = 16 * warp < rows;
         // rows of this lane: 16 warp + lane / 4 and 8 further on
+        const int my_row = 16 * warp + (lane >> 2);
         int j[2];
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const int row = 16 * warp + (lane >> 2) + 8 * h;
-            j[h] = row < rows ? (int)((first + row) / S.heads) : -1;
-        }
-        const int see_all = A.parents ? q.len - q.n : q.len - q.n + (int)(first / S.heads) + 1;
+        for (int h = 0; h < 2; h++) j[h] = my_row + 8 * h < rows ? (int)((uint32_t)(first + my_row + 8 * h) / heads) : -1;
+        const int see_all = A.parents ? q.len - q.n : q.len - q.n + (int)((uint32_t)first / heads) + 1;
         float m[2] = {KV_M_NONE, KV_M_NONE}, l[2] = {0.f, 0.f};
         for (int i = walk.from; i < walk.to && !halted; i++, c++) {
             const int t0 = i * LT_TOKENS, set = c % 3;
             // what is known of the tile first, while its scores are made
-            fine = kv_warp_wait(bars + 8 * (LT_A_IN + c % T::STAGES), c / T::STAGES & 1, stop) && fine;
+            fine = kv_warp_wait(bars + 8 * (LT_A_IN + 2 * (c % T::STAGES) + 1), c / T::STAGES & 1, stop) && fine;
             const uint32_t present = ((volatile uint32_t*)M.present)[c & 7];
             fine = kv_warp_wait(bars + 8 * (LT_A_S + (c & 1)), c >> 1 & 1, stop) && fine;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            uint32_t x[32];
+            uint32_t x[16];
             const bool ragged = t0 + LT_TOKENS > see_all || present != 15u;
             float top[2] = {-KV_INF, -KV_INF};
             if (active) {
                 lt_tmem_load_quads(x, s_at + 64 * (c & 1));
                 if (ragged) {
                     const uint64_t there = lt_there(present, t0, q.len);
-                    uint32_t bad[2] = {0, 0};
-                    uint64_t sees[2];
+                    uint32_t bad = 0, sees[2];
 #pragma unroll
-                    for (int h = 0; h < 2; h++) sees[h] = j[h] < 0 ? 0ull : (lt_sees(A, q, j[h], t0) & there) >> (2 * quad);
+                    for (int h = 0; h < 2; h++) sees[h] = j[h] < 0 ? 0u : (uint32_t)((lt_sees(A, q, j[h], t0) & there) >> (32 * half)) >> (2 * quad);
 #pragma unroll
-                    for (int k = 0; k < 32; k++) {
+                    for (int k = 0; k < 16; k++) {
                         const int bit = 8 * (k >> 2) + (k & 1);              // and 2 quad on
-                        if (!(fabsf(__uint_as_float(x[k])) < KV_INF)) bad[bit >> 5] |= 1u << (bit & 31);
+                        if (!(fabsf(__uint_as_float(x[k])) < KV_INF)) bad |= 1u << bit;
                         x[k] = sees[k >> 1 & 1] >> bit & 1 ? x[k] : 0xff800000u;
                     }
-#pragma unroll
-                    for (int b = 0; b < 2; b++) {
-                        const uint32_t all = __reduce_or_sync(0xffffffffu, bad[b] << (2 * quad));
-                        if (lane == 0 && all) atomicOr(&M.bad[set][b], all);
-                    }
+                    bad = __reduce_or_sync(0xffffffffu, bad << (2 * quad));
+                    if (lane == 0 && bad) atomicOr(&M.bad[set][half], bad);
                 }
 #pragma unroll
-                for (int k = 0; k < 8; k++) {
+                for (int k = 0; k < 4; k++) {
                     top[0] = fmaxf(top[0], fmaxf(__uint_as_float(x[4 * k]), __uint_as_float(x[4 * k + 1])));
                     top[1] = fmaxf(top[1], fmaxf(__uint_as_float(x[4 * k + 2]), __uint_as_float(x[4 * k + 3])));
                 }
@@ -214,7 +216,7 @@ __device__ __forceinline__ void lt_attend_rows(const LtShape& S, const LtBatch& 
                 M.bad[(set + 1) % 3][0] = M.bad[(set + 1) % 3][1] = 0;
                 M.halt[c & 1] = *stop;
             }
-            const bool raise = lt_any(1, 128, top[0] * scale > m[0] + LT_RAISE || top[1] * scale > m[1] + LT_RAISE);
+            const bool raise = lt_any(1, LT_A_ROW_THREADS, top[0] * scale > m[0] + LT_RAISE || top[1] * scale > m[1] + LT_RAISE);
             halted = ((volatile int*)M.halt)[c & 1];
             const uint32_t p_free = kv_ended(bars + 8 * LT_A_O, c + 1 & 1);  // asked early, needed late
             if (raise) {
@@ -222,15 +224,20 @@ __device__ __forceinline__ void lt_attend_rows(const LtShape& S, const LtBatch& 
                 for (int h = 0; h < 2; h++) {
                     top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
                     top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2)) * scale;
-                    const float to = fmaxf(m[h], top[h]), fall = kv_exp2(m[h] - to);
+                    if (quad == 0) M.of_half[half][my_row + 8 * h] = top[h];
+                }
+                lt_sync(2, LT_A_ROW_THREADS);
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    const float to = fmaxf(fmaxf(m[h], top[h]), M.of_half[half ^ 1][my_row + 8 * h]), fall = kv_exp2(m[h] - to);
                     l[h] *= fall;
                     m[h] = to;
-                    if (quad == 0) M.factor[16 * warp + (lane >> 2) + 8 * h] = fall;
+                    if (quad == 0 && half == 0) M.factor[my_row + 8 * h] = fall;
                 }
             }
             if (active) {
 #pragma unroll
-                for (int k = 0; k < 8; k++)
+                for (int k = 0; k < 4; k++)
 #pragma unroll
                     for (int h = 0; h < 2; h++) {
                         const float a = kv_exp2(fmaf(__uint_as_float(x[4 * k + 2 * h]), scale, -m[h])), b = kv_exp2(fmaf(__uint_as_float(x[4 * k + 2 * h + 1]), scale, -m[h]));
@@ -239,11 +246,17 @@ __device__ __forceinline__ void lt_attend_rows(const LtShape& S, const LtBatch& 
                     }
             }
             // the product before is done: P is free, and O rests
-            if (!__all_sync(0xffffffffu, p_free)) fine = kv_warp_wait(bars + 8 * LT_A_O, c + 1 & 1, stop) && fine;
+            if (c > 0 && !__all_sync(0xffffffffu, p_free)) fine = kv_warp_wait(bars + 8 * LT_A_O, c + 1 & 1, stop) && fine;
+            if (active) {
+#pragma unroll
+                for (int k = 0; k < 4; k++)
+#pragma unroll
+                    for (int h = 0; h < 2; h++) *(uint32_t*)(p_sm + lt_at(my_row + 8 * h, 4 * half + k) + 4 * quad) = x[2 * k + h];
+            }
             if (raise && i > walk.from) {
-                lt_sync(2, 128);
+                lt_sync(2, LT_A_ROW_THREADS);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                for (int b = 0; b < PAIRS; b++)
+                for (int b = half; b < PAIRS; b += 2)
 #pragma unroll 1
                     for (int n = 0; n < rows; n += 32) {
                         uint32_t y[32];
@@ -254,13 +267,6 @@ __device__ __forceinline__ void lt_attend_rows(const LtShape& S, const LtBatch& 
                     }
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
             }
-            if (active) {
-#pragma unroll
-                for (int k = 0; k < 8; k++)
-#pragma unroll
-                    for (int h = 0; h < 2; h++)
-                        *(uint32_t*)(p_sm + lt_at(16 * warp + (lane >> 2) + 8 * h, k) + 4 * quad) = x[2 * k + h];
-            }
             if (ragged) {
                 // Tokens that are not there become zeros, and so does what is not finite in tokens that some rows do not see: a weight of 0
                 // times it would not be 0.  Such a token shows by its scores, of which every one is not finite: its values all enter them.
@@ -268,70 +274,77 @@ __device__ __forceinline__ void lt_attend_rows(const LtShape& S, const LtBatch& 
                 const uint64_t there = lt_there(present, t0, q.len);
                 const uint64_t some = see_all - t0 >= 64 ? 0ull : see_all <= t0 ? ~0ull : ~((1ull << (see_all - t0)) - 1);
                 uint64_t todo = ~there | (some & ((uint64_t)((volatile uint32_t*)M.bad[set])[1] << 32 | ((volatile uint32_t*)M.bad[set])[0]));
-                for (int n = threadIdx.x; todo; todo &= todo - 1) {
+                for (int n = threadIdx.x & 63, turn = threadIdx.x >> 6; todo; todo &= todo - 1, turn--) {
                     const int t = __ffsll((long long)todo) - 1;
-                    if (n < 8 * chunks) {
-                        uint4* const at = (uint4*)(tile + (n >> 3) * LT_TOKENS * LT_CHUNK_ROW + lt_at(t, n & 7));
-                        uint4 w = make_uint4(0, 0, 0, 0);
-                        if (there >> t & 1) {
-                            w = *at;
-                            w = make_uint4(lt_finite2<BF>(w.x), lt_finite2<BF>(w.y), lt_finite2<BF>(w.z), lt_finite2<BF>(w.w));
-                        }
-                        *at = w;
+                    if (turn & 3 || n >= 8 * chunks) continue;               // 64 threads take every fourth token
+                    uint4* const at = (uint4*)(tile + (n >> 3) * LT_TOKENS * LT_CHUNK_ROW + lt_at(t, n & 7));
+                    uint4 w = make_uint4(0, 0, 0, 0);
+                    if (there >> t & 1) {
+                        w = *at;
+                        w = make_uint4(lt_finite2<BF>(w.x), lt_finite2<BF>(w.y), lt_finite2<BF>(w.z), lt_finite2<BF>(w.w));
                     }
+                    *at = w;
                 }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             kv_warp_arrive(bars + 8 * LT_A_P);
         }
-        // the piece's end
-        fine = kv_warp_wait(bars + 8 * LT_A_O, c - 1 & 1, stop) && fine && !*stop;
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        // the piece's end: the halves' sums
         const int64_t slot = ((int64_t)2 * g + (walk.from == 0)) * A.group_tiles + r;
+        lt_sync(2, LT_A_ROW_THREADS);                    // the last tile's largest scores have been read
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
             l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+            if (quad == 0) M.of_half[half][my_row + 8 * h] = l[h];
+        }
+        fine = kv_warp_wait(bars + 8 * LT_A_O, c - 1 & 1, stop) && fine && !*stop;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        lt_sync(2, LT_A_ROW_THREADS);
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const int row = my_row + 8 * h;
+            l[h] += M.of_half[half ^ 1][row];
             if (!fine) l[h] = __int_as_float(0x7fffffff);
-            const int row = 16 * warp + (lane >> 2) + 8 * h;
-            if (quad == 0) {
+            if (quad == 0 && half == 0) {
                 M.factor[row] = l[h] == 0.f ? 0.f : 1.f / l[h];
                 if (row < rows) {
                     if (!whole) *(float2*)(A.part_ml + 2 * (slot * LT_ROWS + row)) = make_float2(m[h], l[h]);
-                    else if (A.lse) A.lse[(q.start + (int64_t)j[h]) * S.heads + (first + row) % S.heads] = l[h] == 0.f ? -KV_INF : (m[h] + log2f(l[h])) * 0.6931471805599453f;
+                    else if (A.lse) A.lse[(q.start + (int64_t)j[h]) * S.heads + ((uint32_t)(first + row) - j[h] * heads)] = l[h] == 0.f ? -KV_INF : (m[h] + log2f(l[h])) * 0.6931471805599453f;
                 }
             }
         }
-        lt_sync(2, 128);
-        for (int b = 0; b < PAIRS; b++) {
+        lt_sync(2, LT_A_ROW_THREADS);
+        for (int b = half; b < PAIRS; b += 2) {
             const int ch = 128 * b + 32 * warp + lane;
 #pragma unroll 1
             for (int n = 0; n < rows; n += 32) {
                 uint32_t y[32];
                 kv_tmem_load32(y, o_at + 64 * b + n);
                 if (whole) {
+                    const bool odd = lane & 1;
 #pragma unroll
                     for (int k = 0; k < 32; k += 2) {
                         // two lanes, two rows: each lane gets a pair of channels of one row
                         const float u = __uint_as_float(y[k]) * M.factor[n + k], w = __uint_as_float(y[k + 1]) * M.factor[n + k + 1];
-                        const bool odd = lane & 1;
                         const float got = __shfl_xor_sync(0xffffffffu, odd ? u : w, 1);
                         const int row = n + k + odd;
                         if (row < rows) *(uint32_t*)((uint16_t*)A.out.data + M.out_at[row] + (ch & ~1)) = odd ? kv_pack<BF>(got, w) : kv_pack<BF>(u, got);
                     }
                 } else {
+                    float* const to = A.part_o + (slot * LT_ROWS + n) * latent + ch;
 #pragma unroll
                     for (int k = 0; k < 32; k++)
-                        if (n + k < rows) A.part_o[(slot * LT_ROWS + n + k) * latent + ch] = __uint_as_float(y[k]);
+                        if (n + k < rows) to[k * latent] = __uint_as_float(y[k]);
                 }
             }
         }
-        lt_sync(2, 128);                                 // factor and out_at have been read
+        lt_sync(2, LT_A_ROW_THREADS);                    // factor, of_half and out_at have been read
     }
 }
 
-// Warp 4: the tiles.  It and warp 5 are one chain of instructions each, of which every one counts: no divisions, addresses known early.
+// Warp 8: the tiles.  It and warp 9 are one chain of instructions each, of which every one counts: no divisions, addresses known early.
 template <int PAIRS>
 __device__ __forceinline__ void lt_attend_bring(const LtShape& S, const LtBatch& B, const LtAttend& A, const CUtensorMap* map, const CUtensorMap* pairs_map, LtWalk walk,
                                                 uint32_t sm_at, LtMisc& M, uint32_t bars)
@@ -344,12 +357,12 @@ __device__ __forceinline__ void lt_attend_bring(const LtShape& S, const LtBatch&
     bool fine = true;
     int c = 0;                                           // tiles so far
     while (fine && walk.next(S, B, A)) {
-        if (((int64_t)walk.group * A.group_tiles + r) * LT_ROWS >= (int64_t)walk.q.n * S.heads) continue;
+        if ((walk.group * A.group_tiles + r) * LT_ROWS >= walk.q.n * S.heads) continue;
         int known = -1, pages = -1;                      // lane: page of the block known + lane
         for (int i = walk.from; i < walk.to && fine; i++) {
-            const uint32_t stage = c % T::STAGES, in = bars + 8 * (LT_A_IN + stage), to = sm_at + (1 + stage) * T::BYTES;
+            const uint32_t stage = c % T::STAGES, in = bars + 8 * (LT_A_IN + 2 * stage), out = bars + 8 * (LT_A_OUT + 2 * stage), phase = c / T::STAGES & 1, to = sm_at + (1 + stage) * T::BYTES;
             const int block = i * LT_TOKENS >> S.block_shift, y = i * LT_TOKENS & (S.block_tokens - 1);
-            if (known < 0 || block + 4 > known + 32) {
+            if (known < 0 || block + 4 + (LT_A_AHEAD * LT_TOKENS >> S.block_shift) > known + 32) {
                 known = block;
                 pages = (int64_t)(block + lane) << S.block_shift < walk.q.len ? lt_page(B, walk.seq, block + lane) : -1;
             }
@@ -365,31 +378,60 @@ __device__ __forceinline__ void lt_attend_bring(const LtShape& S, const LtBatch&
                     if (page[b] >= 0) present |= box_bits << (b << box_shift >> 4);
                 }
             }
-            fine = kv_warp_wait(bars + 8 * (LT_A_OUT + stage), (c / T::STAGES & 1) ^ 1, stop);
+            const uint32_t bytes = __popc(present) * 16 * LT_CHUNK_ROW;
+            fine = kv_warp_wait(out, phase ^ 1, stop);
             if (!fine) break;
-            if (lane == 0) ((volatile uint32_t*)M.present)[c & 7] = present;
-            __syncwarp();
-            lt_expect(in, __popc(present) * 16 * LT_CHUNK_ROW * T::CHUNKS);
+            const uint32_t second_out = kv_ended(out + 8, phase ^ 1);
+            lt_expect(in, bytes * 2 * T::FIRST);
             if (box_shift == 6) {
-                if (present) {
-                    lt_tma(to + 2 * PAIRS * LT_TOKENS * LT_CHUNK_ROW, map, 128 * PAIRS, y, page[0], in);
-                    lt_tma(to, pairs_map, 0, y, 0, page[0], in);
-                }
+                if (present)
+#pragma unroll
+                    for (int p = 0; p < T::FIRST; p++) lt_tma(to + p * LT_PART, pairs_map, 0, y, 2 * p, page[0], in);
             } else {
-#pragma unroll 1
-                for (int k = 0; k < T::CHUNKS; k++)
+#pragma unroll
+                for (int k = 0; k < 2 * T::FIRST; k++)
 #pragma unroll
                     for (int b = 0; b < 4; b++)
                         if (page[b] >= 0) lt_tma(to + (k * LT_TOKENS + (b << box_shift)) * LT_CHUNK_ROW, map, 64 * k, 0, page[b], in);
             }
+            if (!__all_sync(0xffffffffu, second_out)) fine = kv_warp_wait(out + 8, phase ^ 1, stop);
+            if (!fine) break;
+            if (lane == 0) ((volatile uint32_t*)M.present)[c & 7] = present;
+            __syncwarp();
+            lt_expect(in + 8, bytes * (T::CHUNKS - 2 * T::FIRST));
+            if (box_shift == 6) {
+                if (present) {
+#pragma unroll
+                    for (int p = T::FIRST; p < PAIRS; p++) lt_tma(to + p * LT_PART, pairs_map, 0, y, 2 * p, page[0], in + 8);
+                    lt_tma(to + PAIRS * LT_PART, map, 128 * PAIRS, y, page[0], in + 8);
+                }
+            } else {
+#pragma unroll
+                for (int k = 2 * T::FIRST; k < T::CHUNKS; k++)
+#pragma unroll
+                    for (int b = 0; b < 4; b++)
+                        if (page[b] >= 0) lt_tma(to + (k * LT_TOKENS + (b << box_shift)) * LT_CHUNK_ROW, map, 64 * k, 0, page[b], in + 8);
+            }
+            // Two stages do not hold what has to be on its way from memory: tiles further on are brought to L2.
+            for (int j = i + LT_A_AHEAD; i > walk.from && j <= i + LT_A_AHEAD && j < walk.to; j++)
+#pragma unroll 1
+                for (int b = 0; b << box_shift < LT_TOKENS; b++) {
+                    const int far = lt_uniform(pages, ((j * LT_TOKENS + (b << box_shift)) >> S.block_shift) - known);
+                    if (far >= 0)
+                        lt_prefetch(B.pool + ((int64_t)far * S.block_tokens + (j * LT_TOKENS + (b << box_shift) & (S.block_tokens - 1))) * S.row, (uint32_t)(2 * S.row) << box_shift);
+                }
             c++;
         }
     }
     // what is on its way arrives before the CTA ends
-    for (int back = 1; back <= T::STAGES && back <= c; back++) (void)kv_wait(bars + 8 * (LT_A_IN + (c - back) % T::STAGES), (c - back) / T::STAGES & 1);
+    for (int back = fine ? 1 : 0; back <= T::STAGES && back <= c; back++) {
+        const int tile = c - back;
+        // of a tile that was not finished, the first part may have been asked for; if not, the wait runs out, bounded
+        for (int part = 0; part < (back ? 2 : 1); part++) (void)kv_wait(bars + 8 * (LT_A_IN + 2 * (tile % T::STAGES) + part), tile / T::STAGES & 1);
+    }
 }
 
-// Warp 5: the products
+// Warp 9: the products
 template <int PAIRS, bool BF>
 __device__ __forceinline__ void lt_attend_products(const LtShape& S, const LtBatch& B, const LtAttend& A, LtWalk walk, uint32_t sm_at, LtMisc& M, uint32_t bars, uint32_t tmem)
 {
@@ -405,20 +447,27 @@ __device__ __forceinline__ void lt_attend_products(const LtShape& S, const LtBat
     auto scores = [&](int c) {
         const uint32_t stage = c % T::STAGES, s_at = tmem + 256 + 64 * (c & 1);
         const uint64_t k = k_desc + stage * (T::BYTES >> 4);
-        fine = kv_warp_wait(bars + 8 * (LT_A_IN + stage), c / T::STAGES & 1, stop);
+        const uint32_t in = bars + 8 * (LT_A_IN + 2 * stage), phase = c / T::STAGES & 1;
+        fine = kv_warp_wait(in, phase, stop);
+        if (!fine) return;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t second = kv_ended(in + 8, phase);
+#pragma unroll
+        for (int n = 0; n < 2 * T::FIRST; n++) lt_mma_ss<4, 2, 2>(s_at, q_desc + n * CHUNK, k + n * CHUNK, s_what, n > 0);
+        if (!__all_sync(0xffffffffu, second)) fine = kv_warp_wait(in + 8, phase, stop);
         if (!fine) return;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-        for (int n = 0; n < 2 * PAIRS; n++) lt_mma_ss<4, 2, 2>(s_at, q_desc + n * CHUNK, k + n * CHUNK, s_what, n > 0);
+        for (int n = 2 * T::FIRST; n < 2 * PAIRS; n++) lt_mma_ss<4, 2, 2>(s_at, q_desc + n * CHUNK, k + n * CHUNK, s_what, n > 0);
         lt_mma_ss<2, 2, 2>(s_at, q_desc + 2 * PAIRS * CHUNK, k + 2 * PAIRS * CHUNK, s_what, true);
         if (S.rope == 64) lt_mma_ss<2, 2, 2>(s_at, q_desc + 2 * PAIRS * CHUNK + 4, k + 2 * PAIRS * CHUNK + 4, s_what, true);
         kv_commit(bars + 8 * (LT_A_S + (c & 1)));
     };
     int c = 0, piece = 0;
     while (fine && walk.next(S, B, A)) {
-        const int64_t left = (int64_t)walk.q.n * S.heads - ((int64_t)walk.group * A.group_tiles + r) * LT_ROWS;
+        const int left = walk.q.n * S.heads - (walk.group * A.group_tiles + r) * LT_ROWS;
         if (left <= 0) continue;
-        const uint32_t n = (uint32_t)(min(left, (int64_t)LT_ROWS) + 15) / 16 * 16;
+        const uint32_t n = (uint32_t)(min(left, LT_ROWS) + 15) / 16 * 16;
         const uint32_t o_what = kind | 8u << 24 | n / 8 << 17 | 1u << 15;                    // A's M runs along the row
         fine = kv_warp_wait(bars + 8 * LT_A_Q, piece & 1, stop);
         if (fine) scores(c);
@@ -426,13 +475,13 @@ __device__ __forceinline__ void lt_attend_products(const LtShape& S, const LtBat
             // The next tile's scores first, if it is there before this one's weights are: where memory is the bound it is not, and this one's
             // answers must not wait for it (they free the place that the tile after it comes to).
             bool next = i + 1 < walk.to;
-            const uint32_t next_in = bars + 8 * (LT_A_IN + (c + 1) % T::STAGES);
+            const uint32_t next_in = bars + 8 * (LT_A_IN + 2 * ((c + 1) % T::STAGES));
             for (int turn = 0; next && fine && turn < 1 << 18; turn++) {
-                if (__all_sync(0xffffffffu, kv_ended(next_in, (c + 1) / T::STAGES & 1))) {
+                const uint32_t data = kv_ended(next_in, (c + 1) / T::STAGES & 1), weights = kv_ended(bars + 8 * LT_A_P, c & 1), end = *stop;
+                if (__any_sync(0xffffffffu, weights | end)) break;
+                if (__all_sync(0xffffffffu, data)) {
                     scores(c + 1);
                     next = false;
-                } else if (__all_sync(0xffffffffu, kv_ended(bars + 8 * LT_A_P, c & 1)) || *stop) {
-                    break;
                 }
             }
             if (fine) fine = kv_warp_wait(bars + 8 * LT_A_P, c & 1, stop);
@@ -442,8 +491,12 @@ __device__ __forceinline__ void lt_attend_products(const LtShape& S, const LtBat
             const uint64_t v = v_desc + stage * (T::BYTES >> 4);
             const bool add = i > walk.from;
 #pragma unroll
-            for (int p = 0; p < PAIRS; p++) lt_mma_ss<4, 2048 / 16, 2>(tmem + 64 * p, v + p * (LT_PART >> 4), p_desc, o_what, add);
-            kv_commit(bars + 8 * (LT_A_OUT + stage));
+            for (int p = 0; p < PAIRS; p++) {
+                lt_mma_ss<4, 2048 / 16, 2>(tmem + 64 * p, v + p * (LT_PART >> 4), p_desc, o_what, add);
+                if (p + 1 == T::FIRST && PAIRS > 1) kv_commit(bars + 8 * (LT_A_OUT + 2 * stage));
+            }
+            if (PAIRS == 1) kv_commit(bars + 8 * (LT_A_OUT + 2 * stage));
+            kv_commit(bars + 8 * (LT_A_OUT + 2 * stage + 1));
             kv_commit(bars + 8 * LT_A_O);
             if (next) scores(c + 1);
         }
@@ -463,34 +516,42 @@ __global__ void __launch_bounds__(LT_A_THREADS, 1) lt_attend_kernel(const LtShap
     const uint32_t bars = (uint32_t)__cvta_generic_to_shared(M.bars);
     asm volatile("griddepcontrol.launch_dependents;");
     if (threadIdx.x == 0) {
-        for (int i = 0; i < LT_A_BARS; i++) lt_init(bars + 8 * i, i == LT_A_P || i == LT_A_Q ? 4 : 1);
+        for (int i = 0; i < LT_A_BARS; i++) lt_init(bars + 8 * i, i == LT_A_P || i == LT_A_Q ? LT_A_ROW_THREADS / 32 : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         M.stop = 0;
         for (int i = 0; i < 3; i++) M.bad[i][0] = M.bad[i][1] = 0;
     }
-    if (warp == 5) asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"((uint32_t)__cvta_generic_to_shared(&M.tmem)) : "memory");
+    if (warp == 9) asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"((uint32_t)__cvta_generic_to_shared(&M.tmem)) : "memory");
 
     // the line's length, and where this run begins
-    auto tiles_of = [&](int64_t item) { return lt_item_tiles(S, A, lt_seq(B, (int)(item / A.seq_groups)), (int)(item % A.seq_groups)); };
+    auto tiles_of = [&](int64_t item) {
+        const int seq = A.seq_groups == 1 ? (int)item : (int)(item / A.seq_groups);
+        return lt_item_tiles(S, A, lt_seq(B, seq), (int)(item - (int64_t)seq * A.seq_groups));
+    };
     LtStretch mine = lt_stretch<LT_A_THREADS>((int64_t)B.n_seqs * A.seq_groups, tiles_of, M.warp_sum);
     const int64_t share = max((mine.total + A.groups - 1) / A.groups, (int64_t)A.least);
-    LtWalk walk;
-    walk.at = blockIdx.x / A.group_tiles * share;
-    walk.end = min(walk.at + share, mine.total);
-    if (mine.holds(walk.at)) {
-        mine.find(walk.at, tiles_of);
-        M.item = mine.item;
-        M.item_at = mine.before;
+    const int64_t begin = blockIdx.x / A.group_tiles * share;
+    if (mine.holds(begin)) {
+        mine.find(begin, tiles_of);
+        LtWalk w;
+        w.item_at = mine.before;
+        w.at = begin;
+        w.end = min(begin + share, mine.total);
+        w.seq = (int)(mine.item / A.seq_groups);
+        w.group = (int)(mine.item % A.seq_groups);
+        w.q = lt_seq(B, w.seq);
+        w.tiles = lt_item_tiles(S, A, w.q, w.group);
+        M.walk = w;
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    walk.item = M.item;
-    walk.item_at = M.item_at;
+    LtWalk walk = M.walk;
+    if (begin >= mine.total) walk.at = walk.end = 0;     // nothing to do
     const uint32_t tmem = *(volatile uint32_t*)&M.tmem;  // O: 64 columns per 128 channels; S: 2 x 64 from 256 on
-    if (warp < 4) {
+    if (warp < 8) {
         lt_attend_rows<PAIRS, BF>(S, B, A, walk, share, sm, sm_at, M, bars, tmem);
-    } else if (warp == 4) {
+    } else if (warp == 8) {
         lt_attend_bring<PAIRS>(S, B, A, &map, &pairs_map, walk, sm_at, M, bars);
     } else {
         lt_attend_products<PAIRS, BF>(S, B, A, walk, sm_at, M, bars, tmem);
@@ -501,7 +562,7 @@ __global__ void __launch_bounds__(LT_A_THREADS, 1) lt_attend_kernel(const LtShap
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    if (warp == 5) {
+    if (warp == 9) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
@@ -534,33 +595,38 @@ template <bool BF> __global__ void __launch_bounds__(LT_JOIN_THREADS) lt_join_ke
         if (lane == 0) cut_count = n;
     }
     __syncthreads();
-    const int64_t work = (int64_t)cut_count * rows_of * pairs, step = (int64_t)gridDim.x * (LT_JOIN_THREADS / 32);
-    for (int64_t w = (int64_t)blockIdx.x * (LT_JOIN_THREADS / 32) + (threadIdx.x >> 5); w < work; w += step) {
-        const int g = cut_runs[w / (rows_of * pairs)], at = (int)(w % (rows_of * pairs)), i = at / pairs, ch = at % pairs * 128 + 4 * lane;
+    const int of_cut = rows_of * pairs, work = cut_count * of_cut, step = gridDim.x * (LT_JOIN_THREADS / 32);
+    for (int w = blockIdx.x * (LT_JOIN_THREADS / 32) + (threadIdx.x >> 5); w < work; w += step) {
+        const int g = cut_runs[w / of_cut], at = w % of_cut, i = at / pairs, ch = at % pairs * 128 + 4 * lane;
         const int4 cut = *(const int4*)(A.cuts + 4 * g);
-        const LtSeq q = lt_seq(B, cut.x);
-        const int64_t row = (int64_t)cut.y * rows_of + i;
-        if (row >= (int64_t)q.n * S.heads) continue;
-        auto slot = [&](int s) { return ((s == 0 ? (int64_t)2 * g + 1 : (int64_t)2 * (g + s)) * A.group_tiles + i / LT_ROWS) * LT_ROWS + i % LT_ROWS; };
+        const int row = cut.y + i;
+        const int64_t first_slot = (((int64_t)2 * g + 1) * A.group_tiles + i / LT_ROWS) * LT_ROWS + i % LT_ROWS, next_slot = first_slot + A.group_tiles * LT_ROWS,
+                      slot_step = (int64_t)2 * A.group_tiles * LT_ROWS;      // pieces: the last of this run, the first of the next runs
+        auto slot = [&](int s) { return s == 0 ? first_slot : next_slot + (s - 1) * slot_step; };
+        if (row >= cut.w) continue;
         float m = KV_M_NONE, l = 0.f;
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int s0 = 0; s0 < cut.z; s0 += 32) {
             const float2 ml = s0 + lane < cut.z ? *(const float2*)(A.part_ml + 2 * slot(s0 + lane)) : make_float2(KV_M_NONE, 0.f);
-            float top = ml.x;
-#pragma unroll
-            for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-            top = fmaxf(top, m);
-            const float fall = kv_exp2(m - top), weight = kv_exp2(ml.x - top);
-            m = top;
-            float part = ml.y * weight;
-#pragma unroll
-            for (int d = 16; d; d >>= 1) part += __shfl_xor_sync(0xffffffffu, part, d);
-            l = l * fall + part;
-            sum = make_float4(sum.x * fall, sum.y * fall, sum.z * fall, sum.w * fall);
+            float weight = 0.f;
             for (int s = 0; s < 32 && s0 + s < cut.z; s += 8) {
                 float4 o[8];
 #pragma unroll
                 for (int k = 0; k < 8; k++) o[k] = s0 + s + k < cut.z ? *(const float4*)(A.part_o + slot(s0 + s + k) * S.latent + ch) : make_float4(0.f, 0.f, 0.f, 0.f);
+                if (s == 0) {
+                    float top = ml.x;
+#pragma unroll
+                    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                    top = fmaxf(top, m);
+                    const float fall = kv_exp2(m - top);
+                    m = top;
+                    weight = kv_exp2(ml.x - top);
+                    float part = ml.y * weight;
+#pragma unroll
+                    for (int d = 16; d; d >>= 1) part += __shfl_xor_sync(0xffffffffu, part, d);
+                    l = l * fall + part;
+                    sum = make_float4(sum.x * fall, sum.y * fall, sum.z * fall, sum.w * fall);
+                }
 #pragma unroll
                 for (int k = 0; k < 8; k++) {
                     const float by = __shfl_sync(0xffffffffu, weight, s + k);
@@ -569,8 +635,8 @@ template <bool BF> __global__ void __launch_bounds__(LT_JOIN_THREADS) lt_join_ke
             }
         }
         const float by = l == 0.f ? 0.f : 1.f / l;
-        const int64_t token = q.start + row / S.heads;
-        const int head = (int)(row % S.heads);
+        const int j = (int)((uint32_t)row / (uint32_t)S.heads), head = row - j * S.heads;
+        const int64_t token = cut.x + (int64_t)j;
         *(uint2*)((uint16_t*)A.out.data + token * A.out.token_stride + head * A.out.head_stride + ch) = make_uint2(kv_pack<BF>(sum.x * by, sum.y * by), kv_pack<BF>(sum.z * by, sum.w * by));
         if (ch == 0 && A.lse) A.lse[token * S.heads + head] = l == 0.f ? -KV_INF : (m + log2f(l)) * 0.6931471805599453f;
     }

@@ -69,6 +69,11 @@ __device__ __forceinline__ void lt_tma(uint32_t smem, const CUtensorMap* map, in
                  "@e cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}"
                  ::"r"(smem), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
 }
+// Asks for memory to come to L2
+__device__ __forceinline__ void lt_prefetch(const void* at, uint32_t bytes)
+{
+    asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t@e cp.async.bulk.prefetch.L2.global [%0], %1;\n\t}" ::"l"(at), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void lt_expect(uint32_t bar, uint32_t bytes)      // and arrive
 {
     asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t@e mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar), "r"(bytes) : "memory");
@@ -119,13 +124,13 @@ template <bool BF> __device__ __forceinline__ uint32_t lt_finite2(uint32_t w)
     return w;
 }
 
-// S of 64 rows (tensor memory, 16 lanes of each warp's 32): lane l of the warp gets of its 16 rows the rows l / 4 and l / 4 + 8, and of every 8 columns
-// the columns 2 (l % 4) and the next: x[4 k], x[4 k + 1] of the first row and x[4 k + 2], x[4 k + 3] of the second, columns 8 k on.
-__device__ __forceinline__ void lt_tmem_load_quads(uint32_t (&x)[32], uint32_t at)
+// S of 64 rows (tensor memory, 16 lanes of each warp's 32), 32 columns: lane l of the warp gets of its 16 rows the rows l / 4 and l / 4 + 8, and of every
+// 8 columns the columns 2 (l % 4) and the next: x[4 k], x[4 k + 1] of the first row and x[4 k + 2], x[4 k + 3] of the second, columns 8 k on.
+__device__ __forceinline__ void lt_tmem_load_quads(uint32_t (&x)[16], uint32_t at)
 {
-    asm volatile("tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\t"
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
                  "tcgen05.wait::ld.sync.aligned;"
-                 : KV_R8(x, 0), KV_R8(x, 8), KV_R8(x, 16), KV_R8(x, 24) : "r"(at) : "memory");
+                 : KV_R8(x, 0), KV_R8(x, 8) : "r"(at) : "memory");
 }
 
 // A line of work: items one behind the other, `size(item)` units each.  Every thread of a CTA adds up a stretch of items, and the one in whose

@@ -15,7 +15,8 @@
 // out of L2).  What a run cuts is joined by a kernel of its own; a run has at most two such pieces, its first and its last.
 #define LT_ROWS 64
 #define LT_TOKENS 64
-#define LT_A_THREADS 320
+#define LT_A_THREADS 384
+#define LT_A_BRINGERS 3                 // warps that bring tiles of small blocks
 #define LT_A_STAGES 4                   // at most
 // PAIRS: of 64 channels of the latent
 template <int PAIRS> struct LtTile {
@@ -345,8 +346,10 @@ __device__ __forceinline__ void lt_attend_rows(const LtShape& S, const LtBatch& 
 }
 
 // Warp 8: the tiles.  It and warp 9 are one chain of instructions each, of which every one counts: no divisions, addresses known early.
+// A copy takes some 120 cycles to issue.  Blocks of less than 64 tokens need one for every block and 64 channels; these warps 8, 10 and 11 share
+// (`turn` 0, 1, 2), and each arrives for its own.
 template <int PAIRS>
-__device__ __forceinline__ void lt_attend_bring(const LtShape& S, const LtBatch& B, const LtAttend& A, const CUtensorMap* map, const CUtensorMap* pairs_map, LtWalk walk,
+__device__ __forceinline__ void lt_attend_bring(const LtShape& S, const LtBatch& B, const LtAttend& A, const CUtensorMap* map, const CUtensorMap* pairs_map, LtWalk walk, int turn,
                                                 uint32_t sm_at, LtMisc& M, uint32_t bars)
 {
     using T = LtTile<PAIRS>;
@@ -379,41 +382,41 @@ __device__ __forceinline__ void lt_attend_bring(const LtShape& S, const LtBatch&
                 }
             }
             const uint32_t bytes = __popc(present) * 16 * LT_CHUNK_ROW;
+            // chunks from .. upto - 1 of the tile's small blocks that are this warp's, and their bytes
+            auto small = [&](int from, int upto, uint32_t bar) {
+                lt_expect(bar, bytes * ((upto - from + LT_A_BRINGERS - 1 - turn) / LT_A_BRINGERS));
+                for (int k = from + turn; k < upto; k += LT_A_BRINGERS)
+#pragma unroll
+                    for (int b = 0; b < 4; b++)
+                        if (page[b] >= 0) lt_tma(to + (k * LT_TOKENS + (b << box_shift)) * LT_CHUNK_ROW, map, 64 * k, 0, page[b], bar);
+            };
             fine = kv_warp_wait(out, phase ^ 1, stop);
             if (!fine) break;
             const uint32_t second_out = kv_ended(out + 8, phase ^ 1);
-            lt_expect(in, bytes * 2 * T::FIRST);
             if (box_shift == 6) {
+                lt_expect(in, bytes * 2 * T::FIRST);
                 if (present)
 #pragma unroll
                     for (int p = 0; p < T::FIRST; p++) lt_tma(to + p * LT_PART, pairs_map, 0, y, 2 * p, page[0], in);
             } else {
-#pragma unroll
-                for (int k = 0; k < 2 * T::FIRST; k++)
-#pragma unroll
-                    for (int b = 0; b < 4; b++)
-                        if (page[b] >= 0) lt_tma(to + (k * LT_TOKENS + (b << box_shift)) * LT_CHUNK_ROW, map, 64 * k, 0, page[b], in);
+                small(0, 2 * T::FIRST, in);
             }
             if (!__all_sync(0xffffffffu, second_out)) fine = kv_warp_wait(out + 8, phase ^ 1, stop);
             if (!fine) break;
-            if (lane == 0) ((volatile uint32_t*)M.present)[c & 7] = present;
+            if (lane == 0 && turn == 0) ((volatile uint32_t*)M.present)[c & 7] = present;
             __syncwarp();
-            lt_expect(in + 8, bytes * (T::CHUNKS - 2 * T::FIRST));
             if (box_shift == 6) {
+                lt_expect(in + 8, bytes * (T::CHUNKS - 2 * T::FIRST));
                 if (present) {
 #pragma unroll
                     for (int p = T::FIRST; p < PAIRS; p++) lt_tma(to + p * LT_PART, pairs_map, 0, y, 2 * p, page[0], in + 8);
                     lt_tma(to + PAIRS * LT_PART, map, 128 * PAIRS, y, page[0], in + 8);
                 }
             } else {
-#pragma unroll
-                for (int k = 2 * T::FIRST; k < T::CHUNKS; k++)
-#pragma unroll
-                    for (int b = 0; b < 4; b++)
-                        if (page[b] >= 0) lt_tma(to + (k * LT_TOKENS + (b << box_shift)) * LT_CHUNK_ROW, map, 64 * k, 0, page[b], in + 8);
+                small(2 * T::FIRST, T::CHUNKS, in + 8);
             }
             // Two stages do not hold what has to be on its way from memory: tiles further on are brought to L2.
-            for (int j = i + LT_A_AHEAD; i > walk.from && j <= i + LT_A_AHEAD && j < walk.to; j++)
+            if (const int j = i + LT_A_AHEAD; turn == 0 && i > walk.from && j < walk.to)
 #pragma unroll 1
                 for (int b = 0; b << box_shift < LT_TOKENS; b++) {
                     const int far = lt_uniform(pages, ((j * LT_TOKENS + (b << box_shift)) >> S.block_shift) - known);
@@ -426,8 +429,8 @@ __device__ __forceinline__ void lt_attend_bring(const LtShape& S, const LtBatch&
     // what is on its way arrives before the CTA ends
     for (int back = fine ? 1 : 0; back <= T::STAGES && back <= c; back++) {
         const int tile = c - back;
-        // of a tile that was not finished, the first part may have been asked for; if not, the wait runs out, bounded
-        for (int part = 0; part < (back ? 2 : 1); part++) (void)kv_wait(bars + 8 * (LT_A_IN + 2 * (tile % T::STAGES) + part), tile / T::STAGES & 1);
+        // of a tile that was not finished, parts may have been asked for; if not, the wait runs out, bounded
+        for (int part = 0; part < 2; part++) (void)kv_wait(bars + 8 * (LT_A_IN + 2 * (tile % T::STAGES) + part), tile / T::STAGES & 1);
     }
 }
 
@@ -444,11 +447,11 @@ __device__ __forceinline__ void lt_attend_products(const LtShape& S, const LtBat
     const uint64_t q_desc = kv_desc(sm_at, 16, 1024), k_desc = kv_desc(sm_at + T::BYTES, 16, 1024), v_desc = kv_desc(sm_at + T::BYTES, LT_TOKENS * LT_CHUNK_ROW, 1024),
                    p_desc = kv_desc(sm_at + T::P, 16, 1024);
     bool fine = true;
-    auto scores = [&](int c) {
+    auto scores = [&](int c, bool there) {               // there: the first part is known to be
         const uint32_t stage = c % T::STAGES, s_at = tmem + 256 + 64 * (c & 1);
         const uint64_t k = k_desc + stage * (T::BYTES >> 4);
         const uint32_t in = bars + 8 * (LT_A_IN + 2 * stage), phase = c / T::STAGES & 1;
-        fine = kv_warp_wait(in, phase, stop);
+        if (!there) fine = kv_warp_wait(in, phase, stop);
         if (!fine) return;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t second = kv_ended(in + 8, phase);
@@ -470,21 +473,22 @@ __device__ __forceinline__ void lt_attend_products(const LtShape& S, const LtBat
         const uint32_t n = (uint32_t)(min(left, LT_ROWS) + 15) / 16 * 16;
         const uint32_t o_what = kind | 8u << 24 | n / 8 << 17 | 1u << 15;                    // A's M runs along the row
         fine = kv_warp_wait(bars + 8 * LT_A_Q, piece & 1, stop);
-        if (fine) scores(c);
+        if (fine) scores(c, false);
         for (int i = walk.from; i < walk.to && fine; i++, c++) {
             // The next tile's scores first, if it is there before this one's weights are: where memory is the bound it is not, and this one's
             // answers must not wait for it (they free the place that the tile after it comes to).
-            bool next = i + 1 < walk.to;
+            bool next = i + 1 < walk.to, made = false;
             const uint32_t next_in = bars + 8 * (LT_A_IN + 2 * ((c + 1) % T::STAGES));
             for (int turn = 0; next && fine && turn < 1 << 18; turn++) {
                 const uint32_t data = kv_ended(next_in, (c + 1) / T::STAGES & 1), weights = kv_ended(bars + 8 * LT_A_P, c & 1), end = *stop;
-                if (__any_sync(0xffffffffu, weights | end)) break;
+                made = __all_sync(0xffffffffu, weights);
+                if (made || __any_sync(0xffffffffu, end)) break;
                 if (__all_sync(0xffffffffu, data)) {
-                    scores(c + 1);
+                    scores(c + 1, true);
                     next = false;
                 }
             }
-            if (fine) fine = kv_warp_wait(bars + 8 * LT_A_P, c & 1, stop);
+            if (fine && !made) fine = kv_warp_wait(bars + 8 * LT_A_P, c & 1, stop);
             if (!fine) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t stage = c % T::STAGES;
@@ -498,7 +502,7 @@ __device__ __forceinline__ void lt_attend_products(const LtShape& S, const LtBat
             if (PAIRS == 1) kv_commit(bars + 8 * (LT_A_OUT + 2 * stage));
             kv_commit(bars + 8 * (LT_A_OUT + 2 * stage + 1));
             kv_commit(bars + 8 * LT_A_O);
-            if (next) scores(c + 1);
+            if (next) scores(c + 1, false);
         }
         piece++;
     }
@@ -516,7 +520,7 @@ __global__ void __launch_bounds__(LT_A_THREADS, 1) lt_attend_kernel(const LtShap
     const uint32_t bars = (uint32_t)__cvta_generic_to_shared(M.bars);
     asm volatile("griddepcontrol.launch_dependents;");
     if (threadIdx.x == 0) {
-        for (int i = 0; i < LT_A_BARS; i++) lt_init(bars + 8 * i, i == LT_A_P || i == LT_A_Q ? LT_A_ROW_THREADS / 32 : 1);
+        for (int i = 0; i < LT_A_BARS; i++) lt_init(bars + 8 * i, i == LT_A_P || i == LT_A_Q ? LT_A_ROW_THREADS / 32 : i < LT_A_OUT && S.block_tokens < LT_TOKENS ? LT_A_BRINGERS : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         M.stop = 0;
         for (int i = 0; i < 3; i++) M.bad[i][0] = M.bad[i][1] = 0;
@@ -551,8 +555,8 @@ __global__ void __launch_bounds__(LT_A_THREADS, 1) lt_attend_kernel(const LtShap
     const uint32_t tmem = *(volatile uint32_t*)&M.tmem;  // O: 64 columns per 128 channels; S: 2 x 64 from 256 on
     if (warp < 8) {
         lt_attend_rows<PAIRS, BF>(S, B, A, walk, share, sm, sm_at, M, bars, tmem);
-    } else if (warp == 8) {
-        lt_attend_bring<PAIRS>(S, B, A, &map, &pairs_map, walk, sm_at, M, bars);
+    } else if (warp != 9) {
+        if (warp == 8 || S.block_tokens < LT_TOKENS) lt_attend_bring<PAIRS>(S, B, A, &map, &pairs_map, walk, warp == 8 ? 0 : warp - 9, sm_at, M, bars);
     } else {
         lt_attend_products<PAIRS, BF>(S, B, A, walk, sm_at, M, bars, tmem);
         __syncwarp();

@@ -98,7 +98,8 @@ __device__ __forceinline__ void lt_expand_bring(const LtShape& S, const LtBatch&
 {
     const int lane = threadIdx.x & 31, chunks = S.latent / 64, box = min(S.block_tokens, 64);
     const uint32_t weights_at = sm_at + chunks * LT_E_CHUNK;
-    int c = 0, pieces = 0;                               // chunks of weights, pieces of latents
+    int c = 0, pieces = 0, s = 0;                        // chunks of weights, pieces of latents; the next chunk's stage
+    uint32_t phase = 0, free = 0;                        // free: whether the stage is known to be
     bool fine = true;
     while (fine && walk.next(B, A)) {
         // lane: a box of the tile's tokens
@@ -118,11 +119,14 @@ __device__ __forceinline__ void lt_expand_bring(const LtShape& S, const LtBatch&
         for (int u = walk.from; u < walk.to && fine; u++) {
             const int width = u & 1 ? S.value : S.key;
             for (int k = 0; k < chunks; k++, c++) {
-                const int s = c % LT_E_STAGES;
-                fine = kv_warp_wait(bars + 8 * (LT_E_B_OUT + s), (c / LT_E_STAGES & 1) ^ 1, stop);
+                if (!__all_sync(0xffffffffu, free)) fine = kv_warp_wait(bars + 8 * (LT_E_B_OUT + s), phase ^ 1, stop);
                 if (!fine) break;
-                lt_expect(bars + 8 * (LT_E_B_IN + s), width * LT_CHUNK_ROW);
-                lt_tma(weights_at + s * LT_E_CHUNK, u & 1 ? v_weights : k_weights, 64 * k, 0, u >> 1, bars + 8 * (LT_E_B_IN + s));
+                const int now = s;
+                s = s == LT_E_STAGES - 1 ? 0 : s + 1;
+                phase ^= s == 0;
+                free = kv_ended(bars + 8 * (LT_E_B_OUT + s), phase ^ 1);
+                lt_expect(bars + 8 * (LT_E_B_IN + now), width * LT_CHUNK_ROW);
+                lt_tma(weights_at + now * LT_E_CHUNK, u & 1 ? v_weights : k_weights, 64 * k, 0, u >> 1, bars + 8 * (LT_E_B_IN + now));
             }
         }
     }
@@ -137,19 +141,25 @@ __device__ __forceinline__ void lt_expand_products(const LtShape& S, const LtBat
 {
     const int chunks = S.latent / 64;
     constexpr uint32_t kind = 1u << 4 | (BF ? 1u << 7 | 1u << 10 : 0u) | 8u << 24;
-    int c = 0, units = 0, pieces = 0;
+    // A barrier's answer takes some 270 cycles while the tensor cores read: it is asked a chunk ahead.
+    int s = 0, units = 0, pieces = 0;                    // s: the chunk's stage
+    uint32_t phase = 0, there = 0;                       // there: whether this chunk is known to be
+    const uint64_t a0 = kv_desc(sm_at, 16, 1024), b0 = kv_desc(sm_at + chunks * LT_E_CHUNK, 16, 1024);
     while (walk.next(B, A)) {
         if (!kv_warp_wait(bars + 8 * LT_E_A_IN, pieces++ & 1, stop)) return;
         for (int u = walk.from; u < walk.to; u++, units++) {
-            const uint32_t what = kind | (uint32_t)(u & 1 ? S.value : S.key) / 8 << 17;
+            const uint32_t what = kind | (uint32_t)(u & 1 ? S.value : S.key) / 8 << 17, d = tmem + 128 * (units & 1);
             if (!kv_warp_wait(bars + 8 * (LT_E_D_OUT + (units & 1)), (units >> 1 & 1) ^ 1, stop)) return;
-            for (int k = 0; k < chunks; k++, c++) {
-                const int s = c % LT_E_STAGES;
-                if (!kv_warp_wait(bars + 8 * (LT_E_B_IN + s), c / LT_E_STAGES & 1, stop)) return;
+#pragma unroll 1
+            for (int k = 0; k < chunks; k++) {
+                if (!__all_sync(0xffffffffu, there) && !kv_warp_wait(bars + 8 * (LT_E_B_IN + s), phase, stop)) return;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint64_t a = kv_desc(sm_at + k * LT_E_CHUNK, 16, 1024), b = kv_desc(sm_at + (chunks + s) * LT_E_CHUNK, 16, 1024);
-                lt_mma_ss<4, 2, 2>(tmem + 128 * (units & 1), a, b, what, k > 0);
-                kv_commit(bars + 8 * (LT_E_B_OUT + s));
+                const int now = s;
+                s = s == LT_E_STAGES - 1 ? 0 : s + 1;
+                phase ^= s == 0;
+                there = kv_ended(bars + 8 * (LT_E_B_IN + s), phase);
+                lt_mma_ss<4, 2, 2>(d, a0 + k * (LT_E_CHUNK >> 4), b0 + now * (LT_E_CHUNK >> 4), what, k > 0);
+                kv_commit(bars + 8 * (LT_E_B_OUT + now));
             }
             kv_commit(bars + 8 * (LT_E_D_IN + (units & 1)));
         }

@@ -455,14 +455,14 @@ extern "C" int fastrack_latent_expand(fastrack_latent* lt, const fastrack_latent
     if (int rc = lt_check_device(lt)) return rc;
     const LtShape& S = lt->shape;
     const LtBatch B = lt_batch(batch);
-    const LtExpand A = {lt_rows(k_out), lt_rows(v_out), d_key_starts, total_keys, 2 * S.heads};
-    CUtensorMap pool, k_weights, v_weights;
-    const int64_t row = (int64_t)2 * S.latent, head = row * (S.key + S.value);
+    const LtExpand A = {lt_rows(k_out), lt_rows(v_out), d_key_starts, total_keys, S.heads};
+    CUtensorMap pool, weights;
+    const int64_t row = (int64_t)2 * S.latent;
+    const int width = S.key + S.value;
     if (int rc = lt_pool_map(lt, B, &pool)) return rc;
-    if (int rc = lt_map(lt, &k_weights, const_cast<void*>(d_weights), S.latent, S.key, S.heads, row, head, S.key)) return rc;
-    if (int rc = lt_map(lt, &v_weights, (char*)const_cast<void*>(d_weights) + row * S.key, S.latent, S.value, S.heads, row, head, S.value)) return rc;
+    if (int rc = lt_map(lt, &weights, const_cast<void*>(d_weights), S.latent, width, S.heads, row, row * width, width / 2)) return rc;
     auto kernel = lt->config.dtype == FASTRACK_KV_BF16 ? lt_expand_kernel<true> : lt_expand_kernel<false>;
-    kernel<<<lt->num_sms, LT_E_THREADS, lt_expand_smem(S.latent), (cudaStream_t)stream>>>(S, B, A, pool, k_weights, v_weights);
+    kernel<<<lt->num_sms / 2 * 2, LT_E_THREADS, lt_expand_smem(S.latent), (cudaStream_t)stream>>>(S, B, A, pool, weights);
     return lt_launched(lt);
 }
 

@@ -124,6 +124,61 @@ template <bool BF> __device__ __forceinline__ uint32_t lt_finite2(uint32_t w)
     return w;
 }
 
+// Two CTAs of a cluster whose SMs work on one product (cta_group::2): each has its own half of A's rows, of B's columns and of D's rows.  The first of
+// the pair issues; barriers that it waits for are its own, and what both wait for is told to both.  (No copy is multicast: each brings its half.)
+__device__ __forceinline__ uint32_t lt_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t lt_of_first(uint32_t smem)               // the same place in the pair's first CTA
+{
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"(smem));
+    return at;
+}
+// A box to this CTA's shared memory; a barrier of either of the two is told
+__device__ __forceinline__ void lt_pair_tma(uint32_t smem, const CUtensorMap* map, int x, int y, int z, uint32_t cluster_bar)
+{
+    asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+                 "@e cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n\t}"
+                 ::"r"(smem), "l"(map), "r"(x), "r"(y), "r"(z), "r"(cluster_bar) : "memory");
+}
+// For a whole warp, when all its lanes have come: an arrival at a barrier of either CTA
+__device__ __forceinline__ void lt_pair_arrive(uint32_t cluster_bar)
+{
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ void lt_pair_commit(uint32_t bar)                  // to both
+{
+    asm volatile("{\n\t.reg .pred e;\n\t.reg .b16 both;\n\tmov.b16 both, 3;\n\telect.sync _|e, 0xffffffff;\n\t"
+                 "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], both;\n\t}" ::"r"(bar) : "memory");
+}
+template <int N, int SA, int SB> __device__ __forceinline__ void lt_pair_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add)
+{
+    asm volatile("{\n\t.reg .pred p, e, t;\n\t.reg .b64 a, b;\n\telect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.eq.u32 t, 0, 0;\n\t"
+                 "@e tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t"
+                 "add.u64 a, %1, %5;\n\tadd.u64 b, %2, %6;\n\t@e tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %3, t;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(what), "r"((uint32_t)add), "n"(SA), "n"(SB) : "memory");
+    if constexpr (N > 2) lt_pair_mma_ss<N - 2, SA, SB>(d, a + 2 * SA, b + 2 * SB, what, true);
+}
+// As kv_warp_wait, for barriers that the other CTA arrives at
+__device__ __forceinline__ bool lt_pair_wait(uint32_t bar, uint32_t parity, volatile int* stop)
+{
+    bool done = false;
+#pragma unroll 1
+    for (int i = 0; i < 1 << 18 && !done; i++) {
+        uint32_t d;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(d) : "r"(bar), "r"(parity) : "memory");
+        done = d;
+        if (!done && (i & 15) == 15 && *stop) break;
+    }
+    if (!done) *stop = 1;
+    return __all_sync(0xffffffffu, done);
+}
+
 // S of 64 rows (tensor memory, 16 lanes of each warp's 32), 32 columns: lane l of the warp gets of its 16 rows the rows l / 4 and l / 4 + 8, and of every
 // 8 columns the columns 2 (l % 4) and the next: x[4 k], x[4 k + 1] of the first row and x[4 k + 2], x[4 k + 3] of the second, columns 8 k on.
 __device__ __forceinline__ void lt_tmem_load_quads(uint32_t (&x)[16], uint32_t at)

@@ -466,13 +466,13 @@ extern "C" int fastrack_latent_expand(fastrack_latent* lt, const fastrack_latent
     return lt_launched(lt);
 }
 
-// Rows of keys or values as a tensor (x: channels, y: rows, z: heads, or one where they share their rows); boxes of 128 rows
-static int lt_keys_map(fastrack_latent* lt, const fastrack_kv_rows* r, int width, int total_keys, CUtensorMap* map)
+// Rows of keys or values as a tensor (x: channels, y: rows, z: heads, or one where they share their rows); boxes of `box` rows
+static int lt_keys_map(fastrack_latent* lt, const fastrack_kv_rows* r, int width, int total_keys, int box, CUtensorMap* map)
 {
     memset(map, 0, sizeof *map);
     if (total_keys == 0) return FASTRACK_OK;             // nobody sees anything
     const int heads = r->head_stride ? lt->shape.heads : 1;
-    return lt_map(lt, map, r->data, width, total_keys, heads, r->token_stride ? 2 * r->token_stride : 2 * width, r->head_stride ? 2 * r->head_stride : 2 * width, LT_P_TOKENS);
+    return lt_map(lt, map, r->data, width, total_keys, heads, r->token_stride ? 2 * r->token_stride : 2 * width, r->head_stride ? 2 * r->head_stride : 2 * width, box);
 }
 // Strides that a tensor map takes
 static bool lt_bad_keys(const fastrack_kv_rows* r, int total_keys)
@@ -508,7 +508,7 @@ extern "C" int fastrack_latent_prompt(fastrack_latent* lt, const fastrack_latent
     A.lse = d_lse;
     A.key_starts = d_key_starts;
     A.total_keys = total_keys;
-    A.tiles = (batch->max_new + 2 * LT_P_ROWS - 1) / (2 * LT_P_ROWS);
+    A.tiles = (batch->max_new + 4 * LT_P_ROWS - 1) / (4 * LT_P_ROWS);
     CUtensorMap pool, k_map, v_map;
     memset(&k_map, 0, sizeof k_map);
     memset(&v_map, 0, sizeof v_map);
@@ -519,10 +519,10 @@ extern "C" int fastrack_latent_prompt(fastrack_latent* lt, const fastrack_latent
         A.v_head_stride = v->head_stride;
         A.k_heads = k->head_stride != 0;
         A.v_heads = v->head_stride != 0;
-        if (int rc = lt_keys_map(lt, k, S.key, total_keys, &k_map)) return rc;
-        if (int rc = lt_keys_map(lt, v, S.value, total_keys, &v_map)) return rc;
+        if (int rc = lt_keys_map(lt, k, S.key, total_keys, LT_P_TOKENS / 2, &k_map)) return rc;
+        if (int rc = lt_keys_map(lt, v, S.value, total_keys, LT_P_TOKENS, &v_map)) return rc;
     }
     auto kernel = lt->config.dtype == FASTRACK_KV_BF16 ? lt_prompt_kernel<true> : lt_prompt_kernel<false>;
-    kernel<<<dim3((unsigned)A.tiles * S.heads, 1, batch->n_seqs), LT_P_THREADS, lt_prompt_smem(S), (cudaStream_t)stream>>>(S, B, A, pool, k_map, v_map);
+    kernel<<<dim3(2u * A.tiles * S.heads, 1, batch->n_seqs), LT_P_THREADS, lt_prompt_smem(S), (cudaStream_t)stream>>>(S, B, A, pool, k_map, v_map);
     return lt_launched(lt);
 }

@@ -87,15 +87,6 @@ template <int N, int SA, int SB> __device__ __forceinline__ void lt_mma_ss(uint3
                  ::"r"(d), "l"(a), "l"(b), "r"(what), "r"((uint32_t)add), "n"(SA), "n"(SB) : "memory");
     if constexpr (N > 2) lt_mma_ss<N - 2, SA, SB>(d, a + 2 * SA, b + 2 * SB, what, true);
 }
-// The same with A in tensor memory, 8 columns a step
-template <int N, int SB> __device__ __forceinline__ void lt_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add)
-{
-    asm volatile("{\n\t.reg .pred p, e, t;\n\t.reg .b32 a;\n\t.reg .b64 b;\n\telect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.eq.u32 t, 0, 0;\n\t"
-                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
-                 "add.u32 a, %1, 8;\n\tadd.u64 b, %2, %5;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(what), "r"((uint32_t)add), "n"(SB) : "memory");
-    if constexpr (N > 2) lt_mma_ts<N - 2, SB>(d, a + 16, b + 2 * SB, what, true);
-}
 __device__ __forceinline__ void lt_init(uint32_t bar, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 
 // 16 bytes to shared memory without waiting; zeros where there is no source
@@ -164,7 +155,22 @@ template <int N, int SA, int SB> __device__ __forceinline__ void lt_pair_mma_ss(
                  ::"r"(d), "l"(a), "l"(b), "r"(what), "r"((uint32_t)add), "n"(SA), "n"(SB) : "memory");
     if constexpr (N > 2) lt_pair_mma_ss<N - 2, SA, SB>(d, a + 2 * SA, b + 2 * SB, what, true);
 }
-// As kv_warp_wait, for barriers that the other CTA arrives at
+// The same with A in tensor memory, 8 columns a step
+template <int N, int SB> __device__ __forceinline__ void lt_pair_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add)
+{
+    asm volatile("{\n\t.reg .pred p, e, t;\n\t.reg .b32 a;\n\t.reg .b64 b;\n\telect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.eq.u32 t, 0, 0;\n\t"
+                 "@e tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+                 "add.u32 a, %1, 8;\n\tadd.u64 b, %2, %5;\n\t@e tcgen05.mma.cta_group::2.kind::f16 [%0], [a], b, %3, t;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(what), "r"((uint32_t)add), "n"(SB) : "memory");
+    if constexpr (N > 2) lt_pair_mma_ts<N - 2, SB>(d, a + 16, b + 2 * SB, what, true);
+}
+// As kv_ended and kv_warp_wait, for barriers that the other CTA arrives at
+__device__ __forceinline__ uint32_t lt_pair_ended(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done;
+}
 __device__ __forceinline__ bool lt_pair_wait(uint32_t bar, uint32_t parity, volatile int* stop)
 {
     bool done = false;

@@ -160,7 +160,7 @@ __device__ __forceinline__ void lt_expand_products(const LtShape& S, const LtBat
                 const uint64_t a = a0 + k * (LT_E_CHUNK >> 4), b = b0 + s * (LT_E_CHUNK >> 4);
                 const uint32_t out = bars + 8 * (LT_E_B_OUT + s);
                 there = next_there;
-                next_there = kv_ended(bars + 8 * (LT_E_B_IN + (s + 2) % LT_E_STAGES), phase ^ (s + 2 >= LT_E_STAGES));
+                next_there = lt_pair_ended(bars + 8 * (LT_E_B_IN + (s + 2) % LT_E_STAGES), phase ^ (s + 2 >= LT_E_STAGES));
                 lt_pair_mma_ss<4, 2, 2>(d, a, b, what, k > 0);
                 lt_pair_commit(out);
                 s = (s + 1) % LT_E_STAGES;

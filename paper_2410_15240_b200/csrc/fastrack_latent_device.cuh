@@ -136,8 +136,14 @@ __device__ __forceinline__ void lt_pair_tma(uint32_t smem, const CUtensorMap* ma
                  "@e cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n\t}"
                  ::"r"(smem), "l"(map), "r"(x), "r"(y), "r"(z), "r"(cluster_bar) : "memory");
 }
-// For a whole warp, when all its lanes have come: an arrival at a barrier of either CTA
+// For a whole warp, when all its lanes have come: an arrival at a barrier of either CTA.  The first is for what was done in tensor memory (whose own
+// fence stands in front of it); the second for what was written to shared memory, too, and holds the warp up for 1300 cycles.
 __device__ __forceinline__ void lt_pair_arrive(uint32_t cluster_bar)
+{
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ void lt_pair_release(uint32_t cluster_bar)
 {
     __syncwarp();
     if ((threadIdx.x & 31) == 0) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");

@@ -95,7 +95,7 @@ __device__ __forceinline__ void lt_prompt_rows(const LtShape& S, const LtPrompt&
         }
         lt_copies_done();
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        lt_pair_arrive(lt_of_first(bars) + 8 * LT_P_Q_IN);
+        lt_pair_release(lt_of_first(bars) + 8 * LT_P_Q_IN);
     }
     const int first_place = J.q.len - J.q.n + first_row + 32 * (warp & 3);                   // of this warp's rows
     const uint32_t p_in = lt_of_first(bars) + 8 * (LT_P_P_IN + m_tile);
@@ -350,8 +350,10 @@ __device__ __forceinline__ void lt_prompt_guard(const LtShape& S, const LtPrompt
                 }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            lt_pair_release(v_ok + 8 * stage);
+        } else {
+            lt_pair_arrive(v_ok + 8 * stage);
         }
-        lt_pair_arrive(v_ok + 8 * stage);
         stage = stage == LT_P_STAGES - 1 ? 0 : stage + 1;
         phase ^= stage == 0;
     }

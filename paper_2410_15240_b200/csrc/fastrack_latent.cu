@@ -23,6 +23,7 @@ struct LtAppend { KvRows latent, key, q, q_out; const uint16_t* weight; int toke
 // the queries' part, as kv_rotary_kernel does.
 template <bool BF> __global__ void __launch_bounds__(LT_APPEND_THREADS) lt_append_kernel(const LtShape S, const LtBatch B, const LtAppend A)
 {
+    asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if ((int)blockIdx.x >= A.token_ctas) {
         const int units = S.rope / 16, groups = (S.heads + A.q_per - 1) / A.q_per;
@@ -92,6 +93,7 @@ struct LtAccept { const int32_t *parents, *tokens, *choices; int32_t *path, *n_a
 __global__ void __launch_bounds__(LT_ACCEPT_THREADS) lt_accept_kernel(const LtShape S, const LtBatch B, const LtAccept A)
 {
     __shared__ int path[FASTRACK_LATENT_TREE_MOST], accepted;
+    asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
     const int seq = blockIdx.x, lane = threadIdx.x & 31;
     const LtSeq q = lt_seq(B, seq);
     if (threadIdx.x < 32) {
@@ -158,6 +160,22 @@ static int lt_cuda(fastrack_latent* lt, cudaError_t e)
     lt->last_cuda_error = (int)e;
     (void)cudaGetLastError();
     return FASTRACK_ERR_CUDA;
+}
+// A launch whose start may overlap the end of the kernel before it in the stream; the kernel waits (griddepcontrol.wait) before it reads
+// or writes anything that another may have to do with.  An error stays for cudaGetLastError.
+template <class... P, class... Q> static void lt_launch(cudaStream_t stream, dim3 grid, int threads, int smem, void (*kernel)(P...), const Q&... args)
+{
+    cudaLaunchConfig_t c = {};
+    cudaLaunchAttribute overlap;
+    overlap.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    overlap.val.programmaticStreamSerializationAllowed = 1;
+    c.gridDim = grid;
+    c.blockDim = dim3(threads);
+    c.dynamicSmemBytes = smem;
+    c.stream = stream;
+    c.attrs = &overlap;
+    c.numAttrs = 1;
+    (void)cudaLaunchKernelEx(&c, kernel, P(args)...);
 }
 static int lt_launched(fastrack_latent* lt, int count = 1)
 {
@@ -306,7 +324,7 @@ extern "C" int fastrack_latent_append(fastrack_latent* lt, const fastrack_latent
     if (token_ctas + turn > INT32_MAX) return FASTRACK_ERR_ARG;
     A.token_ctas = (int)token_ctas;
     auto kernel = lt->config.dtype == FASTRACK_KV_BF16 ? lt_append_kernel<true> : lt_append_kernel<false>;
-    kernel<<<(unsigned)(token_ctas + turn), LT_APPEND_THREADS, 0, (cudaStream_t)stream>>>(S, lt_batch(batch), A);
+    lt_launch((cudaStream_t)stream, dim3((unsigned)(token_ctas + turn)), LT_APPEND_THREADS, 0, kernel, S, lt_batch(batch), A);
     return lt_launched(lt);
 }
 
@@ -318,7 +336,7 @@ extern "C" int fastrack_latent_accept(fastrack_latent* lt, const fastrack_latent
     if (batch->total_new > 0 && (lt_misaligned(a->d_tokens, 4) || lt_misaligned(a->d_choices, 4) || lt_misaligned(a->d_path, 4))) return FASTRACK_ERR_ARG;
     if (int rc = lt_check_device(lt)) return rc;
     const LtAccept A = {a->d_parents, a->d_tokens, a->d_choices, a->d_path, a->d_n_accepted, a->d_next, a->d_lens_out};
-    lt_accept_kernel<<<batch->n_seqs, LT_ACCEPT_THREADS, 0, (cudaStream_t)stream>>>(lt->shape, lt_batch(batch), A);
+    lt_launch((cudaStream_t)stream, dim3(batch->n_seqs), LT_ACCEPT_THREADS, 0, lt_accept_kernel, lt->shape, lt_batch(batch), A);
     return lt_launched(lt);
 }
 
@@ -429,18 +447,8 @@ extern "C" int fastrack_latent_attention(fastrack_latent* lt, const fastrack_lat
     const bool bf = lt->config.dtype == FASTRACK_KV_BF16;
     const cudaStream_t st = (cudaStream_t)stream;
     const LtAttendKind& kind = lt_attend_kinds[2 * (S.latent / 128 - 1) + bf];
-    kind.kernel<<<p.groups * p.group_tiles, LT_A_THREADS, kind.smem, st>>>(S, B, A, pool, pairs);
-    // its start may overlap the end of the kernel before it; it waits (griddepcontrol.wait) before it reads anything
-    cudaLaunchConfig_t c = {};
-    cudaLaunchAttribute overlap;
-    overlap.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    overlap.val.programmaticStreamSerializationAllowed = 1;
-    c.gridDim = dim3(16 * lt->num_sms);
-    c.blockDim = dim3(LT_JOIN_THREADS);
-    c.stream = st;
-    c.attrs = &overlap;
-    c.numAttrs = 1;
-    (void)cudaLaunchKernelEx(&c, bf ? lt_join_kernel<true> : lt_join_kernel<false>, S, B, A);   // an error stays for cudaGetLastError
+    lt_launch(st, dim3(p.groups * p.group_tiles), LT_A_THREADS, kind.smem, kind.kernel, S, B, A, pool, pairs);
+    lt_launch(st, dim3(16 * lt->num_sms), LT_JOIN_THREADS, 0, bf ? lt_join_kernel<true> : lt_join_kernel<false>, S, B, A);
     return lt_launched(lt, 2);
 }
 
@@ -462,7 +470,7 @@ extern "C" int fastrack_latent_expand(fastrack_latent* lt, const fastrack_latent
     if (int rc = lt_pool_map(lt, B, &pool)) return rc;
     if (int rc = lt_map(lt, &weights, const_cast<void*>(d_weights), S.latent, width, S.heads, row, row * width, width / 2)) return rc;
     auto kernel = lt->config.dtype == FASTRACK_KV_BF16 ? lt_expand_kernel<true> : lt_expand_kernel<false>;
-    kernel<<<lt->num_sms / 2 * 2, LT_E_THREADS, lt_expand_smem(S.latent), (cudaStream_t)stream>>>(S, B, A, pool, weights);
+    lt_launch((cudaStream_t)stream, dim3(lt->num_sms / 2 * 2), LT_E_THREADS, lt_expand_smem(S.latent), kernel, S, B, A, pool, weights);
     return lt_launched(lt);
 }
 
@@ -523,6 +531,6 @@ extern "C" int fastrack_latent_prompt(fastrack_latent* lt, const fastrack_latent
         if (int rc = lt_keys_map(lt, v, S.value, total_keys, LT_P_TOKENS, &v_map)) return rc;
     }
     auto kernel = lt->config.dtype == FASTRACK_KV_BF16 ? lt_prompt_kernel<true> : lt_prompt_kernel<false>;
-    kernel<<<dim3(2u * A.tiles * S.heads, 1, batch->n_seqs), LT_P_THREADS, lt_prompt_smem(S), (cudaStream_t)stream>>>(S, B, A, pool, k_map, v_map);
+    lt_launch((cudaStream_t)stream, dim3(2u * A.tiles * S.heads, 1, batch->n_seqs), LT_P_THREADS, lt_prompt_smem(S), kernel, S, B, A, pool, k_map, v_map);
     return lt_launched(lt);
 }

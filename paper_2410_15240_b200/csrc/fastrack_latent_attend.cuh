@@ -24,7 +24,7 @@ template <int PAIRS> struct LtTile {
     static constexpr int FIRST = PAIRS > 1 ? PAIRS / 2 : 1;                  // pairs of a tile's first part; the second has the rest and the shared key
     static constexpr int P = (1 + STAGES) * BYTES, MISC = P + 64 * LT_CHUNK_ROW, SMEM = MISC + 2048 + 1024;    // after Q and the stages; room to round the base up
 };
-#define LT_A_AHEAD 4                    // tiles that are brought to L2 in advance
+#define LT_A_AHEAD 2                    // the tile that is brought to L2 in advance (4: 4 x 131072 tokens 130 us, none 125, 2: 122)
 #define LT_PART 16384                   // bytes of 128 channels of a tile
 #define LT_RAISE 8.f                    // a row's reference is raised when a score is 2^8 above it: weights stay below 2^8, and O seldom has to be multiplied
 
@@ -527,6 +527,7 @@ __global__ void __launch_bounds__(LT_A_THREADS, 1) lt_attend_kernel(const LtShap
     }
     if (warp == 9) asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"((uint32_t)__cvta_generic_to_shared(&M.tmem)) : "memory");
 
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     // the line's length, and where this run begins
     auto tiles_of = [&](int64_t item) {
         const int seq = A.seq_groups == 1 ? (int)item : (int)(item / A.seq_groups);
@@ -573,12 +574,14 @@ __global__ void __launch_bounds__(LT_A_THREADS, 1) lt_attend_kernel(const LtShap
     }
 }
 
-// Joins the pieces of items that runs cut.  A warp takes 128 channels of a row, 4 channels a lane, and asks for 8 pieces at a time; the pieces'
+// Joins the pieces of items that runs cut.  A warp takes 128 channels of a row, 4 channels a lane, and asks for some pieces at a time; the pieces'
 // references and sums it has in its lanes, 32 at a time.
 #define LT_JOIN_THREADS 128
-#define LT_JOIN_CUTS 1024               // most groups of CTAs
+#define LT_JOIN_PIECES 4                // asked for at a time: most items are cut into two or three, and fewer registers leave more warps
+#define LT_JOIN_CUTS 512                // most groups of CTAs
 template <bool BF> __global__ void __launch_bounds__(LT_JOIN_THREADS) lt_join_kernel(const LtShape S, const LtBatch B, const LtAttend A)
 {
+    __shared__ int4 cuts[LT_JOIN_CUTS];
     __shared__ int cut_runs[LT_JOIN_CUTS], cut_count;
     const int lane = threadIdx.x & 31, pairs = S.latent / 128, rows_of = A.group_tiles * LT_ROWS;
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -586,13 +589,16 @@ template <bool BF> __global__ void __launch_bounds__(LT_JOIN_THREADS) lt_join_ke
         // the runs whose last item goes on, in order: every CTA has the same list
         int n = 0;
         for (int g0 = 0; g0 < A.groups; g0 += 5 * 32) {
-            bool cut[5];
+            int4 cut[5];
 #pragma unroll
-            for (int k = 0; k < 5; k++) cut[k] = g0 + 32 * k + lane < A.groups && A.cuts[4 * (g0 + 32 * k + lane) + 2] > 1;
+            for (int k = 0; k < 5; k++) cut[k] = g0 + 32 * k + lane < A.groups ? *(const int4*)(A.cuts + 4 * (g0 + 32 * k + lane)) : make_int4(0, 0, 0, 0);
 #pragma unroll
             for (int k = 0; k < 5; k++) {
-                const uint32_t some = __ballot_sync(0xffffffffu, cut[k]);
-                if (cut[k]) cut_runs[n + __popc(some & ((1u << lane) - 1))] = g0 + 32 * k + lane;
+                const uint32_t some = __ballot_sync(0xffffffffu, cut[k].z > 1);
+                if (cut[k].z > 1) {
+                    cut_runs[n + __popc(some & ((1u << lane) - 1))] = g0 + 32 * k + lane;
+                    cuts[n + __popc(some & ((1u << lane) - 1))] = cut[k];
+                }
                 n += __popc(some);
             }
         }
@@ -601,8 +607,8 @@ template <bool BF> __global__ void __launch_bounds__(LT_JOIN_THREADS) lt_join_ke
     __syncthreads();
     const int of_cut = rows_of * pairs, work = cut_count * of_cut, step = gridDim.x * (LT_JOIN_THREADS / 32);
     for (int w = blockIdx.x * (LT_JOIN_THREADS / 32) + (threadIdx.x >> 5); w < work; w += step) {
-        const int g = cut_runs[w / of_cut], at = w % of_cut, i = at / pairs, ch = at % pairs * 128 + 4 * lane;
-        const int4 cut = *(const int4*)(A.cuts + 4 * g);
+        const int nth = w / of_cut, g = cut_runs[nth], at = w % of_cut, i = at / pairs, ch = at % pairs * 128 + 4 * lane;
+        const int4 cut = cuts[nth];
         const int row = cut.y + i;
         const int64_t first_slot = (((int64_t)2 * g + 1) * A.group_tiles + i / LT_ROWS) * LT_ROWS + i % LT_ROWS, next_slot = first_slot + A.group_tiles * LT_ROWS,
                       slot_step = (int64_t)2 * A.group_tiles * LT_ROWS;      // pieces: the last of this run, the first of the next runs
@@ -613,10 +619,10 @@ template <bool BF> __global__ void __launch_bounds__(LT_JOIN_THREADS) lt_join_ke
         for (int s0 = 0; s0 < cut.z; s0 += 32) {
             const float2 ml = s0 + lane < cut.z ? *(const float2*)(A.part_ml + 2 * slot(s0 + lane)) : make_float2(KV_M_NONE, 0.f);
             float weight = 0.f;
-            for (int s = 0; s < 32 && s0 + s < cut.z; s += 8) {
-                float4 o[8];
+            for (int s = 0; s < 32 && s0 + s < cut.z; s += LT_JOIN_PIECES) {
+                float4 o[LT_JOIN_PIECES];
 #pragma unroll
-                for (int k = 0; k < 8; k++) o[k] = s0 + s + k < cut.z ? *(const float4*)(A.part_o + slot(s0 + s + k) * S.latent + ch) : make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int k = 0; k < LT_JOIN_PIECES; k++) o[k] = s0 + s + k < cut.z ? *(const float4*)(A.part_o + slot(s0 + s + k) * S.latent + ch) : make_float4(0.f, 0.f, 0.f, 0.f);
                 if (s == 0) {
                     float top = ml.x;
 #pragma unroll
@@ -632,7 +638,7 @@ template <bool BF> __global__ void __launch_bounds__(LT_JOIN_THREADS) lt_join_ke
                     sum = make_float4(sum.x * fall, sum.y * fall, sum.z * fall, sum.w * fall);
                 }
 #pragma unroll
-                for (int k = 0; k < 8; k++) {
+                for (int k = 0; k < LT_JOIN_PIECES; k++) {
                     const float by = __shfl_sync(0xffffffffu, weight, s + k);
                     if (s0 + s + k < cut.z) sum = make_float4(fmaf(by, o[k].x, sum.x), fmaf(by, o[k].y, sum.y), fmaf(by, o[k].z, sum.z), fmaf(by, o[k].w, sum.w));
                 }

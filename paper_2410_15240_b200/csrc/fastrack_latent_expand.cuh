@@ -190,6 +190,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LT_E_THREADS, 1) lt_
         M.stop = 0;
     }
     if (warp == 9) asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"((uint32_t)__cvta_generic_to_shared(&M.tmem)) : "memory");
+    asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
     auto units_of = [&](int64_t seq) { return (int64_t)((lt_len(B, (int)seq) + 2 * LT_E_TOKENS - 1) / (2 * LT_E_TOKENS)) * A.units; };
     LtStretch mine = lt_stretch<LT_E_THREADS>(B.n_seqs, units_of, M.warp_sum);
     const int pairs = gridDim.x / 2;

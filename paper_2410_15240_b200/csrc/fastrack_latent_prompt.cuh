@@ -370,6 +370,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LT_P_THREADS, 1)
     const int warp = threadIdx.x >> 5, k_chunks = lt_prompt_k_chunks(S);
     LtPromptMisc& M = *(LtPromptMisc*)(sm + 2 * k_chunks * LT_P_CHUNK + LT_P_STAGES * (k_chunks * LT_P_KEYS + LT_P_CHUNK));
     const uint32_t bars = (uint32_t)__cvta_generic_to_shared(M.bars);
+    asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
     LtPromptJob J;
     const int job = blockIdx.x >> 1;
     J.seq = blockIdx.z;

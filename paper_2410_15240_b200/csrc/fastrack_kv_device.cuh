@@ -150,43 +150,6 @@ template <bool BF> __device__ __forceinline__ void kv_turn_raw(const KvShape& S,
     a = kv_narrow8<BF>(x);
     b = kv_narrow8<BF>(x + 8);
 }
-template <bool BF> __device__ __forceinline__ void kv_turn16(const KvShape& S, int u, int64_t position, uint4& a, uint4& b)
-{
-    float cs[8], sn[8];
-    kv_angles(S, u, position, false, cs, sn);
-    kv_turn_raw<BF>(S, cs, sn, a, b);
-}
-
-// One thread turns one unit (16 channels) of a token in heads h0 .. h0 + per - 1: the unit's cosines and sines are made once for them, while
-// the first heads' values are on their way.
-template <bool BF, int AHEAD>
-__device__ __forceinline__ void kv_turn_heads(const KvShape& S, const KvRows& in, const KvRows& out, const int64_t* positions, int64_t token, int u, int h0, int per,
-                                              int heads, bool inverse)
-{
-    const KvUnit unit = kv_unit(S, u);
-    if (!unit.turned && in.data == out.data) return;
-    const uint16_t* src = (const uint16_t*)in.data + token * in.token_stride + h0 * in.head_stride;
-    uint16_t* dst = (uint16_t*)out.data + token * out.token_stride + h0 * out.head_stride;
-    const int n = min(per, heads - h0);
-    float cs[8], sn[8];
-    for (int h = 0; h < n; h += AHEAD) {
-        uint4 a[AHEAD], b[AHEAD];
-#pragma unroll
-        for (int k = 0; k < AHEAD; k++)
-            if (h + k < n) {
-                a[k] = *(const uint4*)(src + (h + k) * in.head_stride + unit.a);
-                b[k] = *(const uint4*)(src + (h + k) * in.head_stride + unit.b);
-            }
-        if (h == 0 && unit.turned) kv_angles(S, u, positions[token], inverse, cs, sn);
-#pragma unroll
-        for (int k = 0; k < AHEAD; k++)
-            if (h + k < n) {
-                if (unit.turned) kv_turn_raw<BF>(S, cs, sn, a[k], b[k]);
-                *(uint4*)(dst + (h + k) * out.head_stride + unit.a) = a[k];
-                *(uint4*)(dst + (h + k) * out.head_stride + unit.b) = b[k];
-            }
-    }
-}
 
 // Codes of 4 values that were multiplied by top / amax (so that rounding leaves none above the top).  int8: the sum with 1.5 * 2^23 is
 // rounded to a whole number, to even, whose last byte is the code.  A NaN gives some code, but none that is a NaN.

@@ -4,12 +4,13 @@
 
 // 256 tokens of a sequence, 128 for each CTA of a pair, times the weights of one head's keys and values (a unit: 128, 192 or 256 columns).  The
 // tokens' latents stay in shared memory for as many units as the pair has of them; the weights come 64 channels at a time, half of the rows to each
-// CTA.  All units form one line, which is cut into equal runs, one for each pair.  Warps 0-7 write the answers, 64 columns at a time, while the next
+// CTA.  All units form one line, which is cut into equal runs, one for each pair.  Warps 0-7 write the answers, 32 columns at a time, while the next
 // unit's are made (two accumulators); warp 8 brings, warp 9 of the first CTA issues the products of both.  What bounds it is shared memory: of
 // its 128 bytes a cycle a product of 128 rows and 128 columns wants all, one of 256 columns shared by two SMs half.
 #define LT_E_TOKENS 128
 #define LT_E_THREADS 320
-#define LT_E_STAGES 4
+#define LT_E_STAGES 8                                    // of weights, at most; what latents of 512 channels leave room for are 5.  (A weight's way in takes some
+                                                         // 2500 cycles from the stage's end of use on, a chunk's products 512: with 4 stages, 232 us instead of 200.)
 #define LT_E_CHUNK (LT_E_TOKENS * LT_CHUNK_ROW)          // bytes of 64 channels of the tokens, or of up to 128 rows of weights
 
 enum { LT_E_A_IN = 0, LT_E_A_OUT, LT_E_B_IN, LT_E_B_OUT = LT_E_B_IN + LT_E_STAGES, LT_E_D_IN = LT_E_B_OUT + LT_E_STAGES, LT_E_D_OUT = LT_E_D_IN + 2, LT_E_END = LT_E_D_OUT + 2, LT_E_BARS };
@@ -20,8 +21,11 @@ struct LtExpandMisc {
     int64_t item, item_at;
     int64_t warp_sum[LT_E_THREADS / 32];
 };
-// latents, weights, 4 KB per writing warp, the rest, room to round the base up
-static inline int lt_expand_smem(int latent) { return latent / 64 * LT_E_CHUNK + LT_E_STAGES * LT_E_CHUNK + 8 * 32 * LT_CHUNK_ROW + 1024 + 1024; }
+#define LT_E_OUT_ROW 64                                  // bytes of 32 columns of a row, on the way out
+// latents, weights, 2 KB per writing warp, the rest, room to round the base up
+__host__ __device__ static inline int lt_expand_stages(int latent) { return latent == 512 ? 5 : latent == 384 ? 7 : LT_E_STAGES; }
+static inline int lt_expand_smem(int latent) { return (latent / 64 + lt_expand_stages(latent)) * LT_E_CHUNK + 8 * 32 * LT_E_OUT_ROW + 2048 + 1024; }
+static_assert(sizeof(LtExpandMisc) <= 2048, "");
 
 struct LtExpand { KvRows k, v; const int32_t* key_starts; int total_keys, units; };          // units: of 256 tokens, the heads
 
@@ -56,7 +60,9 @@ __device__ __forceinline__ void lt_expand_write(const LtShape& S, const LtBatch&
 {
     const int warp = threadIdx.x >> 5 & 3, half = threadIdx.x >> 7, lane = threadIdx.x & 31, rank = lt_rank();
     const uint32_t first_bars = lt_of_first(bars);
-    uint8_t* const mine = stage + (threadIdx.x >> 5) * 32 * LT_CHUNK_ROW;
+    uint8_t* const mine = stage + (threadIdx.x >> 5) * 32 * LT_E_OUT_ROW;
+    // a piece of 16 bytes of a row: rows in pairs fill 128 bytes, swizzled by the pair
+    auto at = [](int row, int piece) { return row * LT_E_OUT_ROW + ((piece ^ (row >> 1 & 3)) << 4); };
     int c = 0;
     bool fine = true;
     while (walk.next(B, A)) {                            // where a wait runs out, the answers from there on are NaN
@@ -66,28 +72,28 @@ __device__ __forceinline__ void lt_expand_write(const LtShape& S, const LtBatch&
         for (int u = walk.from; u < walk.to; u++, c++) {
             fine = fine && lt_pair_wait(bars + 8 * (LT_E_D_IN + (c & 1)), c >> 1 & 1, stop);
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            for (int b = 64 * half; b < S.key + S.value; b += 128) {
+            for (int b = 32 * half; b < S.key + S.value; b += 64) {
                 const KvRows& dst = b < S.key ? A.k : A.v;
-                uint16_t* const to_head = (uint16_t*)dst.data + u * dst.head_stride + (b < S.key ? b : b - S.key) + 8 * (lane & 7);
-                uint32_t x[64];
-                kv_tmem_load64(x, tmem + ((uint32_t)warp << 21) + 256 * (c & 1) + b);
-                if (b + 128 >= S.key + S.value) {        // the accumulator has been read
+                uint16_t* const to_head = (uint16_t*)dst.data + u * dst.head_stride + (b < S.key ? b : b - S.key) + 8 * (lane & 3);
+                uint32_t x[32];
+                kv_tmem_load32(x, tmem + ((uint32_t)warp << 21) + 256 * (c & 1) + b);
+                if (b + 64 >= S.key + S.value) {         // the accumulator has been read
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     lt_pair_arrive(first_bars + 8 * (LT_E_D_OUT + (c & 1)));
                 }
 #pragma unroll
-                for (int p = 0; p < 8; p++) {
+                for (int p = 0; p < 4; p++) {
                     float y[8];
 #pragma unroll
                     for (int e = 0; e < 8; e++) y[e] = !fine ? __int_as_float(0x7fffffff) : there >> lane & 1 ? __uint_as_float(x[8 * p + e]) : 0.f;
-                    *(uint4*)(mine + lt_at(lane, p)) = kv_narrow8<BF>(y);
+                    *(uint4*)(mine + at(lane, p)) = kv_narrow8<BF>(y);
                 }
                 __syncwarp();
 #pragma unroll
-                for (int k = 0; k < 8; k++) {
-                    const int row = 4 * k + (lane >> 3);
+                for (int k = 0; k < 4; k++) {
+                    const int row = 8 * k + (lane >> 2);
                     const int64_t to = first + row;
-                    if (t0 + row < walk.len && to >= 0 && to < A.total_keys) *(uint4*)(to_head + to * dst.token_stride) = *(const uint4*)(mine + lt_at(row, lane & 7));
+                    if (t0 + row < walk.len && to >= 0 && to < A.total_keys) *(uint4*)(to_head + to * dst.token_stride) = *(const uint4*)(mine + at(row, lane & 3));
                 }
                 __syncwarp();
             }
@@ -98,7 +104,7 @@ __device__ __forceinline__ void lt_expand_write(const LtShape& S, const LtBatch&
 __device__ __forceinline__ void lt_expand_bring(const LtShape& S, const LtBatch& B, const LtExpand& A, const CUtensorMap* pool, const CUtensorMap* weights,
                                                 LtExpandWalk walk, uint32_t sm_at, uint32_t bars, volatile int* stop)
 {
-    const int lane = threadIdx.x & 31, rank = lt_rank(), chunks = S.latent / 64, box = min(S.block_tokens, 64);
+    const int lane = threadIdx.x & 31, rank = lt_rank(), chunks = S.latent / 64, box = min(S.block_tokens, 64), stages = lt_expand_stages(S.latent);
     const uint32_t weights_at = sm_at + chunks * LT_E_CHUNK, first_bars = lt_of_first(bars);
     int c = 0, pieces = 0, s = 0;                        // chunks of weights, pieces of latents; the next chunk's stage
     uint32_t phase = 0;
@@ -125,14 +131,14 @@ __device__ __forceinline__ void lt_expand_bring(const LtShape& S, const LtBatch&
                 if (!fine) break;
                 if (rank == 0) lt_expect(bars + 8 * (LT_E_B_IN + s), (S.key + S.value) * LT_CHUNK_ROW);
                 lt_pair_tma(weights_at + s * LT_E_CHUNK, weights, 64 * k, rank * ((S.key + S.value) / 2), u, first_bars + 8 * (LT_E_B_IN + s));
-                s = s == LT_E_STAGES - 1 ? 0 : s + 1;
+                s = s == stages - 1 ? 0 : s + 1;
                 phase ^= s == 0;
             }
         }
     }
     // what is on its way, to both CTAs, arrives before they end
     if (rank == 0) {
-        for (int back = 1; back <= LT_E_STAGES && back <= c; back++) (void)kv_wait(bars + 8 * (LT_E_B_IN + (c - back) % LT_E_STAGES), (c - back) / LT_E_STAGES & 1);
+        for (int back = 1; back <= stages && back <= c; back++) (void)kv_wait(bars + 8 * (LT_E_B_IN + (c - back) % stages), (c - back) / stages & 1);
         if (pieces) (void)kv_wait(bars + 8 * LT_E_A_IN, pieces - 1 & 1);
     }
 }
@@ -141,7 +147,7 @@ template <bool BF>
 __device__ __forceinline__ void lt_expand_products(const LtShape& S, const LtBatch& B, const LtExpand& A, LtExpandWalk walk, uint32_t sm_at, uint32_t bars, volatile int* stop,
                                                    uint32_t tmem)
 {
-    const int chunks = S.latent / 64;
+    const int chunks = S.latent / 64, stages = lt_expand_stages(S.latent);
     constexpr uint32_t kind = 1u << 4 | (BF ? 1u << 7 | 1u << 10 : 0u) | (uint32_t)(2 * LT_E_TOKENS / 16) << 24;
     // A barrier's answer takes some 270 cycles while the tensor cores read: it is asked two stages ahead.
     int s = 0, units = 0, pieces = 0;                    // s: the stage
@@ -160,10 +166,11 @@ __device__ __forceinline__ void lt_expand_products(const LtShape& S, const LtBat
                 const uint64_t a = a0 + k * (LT_E_CHUNK >> 4), b = b0 + s * (LT_E_CHUNK >> 4);
                 const uint32_t out = bars + 8 * (LT_E_B_OUT + s);
                 there = next_there;
-                next_there = lt_pair_ended(bars + 8 * (LT_E_B_IN + (s + 2) % LT_E_STAGES), phase ^ (s + 2 >= LT_E_STAGES));
+                const int ahead = s + 2 < stages ? s + 2 : s + 2 - stages;
+                next_there = lt_pair_ended(bars + 8 * (LT_E_B_IN + ahead), phase ^ (s + 2 >= stages));
                 lt_pair_mma_ss<4, 2, 2>(d, a, b, what, k > 0);
                 lt_pair_commit(out);
-                s = (s + 1) % LT_E_STAGES;
+                s = s == stages - 1 ? 0 : s + 1;
                 phase ^= s == 0;
             }
             lt_pair_commit(bars + 8 * (LT_E_D_IN + (units & 1)));
@@ -180,8 +187,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LT_E_THREADS, 1) lt_
     uint8_t* const sm = lt_raw + (-(uint32_t)__cvta_generic_to_shared(lt_raw) & 1023u);
     const uint32_t sm_at = (uint32_t)__cvta_generic_to_shared(sm);
     const int warp = threadIdx.x >> 5;
-    uint8_t* const stage = sm + S.latent / 64 * LT_E_CHUNK + LT_E_STAGES * LT_E_CHUNK;
-    LtExpandMisc& M = *(LtExpandMisc*)(stage + 8 * 32 * LT_CHUNK_ROW);
+    uint8_t* const stage = sm + (S.latent / 64 + lt_expand_stages(S.latent)) * LT_E_CHUNK;
+    LtExpandMisc& M = *(LtExpandMisc*)(stage + 8 * 32 * LT_E_OUT_ROW);
     const uint32_t bars = (uint32_t)__cvta_generic_to_shared(M.bars);
     volatile int* const stop = &M.stop;
     if (threadIdx.x == 0) {

@@ -529,23 +529,27 @@ __global__ void __launch_bounds__(LT_A_THREADS, 1) lt_attend_kernel(const LtShap
 
     asm volatile("griddepcontrol.wait;" ::: "memory");
     // the line's length, and where this run begins
+    // (the last item that a thread has looked at is remembered: with no more items than threads, whoever has the first one need not read again)
+    LtWalk w;
+    int64_t known = -1;
     auto tiles_of = [&](int64_t item) {
-        const int seq = A.seq_groups == 1 ? (int)item : (int)(item / A.seq_groups);
-        return lt_item_tiles(S, A, lt_seq(B, seq), (int)(item - (int64_t)seq * A.seq_groups));
+        if (item != known) {
+            w.seq = A.seq_groups == 1 ? (int)item : (int)(item / A.seq_groups);
+            w.group = (int)(item - (int64_t)w.seq * A.seq_groups);
+            w.q = lt_seq(B, w.seq);
+            w.tiles = lt_item_tiles(S, A, w.q, w.group);
+            known = item;
+        }
+        return w.tiles;
     };
     LtStretch mine = lt_stretch<LT_A_THREADS>((int64_t)B.n_seqs * A.seq_groups, tiles_of, M.warp_sum);
     const int64_t share = max((mine.total + A.groups - 1) / A.groups, (int64_t)A.least);
     const int64_t begin = blockIdx.x / A.group_tiles * share;
     if (mine.holds(begin)) {
-        mine.find(begin, tiles_of);
-        LtWalk w;
+        mine.find(begin, tiles_of);                      // which leaves the item in w
         w.item_at = mine.before;
         w.at = begin;
         w.end = min(begin + share, mine.total);
-        w.seq = (int)(mine.item / A.seq_groups);
-        w.group = (int)(mine.item % A.seq_groups);
-        w.q = lt_seq(B, w.seq);
-        w.tiles = lt_item_tiles(S, A, w.q, w.group);
         M.walk = w;
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");

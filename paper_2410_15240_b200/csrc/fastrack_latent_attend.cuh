@@ -13,6 +13,17 @@
 // All work is one line: for each sequence, for each group of row tiles, the tiles of tokens that the group sees.  The line is cut into equal
 // runs, one for each group of CTAs (a CTA per row tile of a group; the CTAs of a group read the same tokens at the same time, all but the first
 // out of L2).  What a run cuts is joined by a kernel of its own; a run has at most two such pieces, its first and its last.
+//
+// Weights enter the second product in 16 bits, as the latents are held: the answer is off by some half of its own rounding more (error against 64 bits
+// bf16 0.0021 beside the rounding's 0.0017, f16 0.00021 to 0.00029 beside 0.00021).  Scores, references, sums and answers are kept in 32 bits.
+//
+// What bounds it, per tile, 512 + 64 channels and 64 rows: the scores' 36 products take 33 cycles each and the answers' 16 take 48 (64 rows as M,
+// or 64 as N: shared memory's 128 bytes a cycle are what the operands wait for), 1960 together; memory brings a tile in 2500 at its SM's share.  It takes
+// 3300: what is used again comes back some 1900 cycles after its last use, Q and two tiles are all that shared memory holds, and a tile's chain (scores,
+// weights, answers) is 4200 long.  61 sequences of up to 4096 tokens, 128 heads, bf16: 94 us with the join's 14; 4 of up to 131 072, 64 heads, f16: 120 to 138 us
+// (3.7 to 4.3 TB/s); 15 trees of 25 over up to 5000 tokens in blocks of 16, 16 heads: 108 us.  What it came from: copies and products issued by one
+// lane 228, 267 and 224 us; a barrier per 64 or 128 channels and redundant waits 119, 144 and 140.  Tried instead: a part of a tile per 128 channels
+// (107, 160, 136 us), 5 or 9 warps for small blocks' copies (no change).
 #define LT_ROWS 64
 #define LT_TOKENS 64
 #define LT_A_THREADS 384
@@ -39,7 +50,7 @@ struct LtAttend {
     int groups;                         // of CTAs: runs that the line is cut into
     int group_tiles;                    // row tiles, CTAs, of a group
     int seq_groups;                     // groups of row tiles of a sequence, at most
-    int least;                          // tiles of a run
+    int least;                          // tiles of a run, at least (2: 700 tokens in 13.7 us, as with 1; 3: 16)
     float* part_o;                      // [groups][2][group_tiles][64][latent]: the first piece of a run (begun before it), the last
     float* part_ml;                     // [groups][2][group_tiles][64][2]
     int* cuts;                          // [groups][4]: of a run whose last item goes on: first packed row of the sequence, the item's first row, pieces, rows of the sequence

@@ -5,8 +5,12 @@
 // 256 tokens of a sequence, 128 for each CTA of a pair, times the weights of one head's keys and values (a unit: 128, 192 or 256 columns).  The
 // tokens' latents stay in shared memory for as many units as the pair has of them; the weights come 64 channels at a time, half of the rows to each
 // CTA.  All units form one line, which is cut into equal runs, one for each pair.  Warps 0-7 write the answers, 32 columns at a time, while the next
-// unit's are made (two accumulators); warp 8 brings, warp 9 of the first CTA issues the products of both.  What bounds it is shared memory: of
-// its 128 bytes a cycle a product of 128 rows and 128 columns wants all, one of 256 columns shared by two SMs half.
+// unit's are made (two accumulators); warp 8 brings, warp 9 of the first CTA issues the products of both.
+//
+// What bounds it: the products (tensor pipe 75 % active) at the clock that the power leaves.  12 278 tokens of 64 heads, 512 channels, bf16: 192 us in a short
+// run (1250 TFLOP/s), 232 in a long one (1030 of the 1416 that a long matrix product makes here).  What it came from: one SM per tile and
+// 128 columns at a time 302 us (of shared memory's 128 bytes a cycle a product of 128 rows and 128 columns wants all; one of 256 columns
+// shared by two SMs wants half); the answers by 8 instead of 4 warps 288 to 271.
 #define LT_E_TOKENS 128
 #define LT_E_THREADS 320
 #define LT_E_STAGES 8                                    // of weights, at most; what latents of 512 channels leave room for are 5.  (A weight's way in takes some

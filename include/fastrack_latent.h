@@ -48,7 +48,7 @@ typedef struct {
 
 /* The sequences of a call, as fastrack_kv_batch has them: the new tokens of all sequences lie packed, sequence i has rows
  * d_starts[i] .. d_starts[i+1]-1 of the inputs and answers, and they are its LAST tokens: d_lens[i] counts them.  A sequence without
- * new tokens is left alone.  Whatever stands in d_lens, d_starts and d_table, nothing outside the bounds below is touched. */
+ * new tokens is left alone, and so are rows that belong to no sequence.  Whatever stands in d_lens, d_starts and d_table, nothing outside the bounds below is touched. */
 typedef struct {
     int n_seqs;                 /* at most 65535 */
     int total_new;              /* d_starts[n_seqs], or an upper bound of it; times heads below 2^31 */

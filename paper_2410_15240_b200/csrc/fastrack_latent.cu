@@ -68,7 +68,8 @@ template <bool BF> __global__ void __launch_bounds__(LT_APPEND_THREADS) lt_appen
     if ((int)blockIdx.x >= A.token_ctas) {
         const int units = S.rope / 16, groups = (S.heads + A.q_per - 1) / A.q_per;
         const int64_t i = (int64_t)(blockIdx.x - A.token_ctas) * LT_APPEND_THREADS + threadIdx.x, token = i / units / groups;
-        if (token < B.total_new) lt_turn_heads<BF>(S.turn, A.q, A.q_out, B.positions, token, (int)(i % units), (int)(i / units % groups) * A.q_per, A.q_per, S.heads);
+        // rows that belong to no sequence are left alone
+        if (token < B.total_new && token >= B.starts[0] && token < B.starts[B.n_seqs]) lt_turn_heads<BF>(S.turn, A.q, A.q_out, B.positions, token, (int)(i % units), (int)(i / units % groups) * A.q_per, A.q_per, S.heads);
         return;
     }
     const int per_seq = (B.max_new + LT_APPEND_THREADS / 32 - 1) / (LT_APPEND_THREADS / 32);

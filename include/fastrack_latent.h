@@ -114,14 +114,16 @@ FASTRACK_API int fastrack_latent_attention(fastrack_latent* latent, const fastra
 FASTRACK_API int fastrack_latent_expand(fastrack_latent* latent, const fastrack_latent_batch* batch, const void* d_weights, const fastrack_kv_rows* k_out,
                                         const fastrack_kv_rows* v_out, const int32_t* d_key_starts, int total_keys, void* stream);
 
-/* Bytes that fastrack_latent_prompt needs as workspace; 0 for bad arguments (or if it needs none). */
+/* Bytes that fastrack_latent_prompt needs as workspace (the bounds in the struct count): for answers in parts, where there are too few heads, sequences and
+ * new tokens to fill the device; else 0, and 0 for bad arguments. */
 FASTRACK_API size_t fastrack_latent_prompt_workspace(const fastrack_latent* latent, const fastrack_latent_batch* batch);
 
 /* Attention of the new tokens over expanded keys and values (rows as fastrack_latent_expand writes them; total_keys rows) with the shared keys
  * from the pages:
  *     out = sum_t p_t v_t[h],  p = softmax_t(softmax_scale * (q . k_t[h] + q_rope . r_t)),
- * over the tokens up to the query's own place, without absent pages' and without those whose row lies outside 0 .. total_keys - 1.  q rows have key_dim values, out rows value_dim.  Empty
- * rows, d_lse, and what a query does not see are as above. */
+ * over the tokens up to the query's own place, without absent pages' and without those whose row lies outside 0 .. total_keys - 1.  q rows have
+ * key_dim values, out rows value_dim.  Empty rows, d_lse, and what a query does not see are as above.  The result is the same in every run.
+ *   d_workspace 16-byte aligned, fastrack_latent_prompt_workspace bytes, with no requirement on its contents; NULL if that is 0. */
 FASTRACK_API int fastrack_latent_prompt(fastrack_latent* latent, const fastrack_latent_batch* batch, const fastrack_kv_rows* q,
                                         const fastrack_kv_rows* q_rope, const fastrack_kv_rows* k, const fastrack_kv_rows* v,
                                         const int32_t* d_key_starts, int total_keys, const fastrack_kv_rows* out, float* d_lse, void* d_workspace,

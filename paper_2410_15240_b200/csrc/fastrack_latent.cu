@@ -539,23 +539,43 @@ static bool lt_bad_keys(const fastrack_kv_rows* r, int total_keys)
     return lt_bad_rows(r) || r->token_stride < (total_keys > 1) || r->head_stride < 0 || r->token_stride >= (int64_t)1 << 38 || r->head_stride >= (int64_t)1 << 38;
 }
 
+// Where 512 queries of each head and sequence do not fill the pairs of SMs, pairs share a job's tokens between them: as many as there is room for, with
+// LT_P_LEAST steps each at least of those that a query sees on average in the longest sequence that there may be.
+// One pair a job against shares, one sequence, bf16, device time: 16 heads, 512 new of 4000 tokens 81 -> 41 us, of 16000 272 -> 86; 130 new of 32000
+// 489 -> 135; 32 heads, 1 new of 8000 129 -> 72; 2 heads, 10 new of 800 (two shares of 3 steps) 20.1 -> 16.7.  Where the average query sees fewer steps,
+// sharing costs: 16 heads, 1000 new of 1000, whose first queries see little, 32.6 whole and 35.7 in two shares.
+#define LT_P_LEAST 3
+struct LtPromptPlan { int tiles, splits; size_t ml, total; };                // byte offsets in the workspace, part_o at 0
+static LtPromptPlan lt_prompt_plan(const fastrack_latent* lt, const fastrack_latent_batch* b)
+{
+    LtPromptPlan p;
+    p.tiles = (b->max_new + 4 * LT_P_ROWS - 1) / (4 * LT_P_ROWS);
+    const int64_t jobs = (int64_t)p.tiles * lt->shape.heads * b->n_seqs, steps = ((int64_t)b->max_len - b->max_new / 2) / LT_P_TOKENS;
+    int64_t splits = jobs > 0 ? lt->num_sms / 2 / jobs : 1;
+    if (splits > steps / LT_P_LEAST) splits = steps / LT_P_LEAST;
+    p.splits = splits > 1 ? (int)splits : 1;
+    const size_t rows = p.splits > 1 ? (size_t)p.splits * b->total_new * lt->shape.heads : 0;
+    p.ml = rows * lt->shape.value * 4;
+    p.total = p.ml + rows * 8;
+    return p;
+}
+
 extern "C" size_t fastrack_latent_prompt_workspace(const fastrack_latent* lt, const fastrack_latent_batch* batch)
 {
-    (void)lt;
-    (void)batch;
-    return 0;
+    if (!lt || lt_bad_batch(lt, batch)) return 0;
+    return lt_prompt_plan(lt, batch).total;
 }
 
 extern "C" int fastrack_latent_prompt(fastrack_latent* lt, const fastrack_latent_batch* batch, const fastrack_kv_rows* q, const fastrack_kv_rows* q_rope,
                                       const fastrack_kv_rows* k, const fastrack_kv_rows* v, const int32_t* d_key_starts, int total_keys, const fastrack_kv_rows* out,
                                       float* d_lse, void* d_workspace, size_t workspace_bytes, void* stream)
 {
-    (void)d_workspace;
-    (void)workspace_bytes;
     if (!lt || lt_bad_batch(lt, batch) || total_keys < 0) return FASTRACK_ERR_ARG;
     if (batch->n_seqs == 0 || batch->total_new == 0 || batch->max_new == 0) return FASTRACK_OK;
     if (lt_bad_rows(q) || lt_bad_rows(q_rope) || lt_bad_rows(out) || ((uintptr_t)d_lse & 3) || lt_misaligned(d_key_starts, 4)) return FASTRACK_ERR_ARG;
     if (total_keys > 0 && (lt_bad_keys(k, total_keys) || lt_bad_keys(v, total_keys))) return FASTRACK_ERR_ARG;
+    const LtPromptPlan p = lt_prompt_plan(lt, batch);
+    if (p.total > 0 && (lt_misaligned(d_workspace, 16) || workspace_bytes < p.total)) return FASTRACK_ERR_ARG;
     if (int rc = lt_check_device(lt)) return rc;
     const LtShape& S = lt->shape;
     const LtBatch B = lt_batch(batch);
@@ -567,7 +587,10 @@ extern "C" int fastrack_latent_prompt(fastrack_latent* lt, const fastrack_latent
     A.lse = d_lse;
     A.key_starts = d_key_starts;
     A.total_keys = total_keys;
-    A.tiles = (batch->max_new + 4 * LT_P_ROWS - 1) / (4 * LT_P_ROWS);
+    A.tiles = p.tiles;
+    A.splits = p.splits;
+    A.part_o = (float*)d_workspace;
+    A.part_ml = (float*)((char*)d_workspace + p.ml);
     CUtensorMap pool, k_map, v_map;
     memset(&k_map, 0, sizeof k_map);
     memset(&v_map, 0, sizeof v_map);
@@ -581,7 +604,12 @@ extern "C" int fastrack_latent_prompt(fastrack_latent* lt, const fastrack_latent
         if (int rc = lt_keys_map(lt, k, S.key, total_keys, LT_P_TOKENS / 2, &k_map)) return rc;
         if (int rc = lt_keys_map(lt, v, S.value, total_keys, LT_P_TOKENS, &v_map)) return rc;
     }
-    auto kernel = lt->config.dtype == FASTRACK_KV_BF16 ? lt_prompt_kernel<true> : lt_prompt_kernel<false>;
-    lt_launch((cudaStream_t)stream, dim3(2u * A.tiles * S.heads, 1, batch->n_seqs), LT_P_THREADS, lt_prompt_smem(S), kernel, S, B, A, pool, k_map, v_map);
-    return lt_launched(lt);
+    const bool bf = lt->config.dtype == FASTRACK_KV_BF16;
+    const cudaStream_t st = (cudaStream_t)stream;
+    lt_launch(st, dim3(2u * A.tiles * S.heads, A.splits, batch->n_seqs), LT_P_THREADS, lt_prompt_smem(S), bf ? lt_prompt_kernel<true> : lt_prompt_kernel<false>, S, B, A, pool, k_map,
+              v_map);
+    if (A.splits == 1) return lt_launched(lt);
+    const unsigned rows = (unsigned)(((int64_t)batch->max_new * S.heads + LT_P_JOIN_THREADS / 32 - 1) / (LT_P_JOIN_THREADS / 32));
+    lt_launch(st, dim3(rows, batch->n_seqs), LT_P_JOIN_THREADS, 0, bf ? lt_prompt_join_kernel<true> : lt_prompt_join_kernel<false>, S, B, A);
+    return lt_launched(lt, 2);
 }

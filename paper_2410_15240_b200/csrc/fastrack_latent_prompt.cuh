@@ -44,6 +44,9 @@ struct LtPrompt {
     const int32_t* key_starts;
     int total_keys, tiles;                               // tiles: of 512 queries, at most
     bool k_heads, v_heads;                               // whether heads differ
+    int splits;                                          // pairs that share a job's tokens between them, equal runs of its steps
+    float* part_o;                                       // [splits][total_new][heads][value], if there are several
+    float* part_ml;                                      // [splits][total_new][heads][2]
 };
 __host__ __device__ __forceinline__ int lt_prompt_k_chunks(const LtShape& S) { return S.key / 64 + 1; }
 // Q; the stages, of K and then V each; the rest; room to round the base up
@@ -53,7 +56,7 @@ static_assert(sizeof(LtPromptMisc) <= 1024, "");
 // What a CTA works on
 struct LtPromptJob {
     LtSeq q;
-    int seq, head, row, rows, steps0, steps1;            // row: the pair's first query; rows: that there are; steps: of 128 tokens, for each row tile
+    int seq, head, row, rows, first_step, steps0, steps1;  // row: the pair's first query; rows: that there are; steps: of 128 tokens, for each row tile, from first_step on
     int lo, hi;                                          // tokens whose keys lie in the buffers
     int see_all;                                         // tokens before this one are seen by all rows
     int64_t key_start;
@@ -77,7 +80,8 @@ __device__ __forceinline__ uint32_t lt_prompt_there(const LtPromptJob& J, int t0
 }
 
 template <bool BF>
-__device__ __forceinline__ void lt_prompt_rows(const LtShape& S, const LtPrompt& A, const LtPromptJob& J, int m_tile, uint32_t sm_at, LtPromptMisc& M, uint32_t bars, uint32_t tmem)
+__device__ __forceinline__ void lt_prompt_rows(const LtShape& S, const LtPrompt& A, int total_new, const LtPromptJob& J, int m_tile, uint32_t sm_at, LtPromptMisc& M, uint32_t bars,
+                                               uint32_t tmem)
 {
     const int warp = threadIdx.x >> 5, r = threadIdx.x & 127, first_row = J.row + LT_P_ROWS * (2 * m_tile + (int)lt_rank()), row = first_row + r,
               steps = m_tile ? J.steps1 : J.steps0;
@@ -109,7 +113,7 @@ __device__ __forceinline__ void lt_prompt_rows(const LtShape& S, const LtPrompt&
     float m = KV_M_NONE, l = 0.f;
     bool fine = true;
     for (int s = 0; s < steps && fine; s++) {
-        const int t0 = LT_P_TOKENS * s;
+        const int t0 = LT_P_TOKENS * (J.first_step + s);
         // what is known of the tile first, while its scores are made
         fine = kv_warp_wait(bars + 8 * (LT_P_NOTE + s % LT_P_NOTES), s / LT_P_NOTES & 1, stop);
         const uint32_t present = ((volatile uint32_t*)M.present)[s % LT_P_NOTES];
@@ -176,9 +180,12 @@ __device__ __forceinline__ void lt_prompt_rows(const LtShape& S, const LtPrompt&
     }
     fine = lt_pair_wait(bars + 8 * LT_P_END, 0, stop) && fine && !*stop;
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const float by = !fine ? __int_as_float(0x7fffffff) : l == 0.f ? 0.f : 1.f / l;
+    const bool whole = A.splits == 1;
+    const float by = !fine ? __int_as_float(0x7fffffff) : !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
     const int64_t token = J.q.start + (int64_t)row;
-    if (valid && A.lse) A.lse[token * S.heads + J.head] = !fine ? by : l == 0.f ? -KV_INF : (m + log2f(l)) * 0.6931471805599453f;
+    if (!fine) l = by;
+    if (valid && !whole) *(float2*)(A.part_ml + 2 * (((int64_t)blockIdx.y * total_new + token) * S.heads + J.head)) = make_float2(m, l);
+    if (valid && whole && A.lse) A.lse[token * S.heads + J.head] = l == 0.f ? -KV_INF : (m + log2f(l)) * 0.6931471805599453f;
     const int apart_tile = min(J.see_all, J.hi) / LT_P_TOKENS;
     // the other CTA has looked after the other half of V
     uint32_t others, other_at;
@@ -198,7 +205,7 @@ __device__ __forceinline__ void lt_prompt_rows(const LtShape& S, const LtPrompt&
         if (!valid) continue;
         float y[32];
 #pragma unroll
-        for (int i = 0; i < 32; i++) y[i] = l == 0.f && fine ? 0.f : __uint_as_float(x[i]) * by;
+        for (int i = 0; i < 32; i++) y[i] = l == 0.f ? 0.f : __uint_as_float(x[i]) * by;
         // what the guard took out of V, for rows that see the token
 #pragma unroll 1
         for (int w = 0; some_apart && w < 4 * LT_P_APART; w++) {
@@ -219,6 +226,12 @@ __device__ __forceinline__ void lt_prompt_rows(const LtShape& S, const LtPrompt&
                 }
             }
         }
+        if (!whole) {
+            float* dst = A.part_o + (((int64_t)blockIdx.y * total_new + token) * S.heads + J.head) * S.value + b;
+#pragma unroll
+            for (int i = 0; i < 8; i++) *(float4*)(dst + 4 * i) = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+            continue;
+        }
         uint16_t* dst = (uint16_t*)A.out.data + token * A.out.token_stride + J.head * A.out.head_stride + b;
 #pragma unroll
         for (int i = 0; i < 4; i++) *(uint4*)(dst + 8 * i) = kv_narrow8<BF>(y + 8 * i);
@@ -236,7 +249,7 @@ __device__ __forceinline__ void lt_prompt_bring(const LtShape& S, const LtBatch&
     uint32_t phase = 0;
     for (; s < steps; s++) {
         // lane: a box of the tile's shared keys, of both halves of the tokens
-        const int t0 = LT_P_TOKENS * s, t = t0 + lane * box;
+        const int t0 = LT_P_TOKENS * (J.first_step + s), t = t0 + lane * box;
         const int page = lane < boxes && t < J.hi ? lt_page(B, J.seq, t >> S.block_shift) : -1;
         const uint32_t some = __ballot_sync(0xffffffffu, page >= 0);
         uint32_t present = 0;
@@ -335,7 +348,7 @@ __device__ __forceinline__ void lt_prompt_guard(const LtShape& S, const LtPrompt
     for (int s = 0; s < steps; s++) {
         if (!kv_warp_wait(bars + 8 * (LT_P_NOTE + s % LT_P_NOTES), s / LT_P_NOTES & 1, stop)) return;
         if (!kv_warp_wait(bars + 8 * (LT_P_V_IN + stage), phase, stop)) return;
-        const int t0 = LT_P_TOKENS * s;
+        const int t0 = LT_P_TOKENS * (J.first_step + s), nth_apart = J.first_step + s - apart_tile;
         const uint32_t present = ((volatile uint32_t*)M.present)[s % LT_P_NOTES];
         if (lt_prompt_ragged(J, t0, present)) {
             uint8_t* const v_sm = ring + stage * (k_chunks * LT_P_KEYS + LT_P_CHUNK);
@@ -349,8 +362,8 @@ __device__ __forceinline__ void lt_prompt_guard(const LtShape& S, const LtPrompt
                 if (there) f = make_uint4(lt_finite2<BF>(w.x), lt_finite2<BF>(w.y), lt_finite2<BF>(w.z), lt_finite2<BF>(w.w));
                 if (f.x != w.x || f.y != w.y || f.z != w.z || f.w != w.w) {
                     *at = f;
-                    if (there && s - apart_tile < LT_P_APART) {
-                        atomicOr(&M.apart[s - apart_tile][t >> 5], 1u << (t & 31));
+                    if (there && nth_apart < LT_P_APART) {
+                        atomicOr(&M.apart[nth_apart][t >> 5], 1u << (t & 31));
                         M.some_apart = 1;
                     }
                 }
@@ -396,6 +409,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LT_P_THREADS, 1)
     };
     J.steps0 = steps_to(min(J.rows, 2 * LT_P_ROWS));
     J.steps1 = parts == 2 ? steps_to(J.rows) : 0;
+    const int share = (max(J.steps0, J.steps1) + A.splits - 1) / A.splits;   // this pair's run of them
+    J.first_step = share * blockIdx.y;
+    J.steps0 = min(max(J.steps0 - J.first_step, 0), share);
+    J.steps1 = min(max(J.steps1 - J.first_step, 0), share);
     const int steps = max(J.steps0, J.steps1);
     if (threadIdx.x == 0) {
         for (int i = 0; i < LT_P_BARS; i++)
@@ -412,7 +429,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LT_P_THREADS, 1)
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = *(volatile uint32_t*)&M.tmem;  // S_0, S_1, O_0, O_1: 128 columns each
     if (warp < 8) {
-        if (warp < 4 * parts) lt_prompt_rows<BF>(S, A, J, warp >> 2, sm_at, M, bars, tmem);
+        if (warp < 4 * parts) lt_prompt_rows<BF>(S, A, B.total_new, J, warp >> 2, sm_at, M, bars, tmem);
     } else if (warp == 8) {
         lt_prompt_bring(S, B, A, J, steps, &pool, &k_map, &v_map, sm_at, M, bars);
     } else if (warp == 9) {
@@ -434,4 +451,40 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LT_P_THREADS, 1)
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
     }
+}
+
+// Joins the answers of pairs that shared a job's tokens, each with its own largest score m and sum l, in the shares' order: a warp takes a row,
+// 128 / 32 or 64 / 32 channels a lane.  Answers wait in 32 bits, so that the only further rounding is the answer's own.
+#define LT_P_JOIN_THREADS 128
+template <bool BF> __global__ void __launch_bounds__(LT_P_JOIN_THREADS) lt_prompt_join_kernel(const LtShape S, const LtBatch B, const LtPrompt A)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int lane = threadIdx.x & 31, w = blockIdx.x * (LT_P_JOIN_THREADS / 32) + (threadIdx.x >> 5), j = w / S.heads, head = w - j * S.heads;
+    const LtSeq q = lt_seq(B, blockIdx.y);
+    if (j >= q.n) return;
+    const int64_t token = q.start + (int64_t)j, row = token * S.heads + head, step = (int64_t)B.total_new * S.heads;
+    float m = KV_M_NONE, l = 0.f, sum[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < A.splits; s++) m = fmaxf(m, A.part_ml[2 * (s * step + row)]);
+#pragma unroll 4
+    for (int s = 0; s < A.splits; s++) {
+        const float2 ml = *(const float2*)(A.part_ml + 2 * (s * step + row));
+        const float by = kv_exp2(ml.x - m), *o = A.part_o + (s * step + row) * S.value;
+        l += ml.y * by;
+        if (S.value == 128) {
+            const float4 x = *(const float4*)(o + 4 * lane);
+            sum[0] = fmaf(x.x, by, sum[0]);
+            sum[1] = fmaf(x.y, by, sum[1]);
+            sum[2] = fmaf(x.z, by, sum[2]);
+            sum[3] = fmaf(x.w, by, sum[3]);
+        } else {
+            const float2 x = *(const float2*)(o + 2 * lane);
+            sum[0] = fmaf(x.x, by, sum[0]);
+            sum[1] = fmaf(x.y, by, sum[1]);
+        }
+    }
+    const float by = l == 0.f ? 0.f : 1.f / l;
+    uint16_t* const out = (uint16_t*)A.out.data + token * A.out.token_stride + head * A.out.head_stride;
+    if (S.value == 128) *(uint2*)(out + 4 * lane) = make_uint2(kv_pack<BF>(sum[0] * by, sum[1] * by), kv_pack<BF>(sum[2] * by, sum[3] * by));
+    else *(uint32_t*)(out + 2 * lane) = kv_pack<BF>(sum[0] * by, sum[1] * by);
+    if (lane == 0 && A.lse) A.lse[row] = l == 0.f ? -KV_INF : (m + log2f(l)) * 0.6931471805599453f;
 }
